@@ -24,7 +24,7 @@
 
 #include <cuda_bf16.h>
 
-#include "ptx.cuh"
+#include "umma.cuh"
 
 namespace moqae {
 
@@ -34,68 +34,12 @@ constexpr int kQTile = 128;                    // query rows per CTA
 constexpr int kKvBlock = 128;                  // tokens per block (four storage tiles)
 constexpr long long kPrefillWaitCycles = 1ll << 31;    // about a second: no wait of a healthy launch comes near
 
-// ---- tcgen05 wrappers -------------------------------------------------------------------
-// Shared-memory matrix descriptor, no swizzle: start address, leading-dimension byte offset
-// (between the two 8-element halves of a K step, or between groups of 8 K rows for an
-// MN-major operand) and stride byte offset (between groups of 8 rows / of 8 MN elements), all
-// in units of 16 bytes; bits 46..47 = 1 is the descriptor version of this architecture.
-__device__ __forceinline__ uint64_t make_desc(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  return static_cast<uint64_t>((saddr >> 4) & 0x3fffu) | (static_cast<uint64_t>((lbo_bytes >> 4) & 0x3fffu) << 16) |
-         (static_cast<uint64_t>((sbo_bytes >> 4) & 0x3fffu) << 32) | (1ull << 46);
-}
 // Instruction descriptor of kind::f16: fp32 accumulator, fp16 A and B, M = 128, N = 128;
 // bit 16 set = B is MN-major (its N index is the contiguous one).
 constexpr uint32_t kIdescS = (1u << 4) | (16u << 17) | (8u << 24);
 constexpr uint32_t kIdescPV = kIdescS | (1u << 16);
 
-// D (tensor memory) = / += A B with the A operand read from tensor memory: row = lane, 16-bit
-// elements packed two per 32-bit column (element 2j in the low half of column j), 8 columns per
-// K step of 16.  The B descriptor arrives as its two words so that the issuing thread only adds
-// a block offset to the low one (start address field; it never carries out of its 14 bits).
-__device__ __forceinline__ void umma_f16_ta(uint32_t tmem_d, uint32_t tmem_a, uint32_t bdesc_lo, uint32_t bdesc_hi, uint32_t idesc,
-                                            uint32_t accumulate) {
-  asm volatile("{\n.reg .pred p;\n.reg .b64 bd;\nsetp.ne.b32 p, %5, 0;\nmov.b64 bd, {%2, %3};\n"
-               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], bd, %4, p;\n}\n"
-               ::"r"(tmem_d), "r"(tmem_a), "r"(bdesc_lo), "r"(bdesc_hi), "r"(idesc), "r"(accumulate) : "memory");
-}
-// The same with both operands in shared memory.
-__device__ __forceinline__ void umma_f16_ss(uint32_t tmem_d, uint32_t adesc_lo, uint32_t adesc_hi, uint32_t bdesc_lo, uint32_t bdesc_hi,
-                                            uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n.reg .pred p;\n.reg .b64 ad, bd;\nsetp.ne.b32 p, %6, 0;\nmov.b64 ad, {%1, %2};\nmov.b64 bd, {%3, %4};\n"
-               "tcgen05.mma.cta_group::1.kind::f16 [%0], ad, bd, %5, p;\n}\n"
-               ::"r"(tmem_d), "r"(adesc_lo), "r"(adesc_hi), "r"(bdesc_lo), "r"(bdesc_hi), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void umma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
-__device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
-
-// 32 consecutive fp32 columns of this thread's tensor-memory lane
-__device__ __forceinline__ void tmem_ld32(float (&v)[32], uint32_t taddr) {
-  uint32_t r[32];
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-               "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-               "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-                 "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-                 "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-               : "r"(taddr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-}
-
 // ---- operand tiles in shared memory -------------------------------------------------------
-// K-major operand (Q; K^ with the 128 token rows of a block): element (row n, k) of a
-// ROWS x 128 fp16 tile.  Core matrix = 8 rows x 8 elements (128 bytes); the ROWS/8 core matrices
-// of one 8-element K slab are contiguous (128 B between row groups), K slabs follow each other.
-template <int ROWS>
-__device__ __forceinline__ int kmajor_unit_offset(int n, int k8) {       // byte offset of the 16-byte unit (n, k8*8..+7)
-  return (k8 * (ROWS / 8) + (n >> 3)) * 128 + (n & 7) * 16;
-}
 // MN-major operand (V^: rows = tokens (K of the MMA), contiguous index = channels): core
 // matrix = 8 tokens x 8 channels; the 16 channel groups of one 8-token slab are contiguous.
 __device__ __forceinline__ int mnmajor_unit_offset(int t, int c8) {      // byte offset of the 16-byte unit (t, c8*8..+7)
@@ -109,10 +53,6 @@ template <bool ROWS, bool IS_V> __device__ __forceinline__ int dst_unit_offset(i
   return ROWS ? t * 256 + c8 * 16 : (IS_V ? mnmajor_unit_offset(t, c8) : kmajor_unit_offset<128>(t, c8));
 }
 
-__device__ __forceinline__ uint32_t pack_h2(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 // eight 16-bit inputs (one uint4) -> eight fp16
 template <bool BF16> __device__ __forceinline__ uint4 to_fp16x8(uint4 v) {
   if (!BF16) return v;
@@ -123,31 +63,6 @@ template <bool BF16> __device__ __forceinline__ uint4 to_fp16x8(uint4 v) {
   o.w = pack_h2(__uint_as_float(v.w << 16), __uint_as_float(v.w & 0xffff0000u));
   return o;
 }
-__device__ __forceinline__ float ex2_approx(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
-  return r;
-}
-// packed fp32 pairs: one instruction for two lanes of arithmetic
-__device__ __forceinline__ uint64_t pack_f2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void unpack_f2(uint64_t v, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(v));
-}
-__device__ __forceinline__ uint64_t fma_f2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-
 // ---- dequantisation of one 32-token storage tile into the operand tiles --------------------
 // The packed layout is the one the decode kernel's lanes consume (lane = 4g + t4); the same
 // 16-byte units are read here, straight from global memory, and expanded to fp16.
@@ -340,45 +255,6 @@ constexpr int kQTileBytes = kQTile * 128 * 2;
 enum { BAR_KFULL = 0, BAR_VFULL = kStages, BAR_KFREE = 2 * kStages, BAR_VFREE = 3 * kStages,
        BAR_SFULL = 4 * kStages, BAR_PFULL = 4 * kStages + 2, BAR_OFULL = 4 * kStages + 4, BAR_COUNT = 4 * kStages + 6 };
 
-// 32 consecutive 32-bit columns of this thread's tensor-memory lane
-__device__ __forceinline__ void tmem_st32u(uint32_t taddr, const uint32_t (&v)[32]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-               "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-               "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};\n"
-               ::"r"(taddr),
-                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-                 "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
-                 "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-                 "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
-               : "memory");
-  asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const float (&v)[32]) {
-  uint32_t r[32];
-#pragma unroll
-  for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(v[i]);
-  tmem_st32u(taddr, r);
-}
-
-// 16 consecutive 32-bit columns; the store is not waited for here (tmem_st_wait)
-__device__ __forceinline__ void tmem_st16u_nowait(uint32_t taddr, const uint32_t (&v)[16]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
-               "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};\n"
-               ::"r"(taddr),
-                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
-                 "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-               : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
-__device__ __forceinline__ void tmem_ld16u(uint32_t (&r)[16], uint32_t taddr) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-               "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-                 "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-               : "r"(taddr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
-}
-
 // Where the cache of one (layer, sequence, kv head) lives, and how to reach a 32-token tile of it.
 struct KvSource {
   const CacheView* cv;
@@ -444,15 +320,6 @@ __global__ void __launch_bounds__(64) prefill_dequant_kernel(Dims dm, CacheView 
   const KvSource ks = kv_source(cv, dm, layer, b, h);
   uint8_t* dst = (warp ? vd : kd) + ((static_cast<long long>(b) * dm.n_kv_heads + h) * t_pad + pos0) * 256;
   dequant_subtile<BF16, true>(ks, pos0, 0, warp != 0, dst, lane);
-}
-
-// Descriptors of the 128-byte swizzled layouts TMA writes (bits 61..63 = 2).  K-major (K^: one
-// row of 64 channels = 128 bytes, 1 KiB between groups of 8 token rows; the leading offset is not
-// used) and MN-major (V^: 64 channels contiguous, 128 bytes between the 8 tokens of a group,
-// leading offset = distance between the two 64-channel halves, stride offset = 1 KiB between
-// groups of 8 tokens).
-__device__ __forceinline__ uint64_t make_desc_sw128(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
-  return make_desc(saddr, lbo_bytes, sbo_bytes) | (2ull << 61);
 }
 
 template <bool BF16, bool PRE>
