@@ -386,6 +386,158 @@ int moqae_validate_tables(const moqae_config* cfg, const moqae_cache* cache, int
  */
 int moqae_poll_status(const moqae_cache* cache, void* stream, int32_t* out_status);
 
+/* ------------------------------------------------------------------------------------------------
+ * Paged 16-bit cache.  Beside the quantised cache, whose sequences all have one length, stands a cache
+ * of plain 16-bit pages for sequences of any lengths: the form that the quantised results are compared
+ * with, and the home of the tokens that are not (or not yet) quantised (Section 3.2 keeps the
+ * tokens that do not fill a chunk in 16 bits).  (No counterpart in the paper.)
+ *
+ *   page   = page_size consecutive tokens of one sequence, the keys (values) of all kv heads:
+ *            k_pages[page * k_stride[0] + head * k_stride[1] + slot * k_stride[2] + channel].
+ *            page_size is 16, 32, 64, 128 or 256; the three strides count elements, are positive
+ *            multiples of 8, and leave the 128 channels of a row contiguous.  Both orders
+ *            [page][head][slot][128] and [page][slot][head][128], and keys and values side by side
+ *            in one buffer, are such strides.
+ *   token t of sequence b is row t % page_size of page block_table[b][t / page_size].
+ *   kv_len[b] = tokens of sequence b.  Entries of the table behind the last page of a sequence, and
+ *            rows of its last page behind its last token, may hold anything (NaN included) and are
+ *            never used.  Keys and values of a sequence's own tokens must be finite.
+ *   status = int32[4], zeroed by the caller, or NULL: the first device-side error and two detail
+ *            words (moqae_paged_poll_status).  MOQAE_ERR_CORRUPT_TABLE: a page index outside
+ *            0 .. n_pages - 1, or a kv_len outside 0 .. max_pages * page_size, was met (details:
+ *            sequence, entry; entry -1 for a length).  Such a page is never followed: its tokens are
+ *            read as zeros, by moqae_paged_append left out; such a length counts as 0.
+ * The struct is plain data in host memory; block_table and kv_len are read on the device, so a
+ * captured CUDA graph that is replayed sees their contents at that time.
+ */
+typedef struct moqae_paged_cache {
+  void* k_pages;
+  void* v_pages;
+  int64_t k_stride[3];         /* elements between pages, kv heads, slots */
+  int64_t v_stride[3];
+  const int32_t* block_table;  /* [batch][max_pages] */
+  const int32_t* kv_len;       /* [batch] */
+  int32_t* status;             /* int32[4] or NULL */
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t dtype;               /* MOQAE_DTYPE_* */
+  int32_t batch;
+  int32_t max_pages;           /* entries per row of block_table */
+} moqae_paged_cache;
+
+/* Rows [n][n_heads][128] of 16-bit elements: element (t, h, c) is data[t * token_stride + h * head_stride + c].
+ * Strides count elements and are multiples of 8 (>= 0; of an output no two rows may overlap), data is
+ * 16-byte aligned; so a slice of the rows that a fused projection wrote can be given as it is. */
+typedef struct moqae_rows {
+  void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+  int32_t n_heads;
+} moqae_rows;
+
+/* RMS norm of the heads and rotation by position, as moqae_norm_rope applies them. */
+typedef struct moqae_rope {
+  const float* cos_sin;        /* [n_positions][rot_dim]: cos of the rot_dim / 2 angles of a position, then their
+                                  sines; NULL with rot_dim = 0: no rotation */
+  const void* q_weight;        /* [128] in the rows' dtype; NULL: queries are not normalised */
+  const void* k_weight;        /* [128] in the rows' dtype; NULL: keys are not normalised */
+  int32_t n_positions;
+  int32_t rot_dim;             /* channels 0 .. rot_dim - 1 are rotated: a multiple of 16, 0 .. 128 */
+  int32_t interleaved;         /* pairs of a rotation: 0 = (i, i + rot_dim / 2), 1 = (2 i, 2 i + 1) */
+  float eps;                   /* >= 0, added to the mean square */
+} moqae_rope;
+
+/* How scores become weights.  x = scale * q.k;  with cap > 0  x = cap * tanh(x / cap);  with slopes
+ * x -= slopes[query head] * |query position - key position|.  A query at position p sees the tokens
+ * j <= p, with window > 0 only those with p - j < window, and with prefix_len every token j < prefix_len[b]
+ * (before or behind p; a window does not hide them).  A query that sees nothing gets zeros. */
+typedef struct moqae_attn_options {
+  const float* slopes;         /* [n_q_heads] float32, finite, or NULL */
+  const int32_t* prefix_len;   /* [batch], values below 0 count as 0, or NULL */
+  float scale;                 /* <= 0: 1/sqrt(128) */
+  float cap;                   /* 0: none */
+  int32_t window;              /* 0: none */
+} moqae_attn_options;
+
+/*
+ * Norm and rotation of the query and key heads of n_tokens tokens in one pass (Section 3.1: the rows
+ * that moqae_quantize_kv, moqae_append_kv and the attention calls take are the rotated ones).  Per head
+ * row x: with a weight  x = x / sqrt(mean(x^2) + eps) * weight;  then every pair (a, b) of the rotated
+ * channels becomes (a cos - b sin, a sin + b cos) with the angles of positions[t].  Everything is
+ * float32 and is rounded once, to dtype.
+ *   q, k may each be NULL (with its output); q_out, k_out have the head counts of q and k, may be the same
+ *   rows (in place) and must not overlap them otherwise.
+ *   positions int32 [n_tokens]: a token with a negative position is padding, its output rows are
+ *   left as they were.  So are those of a token whose position is >= n_positions (with rot_dim > 0), and
+ *   status (int32[4] or NULL) becomes MOQAE_ERR_INVALID_ARG with the token and its position.
+ */
+int moqae_norm_rope(const moqae_rope* rope, int32_t dtype, const moqae_rows* q, const moqae_rows* k,
+                    const moqae_rows* q_out, const moqae_rows* k_out, const int32_t* positions,
+                    int32_t n_tokens, int32_t* status, void* stream);
+
+/*
+ * Put the keys and values of n_tokens new tokens into their pages, the keys (and, where given, the
+ * queries) normalised and rotated as by moqae_norm_rope in the same pass.  Values are copied.
+ *   Token t belongs to sequence seq[t] (NULL: sequence t) and is its token positions[t], whose page must
+ *   be in block_table; kv_len is not read and not changed.  rope = NULL: rows are copied as they are.
+ *   q, q_out: both NULL, or the queries of the tokens and where they go.
+ *   A token with a negative position is padding and is left out whole.  So is one whose sequence,
+ *   position or page does not exist (status: MOQAE_ERR_CORRUPT_TABLE with token and position).  No two
+ *   tokens of a call may have the same sequence and position.
+ */
+int moqae_paged_append(const moqae_paged_cache* cache, const moqae_rope* rope, const moqae_rows* k,
+                       const moqae_rows* v, const moqae_rows* q, const moqae_rows* q_out,
+                       const int32_t* positions, const int32_t* seq, int32_t n_tokens, void* stream);
+
+/*
+ * Attention of one new token per sequence over its pages: for every query head h of sequence b, whose
+ * position is kv_len[b] - 1 (its own key and value have been appended),
+ *   out[b][h] = softmax(x) V  over the tokens it sees, of kv head h / (n_q_heads / n_kv_heads).
+ *   q, out rows [batch][n_q_heads][128] in the cache's dtype, n_q_heads / n_kv_heads in {1, .., 8};
+ *   options NULL: scale 1/sqrt(128), nothing else.  Tokens that are not seen are not read.
+ *   workspace: moqae_paged_decode_attn_workspace bytes, 16-byte aligned, ZEROED ONCE after it was
+ *   allocated (it ends with arrival counters that every completed call leaves at zero).  Calls, and
+ *   replays of captured calls, that share a workspace must be ordered after one another.
+ */
+int moqae_paged_decode_attn_workspace(const moqae_paged_cache* cache, int32_t n_q_heads, int64_t* out_bytes);
+int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q, const moqae_rows* out,
+                            const moqae_attn_options* options, void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+/*
+ * Attention of several new tokens per sequence over its pages (a prompt, the next piece of one, a few
+ * proposed tokens).  The query rows cu_q[b] .. cu_q[b + 1] - 1 of q belong to sequence b and are its last
+ * tokens: row i of them has position kv_len[b] - (cu_q[b + 1] - cu_q[b]) + i, so sequences do not see
+ * one another.  All keys and values have been appended.
+ *   q, out rows [n_tokens][n_q_heads][128] in the cache's dtype; cu_q int32 [batch + 1], not
+ *   decreasing, 0 <= cu_q <= n_tokens.  Rows of out that belong to no sequence (those behind
+ *   cu_q[batch], of a padded batch) are left as they were.
+ *   Weights are rounded to the cache's dtype before they meet the values, products accumulate in float32.
+ *   workspace: NULL, or moqae_paged_prefill_attn_workspace bytes under the rules of
+ *   moqae_paged_decode_attn; with one, the tokens of few queries over a long context are
+ *   shared out among the SMs.  The call encodes the pages' strides for the copy engine and refuses
+ *   strides it cannot express (MOQAE_ERR_UNSUPPORTED).
+ */
+int moqae_paged_prefill_attn_workspace(const moqae_paged_cache* cache, int32_t n_q_heads, int32_t n_tokens,
+                                       int64_t* out_bytes);
+int moqae_paged_prefill_attn(const moqae_paged_cache* cache, const moqae_rows* q, const int32_t* cu_q,
+                             int32_t n_tokens, const moqae_rows* out, const moqae_attn_options* options,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Debugging aid: every page that kv_len makes a sequence use is an index 0 .. n_pages - 1, and
+ * 0 <= kv_len <= max_pages * page_size.  Returns MOQAE_OK or MOQAE_ERR_CORRUPT_TABLE with the first
+ * offending sequence and entry (entry -1: its kv_len).  _host: block_table and kv_len are HOST arrays and
+ * nothing but them and the sizes is looked at; the other form copies them from the device (waits for `stream`).
+ */
+int moqae_paged_validate_host(const int32_t* block_table, const int32_t* kv_len, int32_t batch, int32_t max_pages,
+                              int32_t n_pages, int32_t page_size, int32_t* bad_seq, int32_t* bad_entry);
+int moqae_paged_validate(const moqae_paged_cache* cache, void* stream, int32_t* bad_seq, int32_t* bad_entry);
+
+/* Synchronous read of a paged cache's status word (MOQAE_OK where the cache has none).  Waits for `stream`. */
+int moqae_paged_poll_status(const moqae_paged_cache* cache, void* stream, int32_t* out_status);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,7 +28,10 @@ EXPORTS = ["moqae_version", "moqae_last_cuda_error", "moqae_error_string", "moqa
            "moqae_decode_attn_workspace", "moqae_decode_attn", "moqae_poll_status",
            "moqae_decode_attn_static", "moqae_decode_attn_static_max_bytes", "moqae_flush_tail", "moqae_prefill_attn",
            "moqae_prefill_attn_workspace", "moqae_decode_attn_ex", "moqae_project_quantize_kv",
-           "moqae_validate_tables", "moqae_validate_tables_host", "moqae_decode_attn_step"]
+           "moqae_validate_tables", "moqae_validate_tables_host", "moqae_decode_attn_step",
+           "moqae_norm_rope", "moqae_paged_append", "moqae_paged_decode_attn_workspace", "moqae_paged_decode_attn",
+           "moqae_paged_prefill_attn_workspace", "moqae_paged_prefill_attn", "moqae_paged_validate_host",
+           "moqae_paged_validate", "moqae_paged_poll_status"]
 
 
 class MoqaeConfig(C.Structure):
@@ -45,6 +48,27 @@ class MoqaeCache(C.Structure):
                 ("slot", C.c_void_p), ("count", C.c_void_p), ("votes", C.c_void_p),
                 ("tail_k", C.c_void_p), ("tail_v", C.c_void_p), ("tail_len", C.c_void_p),
                 ("status", C.c_void_p)]
+
+
+class MoqaePagedCache(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+                ("block_table", C.c_void_p), ("kv_len", C.c_void_p), ("status", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("dtype", C.c_int32), ("batch", C.c_int32),
+                ("max_pages", C.c_int32)]
+
+
+class MoqaeRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("n_heads", C.c_int32)]
+
+
+class MoqaeRope(C.Structure):
+    _fields_ = [("cos_sin", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("n_positions", C.c_int32),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float)]
+
+
+class MoqaeAttnOptions(C.Structure):
+    _fields_ = [("slopes", C.c_void_p), ("prefix_len", C.c_void_p), ("scale", C.c_float), ("cap", C.c_float),
+                ("window", C.c_int32)]
 
 
 class MoqaeError(RuntimeError):
@@ -110,6 +134,19 @@ def lib() -> C.CDLL:
         L.moqae_decode_attn_static.argtypes = [C.POINTER(MoqaeConfig), C.c_void_p, C.c_int32,
                                                C.POINTER(MoqaeCache), C.c_void_p, C.c_float, C.c_void_p]
         L.moqae_decode_attn_static_max_bytes.argtypes = []
+        pc, rows, opts = C.POINTER(MoqaePagedCache), C.POINTER(MoqaeRows), C.POINTER(MoqaeAttnOptions)
+        L.moqae_norm_rope.argtypes = [C.POINTER(MoqaeRope), C.c_int32, rows, rows, rows, rows, C.c_void_p, C.c_int32,
+                                      C.c_void_p, C.c_void_p]
+        L.moqae_paged_append.argtypes = [pc, C.POINTER(MoqaeRope), rows, rows, rows, rows, C.c_void_p, C.c_void_p,
+                                         C.c_int32, C.c_void_p]
+        L.moqae_paged_decode_attn_workspace.argtypes = [pc, C.c_int32, C.POINTER(C.c_int64)]
+        L.moqae_paged_decode_attn.argtypes = [pc, rows, rows, opts, C.c_void_p, C.c_int64, C.c_void_p]
+        L.moqae_paged_prefill_attn_workspace.argtypes = [pc, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
+        L.moqae_paged_prefill_attn.argtypes = [pc, rows, C.c_void_p, C.c_int32, rows, opts, C.c_void_p, C.c_int64, C.c_void_p]
+        L.moqae_paged_validate_host.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
+                                                C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+        L.moqae_paged_validate.argtypes = [pc, C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+        L.moqae_paged_poll_status.argtypes = [pc, C.c_void_p, C.POINTER(C.c_int32)]
         for name in EXPORTS:
             if name not in ("moqae_error_string",):
                 getattr(L, name).restype = C.c_int
@@ -343,4 +380,249 @@ def moqae_validate_tables_host(map_u8, slot_i32, count_i32, n_chunks, capacity):
 def moqae_poll_status(cache: Cache) -> int:
     out = C.c_int32(0)
     _check(lib().moqae_poll_status(C.byref(cache.view), _stream(), C.byref(out)), "moqae_poll_status")
+    return int(out.value)
+
+
+# ---- paged 16-bit cache ---------------------------------------------------------------------------
+
+_DTYPE_CODE = {torch.float16: DT_FP16, torch.bfloat16: DT_BF16}
+
+
+def _need(ok: bool, where: str, code: int = ERR_INVALID_ARG):
+    if not ok:
+        raise MoqaeError(code, where)
+
+
+def _vector(t, dtype, n, device, where):
+    """A contiguous tensor of `n` values on `device`, or None."""
+    if t is not None:
+        _need(t.dtype == dtype and t.numel() == n and t.is_contiguous() and t.device == device, where)
+    return t
+
+
+def _call(where, fn, device, *args):
+    """Run a library function on the current stream of the tensors' device."""
+    if device.index == torch.cuda.current_device():
+        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    if rc != OK:
+        raise MoqaeError(rc, where)
+
+
+def _rows(t, dtype, device, where, n=None):
+    """MoqaeRows of a tensor [n, heads, 128] whose rows are contiguous; None stays None."""
+    if t is None:
+        return None
+    shape, stride = t.shape, t.stride()
+    _need(t.dtype == dtype and t.device == device and len(shape) == 3 and shape[2] == 128 and (stride[2] == 1 or not t.numel())
+          and (n is None or shape[0] == n), where)
+    return MoqaeRows(t.data_ptr(), stride[0], stride[1], shape[1])
+
+
+def _ref(x):
+    return None if x is None else C.byref(x)
+
+
+@dataclass
+class Rope:
+    """A moqae_rope and the tensors it points to."""
+    view: MoqaeRope
+    dtype: torch.dtype
+    device: torch.device
+    tensors: tuple
+
+
+def rope_table(n_positions, rot_dim, base=10000.0, device="cuda"):
+    """float32 [n_positions, rot_dim]: cosines, then sines, of p * base^(-2 i / rot_dim), angles taken in 64 bits."""
+    freq = base ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / max(rot_dim, 1))
+    angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * freq
+    return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def make_rope(cos_sin, rot_dim, *, interleaved=False, q_weight=None, k_weight=None, eps=1e-6) -> Rope:
+    """Norm and rotation of moqae_norm_rope / moqae_paged_append.  cos_sin float32 [n_positions, rot_dim]
+    (rope_table), or None with rot_dim = 0; weights [128] in the rows' dtype, or None for no norm."""
+    where = "make_rope"
+    given = [t for t in (cos_sin, q_weight, k_weight) if t is not None]
+    _need(all(t.is_cuda and t.is_contiguous() and t.device == given[0].device for t in given), where)
+    _need((cos_sin is None) == (rot_dim == 0), where)
+    if cos_sin is not None:
+        _need(cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.shape[1] == rot_dim, where)
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    _need(all(w.shape == (128,) and w.dtype == weights[0].dtype and w.dtype in _DTYPE_CODE for w in weights), where)
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    view = MoqaeRope(ptr(cos_sin), ptr(q_weight), ptr(k_weight), 0 if cos_sin is None else cos_sin.shape[0], int(rot_dim),
+                     int(bool(interleaved)), float(eps))
+    return Rope(view, weights[0].dtype if weights else None, given[0].device if given else None, (cos_sin, q_weight, k_weight))
+
+
+def moqae_norm_rope(rope: Rope, q, k, positions, q_out=None, k_out=None, status=None):
+    """Norm and rotate query rows q [n, heads, 128] and key rows k (either may be None) into q_out / k_out, which
+    default to q and k themselves.  positions int32 [n], negative = padding; status int32 [4] or None."""
+    where = "moqae_norm_rope"
+    some = q if q is not None else k
+    _need(some is not None and some.is_cuda and some.dtype in _DTYPE_CODE, where)
+    dtype, device, n = some.dtype, some.device, some.shape[0]
+    _need(rope.dtype in (None, dtype) and rope.device in (None, device), where)
+    _vector(positions, torch.int32, n, device, where)
+    _vector(status, torch.int32, 4, device, where)
+    a, b = _rows(q, dtype, device, where, n), _rows(k, dtype, device, where, n)
+    c, d = (x if y is None else _rows(y, dtype, device, where, n) for x, y in ((a, q_out), (b, k_out)))
+    _call(where, lib().moqae_norm_rope, device, C.byref(rope.view), _DTYPE_CODE[dtype], _ref(a), _ref(b), _ref(c), _ref(d),
+          positions.data_ptr(), n, None if status is None else status.data_ptr())
+
+
+@dataclass
+class PagedCache:
+    """The tensors of a paged 16-bit cache and the C view handed to the library."""
+    k_pages: torch.Tensor        # [n_pages, n_kv_heads, page_size, 128], any strides of whole rows
+    v_pages: torch.Tensor
+    block_table: torch.Tensor    # int32 [batch, max_pages]
+    kv_len: torch.Tensor         # int32 [batch]
+    status: torch.Tensor         # int32 [4]
+    view: MoqaePagedCache = None
+
+    @property
+    def dtype(self):
+        return self.k_pages.dtype
+
+    @property
+    def device(self):
+        return self.k_pages.device
+
+
+def moqae_paged_bind(k_pages, v_pages, block_table, kv_len, status=None) -> PagedCache:
+    """A paged cache over the caller's tensors.  k_pages, v_pages [n_pages, n_kv_heads, page_size, 128] with
+    contiguous rows (a [n_pages, page_size, n_kv_heads, 128] buffer is given transposed); block_table int32
+    [batch, max_pages]; kv_len int32 [batch].  The contents of all of them may change between calls."""
+    where = "moqae_paged_bind"
+    _need(k_pages.is_cuda and k_pages.dtype in _DTYPE_CODE and k_pages.dim() == 4 and k_pages.shape[3] == 128, where)
+    device = k_pages.device
+    _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == device, where)
+    _need(k_pages.stride(3) == 1 and v_pages.stride(3) == 1, where)
+    _need(block_table.dim() == 2 and block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.device == device, where)
+    _vector(kv_len, torch.int32, block_table.shape[0], device, where)
+    if status is None:
+        status = torch.zeros(4, dtype=torch.int32, device=device)
+    _vector(status, torch.int32, 4, device, where)
+    view = MoqaePagedCache(k_pages.data_ptr(), v_pages.data_ptr(), (C.c_int64 * 3)(*k_pages.stride()[:3]),
+                           (C.c_int64 * 3)(*v_pages.stride()[:3]), block_table.data_ptr(), kv_len.data_ptr(), status.data_ptr(),
+                           k_pages.shape[0], k_pages.shape[2], k_pages.shape[1], _DTYPE_CODE[k_pages.dtype],
+                           block_table.shape[0], block_table.shape[1])
+    return PagedCache(k_pages, v_pages, block_table, kv_len, status, view)
+
+
+def moqae_paged_append(cache: PagedCache, k, v, positions, *, seq=None, rope: Rope = None, q=None, q_out=None):
+    """Put key and value rows k, v [n, n_kv_heads, 128] into their pages: token t is token positions[t] (negative =
+    padding) of sequence seq[t] (None: sequence t).  With `rope` keys, and queries q into q_out (default: in
+    place), are normalised and rotated on the way."""
+    where = "moqae_paged_append"
+    dtype, device = cache.k_pages.dtype, cache.k_pages.device
+    n = k.shape[0]
+    if rope is not None:
+        _need(rope.dtype in (None, dtype) and rope.device in (None, device), where)
+    _vector(positions, torch.int32, n, device, where)
+    _vector(seq, torch.int32, n, device, where)
+    _need(q is not None or q_out is None, where)
+    a, b, c = _rows(k, dtype, device, where, n), _rows(v, dtype, device, where, n), _rows(q, dtype, device, where, n)
+    d = c if q_out is None else _rows(q_out, dtype, device, where, n)
+    _call(where, lib().moqae_paged_append, device, C.byref(cache.view), None if rope is None else C.byref(rope.view), _ref(a), _ref(b),
+          _ref(c), _ref(d), positions.data_ptr(), None if seq is None else seq.data_ptr(), n)
+
+
+@dataclass
+class AttnOptions:
+    """A moqae_attn_options and the tensors it points to."""
+    view: MoqaeAttnOptions
+    slopes: torch.Tensor
+    prefix_len: torch.Tensor
+
+
+def make_attn_options(*, scale=0.0, cap=0.0, window=0, slopes=None, prefix_len=None) -> AttnOptions:
+    """Options of the paged attention calls: scale (<= 0: 1/sqrt(128)), tanh cap of the scores (0: none), sliding
+    window (0: none), slopes float32 [n_q_heads] of the distance bias, prefix_len int32 [batch]."""
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    return AttnOptions(MoqaeAttnOptions(ptr(slopes), ptr(prefix_len), float(scale), float(cap), int(window)), slopes, prefix_len)
+
+
+def _options(options, cache, n_q_heads, where):
+    if options is None:
+        return None
+    _vector(options.slopes, torch.float32, n_q_heads, cache.k_pages.device, where)
+    _vector(options.prefix_len, torch.int32, cache.block_table.shape[0], cache.k_pages.device, where)
+    return C.byref(options.view)
+
+
+def _space(workspace, device, where):
+    if workspace is None:
+        return None, 0
+    _need(workspace.is_contiguous() and workspace.device == device, where)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def moqae_paged_decode_attn_workspace(cache: PagedCache, n_q_heads) -> int:
+    out = C.c_int64(0)
+    _check(lib().moqae_paged_decode_attn_workspace(C.byref(cache.view), int(n_q_heads), C.byref(out)), "moqae_paged_decode_attn_workspace")
+    return int(out.value)
+
+
+def moqae_paged_decode_attn(cache: PagedCache, q, out, workspace, options: AttnOptions = None):
+    """Attention of one new token per sequence: q, out [batch, n_q_heads, 128] in the cache's dtype; workspace a
+    tensor of moqae_paged_decode_attn_workspace bytes, zeroed once."""
+    where = "moqae_paged_decode_attn"
+    dtype, device, n = cache.k_pages.dtype, cache.k_pages.device, cache.block_table.shape[0]
+    a, b = _rows(q, dtype, device, where, n), _rows(out, dtype, device, where, n)
+    ptr, nbytes = _space(workspace, device, where)
+    _call(where, lib().moqae_paged_decode_attn, device, C.byref(cache.view), C.byref(a), C.byref(b), _options(options, cache, a.n_heads, where),
+          ptr, nbytes)
+
+
+def moqae_paged_prefill_attn_workspace(cache: PagedCache, n_q_heads, n_tokens) -> int:
+    out = C.c_int64(0)
+    _check(lib().moqae_paged_prefill_attn_workspace(C.byref(cache.view), int(n_q_heads), int(n_tokens), C.byref(out)),
+           "moqae_paged_prefill_attn_workspace")
+    return int(out.value)
+
+
+def moqae_paged_prefill_attn(cache: PagedCache, q, cu_q, out, workspace=None, options: AttnOptions = None):
+    """Attention of the last cu_q[b + 1] - cu_q[b] tokens of every sequence: q, out [n_tokens, n_q_heads, 128] in the
+    cache's dtype, cu_q int32 [batch + 1]; workspace None, or moqae_paged_prefill_attn_workspace bytes zeroed once."""
+    where = "moqae_paged_prefill_attn"
+    dtype, device = cache.k_pages.dtype, cache.k_pages.device
+    n = q.shape[0]
+    _vector(cu_q, torch.int32, cache.block_table.shape[0] + 1, device, where)
+    a, b = _rows(q, dtype, device, where, n), _rows(out, dtype, device, where, n)
+    ptr, nbytes = _space(workspace, device, where)
+    _call(where, lib().moqae_paged_prefill_attn, device, C.byref(cache.view), C.byref(a), cu_q.data_ptr(), n, C.byref(b),
+          _options(options, cache, a.n_heads, where), ptr, nbytes)
+
+
+def moqae_paged_validate(cache: PagedCache):
+    """(code, bad_seq, bad_entry): OK, or ERR_CORRUPT_TABLE with the first offending table entry (-1: the length)."""
+    b, e = C.c_int32(-1), C.c_int32(-1)
+    with torch.cuda.device(cache.device):
+        rc = lib().moqae_paged_validate(C.byref(cache.view), torch.cuda.current_stream().cuda_stream, C.byref(b), C.byref(e))
+    if rc not in (OK, ERR_CORRUPT_TABLE):
+        raise MoqaeError(rc, "moqae_paged_validate")
+    return rc, int(b.value), int(e.value)
+
+
+def moqae_paged_validate_host(block_table, kv_len, n_pages, page_size):
+    """The same check on host numpy arrays block_table [batch, max_pages] and kv_len [batch]."""
+    import numpy as np
+    t = np.ascontiguousarray(block_table, dtype=np.int32)
+    n = np.ascontiguousarray(kv_len, dtype=np.int32)
+    b, e = C.c_int32(-1), C.c_int32(-1)
+    rc = lib().moqae_paged_validate_host(t.ctypes.data_as(C.c_void_p), n.ctypes.data_as(C.c_void_p), t.shape[0], t.shape[1],
+                                         int(n_pages), int(page_size), C.byref(b), C.byref(e))
+    return rc, int(b.value), int(e.value)
+
+
+def moqae_paged_poll_status(cache: PagedCache) -> int:
+    out = C.c_int32(0)
+    with torch.cuda.device(cache.device):
+        _check(lib().moqae_paged_poll_status(C.byref(cache.view), torch.cuda.current_stream().cuda_stream, C.byref(out)),
+               "moqae_paged_poll_status")
     return int(out.value)

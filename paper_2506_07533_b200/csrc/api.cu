@@ -101,7 +101,7 @@ int sm_count_of_current_device() {
 #pragma GCC visibility push(default)
 extern "C" {
 
-int moqae_version(void) { return 200; }
+int moqae_version(void) { return 300; }
 
 int moqae_last_cuda_error(void) { return g_last_cuda_error; }
 

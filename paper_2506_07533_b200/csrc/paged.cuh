@@ -1,0 +1,84 @@
+// Shared declarations of the paged 16-bit cache: kernel-side views and launchers.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+
+namespace moqae {
+
+// A cache of 16-bit pages as the kernels see it (passed by value).
+struct PagedView {
+  uint16_t* k;
+  uint16_t* v;
+  long long k_page, k_head, k_slot, v_page, v_head, v_slot;   // element strides
+  const int32_t* table;
+  const int32_t* kv_len;
+  int32_t* status;                                             // may be null
+  int n_pages, page_size, page_shift, n_kv_heads, batch, max_pages, dtype;
+};
+
+// rows [n][heads][128]
+struct RowsView {
+  uint16_t* data;
+  long long token, head;
+  int n_heads;
+};
+
+struct RopeView {
+  const float* cos_sin;
+  const uint16_t* q_weight;
+  const uint16_t* k_weight;
+  int n_positions, rot_dim, interleaved;
+  float eps;
+};
+
+struct AttnOptions {
+  const float* slopes;
+  const int32_t* prefix_len;
+  float scale, cap;
+  int window;
+};
+
+__device__ __forceinline__ void paged_status(int32_t* status, int code, int d0, int d1) {
+  if (status) set_status(status, code, d0, d1);
+}
+
+// kv_len[b]; a length that its row of the table cannot hold counts as 0.
+__device__ __forceinline__ int paged_len(const PagedView& pv, int b, bool report) {
+  const int n = pv.kv_len[b];
+  if (n >= 0 && n <= static_cast<long long>(pv.max_pages) * pv.page_size) return n;
+  if (report) paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, b, -1);
+  return 0;
+}
+
+// 16-bit element <-> float, in the dtype of the template
+template <bool BF16> __device__ __forceinline__ float half_bits_to_float(uint16_t u) {
+  return BF16 ? __uint_as_float(static_cast<uint32_t>(u) << 16) : __half2float(__ushort_as_half(u));
+}
+template <bool BF16> __device__ __forceinline__ float2 pair_to_float2(uint32_t u) {
+  if (BF16) return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&u));
+}
+template <bool BF16> __device__ __forceinline__ uint32_t float2_to_pair(float a, float b) {
+  if (BF16) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+cudaError_t launch_norm_rope(const RopeView& rope, int dtype, const RowsView& q, const RowsView& k, const RowsView& q_out,
+                             const RowsView& k_out, const int32_t* positions, int n_tokens, int32_t* status, cudaStream_t st);
+cudaError_t launch_paged_append(const PagedView& pv, const RopeView& rope, const RowsView& q, const RowsView& q_out,
+                                const RowsView& k, const RowsView& v, const int32_t* positions, const int32_t* seq, int n_tokens,
+                                cudaStream_t st);
+long long paged_decode_workspace_bytes(int batch, int n_kv_heads, int group);
+cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
+                                cudaStream_t st);
+long long paged_prefill_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens);
+cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
+                                 const AttnOptions& opt, void* workspace, cudaStream_t st);
+
+}  // namespace moqae
