@@ -394,7 +394,7 @@ int moqae_poll_status(const moqae_cache* cache, void* stream, int32_t* out_statu
  *
  *   page   = page_size consecutive tokens of one sequence, the keys (values) of all kv heads:
  *            k_pages[page * k_stride[0] + head * k_stride[1] + slot * k_stride[2] + channel].
- *            page_size is 16, 32, 64, 128 or 256; the three strides count elements, are positive
+ *            page_size is 16, 32, 64, 128 or 256, max_pages * page_size at most 2^30; the three strides count elements, are positive
  *            multiples of 8, and leave the 128 channels of a row contiguous.  Both orders
  *            [page][head][slot][128] and [page][slot][head][128], and keys and values side by side
  *            in one buffer, are such strides.
@@ -510,8 +510,8 @@ int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q,
  * proposed tokens).  The query rows cu_q[b] .. cu_q[b + 1] - 1 of q belong to sequence b and are its last
  * tokens: row i of them has position kv_len[b] - (cu_q[b + 1] - cu_q[b]) + i, so sequences do not see
  * one another.  All keys and values have been appended.
- *   q, out rows [n_tokens][n_q_heads][128] in the cache's dtype; cu_q int32 [batch + 1], not
- *   decreasing, 0 <= cu_q <= n_tokens.  Rows of out that belong to no sequence (those behind
+ *   q, out rows [n_tokens][n_q_heads][128] in the cache's dtype, n_tokens and batch at most 2^24;
+ *   cu_q int32 [batch + 1], not decreasing, 0 <= cu_q <= n_tokens.  Rows of out that belong to no sequence (those behind
  *   cu_q[batch], of a padded batch) are left as they were.
  *   Weights are rounded to the cache's dtype before they meet the values, products accumulate in float32.
  *   workspace: NULL, or moqae_paged_prefill_attn_workspace bytes under the rules of

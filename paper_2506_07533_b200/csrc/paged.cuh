@@ -33,6 +33,8 @@ struct RopeView {
   float eps;
 };
 
+constexpr int kMaxQueryTokens = 1 << 24;     // of one call, so that its rows and their tiles count in 32 bits
+
 struct AttnOptions {
   const float* slopes;
   const int32_t* prefix_len;

@@ -29,8 +29,8 @@ int check_pages(const moqae_paged_cache* c, PagedView* v) {
   int shift = 4;
   while (shift < 8 && (1 << shift) != c->page_size) ++shift;
   if ((1 << shift) != c->page_size) return MOQAE_ERR_UNSUPPORTED;
-  // positions are 32-bit
-  if (static_cast<int64_t>(c->max_pages) * c->page_size > (1ll << 31) - 512) return MOQAE_ERR_UNSUPPORTED;
+  // positions, and differences of them, are 32-bit
+  if (static_cast<int64_t>(c->max_pages) * c->page_size > (1ll << 30)) return MOQAE_ERR_UNSUPPORTED;
   for (int i = 0; i < 3; ++i) {
     if (c->k_stride[i] <= 0 || c->v_stride[i] <= 0) return MOQAE_ERR_INVALID_ARG;
     if (c->k_stride[i] % 8 != 0 || c->v_stride[i] % 8 != 0) return MOQAE_ERR_MISALIGNED;
@@ -126,6 +126,8 @@ int check_attention(const moqae_paged_cache* cache, const moqae_rows* q, const m
   if (rc == MOQAE_OK && qv->n_heads != ov->n_heads) rc = MOQAE_ERR_INVALID_ARG;
   if (rc == MOQAE_OK) rc = check_group(*pv, qv->n_heads);
   if (rc == MOQAE_OK) rc = check_options(options, opt);
+  // a window as long as the longest sequence hides nothing
+  if (rc == MOQAE_OK && opt->window >= static_cast<int64_t>(pv->max_pages) * pv->page_size) opt->window = 0;
   return rc;
 }
 
@@ -204,6 +206,7 @@ int moqae_paged_prefill_attn_workspace(const moqae_paged_cache* cache, int32_t n
   if (rc == MOQAE_OK) rc = check_group(pv, n_q_heads);
   if (rc != MOQAE_OK) return rc;
   if (!out_bytes || n_tokens < 0) return MOQAE_ERR_INVALID_ARG;
+  if (n_tokens > moqae::kMaxQueryTokens || pv.batch > moqae::kMaxQueryTokens) return MOQAE_ERR_UNSUPPORTED;
   *out_bytes = moqae::paged_prefill_workspace_bytes(pv.batch, pv.n_kv_heads, n_q_heads / pv.n_kv_heads, n_tokens);
   return MOQAE_OK;
 }
@@ -215,6 +218,7 @@ int moqae_paged_prefill_attn(const moqae_paged_cache* cache, const moqae_rows* q
   RowsView qv, ov;
   AttnOptions opt;
   if (n_tokens < 0) return MOQAE_ERR_INVALID_ARG;
+  if (n_tokens > moqae::kMaxQueryTokens || (cache && cache->batch > moqae::kMaxQueryTokens)) return MOQAE_ERR_UNSUPPORTED;
   const int rc = check_attention(cache, q, out, n_tokens, options, &pv, &qv, &ov, &opt);
   if (rc != MOQAE_OK) return rc;
   if (pv.batch > 0 && !cu_q) return MOQAE_ERR_INVALID_ARG;

@@ -51,7 +51,7 @@ BAD_CACHES = [
     (dict(dtype=2), mq.ERR_UNSUPPORTED), (dict(page_size=24), mq.ERR_UNSUPPORTED), (dict(page_size=8), mq.ERR_UNSUPPORTED),
     (dict(page_size=512), mq.ERR_UNSUPPORTED), (dict(page_size=0), mq.ERR_UNSUPPORTED), (dict(n_pages=-1), mq.ERR_INVALID_ARG),
     (dict(n_kv_heads=0), mq.ERR_INVALID_ARG), (dict(batch=-1), mq.ERR_INVALID_ARG), (dict(max_pages=-1), mq.ERR_INVALID_ARG),
-    (dict(max_pages=1 << 28), mq.ERR_UNSUPPORTED),                       # positions past 32 bits
+    (dict(max_pages=(1 << 26) + 1), mq.ERR_UNSUPPORTED),                 # more than 2^30 tokens
     (dict(k_stride=(4096, 0, 128)), mq.ERR_INVALID_ARG), (dict(v_stride=(4096, 2048, -128)), mq.ERR_INVALID_ARG),
     (dict(k_stride=(4096, 2048, 132)), mq.ERR_MISALIGNED), (dict(v_stride=(4100, 2048, 128)), mq.ERR_MISALIGNED),
     (dict(k_pages=None), mq.ERR_INVALID_ARG), (dict(v_pages=A + 2), mq.ERR_MISALIGNED), (dict(block_table=None), mq.ERR_INVALID_ARG),
@@ -95,6 +95,8 @@ def test_missing_arguments(lib):
     assert lib.moqae_paged_prefill_attn(c, q, A, -3, q, None, None, 0, None) == bad
     assert lib.moqae_paged_prefill_attn(c, q, A, 3, k, None, None, 0, None) == bad
     assert lib.moqae_paged_prefill_attn_workspace(c, 8, -1, C.byref(n)) == bad
+    assert lib.moqae_paged_prefill_attn_workspace(c, 8, (1 << 24) + 1, C.byref(n)) == mq.ERR_UNSUPPORTED
+    assert lib.moqae_paged_prefill_attn(c, q, A, (1 << 24) + 1, q, None, None, 0, None) == mq.ERR_UNSUPPORTED
     assert lib.moqae_paged_prefill_attn_workspace(c, 8, 3, C.byref(n)) == mq.OK and n.value > 0
     assert lib.moqae_paged_prefill_attn(c, q, A, 3, q, None, A, n.value - 1, None) == mq.ERR_WORKSPACE_TOO_SMALL
     assert lib.moqae_paged_poll_status(None, None, None) == bad
