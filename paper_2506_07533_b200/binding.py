@@ -388,36 +388,47 @@ def moqae_poll_status(cache: Cache) -> int:
 _DTYPE_CODE = {torch.float16: DT_FP16, torch.bfloat16: DT_BF16}
 
 
+# The calls below are made once per layer and generated token, so their host side is kept short: devices are
+# compared as indices, streams are taken as raw handles.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
 def _need(ok: bool, where: str, code: int = ERR_INVALID_ARG):
     if not ok:
         raise MoqaeError(code, where)
 
 
-def _vector(t, dtype, n, device, where):
-    """A contiguous tensor of `n` values on `device`, or None."""
-    if t is not None:
-        _need(t.dtype == dtype and t.numel() == n and t.is_contiguous() and t.device == device, where)
-    return t
+def _vector(t, dtype, n, index, where):
+    """Address of a contiguous tensor of `n` values on device `index`; None stays None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != index or t.numel() != n or not t.is_contiguous():
+        raise MoqaeError(ERR_INVALID_ARG, where)
+    return t.data_ptr()
 
 
-def _call(where, fn, device, *args):
-    """Run a library function on the current stream of the tensors' device."""
-    if device.index == torch.cuda.current_device():
-        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+def _call(where, fn, index, *args):
+    """Run a library function on the current stream of device `index`."""
+    if index == _current_device():
+        rc = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        with torch.cuda.device(index):
+            rc = fn(*args, _raw_stream(index))
     if rc != OK:
         raise MoqaeError(rc, where)
 
 
-def _rows(t, dtype, device, where, n=None):
+def _rows(t, dtype, index, where, n):
     """MoqaeRows of a tensor [n, heads, 128] whose rows are contiguous; None stays None."""
     if t is None:
         return None
-    shape, stride = t.shape, t.stride()
-    _need(t.dtype == dtype and t.device == device and len(shape) == 3 and shape[2] == 128 and (stride[2] == 1 or not t.numel())
-          and (n is None or shape[0] == n), where)
+    shape = t.shape
+    if t.dtype is not dtype or t.get_device() != index or len(shape) != 3 or shape[2] != 128 or shape[0] != n:
+        raise MoqaeError(ERR_INVALID_ARG, where)
+    stride = t.stride()
+    if stride[2] != 1 and t.numel():
+        raise MoqaeError(ERR_INVALID_ARG, where)
     return MoqaeRows(t.data_ptr(), stride[0], stride[1], shape[1])
 
 
@@ -430,7 +441,7 @@ class Rope:
     """A moqae_rope and the tensors it points to."""
     view: MoqaeRope
     dtype: torch.dtype
-    device: torch.device
+    device: int                  # device index, None without tensors
     tensors: tuple
 
 
@@ -446,7 +457,7 @@ def make_rope(cos_sin, rot_dim, *, interleaved=False, q_weight=None, k_weight=No
     (rope_table), or None with rot_dim = 0; weights [128] in the rows' dtype, or None for no norm."""
     where = "make_rope"
     given = [t for t in (cos_sin, q_weight, k_weight) if t is not None]
-    _need(all(t.is_cuda and t.is_contiguous() and t.device == given[0].device for t in given), where)
+    _need(all(t.is_cuda and t.is_contiguous() and t.get_device() == given[0].get_device() for t in given), where)
     _need((cos_sin is None) == (rot_dim == 0), where)
     if cos_sin is not None:
         _need(cos_sin.dtype == torch.float32 and cos_sin.dim() == 2 and cos_sin.shape[1] == rot_dim, where)
@@ -455,7 +466,7 @@ def make_rope(cos_sin, rot_dim, *, interleaved=False, q_weight=None, k_weight=No
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     view = MoqaeRope(ptr(cos_sin), ptr(q_weight), ptr(k_weight), 0 if cos_sin is None else cos_sin.shape[0], int(rot_dim),
                      int(bool(interleaved)), float(eps))
-    return Rope(view, weights[0].dtype if weights else None, given[0].device if given else None, (cos_sin, q_weight, k_weight))
+    return Rope(view, weights[0].dtype if weights else None, given[0].get_device() if given else None, (cos_sin, q_weight, k_weight))
 
 
 def moqae_norm_rope(rope: Rope, q, k, positions, q_out=None, k_out=None, status=None):
@@ -464,14 +475,13 @@ def moqae_norm_rope(rope: Rope, q, k, positions, q_out=None, k_out=None, status=
     where = "moqae_norm_rope"
     some = q if q is not None else k
     _need(some is not None and some.is_cuda and some.dtype in _DTYPE_CODE, where)
-    dtype, device, n = some.dtype, some.device, some.shape[0]
-    _need(rope.dtype in (None, dtype) and rope.device in (None, device), where)
-    _vector(positions, torch.int32, n, device, where)
-    _vector(status, torch.int32, 4, device, where)
-    a, b = _rows(q, dtype, device, where, n), _rows(k, dtype, device, where, n)
-    c, d = (x if y is None else _rows(y, dtype, device, where, n) for x, y in ((a, q_out), (b, k_out)))
-    _call(where, lib().moqae_norm_rope, device, C.byref(rope.view), _DTYPE_CODE[dtype], _ref(a), _ref(b), _ref(c), _ref(d),
-          positions.data_ptr(), n, None if status is None else status.data_ptr())
+    dtype, index, n = some.dtype, some.get_device(), some.shape[0]
+    _need(rope.dtype in (None, dtype) and rope.device in (None, index), where)
+    a, b = _rows(q, dtype, index, where, n), _rows(k, dtype, index, where, n)
+    c = a if q_out is None else _rows(q_out, dtype, index, where, n)
+    d = b if k_out is None else _rows(k_out, dtype, index, where, n)
+    _call(where, lib().moqae_norm_rope, index, C.byref(rope.view), _DTYPE_CODE[dtype], _ref(a), _ref(b), _ref(c), _ref(d),
+          _vector(positions, torch.int32, n, index, where), n, _vector(status, torch.int32, 4, index, where))
 
 
 @dataclass
@@ -482,15 +492,10 @@ class PagedCache:
     block_table: torch.Tensor    # int32 [batch, max_pages]
     kv_len: torch.Tensor         # int32 [batch]
     status: torch.Tensor         # int32 [4]
-    view: MoqaePagedCache = None
-
-    @property
-    def dtype(self):
-        return self.k_pages.dtype
-
-    @property
-    def device(self):
-        return self.k_pages.device
+    view: MoqaePagedCache
+    dtype: torch.dtype
+    device: int                  # device index
+    batch: int
 
 
 def moqae_paged_bind(k_pages, v_pages, block_table, kv_len, status=None) -> PagedCache:
@@ -499,19 +504,18 @@ def moqae_paged_bind(k_pages, v_pages, block_table, kv_len, status=None) -> Page
     [batch, max_pages]; kv_len int32 [batch].  The contents of all of them may change between calls."""
     where = "moqae_paged_bind"
     _need(k_pages.is_cuda and k_pages.dtype in _DTYPE_CODE and k_pages.dim() == 4 and k_pages.shape[3] == 128, where)
-    device = k_pages.device
-    _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.device == device, where)
+    index = k_pages.get_device()
+    _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.get_device() == index, where)
     _need(k_pages.stride(3) == 1 and v_pages.stride(3) == 1, where)
-    _need(block_table.dim() == 2 and block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.device == device, where)
-    _vector(kv_len, torch.int32, block_table.shape[0], device, where)
+    _need(block_table.dim() == 2 and block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.get_device() == index, where)
     if status is None:
-        status = torch.zeros(4, dtype=torch.int32, device=device)
-    _vector(status, torch.int32, 4, device, where)
+        status = torch.zeros(4, dtype=torch.int32, device=k_pages.device)
     view = MoqaePagedCache(k_pages.data_ptr(), v_pages.data_ptr(), (C.c_int64 * 3)(*k_pages.stride()[:3]),
-                           (C.c_int64 * 3)(*v_pages.stride()[:3]), block_table.data_ptr(), kv_len.data_ptr(), status.data_ptr(),
+                           (C.c_int64 * 3)(*v_pages.stride()[:3]), block_table.data_ptr(),
+                           _vector(kv_len, torch.int32, block_table.shape[0], index, where), _vector(status, torch.int32, 4, index, where),
                            k_pages.shape[0], k_pages.shape[2], k_pages.shape[1], _DTYPE_CODE[k_pages.dtype],
                            block_table.shape[0], block_table.shape[1])
-    return PagedCache(k_pages, v_pages, block_table, kv_len, status, view)
+    return PagedCache(k_pages, v_pages, block_table, kv_len, status, view, k_pages.dtype, index, block_table.shape[0])
 
 
 def moqae_paged_append(cache: PagedCache, k, v, positions, *, seq=None, rope: Rope = None, q=None, q_out=None):
@@ -519,17 +523,13 @@ def moqae_paged_append(cache: PagedCache, k, v, positions, *, seq=None, rope: Ro
     padding) of sequence seq[t] (None: sequence t).  With `rope` keys, and queries q into q_out (default: in
     place), are normalised and rotated on the way."""
     where = "moqae_paged_append"
-    dtype, device = cache.k_pages.dtype, cache.k_pages.device
-    n = k.shape[0]
-    if rope is not None:
-        _need(rope.dtype in (None, dtype) and rope.device in (None, device), where)
-    _vector(positions, torch.int32, n, device, where)
-    _vector(seq, torch.int32, n, device, where)
+    dtype, index, n = cache.dtype, cache.device, k.shape[0]
+    _need(rope is None or (rope.dtype in (None, dtype) and rope.device in (None, index)), where)
     _need(q is not None or q_out is None, where)
-    a, b, c = _rows(k, dtype, device, where, n), _rows(v, dtype, device, where, n), _rows(q, dtype, device, where, n)
-    d = c if q_out is None else _rows(q_out, dtype, device, where, n)
-    _call(where, lib().moqae_paged_append, device, C.byref(cache.view), None if rope is None else C.byref(rope.view), _ref(a), _ref(b),
-          _ref(c), _ref(d), positions.data_ptr(), None if seq is None else seq.data_ptr(), n)
+    a, b, c = _rows(k, dtype, index, where, n), _rows(v, dtype, index, where, n), _rows(q, dtype, index, where, n)
+    d = c if q_out is None else _rows(q_out, dtype, index, where, n)
+    _call(where, lib().moqae_paged_append, index, C.byref(cache.view), None if rope is None else C.byref(rope.view), _ref(a), _ref(b),
+          _ref(c), _ref(d), _vector(positions, torch.int32, n, index, where), _vector(seq, torch.int32, n, index, where), n)
 
 
 @dataclass
@@ -550,15 +550,15 @@ def make_attn_options(*, scale=0.0, cap=0.0, window=0, slopes=None, prefix_len=N
 def _options(options, cache, n_q_heads, where):
     if options is None:
         return None
-    _vector(options.slopes, torch.float32, n_q_heads, cache.k_pages.device, where)
-    _vector(options.prefix_len, torch.int32, cache.block_table.shape[0], cache.k_pages.device, where)
+    _vector(options.slopes, torch.float32, n_q_heads, cache.device, where)
+    _vector(options.prefix_len, torch.int32, cache.batch, cache.device, where)
     return C.byref(options.view)
 
 
-def _space(workspace, device, where):
+def _space(workspace, index, where):
     if workspace is None:
         return None, 0
-    _need(workspace.is_contiguous() and workspace.device == device, where)
+    _need(workspace.is_contiguous() and workspace.get_device() == index, where)
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
@@ -572,11 +572,11 @@ def moqae_paged_decode_attn(cache: PagedCache, q, out, workspace, options: AttnO
     """Attention of one new token per sequence: q, out [batch, n_q_heads, 128] in the cache's dtype; workspace a
     tensor of moqae_paged_decode_attn_workspace bytes, zeroed once."""
     where = "moqae_paged_decode_attn"
-    dtype, device, n = cache.k_pages.dtype, cache.k_pages.device, cache.block_table.shape[0]
-    a, b = _rows(q, dtype, device, where, n), _rows(out, dtype, device, where, n)
-    ptr, nbytes = _space(workspace, device, where)
-    _call(where, lib().moqae_paged_decode_attn, device, C.byref(cache.view), C.byref(a), C.byref(b), _options(options, cache, a.n_heads, where),
-          ptr, nbytes)
+    dtype, index, n = cache.dtype, cache.device, cache.batch
+    a, b = _rows(q, dtype, index, where, n), _rows(out, dtype, index, where, n)
+    ptr, nbytes = _space(workspace, index, where)
+    _call(where, lib().moqae_paged_decode_attn, index, C.byref(cache.view), C.byref(a), C.byref(b),
+          _options(options, cache, a.n_heads, where), ptr, nbytes)
 
 
 def moqae_paged_prefill_attn_workspace(cache: PagedCache, n_q_heads, n_tokens) -> int:
@@ -590,13 +590,11 @@ def moqae_paged_prefill_attn(cache: PagedCache, q, cu_q, out, workspace=None, op
     """Attention of the last cu_q[b + 1] - cu_q[b] tokens of every sequence: q, out [n_tokens, n_q_heads, 128] in the
     cache's dtype, cu_q int32 [batch + 1]; workspace None, or moqae_paged_prefill_attn_workspace bytes zeroed once."""
     where = "moqae_paged_prefill_attn"
-    dtype, device = cache.k_pages.dtype, cache.k_pages.device
-    n = q.shape[0]
-    _vector(cu_q, torch.int32, cache.block_table.shape[0] + 1, device, where)
-    a, b = _rows(q, dtype, device, where, n), _rows(out, dtype, device, where, n)
-    ptr, nbytes = _space(workspace, device, where)
-    _call(where, lib().moqae_paged_prefill_attn, device, C.byref(cache.view), C.byref(a), cu_q.data_ptr(), n, C.byref(b),
-          _options(options, cache, a.n_heads, where), ptr, nbytes)
+    dtype, index, n = cache.dtype, cache.device, q.shape[0]
+    a, b = _rows(q, dtype, index, where, n), _rows(out, dtype, index, where, n)
+    ptr, nbytes = _space(workspace, index, where)
+    _call(where, lib().moqae_paged_prefill_attn, index, C.byref(cache.view), C.byref(a),
+          _vector(cu_q, torch.int32, cache.batch + 1, index, where), n, C.byref(b), _options(options, cache, a.n_heads, where), ptr, nbytes)
 
 
 def moqae_paged_validate(cache: PagedCache):

@@ -1,6 +1,8 @@
 // Shared declarations of the paged 16-bit cache: kernel-side views and launchers.
 #pragma once
 
+#include <atomic>
+
 #include <cuda_bf16.h>
 
 #include "common.cuh"
@@ -69,6 +71,19 @@ template <bool BF16> __device__ __forceinline__ uint32_t float2_to_pair(float a,
   }
   const __half2 h = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// Let `kernel` use `bytes` of dynamic shared memory on the current device; the driver is asked once per device
+// (`done`: one bit per device, a variable of the kernel's own).
+template <typename K> inline cudaError_t allow_shared_memory(K* kernel, size_t bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev >= 0 && dev < 64 ? 1ull << dev : 0ull;
+  if (bit && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 cudaError_t launch_norm_rope(const RopeView& rope, int dtype, const RowsView& q, const RowsView& k, const RowsView& q_out,

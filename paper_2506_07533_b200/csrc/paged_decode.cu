@@ -488,8 +488,8 @@ template <bool BF16, bool SMALL>
 cudaError_t launch(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, int group, const Workspace& ws,
                    int grid, cudaStream_t st) {
   const size_t smem = decode_smem(group);
-  cudaError_t e = cudaFuncSetAttribute(paged_decode_kernel<BF16, SMALL>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(decode_smem(SMALL ? 4 : kMaxQueryGroup)));
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = allow_shared_memory(paged_decode_kernel<BF16, SMALL>, decode_smem(SMALL ? 4 : kMaxQueryGroup), done);
   if (e != cudaSuccess) return e;
   paged_decode_kernel<BF16, SMALL><<<grid, kWarps * 32, smem, st>>>(pv, q, out, opt, group, ws);
   return cudaGetLastError();

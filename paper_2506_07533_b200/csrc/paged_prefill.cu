@@ -21,6 +21,7 @@
 // Every mbarrier wait is bounded; on expiry the CTA records MOQAE_ERR_TIMEOUT, every role stops and the
 // tensor memory is still freed.
 #include <cstring>
+#include <type_traits>
 
 #include "paged.cuh"
 #include "umma.cuh"
@@ -50,6 +51,12 @@ enum { BAR_KFULL = 0, BAR_VFULL = kStages, BAR_KFREE = 2 * kStages, BAR_VFREE = 
 
 constexpr int kExchangeBytes = kItemRows * 2 * 4 + 2 * 8 * 2 * 4;
 constexpr size_t kSmemBytes = 1024 + 2 * kTileBytes + 2 * kStages * kTileBytes + BAR_COUNT * 8 + 24 + kExchangeBytes;
+
+__device__ __forceinline__ float rcp_approx(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
+  return r;
+}
 
 struct PrefillJob {
   RowsView q, out;
@@ -153,9 +160,19 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
   const int H = pv.n_kv_heads;
   const int per_seg = job.n_rb * H;
   const int seg = static_cast<int>(blockIdx.x) / per_seg, rest = static_cast<int>(blockIdx.x) - seg * per_seg;
-  const int h = rest / job.n_rb, flat = rest - h * job.n_rb;
-  Item it;
-  if (!find_item(pv, opt, job, flat, lane, it)) return;
+  const int flat = rest / H, h = rest - flat * H;        // heads side by side: the longest rows of all heads start first
+  __shared__ Item it;                                  // in shared memory: its fields would cost the softmax threads registers
+  __shared__ int found;
+  if (warp == 0) {
+    Item x;
+    const bool ok = find_item(pv, opt, job, flat, lane, x);
+    if (lane == 0) {
+      found = ok;
+      if (ok) it = x;
+    }
+  }
+  __syncthreads();
+  if (!found) return;
   // this CTA's piece of the walk
   const int n_seg = max(1, min(job.n_seg, it.total / kMinSegBlocks));
   if (seg >= n_seg) return;
@@ -209,7 +226,9 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     const int row = 128 * i + 32 * (warp & 3) + lane;
     // rows behind the last one take its position: they cost no extra mask and are not stored
     auto position = [&](int r) { return it.pos0 + (row0 + min(r, it.rows - 1)) / job.group; };
-    const int qpos = position(row), warp_lo = position(row - lane), warp_hi = position(row - lane + 31);
+    const int qpos = position(row);
+    // tokens all_from .. all_to are seen by every row of the warp
+    const int all_to = position(row - lane), all_from = opt.window > 0 ? position(row - lane + 31) - opt.window + 1 : -0x40000000;
     const int token = (row0 + row) / job.group, head = h * job.group + row0 + row - token * job.group;
     const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = lane_addr + 128 * i + 64 * half, p_addr = lane_addr + 128 * i + 32 * half;
@@ -217,64 +236,61 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;\n" ::"r"(1 + pair_id) : "memory"); };
     const float scale_log2 = opt.scale * kLog2e;
     const float slope = SHAPED && opt.slopes && row < it.rows ? opt.slopes[head] * kLog2e : 0.0f;
+    const float score_in = SHAPED && opt.cap > 0.0f ? 2.0f * scale_log2 / opt.cap : scale_log2, cap2 = opt.cap * kLog2e;
+    // columns 32 c .. 32 c + 31 of this thread: scores as the options shape them; column e is seen if lo < e <= hi or e < pre
+    auto scores = [&](auto masked, float (&v)[32], int c, int hi, int lo, int pre) {
+      tmem_ld32(v, s_addr + 32 * c);
+      if (SHAPED) {
+        const float dist0 = static_cast<float>(hi - 32 * c);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          float y = v[e] * score_in;
+          // tanh(z) = 1 - 2 / (exp(2 z) + 1), accurate to a few float32 roundings of the cap
+          if (opt.cap > 0.0f) y = fmaf(-2.0f * cap2, rcp_approx(ex2_approx(y) + 1.0f), cap2);
+          v[e] = fmaf(-slope, fabsf(dist0 - static_cast<float>(e)), y);
+        }
+      }
+      if (masked) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if (!((32 * c + e <= hi && 32 * c + e > lo) || 32 * c + e < pre)) v[e] = -INFINITY;
+      }
+    };
+    uint32_t pk[32];
+    // weights of this thread's 64 columns against the reference, packed; their sum
+    auto weights = [&](auto masked, float ref, int hi, int lo, int pre) -> float {
+      float sum = 0.0f;
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float v[32];
+        scores(masked, v, c, hi, lo, pre);
+        const uint64_t scale2 = pack_f2(scale_log2, scale_log2), negm2 = pack_f2(-ref, -ref);
+        uint64_t part[2] = {0ull, 0ull};
+#pragma unroll
+        for (int e2 = 0; e2 < 16; ++e2) {
+          float x0, x1;
+          const uint64_t vv = pack_f2(v[2 * e2], v[2 * e2 + 1]);
+          unpack_f2(SHAPED ? add_f2(vv, negm2) : fma_f2(vv, scale2, negm2), x0, x1);
+          const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+          part[e2 & 1] = add_f2(part[e2 & 1], pack_f2(p0, p1));
+          pk[16 * c + e2] = float2_to_pair<BF16>(p0, p1);
+        }
+        float s0, s1;
+        unpack_f2(add_f2(part[0], part[1]), s0, s1);
+        sum += s0 + s1;
+      }
+      return sum;
+    };
     float m_ref = -INFINITY, l = 0.0f;
     bool ok = true;
     for (int n = 0; n < nb && ok; ++n) {
       const int j0 = block_at(it, idx0 + n) * kBlock + 64 * half;         // token of this thread's first column
+      const int hi = qpos - j0, lo = opt.window > 0 ? hi - opt.window : -0x40000000, pre = it.prefix - j0;
+      const bool masked = !(j0 + 63 <= all_to && j0 >= all_from) && pre < 64;
       ok = __all_sync(0xffffffffu, wait(BAR_SFULL + i, n));
       if (ok) tc_fence_after();
-      const bool masked = !(j0 + 63 <= warp_lo && (opt.window == 0 || j0 > warp_hi - opt.window)) && j0 + 63 >= it.prefix;
-      // column e of the thread is seen if lo < e <= hi or e < pre
-      const int hi = qpos - j0, lo = opt.window > 0 ? hi - opt.window : -0x40000000, pre = it.prefix - j0;
-      uint32_t pk[32];
       float csum = 0.0f;
-      // weights of the 64 columns against the reference `ref`; with want_max the largest score instead
-      auto weights = [&](bool want_max, float ref, float& mx) {
-        csum = 0.0f;
-        mx = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          float v[32];
-          tmem_ld32(v, s_addr + 32 * c);
-          if (SHAPED) {
-            const float dist0 = static_cast<float>(hi - 32 * c);
-            const float in = opt.cap > 0.0f ? 2.0f * scale_log2 / opt.cap : scale_log2, cap2 = opt.cap * kLog2e;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              float y = v[e] * in;
-              // tanh(z) = 1 - 2 / (exp(2 z) + 1), accurate to a few float32 roundings of the cap
-              if (opt.cap > 0.0f) y = fmaf(-2.0f * cap2, __frcp_rn(ex2_approx(y) + 1.0f), cap2);
-              v[e] = fmaf(-slope, fabsf(dist0 - static_cast<float>(e)), y);
-            }
-          }
-          if (masked) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (!((32 * c + e <= hi && 32 * c + e > lo) || 32 * c + e < pre)) v[e] = -INFINITY;
-          }
-          if (want_max) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) mx = fmaxf(mx, v[e]);
-          }
-          const float mul = SHAPED ? 1.0f : scale_log2;
-          const uint64_t scale2 = pack_f2(mul, mul), negm2 = pack_f2(-ref, -ref);
-          uint64_t part[2] = {0ull, 0ull};
-#pragma unroll
-          for (int e2 = 0; e2 < 16; ++e2) {
-            float x0, x1;
-            const uint64_t vv = pack_f2(v[2 * e2], v[2 * e2 + 1]);
-            unpack_f2(SHAPED ? add_f2(vv, negm2) : fma_f2(vv, scale2, negm2), x0, x1);
-            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
-            part[e2 & 1] = add_f2(part[e2 & 1], pack_f2(p0, p1));
-            pk[16 * c + e2] = float2_to_pair<BF16>(p0, p1);
-          }
-          float s0, s1;
-          unpack_f2(add_f2(part[0], part[1]), s0, s1);
-          csum += s0 + s1;
-        }
-      };
-      float mx;
-      if (ok) weights(false, m_ref, mx);
+      if (ok) csum = masked ? weights(std::true_type{}, m_ref, hi, lo, pre) : weights(std::false_type{}, m_ref, hi, lo, pre);
       const bool over = ok && __any_sync(0xffffffffu, !(csum < kSumLimit));
       if (lane == 0) pair_flag[((n & 1) * 8 + pair_id) * 2 + half] = (over ? 1 : 0) | (ok ? 0 : 2);
       pair_sync();
@@ -286,7 +302,14 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       if (flags & 1) {
         // the reference moves to the row's largest score of this block (always on the first block that the
         // row sees; a row that has seen nothing yet keeps -inf and weighs its columns, all masked, against 0)
-        weights(true, 0.0f, mx);
+        float mx = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < 2; ++c) {
+          float v[32];
+          scores(std::true_type{}, v, c, hi, lo, pre);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) mx = fmaxf(mx, v[e]);
+        }
         exch[row * 2 + half] = SHAPED ? mx : mx * scale_log2;
         pair_sync();
         const float m_new = fmaxf(m_ref, ceilf(fmaxf(exch[row * 2], exch[row * 2 + 1])));
@@ -303,7 +326,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
         }
         l *= corr;
         m_ref = m_new;
-        weights(false, m_ref == -INFINITY ? 0.0f : m_ref, mx);
+        csum = weights(std::true_type{}, m_ref == -INFINITY ? 0.0f : m_ref, hi, lo, pre);
         pair_sync();
       }
       l += csum;
@@ -537,8 +560,8 @@ constexpr long long kSplitItems = 512;                // more row tiles than thi
 template <bool BF16, bool SHAPED>
 cudaError_t launch(const PagedView& pv, const AttnOptions& opt, const PrefillJob& job, const CUtensorMap& mk, const CUtensorMap& mv,
                    long long grid, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(paged_prefill_kernel<BF16, SHAPED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       static_cast<int>(kSmemBytes));
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = allow_shared_memory(paged_prefill_kernel<BF16, SHAPED>, kSmemBytes, done);
   if (e != cudaSuccess) return e;
   paged_prefill_kernel<BF16, SHAPED><<<static_cast<unsigned>(grid), kThreads, kSmemBytes, st>>>(pv, opt, job, mk, mv);
   return cudaGetLastError();
@@ -577,7 +600,7 @@ cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const i
   }
   const long long grid = items * job.n_seg;
   if (grid > 0x7fffffffll) return cudaErrorInvalidConfiguration;
-  job.box_rows = pv.page_size < kBlock ? pv.page_size : kBlock;
+  job.box_rows = pv.page_size < 64 ? pv.page_size : 64;
   // one order of dimensions serves keys and values if both are laid out alike; otherwise it is the keys'
   const long long ks[3] = {pv.k_slot, pv.k_head, pv.k_page}, vs[3] = {pv.v_slot, pv.v_head, pv.v_page};
   int order[3] = {0, 1, 2};
