@@ -34,9 +34,18 @@ constexpr int kTile = 16;                        // tokens per tile
 constexpr int kTileBytes = kTile * 256;          // of keys, and of values
 constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kMinTiles = 2;                     // a CTA is worth starting for this many tiles per warp
-constexpr int kPieceFloats = kHeadDim + 2;       // per query: 128 sums, reference, weight sum
+constexpr int kPairTiles = 48;                   // up to so many tiles per pair, a CTA takes whole pairs where it can
 constexpr float kLag = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f;
+
+// A piece: the sums of a pair's tiles, float [group][128], then (reference, weight sum) per query.
+__host__ __device__ constexpr int piece_floats_of(int group) { return (group * (kHeadDim + 2) + 3) / 4 * 4; }
+
+// total * i / n for i <= n < 256
+__device__ __forceinline__ long long share(long long total, int i, int n) {
+  if (total < (1ll << 23)) return static_cast<unsigned>(total) * static_cast<unsigned>(i) / static_cast<unsigned>(n);
+  return total * i / n;
+}
 
 // Tiles of one sequence that its query sees: tokens [lo, len) and [0, pre).
 struct Seen {
@@ -105,60 +114,54 @@ __device__ __forceinline__ void advance(Cursor& c, const PagedView& pv, const At
   } while (c.s.n == 0);
 }
 
-// Piece descriptors in shared memory: which pair a partial result belongs to.
+// Which pair a piece in shared memory belongs to.
 struct Piece {
   int pair;               // b * n_kv_heads + h, or -1
-  int whole_start, whole_end;
+  int starts, ends;       // whether it holds the pair's first and last tile
 };
 
 struct Workspace {
-  float* part;            // [ctas][2][group][kPieceFloats]
+  float* part;            // [ctas][2] pieces
   int* arrived;           // [batch * n_kv_heads]
 };
 
-// Adds `n` pieces of `group` queries and writes the finished rows (out != null) or one joined piece.
-// Piece p of query g: piece(p) + g * kPieceFloats.  Called by the whole CTA.
-template <bool BF16, bool VOLATILE, typename F>
-__device__ __forceinline__ void join_pieces(F piece, int n, int group, uint16_t* out, long long out_head, float* joined) {
-  // a warp takes query g = warp, warp + 8, ..; a lane four channels
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int g = warp; g < group; g += kWarps) {
-    auto load1 = [&](const float* p) { return VOLATILE ? __ldcg(p) : *p; };
-    float m = -INFINITY;
-    for (int p = lane; p < n; p += 32) m = fmaxf(m, load1(piece(p) + g * kPieceFloats + kHeadDim));
+// One warp adds query g of n pieces (piece(p): address of the p-th, in the order of their tokens), a lane four
+// channels, and writes the finished row (out != null) or the joined piece.
+template <bool BF16, bool REMOTE, typename F>
+__device__ __forceinline__ void join_query(F piece, int n, int group, int g, int lane, uint16_t* out, float* joined) {
+  const int at_ml = group * kHeadDim + 2 * g;
+  float m = -INFINITY, l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int p = lane; p < n; p += 32) m = fmaxf(m, REMOTE ? __ldcg(piece(p) + at_ml) : piece(p)[at_ml]);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int p = 0; p < n; ++p) {
-      const float* src = piece(p) + g * kPieceFloats;
-      const float mp = load1(src + kHeadDim), lp = load1(src + kHeadDim + 1);
-      float v[4];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {               // a piece of an odd query starts on 8 bytes
-        const float2 x = VOLATILE ? __ldcg(reinterpret_cast<const float2*>(src + 4 * lane) + j)
-                                  : *(reinterpret_cast<const float2*>(src + 4 * lane) + j);
-        v[2 * j] = x.x;
-        v[2 * j + 1] = x.y;
-      }
-      const float f = m == -INFINITY ? 0.0f : exp2_fast(mp - m);
-      l = fmaf(lp, f, l);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = fmaf(v[j], f, acc[j]);
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  for (int base = 0; base < n; base += 32) {
+    float f = 0.0f, fl = 0.0f;                    // lane p: factor of piece base + p, and its share of the weight sum
+    if (base + lane < n) {
+      const float2* ml = reinterpret_cast<const float2*>(piece(base + lane) + at_ml);
+      const float2 w = REMOTE ? __ldcg(ml) : *ml;
+      f = w.x == -INFINITY ? 0.0f : exp2_fast(w.x - m);
+      fl = w.y * f;
     }
-    if (out) {
-      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-      *reinterpret_cast<uint2*>(out + g * out_head + 4 * lane) =
-          make_uint2(float2_to_pair<BF16>(acc[0] * inv, acc[1] * inv), float2_to_pair<BF16>(acc[2] * inv, acc[3] * inv));
-    } else {
-      float* dst = joined + g * kPieceFloats;
-      *(reinterpret_cast<float2*>(dst + 4 * lane)) = make_float2(acc[0], acc[1]);
-      *(reinterpret_cast<float2*>(dst + 4 * lane) + 1) = make_float2(acc[2], acc[3]);
-      if (lane == 0) {
-        dst[kHeadDim] = m;
-        dst[kHeadDim + 1] = l;
-      }
+    const int many = min(32, n - base);
+#pragma unroll 8
+    for (int p = 0; p < many; ++p) {
+      const float4* src = reinterpret_cast<const float4*>(piece(base + p) + g * kHeadDim) + lane;
+      const float4 v = REMOTE ? __ldcg(src) : *src;
+      const float fp = __shfl_sync(0xffffffffu, f, p);
+      l += __shfl_sync(0xffffffffu, fl, p);
+      acc[0] = fmaf(v.x, fp, acc[0]);
+      acc[1] = fmaf(v.y, fp, acc[1]);
+      acc[2] = fmaf(v.z, fp, acc[2]);
+      acc[3] = fmaf(v.w, fp, acc[3]);
     }
+  }
+  if (out) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    *reinterpret_cast<uint2*>(out + 4 * lane) =
+        make_uint2(float2_to_pair<BF16>(acc[0] * inv, acc[1] * inv), float2_to_pair<BF16>(acc[2] * inv, acc[3] * inv));
+  } else {
+    *(reinterpret_cast<float4*>(joined + g * kHeadDim) + lane) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    if (lane == 0) *reinterpret_cast<float2*>(joined + at_ml) = make_float2(m, l);
   }
 }
 
@@ -168,10 +171,10 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   extern __shared__ __align__(128) uint8_t smem[];
   // [warps][stages] tiles; then the piece each warp may leave behind at the start of its range (the piece
   // at its end goes into its ring, which is empty by then); then descriptors
-  const int piece_floats = group * kPieceFloats;
+  const int piece_floats = piece_floats_of(group);
   float* head_piece = reinterpret_cast<float*>(smem + kWarps * kStages * kStageBytes);
   Piece* desc = reinterpret_cast<Piece*>(head_piece + kWarps * piece_floats);       // [2 * kWarps]
-  int* ctrl = reinterpret_cast<int*>(desc + 2 * kWarps);
+  int* turn = reinterpret_cast<int*>(desc + 2 * kWarps);                            // per pair that spans CTAs: arrivals before this one, first CTA, last CTA
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t4 = lane & 3;
@@ -179,10 +182,11 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   const uint32_t ring_u = smem_u32(ring);
 
   // ---- where the work is: total number of tiles, then this warp's piece ----
-  int mine = 0;
+  int mine = 0, first_n = 0;                      // first_n: tiles of sequence `lane`
   for (int b = lane; b < pv.batch; b += 32) {
     const Seen s = seen_of(pv, opt, b, blockIdx.x == 0 && warp == 0);
     mine += s.n;
+    if (b < 32) first_n = s.n;
     // a sequence without tokens has no tile: its rows are zeros
     if (s.n == 0 && b % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x) && warp == 0)
       for (int h = 0; h < q.n_heads; ++h)
@@ -192,34 +196,39 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
   const long long total = static_cast<long long>(mine) * pv.n_kv_heads;
-  long long ctas = (total + kWarps * kMinTiles - 1) / (kWarps * kMinTiles);
-  if (ctas > gridDim.x) ctas = gridDim.x;
-  if (blockIdx.x >= ctas) return;
-  const long long cta_lo = total * blockIdx.x / ctas, cta_hi = total * (blockIdx.x + 1) / ctas;
-  const long long lo = cta_lo + (cta_hi - cta_lo) * warp / kWarps, hi = cta_lo + (cta_hi - cta_lo) * (warp + 1) / kWarps;
+  const int pairs = pv.batch * pv.n_kv_heads;
+  // A CTA per pair while that is no more than kPairTiles tiles each: with equal lengths no pair then spans CTAs,
+  // which saves the way through the workspace (333 tokens x 8 heads: 8.1 instead of 10.5 us).  Otherwise every
+  // CTA gets at least kMinTiles tiles per warp.
+  const int most = static_cast<int>(gridDim.x);
+  int ctas = most;
+  if (total <= static_cast<long long>(most) * kWarps * kMinTiles) ctas = static_cast<int>((total + kWarps * kMinTiles - 1) / (kWarps * kMinTiles));
+  if (pairs <= most && total <= static_cast<long long>(pairs) * kPairTiles && total >= pairs) ctas = pairs;
+  const int cta = static_cast<int>(blockIdx.x);
+  if (cta >= ctas) return;
+  const long long cta_lo = share(total, cta, ctas), cta_hi = share(total, cta + 1, ctas);
+  const int in_cta = static_cast<int>(cta_hi - cta_lo);
+  const long long lo = cta_lo + share(in_cta, warp, kWarps);
+  int todo = static_cast<int>(cta_lo + share(in_cta, warp + 1, kWarps) - lo);
 
   if (threadIdx.x < 2 * kWarps) desc[threadIdx.x].pair = -1;
   __syncthreads();
 
-  int todo = static_cast<int>(hi - lo);
   if (todo > 0) {
     // ---- the sequence that holds unit `lo` ----
     Cursor put;                                   // next tile to copy
     {
-      long long before = 0;
-      int base = 0;
-      long long seq_first = 0;
-      for (; base < pv.batch; base += 32) {
+      long long before = 0, seq_first = 0;
+      for (int base = 0; base < pv.batch; base += 32) {
         const int b = base + lane;
-        const int n = b < pv.batch ? seen_of(pv, opt, b, false).n : 0;
+        const int n = base == 0 ? first_n : (b < pv.batch ? seen_of(pv, opt, b, false).n : 0);
         int inc = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const int x = __shfl_up_sync(0xffffffffu, inc, o);
           if (lane >= o) inc += x;
         }
-        const long long end = (before + inc) * pv.n_kv_heads;
-        const unsigned hit = __ballot_sync(0xffffffffu, end > lo);
+        const unsigned hit = __ballot_sync(0xffffffffu, (before + inc) * pv.n_kv_heads > lo);
         if (hit) {
           const int l = __ffs(hit) - 1;
           put.b = base + l;
@@ -240,6 +249,17 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
       return pv.table[static_cast<long long>(c.b) * pv.max_pages + ((tile_of(c.s, c.i) * kTile) >> pv.page_shift)];
     };
     int page = page_of(put);
+    // The queries of a pair are loaded while the pair before it is worked on (the next head, or the next sequence).
+    uint32_t qn[16];
+    int qn_b = put.b, qn_h = put.h;
+    auto load_q = [&]() {
+      const int gq = SMALL ? (g & 3) : g;
+      const bool real = gq < group && qn_b < pv.batch;
+      const uint16_t* src = q.data + (real ? qn_b * q.token + (qn_h * group + gq) * q.head : 0) + 2 * t4;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) qn[i] = real ? *reinterpret_cast<const uint32_t*>(src + 8 * i) : 0u;
+    };
+    load_q();
     const int unit = lane & 15, row0 = lane >> 4;
     // asynchronous copy of the next tile into stage st: rows of 16 units, unit u of row r at u ^ (r & 7)
     auto copy_tile = [&](int st) {
@@ -282,11 +302,18 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
       if (fresh) {
         fresh = false;
         from_start = get.i == 0;
-        const int gq = SMALL ? (g & 3) : g;
-        const bool real = gq < group;
-        const uint16_t* src = q.data + get.b * q.token + (get.h * group + (real ? gq : 0)) * q.head + 2 * t4;
+        if (qn_b != get.b || qn_h != get.h) {     // sequences without tokens lie between
+          qn_b = get.b;
+          qn_h = get.h;
+          load_q();
+        }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) qf[i] = real ? *reinterpret_cast<const uint32_t*>(src + 8 * i) : 0u;
+        for (int i = 0; i < 16; ++i) qf[i] = qn[i];
+        if (++qn_h == pv.n_kv_heads) {
+          qn_h = 0;
+          ++qn_b;
+        }
+        if (todo > get.s.n - get.i) load_q();     // otherwise this is the warp's last pair
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           slope[e] = opt.slopes && qi[e] < group ? opt.slopes[get.h * group + qi[e]] * kLog2e : 0.0f;
@@ -405,20 +432,17 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
             if (qq < group) {
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
-                dst[qq * kPieceFloats + 16 * i + g] = o[i][e];
-                dst[qq * kPieceFloats + 16 * i + 8 + g] = o[i][2 + e];
+                dst[qq * kHeadDim + 16 * i + g] = o[i][e];
+                dst[qq * kHeadDim + 16 * i + 8 + g] = o[i][2 + e];
               }
-              if (g == 0) {
-                dst[qq * kPieceFloats + kHeadDim] = m[e];
-                dst[qq * kPieceFloats + kHeadDim + 1] = l[e];
-              }
+              if (g == 0) *reinterpret_cast<float2*>(dst + group * kHeadDim + 2 * qq) = make_float2(m[e], l[e]);
             }
           }
           if (lane == 0) {
             Piece& d = desc[2 * warp + which];
             d.pair = get.b * pv.n_kv_heads + get.h;
-            d.whole_start = from_start;
-            d.whole_end = last_of_pair;
+            d.starts = from_start;
+            d.ends = last_of_pair;
           }
         }
         fresh = true;
@@ -433,55 +457,78 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   auto piece_at = [&](int i) -> const float* {
     return (i & 1) ? reinterpret_cast<const float*>(smem + (i >> 1) * kStages * kStageBytes) : head_piece + (i >> 1) * piece_floats;
   };
-  for (int i = 0; i < 2 * kWarps;) {
-    const int pair = desc[i].pair;
-    if (pair < 0) {
-      ++i;
-      continue;
-    }
-    int idx_n = 0, idx[2 * kWarps], end = i;
-    for (int j = i; j < 2 * kWarps; ++j) {
-      if (desc[j].pair < 0) continue;
-      if (desc[j].pair != pair) break;
-      idx[idx_n++] = j;
-      end = j;
-    }
-    const bool starts = desc[i].whole_start, ends = desc[end].whole_end;
+  const int my_pair = lane < 2 * kWarps ? desc[lane].pair : -1;
+  const unsigned valid = __ballot_sync(0xffffffffu, my_pair >= 0);
+  if (valid == 0) return;
+  auto row_of = [&](int pair, int g) -> uint16_t* {
     const int b = pair / pv.n_kv_heads, h = pair - b * pv.n_kv_heads;
-    uint16_t* dst = out.data + b * out.token + static_cast<long long>(h) * group * out.head;
-    auto local = [&](int k) { return piece_at(idx[k]); };
-    if (starts && ends) {
-      join_pieces<BF16, false>(local, idx_n, group, dst, out.head, nullptr);
-    } else {
-      float* mine_out = ws.part + (static_cast<long long>(blockIdx.x) * 2 + (starts ? 1 : 0)) * piece_floats;
-      join_pieces<BF16, false>(local, idx_n, group, nullptr, 0, mine_out);
-      // the CTAs that hold the pair's first and last tile
-      const Seen s = seen_of(pv, opt, b, false);
-      long long tiles_before = 0;
-      for (int x = lane; x < b; x += 32) tiles_before += seen_of(pv, opt, x, false).n;
+    return out.data + b * out.token + static_cast<long long>(h * group + g) * out.head;
+  };
+  // Runs of pieces of one pair; a warp takes (run, query) jobs.  A run that is not the whole pair goes to the
+  // workspace: slot 1 if it holds the pair's first tile (at most one run, the last), slot 0 otherwise (the first).
+  int job = 0, cross[2] = {-1, -1};
+  for (unsigned rest = valid; rest;) {
+    const int first = __ffs(rest) - 1, pair = __shfl_sync(0xffffffffu, my_pair, first);
+    const unsigned run = __ballot_sync(0xffffffffu, my_pair == pair);
+    rest &= ~run;
+    const bool starts = desc[first].starts, whole = starts && desc[31 - __clz(run)].ends;
+    if (!whole) cross[starts] = pair;
+    float* joined = ws.part + (static_cast<long long>(cta) * 2 + (starts ? 1 : 0)) * piece_floats;
+    for (int g2 = 0; g2 < group; ++g2, ++job)
+      if (job % kWarps == warp)
+        join_query<BF16, false>([&](int p) {
+          unsigned r = run;                       // the p-th piece of the run
+          for (; p > 0; --p) r &= r - 1;
+          return piece_at(__ffs(r) - 1);
+        }, __popc(run), group, g2, lane,
+                                whole ? row_of(pair, g2) : nullptr, joined);
+  }
+  if (cross[0] < 0 && cross[1] < 0) return;
+
+  // ---- pairs that span CTAs: the CTA that arrives last adds the pieces ----
+  auto cta_of = [&](long long unit) -> int {      // largest c with share(total, c, ctas) <= unit
+    int c = static_cast<int>(static_cast<double>(unit) * ctas / static_cast<double>(total));
+    while (c > 0 && share(total, c, ctas) > unit) --c;
+    while (c + 1 < ctas && share(total, c + 1, ctas) <= unit) ++c;
+    return c;
+  };
+  int c0 = 0, c1 = 0;
+  if (warp < 2 && cross[warp] >= 0) {
+    const int pair = cross[warp], b = pair / pv.n_kv_heads, h = pair - b * pv.n_kv_heads;
+    long long before = 0;
+    for (int x = lane; x < b; x += 32) before += x < 32 ? first_n : seen_of(pv, opt, x, false).n;
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) tiles_before += __shfl_xor_sync(0xffffffffu, tiles_before, o);
-      const long long u0 = tiles_before * pv.n_kv_heads + static_cast<long long>(h) * s.n, u1 = u0 + s.n - 1;
-      const int c0 = static_cast<int>(((u0 + 1) * ctas - 1) / total), c1 = static_cast<int>(((u1 + 1) * ctas - 1) / total);
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) ctrl[0] = atomicInc(reinterpret_cast<unsigned*>(ws.arrived) + pair, static_cast<unsigned>(c1 - c0));
-      __syncthreads();
-      if (ctrl[0] == c1 - c0) {                   // the last of the pair's CTAs adds the pieces
-        __threadfence();
-        auto remote = [&](int k) -> const float* {
-          return ws.part + (static_cast<long long>(c0 + k) * 2 + (k == 0 ? 1 : 0)) * piece_floats;
-        };
-        join_pieces<BF16, true>(remote, c1 - c0 + 1, group, dst, out.head, nullptr);
-      }
-      __syncthreads();
-    }
-    i = end + 1;
+    for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+    const int n = seen_of(pv, opt, b, false).n;
+    const long long u0 = before * pv.n_kv_heads + static_cast<long long>(h) * n;
+    c0 = cta_of(u0);
+    c1 = cta_of(u0 + n - 1);
+  }
+  __threadfence();
+  __syncthreads();
+  if (warp < 2 && cross[warp] >= 0 && lane == 0) {
+    turn[warp] = static_cast<int>(atomicInc(reinterpret_cast<unsigned*>(ws.arrived) + cross[warp], static_cast<unsigned>(c1 - c0)));
+    turn[2 + warp] = c0;
+    turn[4 + warp] = c1;
+  }
+  __syncthreads();
+  job = 0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if (cross[k] < 0) continue;
+    const int from = turn[2 + k], to = turn[4 + k];
+    if (turn[k] != to - from) continue;
+    __threadfence();
+    for (int g2 = 0; g2 < group; ++g2, ++job)
+      if (job % kWarps == warp)
+        join_query<BF16, true>([&](int p) -> const float* {
+          return ws.part + (static_cast<long long>(from + p) * 2 + (p == 0 ? 1 : 0)) * piece_floats;
+        }, to - from + 1, group, g2, lane, row_of(cross[k], g2), nullptr);
   }
 }
 
 size_t decode_smem(int group) {
-  return kWarps * kStages * kStageBytes + static_cast<size_t>(kWarps) * group * kPieceFloats * 4 + 2 * kWarps * sizeof(Piece) + 16;
+  return kWarps * kStages * kStageBytes + static_cast<size_t>(kWarps) * piece_floats_of(group) * 4 + 2 * kWarps * sizeof(Piece) + 32;
 }
 
 template <bool BF16, bool SMALL>
@@ -496,7 +543,7 @@ cudaError_t launch(const PagedView& pv, const RowsView& q, const RowsView& out, 
 }
 
 long long part_bytes(int group) {
-  const long long n = 2ll * sm_count_of_current_device() * group * kPieceFloats * 4;
+  const long long n = 2ll * sm_count_of_current_device() * piece_floats_of(group) * 4;
   return (n + 15) / 16 * 16;
 }
 
