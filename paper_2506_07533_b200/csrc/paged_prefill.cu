@@ -14,7 +14,8 @@
 //   Products, softmax and tensor memory as in the prefill attention over the quantised cache (prefill.cu):
 //   S_i = Q_i K^T (M 128, N 128, K 16 steps), two threads per row, P_i written over S_i as 16-bit pairs, O_i += P_i V
 //   with P_i as a tensor-memory operand, a reference that moves only when the weights of 64 columns
-//   would add up to more than 2^14, so O_i is rarely rescaled.  P_i is rounded to the cache's dtype (the
+//   would add up to more than 2^14, so O_i is rarely rescaled.  Blocks are walked from the last to the
+//   first: with a distance bias the largest scores come first (walking forwards moved the reference at every block).  P_i is rounded to the cache's dtype (the
 //   product takes operands of one type): 2^-9 or 2^-12 of each weight, which averages out over the tokens.
 //   Few rows.  Where the rows alone would leave SMs idle, the blocks of a row tile are cut into up to
 //   kMaxSegs pieces for as many CTAs, which leave float32 sums in the workspace; the last to arrive joins them.
@@ -138,7 +139,7 @@ __device__ __forceinline__ bool find_item(const PagedView& pv, const AttnOptions
   return false;
 }
 
-template <bool BF16, bool SHAPED>
+template <bool BF16, bool CAP, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v) {
@@ -179,7 +180,8 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
   const int idx0 = static_cast<int>(static_cast<long long>(it.total) * seg / n_seg);
   const int idx1 = static_cast<int>(static_cast<long long>(it.total) * (seg + 1) / n_seg);
   const int n_blocks = idx1 - idx0;
-  const int nb0 = min(max(it.nb[0] - idx0, 0), n_blocks), nb1 = min(max(it.nb[1] - idx0, 0), n_blocks);
+  // the piece is walked backwards, block idx1 - 1 - n at step n; tile i joins at step first0 / first1
+  const int first0 = min(max(idx1 - it.nb[0], 0), n_blocks), first1 = min(max(idx1 - it.nb[1], 0), n_blocks);
   const int row0 = it.rb * kItemRows;
 
   if (warp == kIssueWarp) {
@@ -222,7 +224,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
   if (warp < kSoftmaxWarps) {
     // ================= softmax, two threads per row (see prefill.cu) =================
     const int half = warp >> 3, i = (warp & 7) >> 2, pair_id = warp & 7;
-    const int nb = i ? nb1 : nb0;
+    const int first = i ? first1 : first0;
     const int row = 128 * i + 32 * (warp & 3) + lane;
     // rows behind the last one take its position: they cost no extra mask and are not stored
     auto position = [&](int r) { return it.pos0 + (row0 + min(r, it.rows - 1)) / job.group; };
@@ -235,19 +237,48 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     const uint32_t o_addr = lane_addr + 256 + 128 * i + 64 * half;
     auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;\n" ::"r"(1 + pair_id) : "memory"); };
     const float scale_log2 = opt.scale * kLog2e;
-    const float slope = SHAPED && opt.slopes && row < it.rows ? opt.slopes[head] * kLog2e : 0.0f;
-    const float score_in = SHAPED && opt.cap > 0.0f ? 2.0f * scale_log2 / opt.cap : scale_log2, cap2 = opt.cap * kLog2e;
-    // columns 32 c .. 32 c + 31 of this thread: scores as the options shape them; column e is seen if lo < e <= hi or e < pre
-    auto scores = [&](auto masked, float (&v)[32], int c, int hi, int lo, int pre) {
+    const float slope = BIAS && row < it.rows ? opt.slopes[head] * kLog2e : 0.0f;
+    // tanh(z) / z for |z| <= 1 as a polynomial in z^2 (minimax, own fit, relative error 6e-7), for z = x / cap2
+    // with x and cap2 in base-2 units: the coefficients take the powers of cap2
+    const float cap2 = opt.cap * kLog2e, w2 = CAP ? 1.0f / (cap2 * cap2) : 0.0f;
+    const float t1 = -0.33329042792f * w2, t2 = 0.13281433284f * w2 * w2, t3 = -0.05160567537f * w2 * w2 * w2;
+    const float t4 = 0.01674311422f * (w2 * w2) * (w2 * w2), t5 = -0.00306706037f * (w2 * w2) * (w2 * w2) * w2;
+    // Scores of columns 32 c .. 32 c + 31 in base-2 units, up to a factor and a term that `mul` and `add` give
+    // (so that both join the subtraction of the reference); column e is seen if lo < e <= hi or e < pre.
+    auto scores = [&](auto masked, float (&v)[32], int c, int hi, int lo, int pre, float& mul, float& add) {
       tmem_ld32(v, s_addr + 32 * c);
-      if (SHAPED) {
-        const float dist0 = static_cast<float>(hi - 32 * c);
+      mul = CAP || BIAS ? 1.0f : scale_log2;
+      add = 0.0f;
+      if (CAP || BIAS) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          float y = v[e] * score_in;
-          // tanh(z) = 1 - 2 / (exp(2 z) + 1), accurate to a few float32 roundings of the cap
-          if (opt.cap > 0.0f) y = fmaf(-2.0f * cap2, rcp_approx(ex2_approx(y) + 1.0f), cap2);
-          v[e] = fmaf(-slope, fabsf(dist0 - static_cast<float>(e)), y);
+        for (int e = 0; e < 32; ++e) v[e] *= scale_log2;
+      }
+      if (CAP) {
+        float big = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) big = fmaxf(big, fabsf(v[e]));
+        if (__all_sync(0xffffffffu, big <= cap2)) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float u = v[e] * v[e];
+            v[e] *= fmaf(fmaf(fmaf(fmaf(fmaf(t5, u, t4), u, t3), u, t2), u, t1), u, 0.99999940395f);
+          }
+        } else {
+          // some score passes the cap: tanh(z) = 1 - 2 / (exp(2 z) + 1), accurate to a few float32 roundings of the cap
+          const float in = 2.0f * kLog2e / cap2;
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = fmaf(-2.0f * cap2, rcp_approx(ex2_approx(v[e] * in) + 1.0f), cap2);
+        }
+      }
+      if (BIAS) {
+        const float dist = static_cast<float>(hi - 32 * c);               // of column 0
+        if (pre > 0) {                                                    // tokens behind the query may be seen
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = fmaf(-slope, fabsf(dist - static_cast<float>(e)), v[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = fmaf(slope, static_cast<float>(e), v[e]);
+          add = -slope * dist;
         }
       }
       if (masked) {
@@ -262,15 +293,15 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       float sum = 0.0f;
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        float v[32];
-        scores(masked, v, c, hi, lo, pre);
-        const uint64_t scale2 = pack_f2(scale_log2, scale_log2), negm2 = pack_f2(-ref, -ref);
+        float v[32], mul, add;
+        scores(masked, v, c, hi, lo, pre, mul, add);
+        const uint64_t scale2 = pack_f2(mul, mul), negm2 = pack_f2(add - ref, add - ref);
         uint64_t part[2] = {0ull, 0ull};
 #pragma unroll
         for (int e2 = 0; e2 < 16; ++e2) {
           float x0, x1;
           const uint64_t vv = pack_f2(v[2 * e2], v[2 * e2 + 1]);
-          unpack_f2(SHAPED ? add_f2(vv, negm2) : fma_f2(vv, scale2, negm2), x0, x1);
+          unpack_f2(CAP || BIAS ? add_f2(vv, negm2) : fma_f2(vv, scale2, negm2), x0, x1);
           const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
           part[e2 & 1] = add_f2(part[e2 & 1], pack_f2(p0, p1));
           pk[16 * c + e2] = float2_to_pair<BF16>(p0, p1);
@@ -283,15 +314,18 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     };
     float m_ref = -INFINITY, l = 0.0f;
     bool ok = true;
-    for (int n = 0; n < nb && ok; ++n) {
-      const int j0 = block_at(it, idx0 + n) * kBlock + 64 * half;         // token of this thread's first column
+    for (int n = first; n < n_blocks && ok; ++n) {
+      const int j0 = block_at(it, idx1 - 1 - n) * kBlock + 64 * half;     // token of this thread's first column
       const int hi = qpos - j0, lo = opt.window > 0 ? hi - opt.window : -0x40000000, pre = it.prefix - j0;
       const bool masked = !(j0 + 63 <= all_to && j0 >= all_from) && pre < 64;
-      ok = __all_sync(0xffffffffu, wait(BAR_SFULL + i, n));
+      ok = __all_sync(0xffffffffu, wait(BAR_SFULL + i, n - first));
       if (ok) tc_fence_after();
       float csum = 0.0f;
-      if (ok) csum = masked ? weights(std::true_type{}, m_ref, hi, lo, pre) : weights(std::false_type{}, m_ref, hi, lo, pre);
-      const bool over = ok && __any_sync(0xffffffffu, !(csum < kSumLimit));
+      bool over = n == first;                          // the first block always sets the reference
+      if (ok && !over) {
+        csum = masked ? weights(std::true_type{}, m_ref, hi, lo, pre) : weights(std::false_type{}, m_ref, hi, lo, pre);
+        over = __any_sync(0xffffffffu, !(csum < kSumLimit));
+      }
       if (lane == 0) pair_flag[((n & 1) * 8 + pair_id) * 2 + half] = (over ? 1 : 0) | (ok ? 0 : 2);
       pair_sync();
       const int flags = pair_flag[((n & 1) * 8 + pair_id) * 2] | pair_flag[((n & 1) * 8 + pair_id) * 2 + 1];
@@ -305,16 +339,18 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
         float mx = -INFINITY;
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
-          float v[32];
-          scores(std::true_type{}, v, c, hi, lo, pre);
+          float v[32], mul, add;
+          scores(std::true_type{}, v, c, hi, lo, pre, mul, add);
+          float top = v[0];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) mx = fmaxf(mx, v[e]);
+          for (int e = 1; e < 32; ++e) top = fmaxf(top, v[e]);
+          mx = fmaxf(mx, fmaf(top, mul, add));         // mul > 0
         }
-        exch[row * 2 + half] = SHAPED ? mx : mx * scale_log2;
+        exch[row * 2 + half] = mx;
         pair_sync();
         const float m_new = fmaxf(m_ref, ceilf(fmaxf(exch[row * 2], exch[row * 2 + 1])));
         const float corr = m_ref == -INFINITY ? 0.0f : ex2_approx(m_ref - m_new);
-        if (n > 0) {
+        if (n > first) {
 #pragma unroll 1
           for (int o4 = 0; o4 < 2; ++o4) {
             float o[32];
@@ -335,7 +371,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(BAR_PFULL + i));
     }
-    if (ok && nb > 0) ok = __all_sync(0xffffffffu, wait(BAR_OFULL + i, 0));
+    if (ok && first < n_blocks) ok = __all_sync(0xffffffffu, wait(BAR_OFULL + i, 0));
     exch[row * 2 + half] = l;
     pair_sync();
     if (ok) {
@@ -346,7 +382,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
 #pragma unroll 1
       for (int c4 = 0; c4 < 2; ++c4) {
         float v[32];
-        if (nb > 0) tmem_ld32(v, o_addr + 32 * c4);
+        if (first < n_blocks) tmem_ld32(v, o_addr + 32 * c4);
         if (lt == 0.0f) {                              // sees nothing here (or its tile ran no block at all)
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = 0.0f;
@@ -375,7 +411,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     const CUtensorMap* map = is_v ? &map_v : &map_k;
     const int boxes = kBlock / job.box_rows;
     int n_raw = 0;
-    auto box_token = [&](int n) { return block_at(it, idx0 + n) * kBlock + lane * job.box_rows; };
+    auto box_token = [&](int n) { return block_at(it, idx1 - 1 - n) * kBlock + lane * job.box_rows; };
     auto look_up = [&](int n) -> int {                // page of this lane's box, -1: not needed
       if (n >= n_blocks || lane >= boxes) return -1;
       const int j = box_token(n);
@@ -390,7 +426,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       const int st = n % kStages;
       const int next = look_up(n + 1);
       if (n >= kStages && !__all_sync(0xffffffffu, wait((is_v ? BAR_VFREE : BAR_KFREE) + st, n / kStages - 1))) break;
-      const int j0 = block_at(it, idx0 + n) * kBlock;
+      const int j0 = block_at(it, idx1 - 1 - n) * kBlock;
       const bool edge = is_v && (j0 + kBlock > it.kv_len || (j0 < it.win_lo && j0 + kBlock > it.prefix));
       const uint32_t full = bar((is_v ? BAR_VFULL : BAR_KFULL) + st), landed = edge ? bar(BAR_VRAW) : full;
       const unsigned need = __ballot_sync(0xffffffffu, page >= 0);
@@ -439,38 +475,39 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
         for (int k = 0; k < 8; ++k)
           umma_f16_ss(d, a_lo + 256 * k, qd_hi, b_lo + (k >> 2) * 1024 + (k & 3) * 2, kd_hi, kIdescS, k > 0);
         umma_commit(bar(BAR_SFULL + i));
-        if (i == 1 || n >= nb1) umma_commit(bar(BAR_KFREE + n % kStages));
+        if (i == 1 || n < first1) umma_commit(bar(BAR_KFREE + n % kStages));
       }
       __syncwarp();
     };
-    auto issue_pv = [&](int i, int n, bool last) {
+    auto issue_pv = [&](int i, int n) {
       if (lane == 0) {
         const uint32_t lo = vd_lo + (n % kStages) * (kTileBytes >> 4), d = tmem + 256 + 128 * i, a = tmem + 128 * i;
-        umma_f16_ta(d, a, lo, vd_hi, kIdescPV, n > 0);
+        umma_f16_ta(d, a, lo, vd_hi, kIdescPV, n > (i ? first1 : first0));
 #pragma unroll
         for (int k = 1; k < 8; ++k) umma_f16_ta(d, a + 8 * k, lo + 128 * k, vd_hi, kIdescPV, 1u);
-        if (i == 1 || n >= nb1) umma_commit(bar(BAR_VFREE + n % kStages));
-        if (last) umma_commit(bar(BAR_OFULL + i));
+        if (i == 1 || n < first1) umma_commit(bar(BAR_VFREE + n % kStages));
+        if (n + 1 == n_blocks) umma_commit(bar(BAR_OFULL + i));
       }
       __syncwarp();
     };
     bool ok = n_blocks > 0 && wait(BAR_KFULL, 0);
     if (ok) {
       tc_fence_after();
-      if (nb0 > 0) issue_s(0, 0);
-      if (nb1 > 0) issue_s(1, 0);
+      if (first0 == 0) issue_s(0, 0);
+      if (first1 == 0) issue_s(1, 0);
     }
     for (int n = 0; n < n_blocks && ok; ++n) {
       ok = wait(BAR_VFULL + n % kStages, n / kStages);
       if (ok && n + 1 < n_blocks) ok = wait(BAR_KFULL + (n + 1) % kStages, (n + 1) / kStages);
       for (int i = 0; i < 2 && ok; ++i) {
-        const int nb = i ? nb1 : nb0;
-        if (n >= nb) continue;
-        ok = wait(BAR_PFULL + i, n);
-        if (!ok) break;
+        const int first = i ? first1 : first0;
+        if (n >= first) {
+          ok = wait(BAR_PFULL + i, n - first);
+          if (!ok) break;
+        }
         tc_fence_after();
-        issue_pv(i, n, n + 1 == nb);
-        if (n + 1 < nb) issue_s(i, n + 1);
+        if (n >= first) issue_pv(i, n);
+        if (n + 1 < n_blocks && n + 1 >= first) issue_s(i, n + 1);
       }
     }
   }
@@ -557,13 +594,13 @@ int pieces(long long items, long long blocks, int sms) {
 
 constexpr long long kSplitItems = 512;                // more row tiles than this are never cut
 
-template <bool BF16, bool SHAPED>
+template <bool BF16, bool CAP, bool BIAS>
 cudaError_t launch(const PagedView& pv, const AttnOptions& opt, const PrefillJob& job, const CUtensorMap& mk, const CUtensorMap& mv,
                    long long grid, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0};
-  cudaError_t e = allow_shared_memory(paged_prefill_kernel<BF16, SHAPED>, kSmemBytes, done);
+  cudaError_t e = allow_shared_memory(paged_prefill_kernel<BF16, CAP, BIAS>, kSmemBytes, done);
   if (e != cudaSuccess) return e;
-  paged_prefill_kernel<BF16, SHAPED><<<static_cast<unsigned>(grid), kThreads, kSmemBytes, st>>>(pv, opt, job, mk, mv);
+  paged_prefill_kernel<BF16, CAP, BIAS><<<static_cast<unsigned>(grid), kThreads, kSmemBytes, st>>>(pv, opt, job, mk, mv);
   return cudaGetLastError();
 }
 
@@ -616,9 +653,13 @@ cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const i
   const void* kb = pv.n_pages > 0 ? pv.k : q.data;     // without pages nothing inside the map is ever named
   const void* vb = pv.n_pages > 0 ? pv.v : q.data;
   if (!make_page_map(&mk, kb, pv, ks, order, job.box_rows) || !make_page_map(&mv, vb, pv, vs, order, job.box_rows)) return cudaErrorNotSupported;
-  const bool bf16 = pv.dtype == MOQAE_DTYPE_BF16, shaped = opt.cap > 0.0f || opt.slopes;
-  if (bf16) return shaped ? launch<true, true>(pv, opt, job, mk, mv, grid, st) : launch<true, false>(pv, opt, job, mk, mv, grid, st);
-  return shaped ? launch<false, true>(pv, opt, job, mk, mv, grid, st) : launch<false, false>(pv, opt, job, mk, mv, grid, st);
+  auto go = [&](auto bf16) {
+    constexpr bool kBf16 = decltype(bf16)::value;
+    if (opt.cap > 0.0f)
+      return opt.slopes ? launch<kBf16, true, true>(pv, opt, job, mk, mv, grid, st) : launch<kBf16, true, false>(pv, opt, job, mk, mv, grid, st);
+    return opt.slopes ? launch<kBf16, false, true>(pv, opt, job, mk, mv, grid, st) : launch<kBf16, false, false>(pv, opt, job, mk, mv, grid, st);
+  };
+  return pv.dtype == MOQAE_DTYPE_BF16 ? go(std::true_type{}) : go(std::false_type{});
 }
 
 }  // namespace moqae
