@@ -46,9 +46,9 @@ constexpr int kMinSegBlocks = 4;                     // a piece is at least this
 constexpr int kPartFloats = kItemRows * (kHeadDim + 2);   // per piece: sums, then (reference, weight sum) per row
 
 // kfull / vfull: bytes of a block have landed (vfull of an edge block: and its rows are zeroed); vraw: the bytes of
-// an edge block of values; kfree / vfree: the products that read the stage are done; sfull, pfull, ofull as in prefill.cu
+// an edge block of values; qfull: the query rows stand in shared memory; kfree / vfree: the products that read the stage are done; sfull, pfull, ofull as in prefill.cu
 enum { BAR_KFULL = 0, BAR_VFULL = kStages, BAR_KFREE = 2 * kStages, BAR_VFREE = 3 * kStages, BAR_SFULL = 4 * kStages,
-       BAR_PFULL = BAR_SFULL + 2, BAR_OFULL = BAR_PFULL + 2, BAR_VRAW = BAR_OFULL + 2, BAR_COUNT = BAR_VRAW + 1 };
+       BAR_PFULL = BAR_SFULL + 2, BAR_OFULL = BAR_PFULL + 2, BAR_VRAW = BAR_OFULL + 2, BAR_QFULL = BAR_VRAW + 1, BAR_COUNT = BAR_QFULL + 1 };
 
 constexpr int kExchangeBytes = kItemRows * 2 * 4 + 2 * 8 * 2 * 4;
 constexpr size_t kSmemBytes = 1024 + 2 * kTileBytes + 2 * kStages * kTileBytes + BAR_COUNT * 8 + 24 + kExchangeBytes;
@@ -63,6 +63,7 @@ struct PrefillJob {
   RowsView q, out;
   const int32_t* cu_q;
   int n_tokens, group, n_rb, n_seg;                  // n_rb: upper bound of the row tiles of all sequences
+  unsigned group_inv;                                // ceil(2^32 / group)
   float* part;                                       // [n_rb][heads][n_seg][kPartFloats]
   unsigned* arrived;                                 // [n_rb][heads]
   int box_rows;                                      // slots per copy
@@ -77,6 +78,10 @@ struct Item {
   int nb[2], total;                                  // blocks of the walk each tile needs; of the item
 };
 
+// row / group (exact for rows below 2^29: the product's error is row * group / 2^32 at most)
+__device__ __forceinline__ int token_of(const PrefillJob& job, int row) {
+  return job.group == 1 ? row : static_cast<int>(__umulhi(static_cast<unsigned>(row), job.group_inv));
+}
 __device__ __forceinline__ int block_at(const Item& it, int idx) { return idx < it.n_pre ? idx : it.first + idx - it.n_pre; }
 __device__ __forceinline__ bool token_used(const Item& it, int j) { return j < it.kv_len && (j >= it.win_lo || j < it.prefix); }
 
@@ -110,7 +115,7 @@ __device__ __forceinline__ bool find_item(const PagedView& pv, const AttnOptions
       it.pos0 = it.kv_len - it.q_len;
       it.prefix = opt.prefix_len ? min(max(opt.prefix_len[it.b], 0), it.kv_len) : 0;
       const int row0 = it.rb * kItemRows;
-      const int p_lo = it.pos0 + row0 / job.group;
+      const int p_lo = it.pos0 + token_of(job, row0);
       it.win_lo = opt.window > 0 ? max(0, p_lo - opt.window + 1) : 0;
       if (it.prefix >= it.win_lo) {
         it.win_lo = 0;
@@ -124,7 +129,7 @@ __device__ __forceinline__ bool find_item(const PagedView& pv, const AttnOptions
         const int last = min(it.rows, kTileRows * (i + 1)) - 1;           // last row of the tile
         int end = 0;
         if (last >= kTileRows * i) {
-          const int p = it.pos0 + (row0 + last) / job.group;
+          const int p = it.pos0 + token_of(job, row0 + last);
           end = p >= 0 ? p / kBlock + 1 : 0;
           if (it.win_lo == 0) end = max(end, (it.prefix + kBlock - 1) / kBlock);
           end = it.n_pre + max(0, end - it.first);
@@ -172,42 +177,35 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       if (ok) it = x;
     }
   }
+  if (warp == kIssueWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
+  }
+  if (tid == kKeyWarp * 32) {
+    for (int i = 0; i < BAR_COUNT; ++i) mbar_init(bar(i), i == BAR_QFULL ? kSoftmaxWarps : (i >= BAR_PFULL && i < BAR_OFULL ? 8 : 1));
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  tc_fence_before();
   __syncthreads();
-  if (!found) return;
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  auto free_tmem = [&]() {
+    if (warp == kIssueWarp)
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  };
   // this CTA's piece of the walk
-  const int n_seg = max(1, min(job.n_seg, it.total / kMinSegBlocks));
-  if (seg >= n_seg) return;
+  const int n_seg = found ? max(1, min(job.n_seg, it.total / kMinSegBlocks)) : 0;
+  if (seg >= n_seg) {
+    free_tmem();
+    return;
+  }
   const int idx0 = static_cast<int>(static_cast<long long>(it.total) * seg / n_seg);
   const int idx1 = static_cast<int>(static_cast<long long>(it.total) * (seg + 1) / n_seg);
   const int n_blocks = idx1 - idx0;
   // the piece is walked backwards, block idx1 - 1 - n at step n; tile i joins at step first0 / first1
   const int first0 = min(max(idx1 - it.nb[0], 0), n_blocks), first1 = min(max(idx1 - it.nb[1], 0), n_blocks);
   const int row0 = it.rb * kItemRows;
-
-  if (warp == kIssueWarp) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
-  }
-  if (tid == 0) {
-    for (int i = 0; i < BAR_COUNT; ++i) mbar_init(bar(i), i >= BAR_PFULL && i < BAR_OFULL ? 8 : 1);
-    *abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
-  }
-  // the query rows as A operands (rows behind the sequence's last are zero)
-  for (int i = tid; i < kItemRows * 16; i += kThreads) {
-    const int row = i >> 4, U = i & 15;
-    uint4 v = make_uint4(0u, 0u, 0u, 0u);
-    if (row < it.rows) {
-      const int t = (row0 + row) / job.group, g = row0 + row - t * job.group;
-      v = *reinterpret_cast<const uint4*>(job.q.data + (it.q_first + t) * job.q.token + (h * job.group + g) * job.q.head + 8 * U);
-    }
-    *reinterpret_cast<uint4*>(sQ + (row >> 7) * kTileBytes + kmajor_unit_offset<128>(row & 127, U)) = v;
-  }
-  fence_async_proxy();
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
 
   // bounded wait that also gives up when another role has given up
   auto wait = [&](int which, int completion) -> bool {
@@ -227,17 +225,35 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     const int first = i ? first1 : first0;
     const int row = 128 * i + 32 * (warp & 3) + lane;
     // rows behind the last one take its position: they cost no extra mask and are not stored
-    auto position = [&](int r) { return it.pos0 + (row0 + min(r, it.rows - 1)) / job.group; };
+    auto position = [&](int r) { return it.pos0 + token_of(job, row0 + min(r, it.rows - 1)); };
     const int qpos = position(row);
     // tokens all_from .. all_to are seen by every row of the warp
     const int all_to = position(row - lane), all_from = opt.window > 0 ? position(row - lane + 31) - opt.window + 1 : -0x40000000;
-    const int token = (row0 + row) / job.group, head = h * job.group + row0 + row - token * job.group;
+    // the query rows as A operands (rows behind the sequence's last are zero): 8 units of 16 bytes per thread
+    {
+      uint4 v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int r = 32 * u + (tid >> 4), t = token_of(job, row0 + r), g = row0 + r - t * job.group;
+        v[u] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < it.rows)
+          v[u] = *reinterpret_cast<const uint4*>(job.q.data + (it.q_first + t) * job.q.token + (h * job.group + g) * job.q.head + 8 * (tid & 15));
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int r = 32 * u + (tid >> 4);
+        *reinterpret_cast<uint4*>(sQ + (r >> 7) * kTileBytes + kmajor_unit_offset<128>(r & 127, tid & 15)) = v[u];
+      }
+      fence_async_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(BAR_QFULL));
+    }
     const uint32_t lane_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
     const uint32_t s_addr = lane_addr + 128 * i + 64 * half, p_addr = lane_addr + 128 * i + 32 * half;
     const uint32_t o_addr = lane_addr + 256 + 128 * i + 64 * half;
     auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;\n" ::"r"(1 + pair_id) : "memory"); };
     const float scale_log2 = opt.scale * kLog2e;
-    const float slope = BIAS && row < it.rows ? opt.slopes[head] * kLog2e : 0.0f;
+    const float slope = BIAS && row < it.rows ? opt.slopes[h * job.group + row0 + row - token_of(job, row0 + row) * job.group] * kLog2e : 0.0f;
     // tanh(z) / z for |z| <= 1 as a polynomial in z^2 (minimax, own fit, relative error 6e-7), for z = x / cap2
     // with x and cap2 in base-2 units: the coefficients take the powers of cap2
     const float cap2 = opt.cap * kLog2e, w2 = CAP ? 1.0f / (cap2 * cap2) : 0.0f;
@@ -379,6 +395,11 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       const float lt = exch[row * 2] + exch[row * 2 + 1];
       const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
       float* piece = job.part + ((static_cast<long long>(flat) * H + h) * job.n_seg + seg) * kPartFloats;
+      // Rows leave through shared memory (the place of this tile's queries, which no product reads any more; 4 KiB
+      // per warp, 128 bytes per row, units swizzled), so that a store covers whole lines: a thread storing its
+      // own row took 32 lines per instruction, 3 us for the 64 KiB of a CTA.
+      uint8_t* stage = sQ + i * kTileBytes + ((warp & 3) * 2 + half) * 4096;
+      const int w_row = 128 * i + 32 * (warp & 3);
 #pragma unroll 1
       for (int c4 = 0; c4 < 2; ++c4) {
         float v[32];
@@ -387,17 +408,32 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = 0.0f;
         }
-        if (row < it.rows && n_seg == 1) {
-          uint4* dst = reinterpret_cast<uint4*>(job.out.data + (it.q_first + token) * job.out.token + head * job.out.head + 64 * half + 32 * c4);
+        if (n_seg == 1) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            dst[e] = make_uint4(float2_to_pair<BF16>(v[8 * e] * inv, v[8 * e + 1] * inv), float2_to_pair<BF16>(v[8 * e + 2] * inv, v[8 * e + 3] * inv),
-                                float2_to_pair<BF16>(v[8 * e + 4] * inv, v[8 * e + 5] * inv), float2_to_pair<BF16>(v[8 * e + 6] * inv, v[8 * e + 7] * inv));
-        } else if (row < it.rows) {
-          float4* dst = reinterpret_cast<float4*>(piece + row * kHeadDim + 64 * half + 32 * c4);
+            *reinterpret_cast<uint4*>(stage + lane * 128 + (((4 * c4 + e) ^ (lane & 7)) << 4)) =
+                make_uint4(float2_to_pair<BF16>(v[8 * e] * inv, v[8 * e + 1] * inv), float2_to_pair<BF16>(v[8 * e + 2] * inv, v[8 * e + 3] * inv),
+                           float2_to_pair<BF16>(v[8 * e + 4] * inv, v[8 * e + 5] * inv), float2_to_pair<BF16>(v[8 * e + 6] * inv, v[8 * e + 7] * inv));
+          if (c4 == 0) continue;
+        } else {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) dst[e >> 2] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+          for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<float4*>(stage + lane * 128 + ((e ^ (lane & 7)) << 4)) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
         }
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int r = 4 * k + (lane >> 3), u = lane & 7;
+          const uint4 x = *reinterpret_cast<const uint4*>(stage + r * 128 + ((u ^ (r & 7)) << 4));
+          if (w_row + r >= it.rows) continue;
+          if (n_seg == 1) {
+            const int t = token_of(job, row0 + w_row + r), g = row0 + w_row + r - t * job.group;
+            *reinterpret_cast<uint4*>(job.out.data + (it.q_first + t) * job.out.token + (h * job.group + g) * job.out.head + 64 * half + 8 * u) = x;
+          } else {
+            *reinterpret_cast<uint4*>(piece + (w_row + r) * kHeadDim + 64 * half + 32 * c4 + 4 * u) = x;
+          }
+        }
+        __syncwarp();
       }
       if (n_seg > 1 && half == 0 && row < it.rows)
         *reinterpret_cast<float2*>(piece + kItemRows * kHeadDim + 2 * row) = make_float2(m_ref, lt);
@@ -490,7 +526,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       }
       __syncwarp();
     };
-    bool ok = n_blocks > 0 && wait(BAR_KFULL, 0);
+    bool ok = n_blocks > 0 && wait(BAR_QFULL, 0) && wait(BAR_KFULL, 0);
     if (ok) {
       tc_fence_after();
       if (first0 == 0) issue_s(0, 0);
@@ -513,8 +549,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kIssueWarp)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  free_tmem();
 
   if (n_seg > 1) {
     // ---- the last piece of the item to arrive joins all of them, in the order of their tokens ----
@@ -527,26 +562,46 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     if (*ticket != static_cast<unsigned>(n_seg - 1)) return;
     __threadfence();
     const float* part = job.part + item * job.n_seg * kPartFloats;
-    for (int x = tid; x < it.rows * 16; x += kThreads) {
-      const int row = x >> 4, c = (x & 15) * 8;
-      const float* ml = part + kItemRows * kHeadDim + 2 * row;
-      float m = -INFINITY;
-      for (int s = 0; s < n_seg; ++s) m = fmaxf(m, __ldcg(ml + static_cast<long long>(s) * kPartFloats));
-      float lsum = 0.0f, acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      for (int s = 0; s < n_seg; ++s) {
-        const float2 w = __ldcg(reinterpret_cast<const float2*>(ml + static_cast<long long>(s) * kPartFloats));
-        const float f = w.x == -INFINITY ? 0.0f : ex2_approx(w.x - m);
-        const float4* src = reinterpret_cast<const float4*>(part + static_cast<long long>(s) * kPartFloats + row * kHeadDim + c);
-        const float4 a = __ldcg(src), b = __ldcg(src + 1);
-        lsum = fmaf(w.y, f, lsum);
-        acc[0] = fmaf(a.x, f, acc[0]); acc[1] = fmaf(a.y, f, acc[1]); acc[2] = fmaf(a.z, f, acc[2]); acc[3] = fmaf(a.w, f, acc[3]);
-        acc[4] = fmaf(b.x, f, acc[4]); acc[5] = fmaf(b.y, f, acc[5]); acc[6] = fmaf(b.z, f, acc[6]); acc[7] = fmaf(b.w, f, acc[7]);
+    // a thread takes four rows' units of 4 channels at a time, so that their loads are in flight together
+    const int units = it.rows * 32;
+    for (int base = tid; base < units; base += 4 * kThreads) {
+      float m[4], lsum[4], acc[4][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        m[k] = -INFINITY;
+        lsum[k] = acc[k][0] = acc[k][1] = acc[k][2] = acc[k][3] = 0.0f;
       }
-      const float inv = lsum == 0.0f ? 0.0f : 1.0f / lsum;
-      const int t = (row0 + row) / job.group, g = row0 + row - t * job.group;
-      *reinterpret_cast<uint4*>(job.out.data + (it.q_first + t) * job.out.token + (h * job.group + g) * job.out.head + c) =
-          make_uint4(float2_to_pair<BF16>(acc[0] * inv, acc[1] * inv), float2_to_pair<BF16>(acc[2] * inv, acc[3] * inv),
-                     float2_to_pair<BF16>(acc[4] * inv, acc[5] * inv), float2_to_pair<BF16>(acc[6] * inv, acc[7] * inv));
+      for (int s = 0; s < n_seg; ++s) {
+        const float* src = part + static_cast<long long>(s) * kPartFloats;
+        float2 w[4];
+        float4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int x = min(base + k * kThreads, units - 1);
+          w[k] = __ldcg(reinterpret_cast<const float2*>(src + kItemRows * kHeadDim) + (x >> 5));
+          v[k] = __ldcg(reinterpret_cast<const float4*>(src) + x);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {               // running reference: both sides are scaled to the larger
+          const float top = fmaxf(m[k], w[k].x);
+          const float f = w[k].x == -INFINITY ? 0.0f : ex2_approx(w[k].x - top), old = m[k] == -INFINITY ? 0.0f : ex2_approx(m[k] - top);
+          m[k] = top;
+          lsum[k] = fmaf(w[k].y, f, lsum[k] * old);
+          acc[k][0] = fmaf(v[k].x, f, acc[k][0] * old);
+          acc[k][1] = fmaf(v[k].y, f, acc[k][1] * old);
+          acc[k][2] = fmaf(v[k].z, f, acc[k][2] * old);
+          acc[k][3] = fmaf(v[k].w, f, acc[k][3] * old);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int x = base + k * kThreads, row = x >> 5, c = (x & 31) * 4;
+        if (x >= units) break;
+        const float inv = lsum[k] == 0.0f ? 0.0f : 1.0f / lsum[k];
+        const int t = token_of(job, row0 + row), g = row0 + row - t * job.group;
+        *reinterpret_cast<uint2*>(job.out.data + (it.q_first + t) * job.out.token + (h * job.group + g) * job.out.head + c) =
+            make_uint2(float2_to_pair<BF16>(acc[k][0] * inv, acc[k][1] * inv), float2_to_pair<BF16>(acc[k][2] * inv, acc[k][3] * inv));
+      }
     }
   }
 }
@@ -626,6 +681,7 @@ cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const i
   job.cu_q = cu_q;
   job.n_tokens = n_tokens;
   job.group = group;
+  job.group_inv = group > 1 ? static_cast<unsigned>(((1ull << 32) + group - 1) / group) : 0u;
   job.n_rb = static_cast<int>(n_rb);
   job.n_seg = 1;
   const long long items = n_rb * pv.n_kv_heads;
