@@ -90,8 +90,10 @@ __device__ __forceinline__ bool find_item(const PagedView& pv, const AttnOptions
   int before = 0;
   for (int base = 0; base < pv.batch; base += 32) {
     const int b = base + lane;
-    int lo = 0, hi = 0;
+    int lo = 0, hi = 0, len = 0, pre = 0;
     if (b < pv.batch) {
+      len = paged_len(pv, b, blockIdx.x == 0);
+      pre = opt.prefix_len ? min(max(opt.prefix_len[b], 0), len) : 0;
       lo = min(max(job.cu_q[b], 0), job.n_tokens);
       hi = min(max(job.cu_q[b + 1], lo), job.n_tokens);
     }
@@ -111,9 +113,9 @@ __device__ __forceinline__ bool find_item(const PagedView& pv, const AttnOptions
       const int n_l = __shfl_sync(0xffffffffu, n, l), start = before + __shfl_sync(0xffffffffu, inc, l) - n_l;
       it.rb = n_l - 1 - (flat - start);                                   // the longest rows first
       it.rows = min(kItemRows, it.q_len * job.group - it.rb * kItemRows);
-      it.kv_len = paged_len(pv, it.b, blockIdx.x == 0 && threadIdx.x == 0);
+      it.kv_len = __shfl_sync(0xffffffffu, len, l);
       it.pos0 = it.kv_len - it.q_len;
-      it.prefix = opt.prefix_len ? min(max(opt.prefix_len[it.b], 0), it.kv_len) : 0;
+      it.prefix = __shfl_sync(0xffffffffu, pre, l);
       const int row0 = it.rb * kItemRows;
       const int p_lo = it.pos0 + token_of(job, row0);
       it.win_lo = opt.window > 0 ? max(0, p_lo - opt.window + 1) : 0;
@@ -182,6 +184,8 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
   }
   if (tid == kKeyWarp * 32) {
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map_v) : "memory");
     for (int i = 0; i < BAR_COUNT; ++i) mbar_init(bar(i), i == BAR_QFULL ? kSoftmaxWarps : (i >= BAR_PFULL && i < BAR_OFULL ? 8 : 1));
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
@@ -229,7 +233,8 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     const int qpos = position(row);
     // tokens all_from .. all_to are seen by every row of the warp
     const int all_to = position(row - lane), all_from = opt.window > 0 ? position(row - lane + 31) - opt.window + 1 : -0x40000000;
-    // the query rows as A operands (rows behind the sequence's last are zero): 8 units of 16 bytes per thread
+    // the query rows as A operands, swizzled like the keys (rows behind the sequence's last are zero): 8 units of 16
+    // bytes per thread
     {
       uint4 v[8];
 #pragma unroll
@@ -242,7 +247,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int r = 32 * u + (tid >> 4);
-        *reinterpret_cast<uint4*>(sQ + (r >> 7) * kTileBytes + kmajor_unit_offset<128>(r & 127, tid & 15)) = v[u];
+        *reinterpret_cast<uint4*>(sQ + (r >> 7) * kTileBytes + ((tid >> 3) & 1) * (kTileBytes / 2) + (r & 127) * 128 + (((tid ^ r) & 7) << 4)) = v[u];
       }
       fence_async_proxy();
       __syncwarp();
@@ -298,9 +303,15 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
         }
       }
       if (masked) {
+        if (pre <= 0 && opt.window == 0) {                                // the diagonal alone
 #pragma unroll
-        for (int e = 0; e < 32; ++e)
-          if (!((32 * c + e <= hi && 32 * c + e > lo) || 32 * c + e < pre)) v[e] = -INFINITY;
+          for (int e = 0; e < 32; ++e)
+            if (32 * c + e > hi) v[e] = -INFINITY;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (!((32 * c + e <= hi && 32 * c + e > lo) || 32 * c + e < pre)) v[e] = -INFINITY;
+        }
       }
     };
     uint32_t pk[32];
@@ -337,7 +348,23 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       ok = __all_sync(0xffffffffu, wait(BAR_SFULL + i, n - first));
       if (ok) tc_fence_after();
       float csum = 0.0f;
-      bool over = n == first;                          // the first block always sets the reference
+      if (ok && n == first) {
+        // The first reference: any score that the row sees will do (its weight is then at most 1 and at least
+        // a half, and larger scores may lead by 2^14).  All rows of the warp see token all_to, if this block
+        // holds it; both threads of a row read its column, without a word between them.
+        const int col = min(all_to - (j0 - 64 * half), kBlock - 1);
+        if (col >= 0 && j0 - 64 * half + col >= all_from) {
+          uint32_t raw;
+          asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n" : "=r"(raw) : "r"(lane_addr + 128 * i + col));
+          asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+          float y = __uint_as_float(raw) * scale_log2;
+          if (CAP) y = fmaf(-2.0f * cap2, rcp_approx(ex2_approx(y * (2.0f * kLog2e / cap2)) + 1.0f), cap2);
+          if (BIAS) y -= slope * static_cast<float>(qpos - (j0 - 64 * half + col));
+          if (y > -1e30f && y < 1e30f) m_ref = ceilf(y);
+        }
+      }
+      bool over = m_ref == -INFINITY;                  // nothing seen yet
+      over = __any_sync(0xffffffffu, over);
       if (ok && !over) {
         csum = masked ? weights(std::true_type{}, m_ref, hi, lo, pre) : weights(std::false_type{}, m_ref, hi, lo, pre);
         over = __any_sync(0xffffffffu, !(csum < kSumLimit));
@@ -350,8 +377,8 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
         break;
       }
       if (flags & 1) {
-        // the reference moves to the row's largest score of this block (always on the first block that the
-        // row sees; a row that has seen nothing yet keeps -inf and weighs its columns, all masked, against 0)
+        // the reference moves to the row's largest score of this block (a row that has seen nothing yet keeps
+        // -inf and weighs its columns, all masked, against 0)
         float mx = -INFINITY;
 #pragma unroll 1
         for (int c = 0; c < 2; ++c) {
@@ -498,7 +525,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     // ================= MMA issue (one thread) =================
     constexpr uint32_t kFormat = BF16 ? (1u << 7) | (1u << 10) : 0u;      // operand type
     constexpr uint32_t kIdescS = (1u << 4) | kFormat | (16u << 17) | (8u << 24), kIdescPV = kIdescS | (1u << 16);
-    const uint64_t qd = make_desc(smem_u32(sQ), 2048, 128);
+    const uint64_t qd = make_desc_sw128(smem_u32(sQ), 16, 1024);
     const uint64_t kd = make_desc_sw128(smem_u32(sK), 16, 1024), vd = make_desc_sw128(smem_u32(sV), kTileBytes / 2, 1024);
     const uint32_t qd_lo = static_cast<uint32_t>(qd), qd_hi = static_cast<uint32_t>(qd >> 32);
     const uint32_t kd_lo = static_cast<uint32_t>(kd), kd_hi = static_cast<uint32_t>(kd >> 32);
@@ -509,7 +536,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
         const uint32_t a_lo = qd_lo + i * (kTileBytes >> 4), b_lo = kd_lo + (n % kStages) * (kTileBytes >> 4), d = tmem + 128 * i;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          umma_f16_ss(d, a_lo + 256 * k, qd_hi, b_lo + (k >> 2) * 1024 + (k & 3) * 2, kd_hi, kIdescS, k > 0);
+          umma_f16_ss(d, a_lo + (k >> 2) * 1024 + (k & 3) * 2, qd_hi, b_lo + (k >> 2) * 1024 + (k & 3) * 2, kd_hi, kIdescS, k > 0);
         umma_commit(bar(BAR_SFULL + i));
         if (i == 1 || n < first1) umma_commit(bar(BAR_KFREE + n % kStages));
       }
