@@ -35,6 +35,7 @@ constexpr int kTileBytes = kTile * 256;          // of keys, and of values
 constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kMinTiles = 2;                     // a CTA is worth starting for this many tiles per warp
 constexpr int kPairTiles = 48;                   // up to so many tiles per pair, a CTA takes whole pairs where it can
+constexpr int kPairCost = 1;                     // what a pair costs beside its tiles, in tiles (its queries, its result)
 constexpr float kLag = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -51,6 +52,7 @@ __device__ __forceinline__ long long share(long long total, int i, int n) {
 struct Seen {
   int len, lo, pre;       // pre <= lo
   int n_pre, first, n;    // tiles of the prefix, first tile behind them, number of tiles
+  __device__ __forceinline__ int units() const { return n > 0 ? n + kPairCost : 0; }
 };
 __device__ __forceinline__ Seen seen_of(const PagedView& pv, const AttnOptions& opt, int b, bool report) {
   Seen s;
@@ -98,20 +100,23 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
-// A position in the order of all tiles: tile `i` of sequence b, head h.
+// A position in the order of all tiles: tile `i` of sequence b, head h.  Work is shared out in units: a pair is
+// kPairCost units without a tile, then one unit per tile.
 struct Cursor {
   int b, h, i;
   Seen s;
 };
-__device__ __forceinline__ void advance(Cursor& c, const PagedView& pv, const AttnOptions& opt) {
-  if (++c.i < c.s.n) return;
+// To the next tile; returns the units that this passes.
+__device__ __forceinline__ int advance(Cursor& c, const PagedView& pv, const AttnOptions& opt) {
+  if (++c.i < c.s.n) return 1;
   c.i = 0;
-  if (++c.h < pv.n_kv_heads) return;
+  if (++c.h < pv.n_kv_heads) return 1 + kPairCost;
   c.h = 0;
   do {
-    if (++c.b >= pv.batch) return;
+    if (++c.b >= pv.batch) break;
     c.s = seen_of(pv, opt, c.b, false);
   } while (c.s.n == 0);
+  return 1 + kPairCost;
 }
 
 // Which pair a piece in shared memory belongs to.
@@ -182,11 +187,11 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   const uint32_t ring_u = smem_u32(ring);
 
   // ---- where the work is: total number of tiles, then this warp's piece ----
-  int mine = 0, first_n = 0;                      // first_n: tiles of sequence `lane`
+  int mine = 0, first_n = 0;                      // first_n: units of a head of sequence `lane`
   for (int b = lane; b < pv.batch; b += 32) {
     const Seen s = seen_of(pv, opt, b, blockIdx.x == 0 && warp == 0);
-    mine += s.n;
-    if (b < 32) first_n = s.n;
+    mine += s.units();
+    if (b < 32) first_n = s.units();
     // a sequence without tokens has no tile: its rows are zeros
     if (s.n == 0 && b % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x) && warp == 0)
       for (int h = 0; h < q.n_heads; ++h)
@@ -203,7 +208,7 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   const int most = static_cast<int>(gridDim.x);
   int ctas = most;
   if (total <= static_cast<long long>(most) * kWarps * kMinTiles) ctas = static_cast<int>((total + kWarps * kMinTiles - 1) / (kWarps * kMinTiles));
-  if (pairs <= most && total <= static_cast<long long>(pairs) * kPairTiles && total >= pairs) ctas = pairs;
+  if (pairs <= most && total <= static_cast<long long>(pairs) * (kPairTiles + kPairCost) && total >= pairs) ctas = pairs;
   const int cta = static_cast<int>(blockIdx.x);
   if (cta >= ctas) return;
   const long long cta_lo = share(total, cta, ctas), cta_hi = share(total, cta + 1, ctas);
@@ -221,7 +226,7 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
       long long before = 0, seq_first = 0;
       for (int base = 0; base < pv.batch; base += 32) {
         const int b = base + lane;
-        const int n = base == 0 ? first_n : (b < pv.batch ? seen_of(pv, opt, b, false).n : 0);
+        const int n = base == 0 ? first_n : (b < pv.batch ? seen_of(pv, opt, b, false).units() : 0);
         int inc = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -239,8 +244,12 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
       }
       put.s = seen_of(pv, opt, put.b, false);
       const int off = static_cast<int>(lo - seq_first);
-      put.h = off / put.s.n;
-      put.i = off - put.h * put.s.n;
+      put.h = off / put.s.units();
+      put.i = off - put.h * put.s.units() - kPairCost;
+      if (put.i < 0) {                            // the piece opens with units that hold no tile
+        todo += put.i;
+        put.i = 0;
+      }
     }
     Cursor get = put;                             // next tile to work on
     int to_put = todo;
@@ -278,8 +287,7 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
         cp_async16(d, kp + 2 * r * pv.k_slot, see);
         cp_async16(d + kTileBytes, vp + 2 * r * pv.v_slot, see);
       }
-      advance(put, pv, opt);
-      --to_put;
+      to_put -= advance(put, pv, opt);
       page = to_put > 0 ? page_of(put) : -1;
     };
 #pragma unroll
@@ -296,7 +304,7 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
     bool from_start = false;
     bool fresh = true;                            // the next tile opens a pair
     int stage = 0;
-    for (; todo > 0; --todo) {
+    while (todo > 0) {
       if (to_put > 0) copy_tile((stage + kStages - 1) % kStages);
       cp_async_commit();
       if (fresh) {
@@ -313,7 +321,7 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
           qn_h = 0;
           ++qn_b;
         }
-        if (todo > get.s.n - get.i) load_q();     // otherwise this is the warp's last pair
+        if (todo > get.s.n - get.i + kPairCost) load_q();   // otherwise this is the warp's last pair
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           slope[e] = opt.slopes && qi[e] < group ? opt.slopes[get.h * group + qi[e]] * kLog2e : 0.0f;
@@ -398,8 +406,8 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
       __syncwarp();                               // the stage may be filled again
       stage = stage + 1 == kStages ? 0 : stage + 1;
 
-      const bool last_of_pair = get.i + 1 == get.s.n;
-      if (last_of_pair || todo == 1) {
+      const bool last_of_pair = get.i + 1 == get.s.n, last_of_all = todo <= (last_of_pair ? 1 + kPairCost : 1);
+      if (last_of_pair || last_of_all) {
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -422,7 +430,7 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
         } else {
           const int which = from_start ? 1 : 0;
           float* dst = which ? reinterpret_cast<float*>(ring) : head_piece + warp * piece_floats;
-          if (which) {                            // the ring holds no tile that is still needed: todo == 1
+          if (which) {                            // the ring holds no tile that is still needed: this was the warp's last
             cp_async_wait<0>();
             __syncwarp();
           }
@@ -447,7 +455,7 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
         }
         fresh = true;
       }
-      advance(get, pv, opt);
+      todo -= advance(get, pv, opt);
     }
     cp_async_wait<0>();
   }
@@ -496,12 +504,12 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   if (warp < 2 && cross[warp] >= 0) {
     const int pair = cross[warp], b = pair / pv.n_kv_heads, h = pair - b * pv.n_kv_heads;
     long long before = 0;
-    for (int x = lane; x < b; x += 32) before += x < 32 ? first_n : seen_of(pv, opt, x, false).n;
+    for (int x = lane; x < b; x += 32) before += x < 32 ? first_n : seen_of(pv, opt, x, false).units();
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-    const int n = seen_of(pv, opt, b, false).n;
+    const int n = seen_of(pv, opt, b, false).units();
     const long long u0 = before * pv.n_kv_heads + static_cast<long long>(h) * n;
-    c0 = cta_of(u0);
+    c0 = cta_of(u0 + kPairCost);
     c1 = cta_of(u0 + n - 1);
   }
   __threadfence();
