@@ -82,6 +82,15 @@ def test_prefill_options(dtype, hq, hkv, opt, workspace):
     check(c, q, cu, prefill(c, q, cu, workspace, **opt), **opt)
 
 
+@pytest.mark.parametrize("window", list(range(900, 1160, 17)))
+def test_prefill_windows_of_uneven_row_tiles(window):
+    """Few row tiles over a long window, which are cut into pieces; the tiles between the first and the last of a
+    sequence may see a block more than either."""
+    c = pages([5000 + window], 2, 16, BF, 91)
+    cu, q = starts([150]), randn(150, 8, 128, dtype=BF, seed=window)
+    check(c, q, cu, prefill(c, q, cu, window=window), window=window)
+
+
 def test_prefill_tokens_before_every_window_may_hold_anything():
     c = pages([4000], 2, 16, BF, 41)
     cu, q = starts([50]), randn(50, 8, 128, dtype=BF, seed=8)
