@@ -94,6 +94,10 @@ cudaError_t launch_paged_append(const PagedView& pv, const RopeView& rope, const
 long long paged_decode_workspace_bytes(int batch, int n_kv_heads, int group);
 cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
                                 cudaStream_t st);
+bool paged_few_rows(int batch, int group, int n_tokens);
+long long paged_few_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens);
+cudaError_t launch_paged_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
+                             const AttnOptions& opt, void* workspace, cudaStream_t st);
 long long paged_prefill_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens);
 cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                                  const AttnOptions& opt, void* workspace, cudaStream_t st);

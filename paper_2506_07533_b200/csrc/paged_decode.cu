@@ -1,26 +1,29 @@
-// Attention of one new token per sequence over a paged 16-bit cache (moqae_paged_decode_attn).
+// Attention of one new token per sequence over a paged 16-bit cache (moqae_paged_decode_attn), and of a few
+// (moqae_paged_prefill_attn where the sequences bring so few rows that the large tiles would be empty).
 //
-// Every cached row is used once per kv head, by the n_q_heads / n_kv_heads <= 8 queries of its group,
-// so the kernel is bound by the bytes of the pages; all else is arranged to keep copies in flight.
+// Every cached row is used once per kv head, by the queries of its group, so the kernel is bound by the bytes of
+// the pages; all else is arranged to keep copies in flight.
 //
-//   Work.  The unit is a tile of 16 tokens of one (sequence, kv head): 4 KiB of keys, 4 KiB of
-//   values, always inside one page.  All tiles that some query sees, in the order (sequence, head, token),
-//   are cut into equal contiguous pieces, one per CTA and, inside it, one per warp: lengths may be as
-//   uneven as they like, every warp streams the same number of bytes, and only tiles at the ends of a
-//   piece belong to pairs that others work on too.  kv_len is read on the device; every warp finds its
-//   own piece with a scan over the sequences.
-//   Copies.  A warp owns a ring of kStages tiles and fills it with 16-byte asynchronous copies, row by
-//   row (any strides); rows that are not seen are filled with zeros instead of being read.
-//   Products, on mma.sync m16n8k16: S^T = K q^T (16 tokens x 8 queries), whose accumulators, transposed
-//   by movmatrix, are the B operand of O^T += V^T P^T.  A 128 x 8 output per 8 KiB leaves the tensor
-//   pipe idle either way; this form needs no operand expansion and no accumulator outside registers.
-//   Weights are kept as high + low 16-bit halves, so rounding them costs nothing visible: with a query group
-//   of at most four the low halves ride in the unused columns 4..7, otherwise they take a second product.
-//   Softmax against a reference that moves only when a score exceeds it by 2^kLag (base-2 units): one
-//   vote per tile instead of a reduction over lanes.
-//   Joining.  A warp that has a pair to itself writes the result.  Other pieces meet in shared memory
-//   after the CTA's last tile; a pair that spans CTAs goes through the workspace, and the CTA that
-//   arrives last adds the pieces in the order of their tokens (results do not depend on timing).
+//   Rows.  The query rows of a (sequence, kv head) are its tokens times the query heads of the group (row r =
+//   token r / group, head r % group); up to 8 of them (one token) or 16 (several) make a set.
+//   Work.  The unit is a tile of 16 tokens of one (set, kv head), a "pair": 4 KiB of keys, 4 KiB of values,
+//   always inside one page.  All tiles that some row sees, in the order (sequence, set, head, token), are cut into
+//   equal contiguous pieces, one per CTA and, inside it, one per warp: lengths may be as uneven as they like, every
+//   warp streams the same number of bytes, and only tiles at the ends of a piece belong to pairs that others
+//   work on too.  Lengths are read on the device; every warp finds its own piece with a scan over the sequences.
+//   Copies.  A warp owns a ring of tiles and fills it with 16-byte asynchronous copies, row by row (any strides);
+//   rows that are not seen are filled with zeros instead of being read.
+//   Products, on mma.sync m16n8k16: S^T = K q^T (16 tokens x 8 rows), whose accumulators, transposed by movmatrix,
+//   are the B operand of O^T += V^T P^T.  A 128 x 8 output per 8 KiB leaves the tensor pipe idle either way; this
+//   form needs no operand expansion and no accumulator outside registers.
+//   Weights of a single token are kept as high + low 16-bit halves, so rounding them costs nothing visible: with a
+//   query group of at most four the low halves ride in the unused columns 4..7, otherwise they take a second
+//   product.  Those of several tokens are rounded to the cache's dtype, as in the large tiles.
+//   Softmax against a reference that moves only when a score exceeds it by 2^kLag (base-2 units): one vote per
+//   tile instead of a reduction over lanes.
+//   Joining.  A warp that has a pair to itself writes the result.  Other pieces meet in shared memory after the
+//   CTA's last tile; a pair that spans CTAs goes through the workspace, and the CTA that arrives last adds the
+//   pieces in the order of their tokens (results do not depend on timing).
 #include "paged.cuh"
 #include "ptx.cuh"
 
@@ -29,18 +32,24 @@ namespace moqae {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kStages = 3;                       // tiles in flight or in use per warp
 constexpr int kTile = 16;                        // tokens per tile
 constexpr int kTileBytes = kTile * 256;          // of keys, and of values
 constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kMinTiles = 2;                     // a CTA is worth starting for this many tiles per warp
 constexpr int kPairTiles = 48;                   // up to so many tiles per pair, a CTA takes whole pairs where it can
 constexpr int kPairCost = 1;                     // what a pair costs beside its tiles, in tiles (its queries, its result)
+constexpr int kFewRows = 48;                     // see paged_few_rows
 constexpr float kLag = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// A piece: the sums of a pair's tiles, float [group][128], then (reference, weight sum) per query.
-__host__ __device__ constexpr int piece_floats_of(int group) { return (group * (kHeadDim + 2) + 3) / 4 * 4; }
+// How a launch forms its sets: one token of a group of at most 4 or 8 heads, or up to 16 rows of several tokens.
+enum { kOne4, kOne8, kFew16 };
+__host__ __device__ constexpr int set_rows(int form) { return form == kFew16 ? 16 : 8; }
+// tiles in flight or in use per warp (the pieces of 16 rows take the room of the third)
+__host__ __device__ constexpr int stages_of(int form) { return form == kFew16 ? 2 : 3; }
+
+// A piece: the sums of a pair's tiles, float [rows][128], then (reference, weight sum) per row.
+__host__ __device__ constexpr int piece_floats_of(int rows) { return (rows * (kHeadDim + 2) + 3) / 4 * 4; }
 
 // total * i / n for i <= n < 256
 __device__ __forceinline__ long long share(long long total, int i, int n) {
@@ -48,21 +57,55 @@ __device__ __forceinline__ long long share(long long total, int i, int n) {
   return total * i / n;
 }
 
-// Tiles of one sequence that its query sees: tokens [lo, len) and [0, pre).
+struct DecodeJob {
+  RowsView q, out;
+  const int32_t* cu_q;    // null: one token per sequence
+  int n_tokens, group;
+  float* part;            // [ctas][2] pieces
+  int* arrived;           // [sets][n_kv_heads]
+};
+
+// A set of rows and the tiles that they see: tokens [lo, len) and [0, pre).
 struct Seen {
   int len, lo, pre;       // pre <= lo
   int n_pre, first, n;    // tiles of the prefix, first tile behind them, number of tiles
+  int sets;               // of the sequence
+  int row0, rows;         // rows of the set
+  int q_first, pos0;      // row of the queries, and position, of the sequence's first query token
+  int prefix;             // what every row sees
   __device__ __forceinline__ int units() const { return n > 0 ? n + kPairCost : 0; }
 };
-__device__ __forceinline__ Seen seen_of(const PagedView& pv, const AttnOptions& opt, int b, bool report) {
+template <int FORM>
+__device__ __forceinline__ Seen seen_of(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, int b, int set, bool report) {
   Seen s;
-  s.len = paged_len(pv, b, report);
-  s.lo = opt.window > 0 ? max(0, s.len - opt.window) : 0;
-  s.pre = opt.prefix_len ? min(max(opt.prefix_len[b], 0), s.len) : 0;
+  const int kv_len = paged_len(pv, b, report);
+  s.prefix = opt.prefix_len ? min(max(opt.prefix_len[b], 0), kv_len) : 0;
+  int p_first;
+  if (FORM == kFew16) {
+    s.q_first = min(max(job.cu_q[b], 0), job.n_tokens);
+    const int q_n = min(max(job.cu_q[b + 1], s.q_first), job.n_tokens) - s.q_first;
+    const int rows = q_n * job.group;
+    s.sets = (rows + 15) / 16;
+    s.row0 = set * 16;
+    s.rows = min(16, rows - s.row0);
+    s.pos0 = kv_len - q_n;
+    p_first = s.pos0 + s.row0 / job.group;
+    s.len = s.rows > 0 ? max(s.pos0 + (s.row0 + s.rows - 1) / job.group + 1, s.prefix) : 0;
+    s.len = max(s.len, 0);
+  } else {
+    s.sets = 1;
+    s.row0 = 0;
+    s.rows = job.group;
+    s.q_first = b;
+    s.pos0 = p_first = kv_len - 1;
+    s.len = kv_len;
+  }
+  s.lo = opt.window > 0 ? max(0, p_first + 1 - opt.window) : 0;
+  s.pre = min(s.prefix, s.len);
   if (s.pre >= s.lo) s.lo = s.pre = 0;
   s.n_pre = (s.pre + kTile - 1) / kTile;
   s.first = max(s.lo / kTile, s.n_pre);
-  s.n = s.n_pre + (s.len + kTile - 1) / kTile - s.first;
+  s.n = s.n_pre + max(0, (s.len + kTile - 1) / kTile - s.first);
   return s;
 }
 __device__ __forceinline__ int tile_of(const Seen& s, int i) { return i < s.n_pre ? i : s.first + i - s.n_pre; }
@@ -100,41 +143,47 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
-// A position in the order of all tiles: tile `i` of sequence b, head h.  Work is shared out in units: a pair is
-// kPairCost units without a tile, then one unit per tile.
+// A position in the order of all tiles: tile i of set `set` of sequence b, head h.  Work is shared out in units: a pair
+// is kPairCost units without a tile, then one unit per tile.
 struct Cursor {
-  int b, h, i;
+  int b, set, h, i;
+  int flat;               // sets before this one, of all sequences
   Seen s;
 };
 // To the next tile; returns the units that this passes.
-__device__ __forceinline__ int advance(Cursor& c, const PagedView& pv, const AttnOptions& opt) {
+template <int FORM> __device__ __forceinline__ int advance(Cursor& c, const PagedView& pv, const AttnOptions& opt, const DecodeJob& job) {
   if (++c.i < c.s.n) return 1;
   c.i = 0;
   if (++c.h < pv.n_kv_heads) return 1 + kPairCost;
   c.h = 0;
   do {
-    if (++c.b >= pv.batch) break;
-    c.s = seen_of(pv, opt, c.b, false);
+    ++c.flat;
+    if (++c.set >= c.s.sets) {
+      c.set = 0;
+      do {
+        if (++c.b >= pv.batch) return 1 + kPairCost;
+        c.s = seen_of<FORM>(pv, opt, job, c.b, 0, false);
+      } while (c.s.sets == 0);
+    } else {
+      c.s = seen_of<FORM>(pv, opt, job, c.b, c.set, false);
+    }
   } while (c.s.n == 0);
   return 1 + kPairCost;
 }
 
 // Which pair a piece in shared memory belongs to.
 struct Piece {
-  int pair;               // b * n_kv_heads + h, or -1
+  int pair;               // set * n_kv_heads + h, or -1
   int starts, ends;       // whether it holds the pair's first and last tile
+  int b, set, n;          // sequence, its set, tiles of the pair
+  long long unit;         // unit of the pair's first tile
 };
 
-struct Workspace {
-  float* part;            // [ctas][2] pieces
-  int* arrived;           // [batch * n_kv_heads]
-};
-
-// One warp adds query g of n pieces (piece(p): address of the p-th, in the order of their tokens), a lane four
+// One warp adds row g of n pieces (piece(p): address of the p-th, in the order of their tokens), a lane four
 // channels, and writes the finished row (out != null) or the joined piece.
 template <bool BF16, bool REMOTE, typename F>
-__device__ __forceinline__ void join_query(F piece, int n, int group, int g, int lane, uint16_t* out, float* joined) {
-  const int at_ml = group * kHeadDim + 2 * g;
+__device__ __forceinline__ void join_row(F piece, int n, int rows, int g, int lane, uint16_t* out, float* joined) {
+  const int at_ml = rows * kHeadDim + 2 * g;
   float m = -INFINITY, l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int p = lane; p < n; p += 32) m = fmaxf(m, REMOTE ? __ldcg(piece(p) + at_ml) : piece(p)[at_ml]);
 #pragma unroll
@@ -170,13 +219,14 @@ __device__ __forceinline__ void join_query(F piece, int n, int group, int g, int
   }
 }
 
-template <bool BF16, bool SMALL>
-__global__ void __launch_bounds__(kWarps * 32, 1)
-paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int group, Workspace ws) {
+template <bool BF16, int FORM>
+__global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView pv, AttnOptions opt, DecodeJob job) {
+  constexpr int kRows = set_rows(FORM), kCols = kRows / 8, kStages = stages_of(FORM);
   extern __shared__ __align__(128) uint8_t smem[];
   // [warps][stages] tiles; then the piece each warp may leave behind at the start of its range (the piece
   // at its end goes into its ring, which is empty by then); then descriptors
-  const int piece_floats = piece_floats_of(group);
+  const int piece_rows = FORM == kFew16 ? kRows : job.group;
+  const int piece_floats = piece_floats_of(piece_rows);
   float* head_piece = reinterpret_cast<float*>(smem + kWarps * kStages * kStageBytes);
   Piece* desc = reinterpret_cast<Piece*>(head_piece + kWarps * piece_floats);       // [2 * kWarps]
   int* turn = reinterpret_cast<int*>(desc + 2 * kWarps);                            // per pair that spans CTAs: arrivals before this one, first CTA, last CTA
@@ -185,30 +235,49 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   const int g = lane >> 2, t4 = lane & 3;
   uint8_t* ring = smem + warp * kStages * kStageBytes;
   const uint32_t ring_u = smem_u32(ring);
+  auto token_of = [&](int row) { return FORM == kFew16 ? row / job.group : 0; };
 
-  // ---- where the work is: total number of tiles, then this warp's piece ----
-  int mine = 0, first_n = 0;                      // first_n: units of a head of sequence `lane`
+  // ---- where the work is: units and sets of every sequence, then this warp's piece ----
+  // sequence b, one head: its units; rows that see nothing are zeros (once per launch: `write`)
+  auto units_of = [&](int b, int& sets, bool write) -> int {
+    int units = 0;
+    sets = 1;
+    for (int set = 0; set < sets; ++set) {
+      const Seen s = seen_of<FORM>(pv, opt, job, b, set, write && set == 0 && blockIdx.x == 0);
+      sets = s.sets;
+      units += s.units();
+      if (s.n == 0 && write && b % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x))
+        for (int h = 0; h < pv.n_kv_heads; ++h)
+          for (int r = 0; r < s.rows; ++r) {
+            const int t = token_of(s.row0 + r);
+            uint16_t* row = job.out.data + (s.q_first + t) * job.out.token + (h * job.group + s.row0 + r - t * job.group) * job.out.head;
+            for (int c = 0; c < kHeadDim; c += 8) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
+          }
+    }
+    return units;
+  };
+  int mine = 0, first_units = 0, first_sets = 0, all_sets = 0;
   for (int b = lane; b < pv.batch; b += 32) {
-    const Seen s = seen_of(pv, opt, b, blockIdx.x == 0 && warp == 0);
-    mine += s.units();
-    if (b < 32) first_n = s.units();
-    // a sequence without tokens has no tile: its rows are zeros
-    if (s.n == 0 && b % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x) && warp == 0)
-      for (int h = 0; h < q.n_heads; ++h)
-        for (int c = 0; c < kHeadDim; c += 8)
-          *reinterpret_cast<uint4*>(out.data + b * out.token + h * out.head + c) = make_uint4(0, 0, 0, 0);
+    int sets;
+    const int u = units_of(b, sets, warp == 0);
+    mine += u;
+    all_sets += sets;
+    if (b < 32) {
+      first_units = u;
+      first_sets = sets;
+    }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  mine = __reduce_add_sync(0xffffffffu, mine);
+  all_sets = __reduce_add_sync(0xffffffffu, all_sets);
   const long long total = static_cast<long long>(mine) * pv.n_kv_heads;
-  const int pairs = pv.batch * pv.n_kv_heads;
+  const long long pairs = static_cast<long long>(all_sets) * pv.n_kv_heads;
   // A CTA per pair while that is no more than kPairTiles tiles each: with equal lengths no pair then spans CTAs,
   // which saves the way through the workspace (333 tokens x 8 heads: 8.1 instead of 10.5 us).  Otherwise every
   // CTA gets at least kMinTiles tiles per warp.
   const int most = static_cast<int>(gridDim.x);
   int ctas = most;
   if (total <= static_cast<long long>(most) * kWarps * kMinTiles) ctas = static_cast<int>((total + kWarps * kMinTiles - 1) / (kWarps * kMinTiles));
-  if (pairs <= most && total <= static_cast<long long>(pairs) * (kPairTiles + kPairCost) && total >= pairs) ctas = pairs;
+  if (pairs <= most && total <= pairs * (kPairTiles + kPairCost) && total >= pairs) ctas = static_cast<int>(pairs);
   const int cta = static_cast<int>(blockIdx.x);
   if (cta >= ctas) return;
   const long long cta_lo = share(total, cta, ctas), cta_hi = share(total, cta + 1, ctas);
@@ -220,34 +289,49 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   __syncthreads();
 
   if (todo > 0) {
-    // ---- the sequence that holds unit `lo` ----
+    // ---- the pair that holds unit `lo` ----
     Cursor put;                                   // next tile to copy
+    long long at = lo;                            // unit of the tile that is worked on
     {
-      long long before = 0, seq_first = 0;
+      int before = 0, sets_before = 0;            // of one head
+      put.b = 0;
       for (int base = 0; base < pv.batch; base += 32) {
         const int b = base + lane;
-        const int n = base == 0 ? first_n : (b < pv.batch ? seen_of(pv, opt, b, false).units() : 0);
-        int inc = n;
+        int n = first_units, sets = first_sets;
+        if (base > 0) n = b < pv.batch ? units_of(b, sets, false) : (sets = 0);
+        int inc = n, sinc = sets;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-          const int x = __shfl_up_sync(0xffffffffu, inc, o);
-          if (lane >= o) inc += x;
+          const int x = __shfl_up_sync(0xffffffffu, inc, o), y = __shfl_up_sync(0xffffffffu, sinc, o);
+          if (lane >= o) {
+            inc += x;
+            sinc += y;
+          }
         }
-        const unsigned hit = __ballot_sync(0xffffffffu, (before + inc) * pv.n_kv_heads > lo);
+        const unsigned hit = __ballot_sync(0xffffffffu, static_cast<long long>(before + inc) * pv.n_kv_heads > lo);
         if (hit) {
           const int l = __ffs(hit) - 1;
           put.b = base + l;
-          seq_first = (before + __shfl_sync(0xffffffffu, inc - n, l)) * pv.n_kv_heads;
+          before += __shfl_sync(0xffffffffu, inc - n, l);
+          sets_before += __shfl_sync(0xffffffffu, sinc - sets, l);
           break;
         }
         before += __shfl_sync(0xffffffffu, inc, 31);
+        sets_before += __shfl_sync(0xffffffffu, sinc, 31);
       }
-      put.s = seen_of(pv, opt, put.b, false);
-      const int off = static_cast<int>(lo - seq_first);
+      int off = static_cast<int>(lo - static_cast<long long>(before) * pv.n_kv_heads);
+      put.set = 0;
+      put.s = seen_of<FORM>(pv, opt, job, put.b, 0, false);
+      while (off >= put.s.units() * pv.n_kv_heads) {
+        off -= put.s.units() * pv.n_kv_heads;
+        put.s = seen_of<FORM>(pv, opt, job, put.b, ++put.set, false);
+      }
+      put.flat = sets_before + put.set;
       put.h = off / put.s.units();
       put.i = off - put.h * put.s.units() - kPairCost;
       if (put.i < 0) {                            // the piece opens with units that hold no tile
         todo += put.i;
+        at -= put.i;
         put.i = 0;
       }
     }
@@ -258,17 +342,21 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
       return pv.table[static_cast<long long>(c.b) * pv.max_pages + ((tile_of(c.s, c.i) * kTile) >> pv.page_shift)];
     };
     int page = page_of(put);
-    // The queries of a pair are loaded while the pair before it is worked on (the next head, or the next sequence).
-    uint32_t qn[16];
+    // The queries of a pair are loaded while the pair before it is worked on (the next head, or the next sequence);
+    // with several tokens the registers for that are not there.
+    constexpr bool kAhead = FORM != kFew16;
+    uint32_t qf[kCols][16], qn[kAhead ? 16 : 1];
     int qn_b = put.b, qn_h = put.h;
-    auto load_q = [&]() {
-      const int gq = SMALL ? (g & 3) : g;
-      const bool real = gq < group && qn_b < pv.batch;
-      const uint16_t* src = q.data + (real ? qn_b * q.token + (qn_h * group + gq) * q.head : 0) + 2 * t4;
+    auto load_ahead = [&]() {
+      if constexpr (kAhead) {
+        const int gq = FORM == kOne4 ? (g & 3) : g;
+        const bool real = gq < job.group && qn_b < pv.batch;
+        const uint16_t* src = job.q.data + (real ? qn_b * job.q.token + (qn_h * job.group + gq) * job.q.head : 0) + 2 * t4;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) qn[i] = real ? *reinterpret_cast<const uint32_t*>(src + 8 * i) : 0u;
+        for (int i = 0; i < 16; ++i) qn[i] = real ? *reinterpret_cast<const uint32_t*>(src + 8 * i) : 0u;
+      }
     };
-    load_q();
+    load_ahead();
     const int unit = lane & 15, row0 = lane >> 4;
     // asynchronous copy of the next tile into stage st: rows of 16 units, unit u of row r at u ^ (r & 7)
     auto copy_tile = [&](int st) {
@@ -287,7 +375,7 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
         cp_async16(d, kp + 2 * r * pv.k_slot, see);
         cp_async16(d + kTileBytes, vp + 2 * r * pv.v_slot, see);
       }
-      to_put -= advance(put, pv, opt);
+      to_put -= advance<FORM>(put, pv, opt, job);
       page = to_put > 0 ? page_of(put) : -1;
     };
 #pragma unroll
@@ -298,9 +386,8 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
 
     const float scale = opt.scale;
     const bool shaped = opt.cap > 0.0f;
-    const int qi[2] = {SMALL ? (2 * t4) & 3 : 2 * t4, SMALL ? (2 * t4 + 1) & 3 : 2 * t4 + 1};   // this lane's queries
-    uint32_t qf[16];
-    float slope[2], m[2], l[2], o[8][4];
+    float slope[kCols][2], m[kCols][2], l[kCols][2], o[kCols][8][4];
+    int pos[kCols][2];                            // positions of this lane's columns 8 c + 2 t4, + 1
     bool from_start = false;
     bool fresh = true;                            // the next tile opens a pair
     int stage = 0;
@@ -310,89 +397,128 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
       if (fresh) {
         fresh = false;
         from_start = get.i == 0;
-        if (qn_b != get.b || qn_h != get.h) {     // sequences without tokens lie between
-          qn_b = get.b;
-          qn_h = get.h;
-          load_q();
+        if constexpr (kAhead) {
+          if (qn_b != get.b || qn_h != get.h) {   // sequences without tokens lie between
+            qn_b = get.b;
+            qn_h = get.h;
+            load_ahead();
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) qf[0][i] = qn[i];
+          if (++qn_h == pv.n_kv_heads) {
+            qn_h = 0;
+            ++qn_b;
+          }
+          if (todo > get.s.n - get.i + kPairCost) load_ahead();   // otherwise this is the warp's last pair
+        } else {
+#pragma unroll
+          for (int c = 0; c < kCols; ++c) {
+            const int r = 8 * c + g, t = token_of(get.s.row0 + r);
+            const bool real = r < get.s.rows;
+            const uint16_t* src = job.q.data + 2 * t4;
+            if (real) src += (get.s.q_first + t) * job.q.token + (get.h * job.group + get.s.row0 + r - t * job.group) * job.q.head;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) qf[c][i] = real ? *reinterpret_cast<const uint32_t*>(src + 8 * i) : 0u;
+          }
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) qf[i] = qn[i];
-        if (++qn_h == pv.n_kv_heads) {
-          qn_h = 0;
-          ++qn_b;
-        }
-        if (todo > get.s.n - get.i + kPairCost) load_q();   // otherwise this is the warp's last pair
+        for (int c = 0; c < kCols; ++c)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          slope[e] = opt.slopes && qi[e] < group ? opt.slopes[get.h * group + qi[e]] * kLog2e : 0.0f;
-          m[e] = -INFINITY;
-          l[e] = 0.0f;
-        }
+          for (int e = 0; e < 2; ++e) {
+            int r = 8 * c + 2 * t4 + e;           // row of the column
+            if (FORM == kOne4) r &= 3;
+            const int rr = min(r, get.s.rows - 1), t = token_of(get.s.row0 + rr);
+            pos[c][e] = get.s.pos0 + t;
+            slope[c][e] = opt.slopes && r < get.s.rows ? opt.slopes[get.h * job.group + get.s.row0 + rr - t * job.group] * kLog2e : 0.0f;
+            m[c][e] = -INFINITY;
+            l[c][e] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[i][e] = 0.0f;
+            for (int i = 0; i < 8; ++i) o[c][i][e] = o[c][i][2 + e] = 0.0f;
+          }
       }
       cp_async_wait<kStages - 1>();
       __syncwarp();
       const uint32_t kt = ring_u + stage * kStageBytes, vt = kt + kTileBytes;
 
       // S^T = K q^T: lanes 0..15 give the rows of the first unit of a step, 16..31 those of the second
-      float s[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+      float s[kCols][2][4];
+#pragma unroll
+      for (int c = 0; c < kCols; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[c][0][e] = s[c][1][e] = 0.0f;
       const int lr = lane & 15, lu = lane >> 4;
 #pragma unroll
       for (int ks = 0; ks < 8; ++ks) {
         uint32_t a[4];
         const int u = 2 * ks + lu;
         ldsm4(a, kt + lr * 256 + (((u & 8) | ((u ^ lr) & 7)) << 4));
-        mma16816<BF16>(s[ks & 1], a, qf[2 * ks], qf[2 * ks + 1]);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) mma16816<BF16>(s[c][ks & 1], a, qf[c][2 * ks], qf[c][2 * ks + 1]);
       }
       const int t0 = tile_of(get.s, get.i) * kTile;
-      float x[4];
+      float x[kCols][4];
+      bool above = false;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = t0 + g + 8 * (e >> 1);
-        float y = (s[0][e] + s[1][e]) * scale;
-        if (shaped) {
-          // tanh(z) = 1 - 2 / (exp(2 z) + 1): an error of a few 2^-24 of the cap, where tanh.approx has 2^-11
-          const float z = exp2_fast(y * (2.0f * kLog2e / opt.cap));
-          y = opt.cap - 2.0f * opt.cap * __frcp_rn(z + 1.0f);
+      for (int c = 0; c < kCols; ++c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = t0 + g + 8 * (e >> 1);
+          float y = (s[c][0][e] + s[c][1][e]) * scale;
+          if (shaped) {
+            // tanh(z) = 1 - 2 / (exp(2 z) + 1): an error of a few 2^-24 of the cap, where tanh.approx has 2^-11
+            const float z = exp2_fast(y * (2.0f * kLog2e / opt.cap));
+            y = opt.cap - 2.0f * opt.cap * __frcp_rn(z + 1.0f);
+          }
+          const int p = pos[c][e & 1];
+          y = fmaf(-slope[c][e & 1], fabsf(static_cast<float>(p - j)), y * kLog2e);
+          const bool see = FORM == kFew16 ? (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix
+                                          : j < get.s.len && (j >= get.s.lo || j < get.s.pre);
+          x[c][e] = see ? y : -INFINITY;
         }
-        y = fmaf(-slope[e & 1], static_cast<float>(get.s.len - 1 - j), y * kLog2e);
-        const bool see = j < get.s.len && (j >= get.s.lo || j < get.s.pre);
-        x[e] = see ? y : -INFINITY;
+        above = above || fmaxf(x[c][0], x[c][2]) > m[c][0] + kLag || fmaxf(x[c][1], x[c][3]) > m[c][1] + kLag;
       }
-      const float top[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
-      if (__any_sync(0xffffffffu, top[0] > m[0] + kLag || top[1] > m[1] + kLag)) {
+      if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float t = fmaxf(top[e], m[e]);
+        for (int c = 0; c < kCols; ++c)
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-          const float f = t == -INFINITY ? 0.0f : exp2_fast(m[e] - t);
-          m[e] = t;
-          l[e] *= f;
+          for (int e = 0; e < 2; ++e) {
+            float t = fmaxf(fmaxf(x[c][e], x[c][2 + e]), m[c][e]);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            o[i][e] *= f;
-            o[i][2 + e] *= f;
+            for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            const float f = t == -INFINITY ? 0.0f : exp2_fast(m[c][e] - t);
+            m[c][e] = t;
+            l[c][e] *= f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              o[c][i][e] *= f;
+              o[c][i][2 + e] *= f;
+            }
+          }
+      }
+      uint32_t b0[kCols], b1[kCols], c0 = 0, c1 = 0;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = x[c][e] == -INFINITY ? 0.0f : exp2_fast(x[c][e] - m[c][e & 1]);
+        l[c][0] += p[0] + p[2];
+        l[c][1] += p[1] + p[3];
+        uint32_t h0 = float2_to_pair<BF16>(p[0], p[1]), h1 = float2_to_pair<BF16>(p[2], p[3]);
+        if (FORM != kFew16) {
+          const float2 f0 = pair_to_float2<BF16>(h0), f1 = pair_to_float2<BF16>(h1);
+          const uint32_t r0 = float2_to_pair<BF16>(p[0] - f0.x, p[1] - f0.y), r1 = float2_to_pair<BF16>(p[2] - f1.x, p[3] - f1.y);
+          if (FORM == kOne4 && t4 >= 2) {         // columns 4..7 carry the low halves of queries 0..3
+            h0 = r0;
+            h1 = r1;
+          }
+          if (FORM == kOne8) {
+            c0 = transpose8(r0);
+            c1 = transpose8(r1);
           }
         }
+        b0[c] = transpose8(h0);
+        b1[c] = transpose8(h1);
       }
-      float p[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[e] = x[e] == -INFINITY ? 0.0f : exp2_fast(x[e] - m[e & 1]);
-      l[0] += p[0] + p[2];
-      l[1] += p[1] + p[3];
-      uint32_t h0 = float2_to_pair<BF16>(p[0], p[1]), h1 = float2_to_pair<BF16>(p[2], p[3]);
-      const float2 f0 = pair_to_float2<BF16>(h0), f1 = pair_to_float2<BF16>(h1);
-      const uint32_t r0 = float2_to_pair<BF16>(p[0] - f0.x, p[1] - f0.y), r1 = float2_to_pair<BF16>(p[2] - f1.x, p[3] - f1.y);
-      if (SMALL && t4 >= 2) {                     // columns 4..7 carry the low halves of queries 0..3
-        h0 = r0;
-        h1 = r1;
-      }
-      const uint32_t b0 = transpose8(h0), b1 = transpose8(h1);
-      const uint32_t c0 = SMALL ? 0u : transpose8(r0), c1 = SMALL ? 0u : transpose8(r1);
       // O^T += V^T P^T: lanes 0..7 tokens 0..7 of a unit, 8..15 the next unit, 16..31 tokens 8..15
       const int vr = (lane & 7) + ((lane >> 4) << 3), vu = (lane >> 3) & 1;
 #pragma unroll
@@ -400,8 +526,9 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
         uint32_t a[4];
         const int u = 2 * i + vu;
         ldsm4_trans(a, vt + vr * 256 + (((u & 8) | ((u ^ vr) & 7)) << 4));
-        mma16816<BF16>(o[i], a, b0, b1);
-        if (!SMALL) mma16816<BF16>(o[i], a, c0, c1);
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) mma16816<BF16>(o[c][i], a, b0[c], b1[c]);
+        if (FORM == kOne8) mma16816<BF16>(o[0][i], a, c0, c1);
       }
       __syncwarp();                               // the stage may be filled again
       stage = stage + 1 == kStages ? 0 : stage + 1;
@@ -409,24 +536,31 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
       const bool last_of_pair = get.i + 1 == get.s.n, last_of_all = todo <= (last_of_pair ? 1 + kPairCost : 1);
       if (last_of_pair || last_of_all) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int c = 0; c < kCols; ++c)
 #pragma unroll
-          for (int d = 4; d < 32; d <<= 1) l[e] += __shfl_xor_sync(0xffffffffu, l[e], d);
-        if (SMALL)
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[c][e] += __shfl_xor_sync(0xffffffffu, l[c][e], d);
+        if (FORM == kOne4)
 #pragma unroll
           for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][e] += __shfl_xor_sync(0xffffffffu, o[i][e], 2);
+            for (int e = 0; e < 4; ++e) o[0][i][e] += __shfl_xor_sync(0xffffffffu, o[0][i][e], 2);
         if (from_start && last_of_pair) {
-          const float inv0 = l[0] == 0.0f ? 0.0f : 1.0f / l[0], inv1 = l[1] == 0.0f ? 0.0f : 1.0f / l[1];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int c = 0; c < kCols; ++c) {
+            const float inv0 = l[c][0] == 0.0f ? 0.0f : 1.0f / l[c][0], inv1 = l[c][1] == 0.0f ? 0.0f : 1.0f / l[c][1];
+            const int r = 8 * c + g, t = token_of(get.s.row0 + r);
+            uint16_t* row = job.out.data + (get.s.q_first + t) * job.out.token + (get.h * job.group + get.s.row0 + r - t * job.group) * job.out.head;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t w = transpose8(float2_to_pair<BF16>(o[i][2 * e] * inv0, o[i][2 * e + 1] * inv1));
-              if (g < group)                      // lane (g, t4): query g, channels 16 i + 8 e + 2 t4
-                *reinterpret_cast<uint32_t*>(out.data + get.b * out.token + (get.h * group + g) * out.head + 16 * i + 8 * e + 2 * t4) = w;
-            }
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const uint32_t w = transpose8(float2_to_pair<BF16>(o[c][i][2 * e] * inv0, o[c][i][2 * e + 1] * inv1));
+                if (r < get.s.rows)               // lane (g, t4): row 8 c + g, channels 16 i + 8 e + 2 t4
+                  *reinterpret_cast<uint32_t*>(row + 16 * i + 8 * e + 2 * t4) = w;
+              }
+          }
         } else {
           const int which = from_start ? 1 : 0;
           float* dst = which ? reinterpret_cast<float*>(ring) : head_piece + warp * piece_floats;
@@ -435,27 +569,35 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
             __syncwarp();
           }
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int qq = 2 * t4 + e;
-            if (qq < group) {
+          for (int c = 0; c < kCols; ++c)
 #pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                dst[qq * kHeadDim + 16 * i + g] = o[i][e];
-                dst[qq * kHeadDim + 16 * i + 8 + g] = o[i][2 + e];
+            for (int e = 0; e < 2; ++e) {
+              const int r = 8 * c + 2 * t4 + e;
+              if (r < piece_rows) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                  dst[r * kHeadDim + 16 * i + g] = o[c][i][e];
+                  dst[r * kHeadDim + 16 * i + 8 + g] = o[c][i][2 + e];
+                }
+                if (g == 0) *reinterpret_cast<float2*>(dst + piece_rows * kHeadDim + 2 * r) = make_float2(m[c][e], l[c][e]);
               }
-              if (g == 0) *reinterpret_cast<float2*>(dst + group * kHeadDim + 2 * qq) = make_float2(m[e], l[e]);
             }
-          }
           if (lane == 0) {
             Piece& d = desc[2 * warp + which];
-            d.pair = get.b * pv.n_kv_heads + get.h;
+            d.pair = get.flat * pv.n_kv_heads + get.h;
             d.starts = from_start;
             d.ends = last_of_pair;
+            d.b = get.b;
+            d.set = get.set;
+            d.n = get.s.n;
+            d.unit = at - get.i;
           }
         }
         fresh = true;
       }
-      todo -= advance(get, pv, opt);
+      const int passed = advance<FORM>(get, pv, opt, job);
+      todo -= passed;
+      at += passed;
     }
     cp_async_wait<0>();
   }
@@ -468,28 +610,33 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
   const int my_pair = lane < 2 * kWarps ? desc[lane].pair : -1;
   const unsigned valid = __ballot_sync(0xffffffffu, my_pair >= 0);
   if (valid == 0) return;
-  auto row_of = [&](int pair, int g) -> uint16_t* {
-    const int b = pair / pv.n_kv_heads, h = pair - b * pv.n_kv_heads;
-    return out.data + b * out.token + static_cast<long long>(h * group + g) * out.head;
+  // rows of the pair of piece i, and where row r of it goes
+  auto rows_of = [&](int i) -> int {
+    return FORM == kFew16 ? seen_of<FORM>(pv, opt, job, desc[i].b, desc[i].set, false).rows : job.group;
   };
-  // Runs of pieces of one pair; a warp takes (run, query) jobs.  A run that is not the whole pair goes to the
+  auto row_of = [&](int i, int r) -> uint16_t* {
+    const int h = desc[i].pair % pv.n_kv_heads, row = desc[i].set * kRows + r, t = token_of(row);
+    const int first = FORM == kFew16 ? min(max(job.cu_q[desc[i].b], 0), job.n_tokens) : desc[i].b;
+    return job.out.data + (first + t) * job.out.token + static_cast<long long>(h * job.group + row - t * job.group) * job.out.head;
+  };
+  // Runs of pieces of one pair; a warp takes (run, row) jobs.  A run that is not the whole pair goes to the
   // workspace: slot 1 if it holds the pair's first tile (at most one run, the last), slot 0 otherwise (the first).
-  int job = 0, cross[2] = {-1, -1};
+  int n_job = 0, cross[2] = {-1, -1};             // first pieces of the runs that span CTAs
   for (unsigned rest = valid; rest;) {
     const int first = __ffs(rest) - 1, pair = __shfl_sync(0xffffffffu, my_pair, first);
     const unsigned run = __ballot_sync(0xffffffffu, my_pair == pair);
     rest &= ~run;
     const bool starts = desc[first].starts, whole = starts && desc[31 - __clz(run)].ends;
-    if (!whole) cross[starts] = pair;
-    float* joined = ws.part + (static_cast<long long>(cta) * 2 + (starts ? 1 : 0)) * piece_floats;
-    for (int g2 = 0; g2 < group; ++g2, ++job)
-      if (job % kWarps == warp)
-        join_query<BF16, false>([&](int p) {
-          unsigned r = run;                       // the p-th piece of the run
-          for (; p > 0; --p) r &= r - 1;
-          return piece_at(__ffs(r) - 1);
-        }, __popc(run), group, g2, lane,
-                                whole ? row_of(pair, g2) : nullptr, joined);
+    if (!whole) cross[starts] = first;
+    float* joined = job.part + (static_cast<long long>(cta) * 2 + (starts ? 1 : 0)) * piece_floats;
+    const int rows = rows_of(first);
+    for (int r = 0; r < rows; ++r, ++n_job)
+      if (n_job % kWarps == warp)
+        join_row<BF16, false>([&](int p) {
+          unsigned bits = run;                    // the p-th piece of the run
+          for (; p > 0; --p) bits &= bits - 1;
+          return piece_at(__ffs(bits) - 1);
+        }, __popc(run), piece_rows, r, lane, whole ? row_of(first, r) : nullptr, joined);
   }
   if (cross[0] < 0 && cross[1] < 0) return;
 
@@ -500,84 +647,103 @@ paged_decode_kernel(PagedView pv, RowsView q, RowsView out, AttnOptions opt, int
     while (c + 1 < ctas && share(total, c + 1, ctas) <= unit) ++c;
     return c;
   };
-  int c0 = 0, c1 = 0;
-  if (warp < 2 && cross[warp] >= 0) {
-    const int pair = cross[warp], b = pair / pv.n_kv_heads, h = pair - b * pv.n_kv_heads;
-    long long before = 0;
-    for (int x = lane; x < b; x += 32) before += x < 32 ? first_n : seen_of(pv, opt, x, false).units();
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-    const int n = seen_of(pv, opt, b, false).units();
-    const long long u0 = before * pv.n_kv_heads + static_cast<long long>(h) * n;
-    c0 = cta_of(u0 + kPairCost);
-    c1 = cta_of(u0 + n - 1);
-  }
   __threadfence();
   __syncthreads();
   if (warp < 2 && cross[warp] >= 0 && lane == 0) {
-    turn[warp] = static_cast<int>(atomicInc(reinterpret_cast<unsigned*>(ws.arrived) + cross[warp], static_cast<unsigned>(c1 - c0)));
+    const Piece& d = desc[cross[warp]];
+    const int c0 = cta_of(d.unit), c1 = cta_of(d.unit + d.n - 1);
+    turn[warp] = static_cast<int>(atomicInc(reinterpret_cast<unsigned*>(job.arrived) + d.pair, static_cast<unsigned>(c1 - c0)));
     turn[2 + warp] = c0;
     turn[4 + warp] = c1;
   }
   __syncthreads();
-  job = 0;
+  n_job = 0;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     if (cross[k] < 0) continue;
     const int from = turn[2 + k], to = turn[4 + k];
     if (turn[k] != to - from) continue;
     __threadfence();
-    for (int g2 = 0; g2 < group; ++g2, ++job)
-      if (job % kWarps == warp)
-        join_query<BF16, true>([&](int p) -> const float* {
-          return ws.part + (static_cast<long long>(from + p) * 2 + (p == 0 ? 1 : 0)) * piece_floats;
-        }, to - from + 1, group, g2, lane, row_of(cross[k], g2), nullptr);
+    const int rows = rows_of(cross[k]);
+    for (int r = 0; r < rows; ++r, ++n_job)
+      if (n_job % kWarps == warp)
+        join_row<BF16, true>([&](int p) -> const float* {
+          return job.part + (static_cast<long long>(from + p) * 2 + (p == 0 ? 1 : 0)) * piece_floats;
+        }, to - from + 1, piece_rows, r, lane, row_of(cross[k], r), nullptr);
   }
 }
 
-size_t decode_smem(int group) {
-  return kWarps * kStages * kStageBytes + static_cast<size_t>(kWarps) * piece_floats_of(group) * 4 + 2 * kWarps * sizeof(Piece) + 32;
+size_t decode_smem(int form, int rows) {
+  return kWarps * stages_of(form) * kStageBytes + static_cast<size_t>(kWarps) * piece_floats_of(rows) * 4 + 2 * kWarps * sizeof(Piece) + 32;
 }
 
-template <bool BF16, bool SMALL>
-cudaError_t launch(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, int group, const Workspace& ws,
-                   int grid, cudaStream_t st) {
-  const size_t smem = decode_smem(group);
+template <bool BF16, int FORM> cudaError_t launch(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
+  const int rows = FORM == kFew16 ? 16 : job.group;
   static std::atomic<unsigned long long> done{0};
-  cudaError_t e = allow_shared_memory(paged_decode_kernel<BF16, SMALL>, decode_smem(SMALL ? 4 : kMaxQueryGroup), done);
+  cudaError_t e = allow_shared_memory(paged_decode_kernel<BF16, FORM>, decode_smem(FORM, FORM == kOne4 ? 4 : set_rows(FORM)), done);
   if (e != cudaSuccess) return e;
-  paged_decode_kernel<BF16, SMALL><<<grid, kWarps * 32, smem, st>>>(pv, q, out, opt, group, ws);
+  paged_decode_kernel<BF16, FORM><<<sm_count_of_current_device(), kWarps * 32, decode_smem(FORM, rows), st>>>(pv, opt, job);
   return cudaGetLastError();
 }
 
-long long part_bytes(int group) {
-  const long long n = 2ll * sm_count_of_current_device() * piece_floats_of(group) * 4;
+long long part_bytes(int rows) {
+  const long long n = 2ll * sm_count_of_current_device() * piece_floats_of(rows) * 4;
   return (n + 15) / 16 * 16;
+}
+
+long long few_sets(int batch, int group, int n_tokens) { return (static_cast<long long>(n_tokens) * group + 15ll * batch) / 16; }
+
+cudaError_t launch_form(PagedView pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
+  if (pv.n_pages == 0) {                          // copies of no bytes still name an address
+    pv.k = pv.v = job.q.data;
+    pv.k_page = pv.k_head = pv.k_slot = pv.v_page = pv.v_head = pv.v_slot = 0;
+  }
+  const bool bf16 = pv.dtype == MOQAE_DTYPE_BF16;
+  if (job.cu_q) return bf16 ? launch<true, kFew16>(pv, opt, job, st) : launch<false, kFew16>(pv, opt, job, st);
+  if (job.group <= 4) return bf16 ? launch<true, kOne4>(pv, opt, job, st) : launch<false, kOne4>(pv, opt, job, st);
+  return bf16 ? launch<true, kOne8>(pv, opt, job, st) : launch<false, kOne8>(pv, opt, job, st);
 }
 
 }  // namespace
 
-// partial results of the CTAs' first and last pairs, then one arrival counter per (sequence, kv head)
+// partial results of the CTAs' first and last pairs, then one arrival counter per pair
 long long paged_decode_workspace_bytes(int batch, int n_kv_heads, int group) {
   return (part_bytes(group) + static_cast<long long>(batch) * n_kv_heads * 4 + 15) / 16 * 16;
 }
 
-cudaError_t launch_paged_decode(const PagedView& cache, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
+cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
                                 cudaStream_t st) {
-  PagedView pv = cache;
   if (pv.batch <= 0) return cudaSuccess;
-  if (pv.n_pages == 0) {                          // copies of no bytes still name an address
-    pv.k = pv.v = q.data;
-    pv.k_page = pv.k_head = pv.k_slot = pv.v_page = pv.v_head = pv.v_slot = 0;
-  }
-  const int group = q.n_heads / pv.n_kv_heads, grid = sm_count_of_current_device();
-  Workspace ws;
-  ws.part = static_cast<float*>(workspace);
-  ws.arrived = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + part_bytes(group));
-  const bool bf16 = pv.dtype == MOQAE_DTYPE_BF16;
-  if (group <= 4)
-    return bf16 ? launch<true, true>(pv, q, out, opt, group, ws, grid, st) : launch<false, true>(pv, q, out, opt, group, ws, grid, st);
-  return bf16 ? launch<true, false>(pv, q, out, opt, group, ws, grid, st) : launch<false, false>(pv, q, out, opt, group, ws, grid, st);
+  DecodeJob job{};
+  job.q = q;
+  job.out = out;
+  job.group = q.n_heads / pv.n_kv_heads;
+  job.part = static_cast<float*>(workspace);
+  job.arrived = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + part_bytes(job.group));
+  return launch_form(pv, opt, job, st);
+}
+
+// Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average.
+bool paged_few_rows(int batch, int group, int n_tokens) {
+  return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * batch;
+}
+
+long long paged_few_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens) {
+  return (part_bytes(16) + few_sets(batch, group, n_tokens) * n_kv_heads * 4 + 15) / 16 * 16;
+}
+
+cudaError_t launch_paged_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
+                             const AttnOptions& opt, void* workspace, cudaStream_t st) {
+  if (pv.batch <= 0 || n_tokens <= 0) return cudaSuccess;
+  DecodeJob job{};
+  job.q = q;
+  job.out = out;
+  job.cu_q = cu_q;
+  job.n_tokens = n_tokens;
+  job.group = q.n_heads / pv.n_kv_heads;
+  job.part = static_cast<float*>(workspace);
+  job.arrived = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + part_bytes(16));
+  return launch_form(pv, opt, job, st);
 }
 
 }  // namespace moqae

@@ -1093,12 +1093,14 @@ long long parts_of(long long items) { return items > kSplitItems ? 0 : (items * 
 
 // claim counter, CTAs that are through, arrivals per row tile; then the pieces' partial sums
 long long paged_prefill_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens) {
+  if (paged_few_rows(batch, group, n_tokens)) return paged_few_workspace_bytes(batch, n_kv_heads, group, n_tokens);
   return kCounterBytes + parts_of(row_tiles(batch, group, n_tokens) * n_kv_heads) * kPartFloats * 4;
 }
 
 cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                                  const AttnOptions& opt, void* workspace, cudaStream_t st) {
   const int group = q.n_heads / pv.n_kv_heads;
+  if (workspace && paged_few_rows(pv.batch, group, n_tokens)) return launch_paged_few(pv, q, cu_q, n_tokens, out, opt, workspace, st);
   const long long n_rb = row_tiles(pv.batch, group, n_tokens);
   if (pv.batch <= 0 || n_tokens <= 0 || n_rb == 0) return cudaSuccess;
   const long long items = n_rb * pv.n_kv_heads;

@@ -82,6 +82,39 @@ def test_prefill_options(dtype, hq, hkv, opt, workspace):
     check(c, q, cu, prefill(c, q, cu, workspace, **opt), **opt)
 
 
+FEW = [dict(), dict(cap=30.0), dict(window=1), dict(window=100), dict(window=33, cap=50.0), dict(scale=0.3), dict(slopes=True), dict(prefix=True),
+       dict(slopes=True, cap=20.0, window=60, prefix=True), dict(window=64, prefix=True)]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("hq, hkv", [(1, 1), (8, 2), (6, 2), (7, 1), (8, 1), (10, 10)])
+@pytest.mark.parametrize("opt", FEW)
+def test_prefill_few_rows(dtype, hq, hkv, opt):
+    """A few tokens per sequence: one, more than a set of 16 rows holds, none, a sequence that is all new, one with more
+    queries than tokens."""
+    group = hq // hkv
+    new = [1, 2, 40 // group, 0, 5, 16 // group + 1, 3]
+    past = [700, 0, 130, 50, 2000, 15, -2]
+    c = pages([a + b for a, b in zip(new, past)], hkv, 16, dtype, 33)
+    cu = starts(new)
+    q = randn(sum(new) + 2, hq, 128, dtype=dtype, seed=7)
+    assert sum(new) * group <= 48 * len(new)                  # the form for few rows
+    opt = dict(opt)
+    if opt.pop("slopes", False):
+        opt["slopes"] = 2.0 ** (-torch.arange(1, hq + 1, device="cuda").float())
+    if opt.pop("prefix", False):
+        opt["prefix_len"] = ints([150, 64, 1000, -3, 129, 8, 1])
+    check(c, q, cu, prefill(c, q, cu, **opt), **opt)
+    assert mq.moqae_paged_poll_status(c) == 0
+
+
+@pytest.mark.parametrize("new, past", [([1], [100000]), ([8], [20000]), ([3] * 100, [77] * 100), ([1, 0] * 60, [9, 3000] * 60), ([2, 5, 1] * 7, [0, 4000, 16] * 7)])
+def test_prefill_few_rows_lengths(new, past):
+    c = pages([a + b for a, b in zip(new, past)], 2, 32, BF, 23)
+    cu, q = starts(new), randn(sum(new), 8, 128, dtype=BF, seed=6)
+    check(c, q, cu, prefill(c, q, cu))
+
+
 @pytest.mark.parametrize("window", list(range(900, 1160, 17)))
 def test_prefill_windows_of_uneven_row_tiles(window):
     """Few row tiles over a long window, which are cut into pieces; the tiles between the first and the last of a
