@@ -38,7 +38,7 @@ constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kMinTiles = 2;                     // a CTA is worth starting for this many tiles per warp
 constexpr int kPairTiles = 48;                   // up to so many tiles per pair, a CTA takes whole pairs where it can
 constexpr int kPairCost = 1;                     // what a pair costs beside its tiles, in tiles (its queries, its result)
-constexpr int kFewRows = 48;                     // see paged_few_rows
+constexpr int kFewRows = 12;                     // see paged_few_rows
 constexpr float kLag = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -143,6 +143,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
+  return r;
+}
+
 // A position in the order of all tiles: tile i of set `set` of sequence b, head h.  Work is shared out in units: a pair
 // is kPairCost units without a tile, then one unit per tile.
 struct Cursor {
@@ -179,43 +185,68 @@ struct Piece {
   long long unit;         // unit of the pair's first tile
 };
 
-// One warp adds row g of n pieces (piece(p): address of the p-th, in the order of their tokens), a lane four
-// channels, and writes the finished row (out != null) or the joined piece.
+// Half a warp adds row r of n pieces (piece(p): address of the p-th, in the order of their tokens), a lane eight
+// channels, and writes the finished row (out != null) or the joined piece.  r >= rows: it only keeps the other half
+// company.  The first pieces' sums are on their way while the references are compared.
 template <bool BF16, bool REMOTE, typename F>
-__device__ __forceinline__ void join_row(F piece, int n, int rows, int g, int lane, uint16_t* out, float* joined) {
-  const int at_ml = rows * kHeadDim + 2 * g;
-  float m = -INFINITY, l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int p = lane; p < n; p += 32) m = fmaxf(m, REMOTE ? __ldcg(piece(p) + at_ml) : piece(p)[at_ml]);
+__device__ __forceinline__ void join_row(F piece, int n, int rows, int r, int lane, uint16_t* out, float* joined) {
+  constexpr int kBatch = 4;
+  const int sub = lane & 15;
+  const bool act = r < rows;
+  r = act ? r : rows - 1;
+  const int at_ml = rows * kHeadDim + 2 * r;
+  float m = -INFINITY, l = 0.0f, acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  float4 v[kBatch][2];
+  auto load = [&](int p0) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  for (int base = 0; base < n; base += 32) {
-    float f = 0.0f, fl = 0.0f;                    // lane p: factor of piece base + p, and its share of the weight sum
-    if (base + lane < n) {
-      const float2* ml = reinterpret_cast<const float2*>(piece(base + lane) + at_ml);
-      const float2 w = REMOTE ? __ldcg(ml) : *ml;
-      f = w.x == -INFINITY ? 0.0f : exp2_fast(w.x - m);
-      fl = w.y * f;
+    for (int k = 0; k < kBatch; ++k) {
+      const float4* src = reinterpret_cast<const float4*>(piece(min(p0 + k, n - 1)) + r * kHeadDim) + 2 * sub;
+      v[k][0] = REMOTE ? __ldcg(src) : src[0];
+      v[k][1] = REMOTE ? __ldcg(src + 1) : src[1];
     }
-    const int many = min(32, n - base);
-#pragma unroll 8
-    for (int p = 0; p < many; ++p) {
-      const float4* src = reinterpret_cast<const float4*>(piece(base + p) + g * kHeadDim) + lane;
-      const float4 v = REMOTE ? __ldcg(src) : *src;
-      const float fp = __shfl_sync(0xffffffffu, f, p);
-      l += __shfl_sync(0xffffffffu, fl, p);
-      acc[0] = fmaf(v.x, fp, acc[0]);
-      acc[1] = fmaf(v.y, fp, acc[1]);
-      acc[2] = fmaf(v.z, fp, acc[2]);
-      acc[3] = fmaf(v.w, fp, acc[3]);
+  };
+  for (int base = 0; base < n; base += 16) {
+    load(base);
+    float2 w = make_float2(-INFINITY, 0.0f);
+    if (base + sub < n) {
+      const float2* ml = reinterpret_cast<const float2*>(piece(base + sub) + at_ml);
+      w = REMOTE ? __ldcg(ml) : *ml;
+    }
+    float top = fmaxf(m, w.x);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float f = w.x == -INFINITY ? 0.0f : exp2_fast(w.x - top), old = m == -INFINITY ? 0.0f : exp2_fast(m - top);
+    float fl = w.y * f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) fl += __shfl_xor_sync(0xffffffffu, fl, o);
+    l = l * old + fl;
+    m = top;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= old;
+    const int many = min(16, n - base);
+    for (int p0 = 0; p0 < many; p0 += kBatch) {
+      if (p0) load(base + p0);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k) {
+        const float fp = __shfl_sync(0xffffffffu, f, p0 + k, 16);          // 0 behind the last piece
+        const float* x = reinterpret_cast<const float*>(v[k]);
+        if (p0 + k < many)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] = fmaf(x[e], fp, acc[e]);
+      }
     }
   }
+  if (!act) return;
   if (out) {
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    *reinterpret_cast<uint2*>(out + 4 * lane) =
-        make_uint2(float2_to_pair<BF16>(acc[0] * inv, acc[1] * inv), float2_to_pair<BF16>(acc[2] * inv, acc[3] * inv));
+    *reinterpret_cast<uint4*>(out + 8 * sub) =
+        make_uint4(float2_to_pair<BF16>(acc[0] * inv, acc[1] * inv), float2_to_pair<BF16>(acc[2] * inv, acc[3] * inv),
+                   float2_to_pair<BF16>(acc[4] * inv, acc[5] * inv), float2_to_pair<BF16>(acc[6] * inv, acc[7] * inv));
   } else {
-    *(reinterpret_cast<float4*>(joined + g * kHeadDim) + lane) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-    if (lane == 0) *reinterpret_cast<float2*>(joined + at_ml) = make_float2(m, l);
+    float4* dst = reinterpret_cast<float4*>(joined + r * kHeadDim) + 2 * sub;
+    dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    if (sub == 0) *reinterpret_cast<float2*>(joined + at_ml) = make_float2(m, l);
   }
 }
 
@@ -357,6 +388,21 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
       }
     };
     load_ahead();
+    auto load_rows = [&](const Cursor& c) {
+      if constexpr (!kAhead) {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) {
+          const int r = 8 * k + g, t = token_of(c.s.row0 + r);
+          const bool real = r < c.s.rows;
+          const uint16_t* src = job.q.data + 2 * t4;
+          if (real) src += (c.s.q_first + t) * job.q.token + (c.h * job.group + c.s.row0 + r - t * job.group) * job.q.head;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) qf[k][i] = real ? *reinterpret_cast<const uint32_t*>(src + 8 * i) : 0u;
+        }
+      }
+    };
+    load_rows(put);
+    bool first_pair = true;
     const int unit = lane & 15, row0 = lane >> 4;
     // asynchronous copy of the next tile into stage st: rows of 16 units, unit u of row r at u ^ (r & 7)
     auto copy_tile = [&](int st) {
@@ -386,6 +432,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
 
     const float scale = opt.scale;
     const bool shaped = opt.cap > 0.0f;
+    const float twice_by_cap = shaped ? 2.0f * kLog2e / opt.cap : 0.0f;
     float slope[kCols][2], m[kCols][2], l[kCols][2], o[kCols][8][4];
     int pos[kCols][2];                            // positions of this lane's columns 8 c + 2 t4, + 1
     bool from_start = false;
@@ -410,17 +457,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
             ++qn_b;
           }
           if (todo > get.s.n - get.i + kPairCost) load_ahead();   // otherwise this is the warp's last pair
-        } else {
-#pragma unroll
-          for (int c = 0; c < kCols; ++c) {
-            const int r = 8 * c + g, t = token_of(get.s.row0 + r);
-            const bool real = r < get.s.rows;
-            const uint16_t* src = job.q.data + 2 * t4;
-            if (real) src += (get.s.q_first + t) * job.q.token + (get.h * job.group + get.s.row0 + r - t * job.group) * job.q.head;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) qf[c][i] = real ? *reinterpret_cast<const uint32_t*>(src + 8 * i) : 0u;
-          }
+        } else if (!first_pair) {
+          load_rows(get);
         }
+        first_pair = false;
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
 #pragma unroll
@@ -466,11 +506,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
           float y = (s[c][0][e] + s[c][1][e]) * scale;
           if (shaped) {
             // tanh(z) = 1 - 2 / (exp(2 z) + 1): an error of a few 2^-24 of the cap, where tanh.approx has 2^-11
-            const float z = exp2_fast(y * (2.0f * kLog2e / opt.cap));
-            y = opt.cap - 2.0f * opt.cap * __frcp_rn(z + 1.0f);
+            const float z = exp2_fast(y * twice_by_cap);
+            y = fmaf(-2.0f * opt.cap, rcp_fast(z + 1.0f), opt.cap);
           }
           const int p = pos[c][e & 1];
-          y = fmaf(-slope[c][e & 1], fabsf(static_cast<float>(p - j)), y * kLog2e);
+          y *= kLog2e;
+          if (opt.slopes) y = fmaf(-slope[c][e & 1], fabsf(static_cast<float>(p - j)), y);
           const bool see = FORM == kFew16 ? (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix
                                           : j < get.s.len && (j >= get.s.lo || j < get.s.pre);
           x[c][e] = see ? y : -INFINITY;
@@ -619,7 +660,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     const int first = FORM == kFew16 ? min(max(job.cu_q[desc[i].b], 0), job.n_tokens) : desc[i].b;
     return job.out.data + (first + t) * job.out.token + static_cast<long long>(h * job.group + row - t * job.group) * job.out.head;
   };
-  // Runs of pieces of one pair; a warp takes (run, row) jobs.  A run that is not the whole pair goes to the
+  // Runs of pieces of one pair; a warp takes jobs of two rows of a run.  A run that is not the whole pair goes to the
   // workspace: slot 1 if it holds the pair's first tile (at most one run, the last), slot 0 otherwise (the first).
   int n_job = 0, cross[2] = {-1, -1};             // first pieces of the runs that span CTAs
   for (unsigned rest = valid; rest;) {
@@ -630,13 +671,16 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     if (!whole) cross[starts] = first;
     float* joined = job.part + (static_cast<long long>(cta) * 2 + (starts ? 1 : 0)) * piece_floats;
     const int rows = rows_of(first);
-    for (int r = 0; r < rows; ++r, ++n_job)
-      if (n_job % kWarps == warp)
-        join_row<BF16, false>([&](int p) {
-          unsigned bits = run;                    // the p-th piece of the run
-          for (; p > 0; --p) bits &= bits - 1;
-          return piece_at(__ffs(bits) - 1);
-        }, __popc(run), piece_rows, r, lane, whole ? row_of(first, r) : nullptr, joined);
+    for (int r0 = 0; r0 < rows; r0 += 2, ++n_job) {
+      if (n_job % kWarps != warp) continue;
+      const int r = r0 + (lane >> 4);
+      // (row `rows` of an odd count reads the last one and is not written)
+      join_row<BF16, false>([&](int p) {
+        unsigned bits = run;                      // the p-th piece of the run
+        for (; p > 0; --p) bits &= bits - 1;
+        return piece_at(__ffs(bits) - 1);
+      }, __popc(run), piece_rows, r < rows ? r : piece_rows, lane, whole && r < rows ? row_of(first, r) : nullptr, joined);
+    }
   }
   if (cross[0] < 0 && cross[1] < 0) return;
 
@@ -665,11 +709,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     if (turn[k] != to - from) continue;
     __threadfence();
     const int rows = rows_of(cross[k]);
-    for (int r = 0; r < rows; ++r, ++n_job)
-      if (n_job % kWarps == warp)
-        join_row<BF16, true>([&](int p) -> const float* {
-          return job.part + (static_cast<long long>(from + p) * 2 + (p == 0 ? 1 : 0)) * piece_floats;
-        }, to - from + 1, piece_rows, r, lane, row_of(cross[k], r), nullptr);
+    for (int r0 = 0; r0 < rows; r0 += 2, ++n_job) {
+      if (n_job % kWarps != warp) continue;
+      const int r = r0 + (lane >> 4);
+      join_row<BF16, true>([&](int p) -> const float* {
+        return job.part + (static_cast<long long>(from + p) * 2 + (p == 0 ? 1 : 0)) * piece_floats;
+      }, to - from + 1, piece_rows, r < rows ? r : piece_rows, lane, r < rows ? row_of(cross[k], r) : nullptr, nullptr);
+    }
   }
 }
 
@@ -723,7 +769,9 @@ cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const Ro
   return launch_form(pv, opt, job, st);
 }
 
-// Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average.
+// Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average.  Measured against
+// the large tiles (us, few / large): 8 sequences of 1008 tokens, 4 rows 19.5 / 20.6, 16 rows 26.5 / 21.0; of 8000 tokens, 16
+// rows 68 / 73, 32 rows 106 / 73; lengths from 100 to 4100, 11 rows 31 / 38.
 bool paged_few_rows(int batch, int group, int n_tokens) {
   return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * batch;
 }

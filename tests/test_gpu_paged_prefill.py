@@ -93,17 +93,17 @@ def test_prefill_few_rows(dtype, hq, hkv, opt):
     """A few tokens per sequence: one, more than a set of 16 rows holds, none, a sequence that is all new, one with more
     queries than tokens."""
     group = hq // hkv
-    new = [1, 2, 40 // group, 0, 5, 16 // group + 1, 3]
-    past = [700, 0, 130, 50, 2000, 15, -2]
+    new = [1, 2, 40 // group, 0, 5, 16 // group + 1, 3] + [0] * 6
+    past = [700, 0, 130, 50, 2000, 15, -2] + [0, 20, 0, 0, 33, 1]
     c = pages([a + b for a, b in zip(new, past)], hkv, 16, dtype, 33)
     cu = starts(new)
     q = randn(sum(new) + 2, hq, 128, dtype=dtype, seed=7)
-    assert sum(new) * group <= 48 * len(new)                  # the form for few rows
+    assert sum(new) * group <= 12 * len(new)                  # the form for few rows
     opt = dict(opt)
     if opt.pop("slopes", False):
         opt["slopes"] = 2.0 ** (-torch.arange(1, hq + 1, device="cuda").float())
     if opt.pop("prefix", False):
-        opt["prefix_len"] = ints([150, 64, 1000, -3, 129, 8, 1])
+        opt["prefix_len"] = ints([150, 64, 1000, -3, 129, 8, 1] + [5] * 6)
     check(c, q, cu, prefill(c, q, cu, **opt), **opt)
     assert mq.moqae_paged_poll_status(c) == 0
 
