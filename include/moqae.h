@@ -456,7 +456,7 @@ typedef struct moqae_attn_options {
   const float* slopes;         /* [n_q_heads] float32, finite, or NULL */
   const int32_t* prefix_len;   /* [batch], values below 0 count as 0, or NULL */
   float scale;                 /* <= 0: 1/sqrt(128) */
-  float cap;                   /* 0: none */
+  float cap;                   /* 0: none; else at least 1e-4 */
   int32_t window;              /* 0: none */
 } moqae_attn_options;
 

@@ -102,11 +102,12 @@ int check_options(const moqae_attn_options* o, AttnOptions* v) {
   v->scale = 0.08838834764831845f;               // 1/sqrt(128)
   if (!o) return MOQAE_OK;
   if (!isfinite(o->scale) || !isfinite(o->cap) || o->cap < 0.0f || o->window < 0) return MOQAE_ERR_INVALID_ARG;
+  if (o->cap > 0.0f && o->cap < 1e-4f) return MOQAE_ERR_UNSUPPORTED;
   if (!aligned(o->slopes, 4) || !aligned(o->prefix_len, 4)) return MOQAE_ERR_MISALIGNED;
   if (o->scale > 0.0f) v->scale = o->scale;
   v->slopes = o->slopes;
   v->prefix_len = o->prefix_len;
-  v->cap = o->cap;
+  v->cap = o->cap > 1e30f ? 0.0f : o->cap;       // a cap that no score can feel
   v->window = o->window;
   return MOQAE_OK;
 }

@@ -143,12 +143,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return r;
 }
 
-__device__ __forceinline__ float rcp_fast(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
-  return r;
-}
-
 // A position in the order of all tiles: tile i of set `set` of sequence b, head h.  Work is shared out in units: a pair
 // is kPairCost units without a tile, then one unit per tile.
 struct Cursor {
@@ -432,7 +426,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
 
     const float scale = opt.scale;
     const bool shaped = opt.cap > 0.0f;
-    const float twice_by_cap = shaped ? 2.0f * kLog2e / opt.cap : 0.0f;
+    const float by_cap = shaped ? 1.0f / opt.cap : 0.0f;
     float slope[kCols][2], m[kCols][2], l[kCols][2], o[kCols][8][4];
     int pos[kCols][2];                            // positions of this lane's columns 8 c + 2 t4, + 1
     bool from_start = false;
@@ -504,11 +498,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
         for (int e = 0; e < 4; ++e) {
           const int j = t0 + g + 8 * (e >> 1);
           float y = (s[c][0][e] + s[c][1][e]) * scale;
-          if (shaped) {
-            // tanh(z) = 1 - 2 / (exp(2 z) + 1): an error of a few 2^-24 of the cap, where tanh.approx has 2^-11
-            const float z = exp2_fast(y * twice_by_cap);
-            y = fmaf(-2.0f * opt.cap, rcp_fast(z + 1.0f), opt.cap);
-          }
+          if (shaped) y = opt.cap * tanh_of(y * by_cap);
           const int p = pos[c][e & 1];
           y *= kLog2e;
           if (opt.slopes) y = fmaf(-slope[c][e & 1], fabsf(static_cast<float>(p - j)), y);

@@ -74,12 +74,6 @@ __device__ __forceinline__ int fresh(int x) {
   return x;
 }
 
-__device__ __forceinline__ float rcp_approx(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
-  return r;
-}
-
 struct PrefillJob {
   RowsView q, out;
   const int32_t* cu_q;
@@ -111,7 +105,7 @@ struct Control {
   int abort;
   unsigned ticket;
   int pair_flag[2][8][2];                            // [turn][warps of the same rows][half]
-  float tanh[7];                                     // cap in base-2 units; coefficients 1 .. 5 of the polynomial; where it holds
+  float cap[9];                                      // products up to which the polynomial holds; its coefficients; cap in base-2 units; scale / cap
   PrefillJob job;                                    // the kernel's arguments, for the functions that are not inlined (a
   AttnOptions opt;                                   // reference to a parameter is read through global memory)
 };
@@ -466,8 +460,6 @@ template <bool BF16, bool CAP, bool BIAS>
 __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, uint32_t tmem, float* exch, uint32_t phase) {
     const AttnOptions& opt = ctl.opt;
     const PrefillJob& job = ctl.job;
-    // both chunks in line for plain scores (2 % faster on a long prompt), a loop where their shaping makes the code long (7 %)
-    constexpr int kChunkUnroll = CAP || BIAS ? 1 : 2;
     const Piece& it = ctl.piece[slot];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int half = warp >> 3, i = (warp & 7) >> 2, pair_id = warp & 7;
@@ -491,36 +483,38 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     };
     const float scale_log2 = opt.scale * kLog2e;
     float slope = 0.0f;
-    // (the constants of the cap stay in shared memory between uses)
-    const volatile float* tanh_of = ctl.tanh;
+    const volatile float* cap_of = ctl.cap;            // (the constants of the cap stay in shared memory between uses)
     // Scores of columns 32 c .. 32 c + 31 in base-2 units, up to a factor and a term that `mul` and `add` give
     // (so that both join the subtraction of the reference); column e is seen if lo < e <= hi or e < pre.
     auto scores = [&](auto masked, float (&v)[32], int c, int hi, int lo, int pre, float& mul, float& add) {
       tmem_ld32(v, s_addr + 32 * c);
       mul = CAP || BIAS ? 1.0f : scale_log2;
       add = 0.0f;
-      if (CAP || BIAS) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] *= scale_log2;
-      }
       if (CAP) {
-        const float cap2 = tanh_of[0];
         float big = 0.0f;
 #pragma unroll
         for (int e = 0; e < 32; ++e) big = fmaxf(big, fabsf(v[e]));
-        if (__all_sync(0xffffffffu, big <= tanh_of[6])) {
-          const float t1 = tanh_of[1], t2 = tanh_of[2], t3 = tanh_of[3], t4 = tanh_of[4], t5 = tanh_of[5];
+        if (__all_sync(0xffffffffu, big <= cap_of[0])) {
+          uint64_t t[6];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) {
-            const float u = v[e] * v[e];
-            v[e] *= fmaf(fmaf(fmaf(fmaf(fmaf(t5, u, t4), u, t3), u, t2), u, t1), u, 0.99999940395f);
+          for (int k = 0; k < 6; ++k) {
+            const float x = cap_of[1 + k];
+            t[k] = pack_f2(x, x);
           }
-        } else {
-          // some score passes the cap: tanh(z) = 1 - 2 / (exp(2 z) + 1), accurate to a few float32 roundings of the cap
-          const float in = 2.0f * kLog2e / cap2;
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = fmaf(-2.0f * cap2, rcp_approx(ex2_approx(v[e] * in) + 1.0f), cap2);
+          for (int e = 0; e < 32; e += 2) {
+            const uint64_t y = pack_f2(v[e], v[e + 1]), u = mul_f2(y, y);
+            unpack_f2(mul_f2(y, fma_f2(fma_f2(fma_f2(fma_f2(fma_f2(t[5], u, t[4]), u, t[3]), u, t[2]), u, t[1]), u, t[0])), v[e], v[e + 1]);
+          }
+        } else {                                                          // some score passes the cap
+          const float w = cap_of[8];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = cap_of[7] * tanh_of(v[e] * w);
         }
+      } else if (BIAS) {
+        const uint64_t scale2 = pack_f2(scale_log2, scale_log2);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) unpack_f2(mul_f2(pack_f2(v[e], v[e + 1]), scale2), v[e], v[e + 1]);
       }
       if (BIAS) {
         const float dist = static_cast<float>(hi - 32 * c);               // of column 0
@@ -602,10 +596,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
           asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n" : "=r"(raw) : "r"(lane_addr + 128 * i + col));
           asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
           float y = __uint_as_float(raw) * scale_log2;
-          if (CAP) {
-            const float cap2 = tanh_of[0];
-            y = fmaf(-2.0f * cap2, rcp_approx(ex2_approx(y * (2.0f * kLog2e / cap2)) + 1.0f), cap2);
-          }
+          if (CAP) y = cap_of[7] * tanh_of(__uint_as_float(raw) * cap_of[8]);
           if (BIAS) y -= slope * static_cast<float>(qpos - (j0 - 64 * half + col));
           if (y > -1e30f && y < 1e30f) m_ref = ceilf(y);
         }
@@ -619,7 +610,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
       float sum = 0.0f;
       bool moved = false;
       if (ok) {
-#pragma unroll kChunkUnroll
+#pragma unroll
         for (int c = 0; c < 2; ++c) {
           uint32_t pk[16];
           float csum = masked ? weights(std::true_type{}, c, m_ref, hi, lo, pre, pk) : weights(std::false_type{}, c, m_ref, hi, lo, pre, pk);
@@ -724,17 +715,15 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     asm volatile("prefetch.tensormap [%0];\n" ::"l"(&map_q) : "memory");
     for (int i = 0; i < BAR_COUNT; ++i) mbar_init(bar(i), arrivals_of(i));
     *abort_flag = 0;
-    // tanh(z) / z for |z| <= 1 as a polynomial in z^2 (minimax, own fit, relative error 6e-7), for z = x / cap2
-    // with x and cap2 in base-2 units: the coefficients take the powers of cap2
     if (CAP) {
-      const float cap2 = opt.cap * kLog2e, w2 = 1.0f / (cap2 * cap2);
-      ctl.tanh[0] = cap2;
-      ctl.tanh[6] = cap2 > 1e-3f && cap2 < 1e3f ? cap2 : -1.0f;         // beyond, the powers leave float32
-      ctl.tanh[1] = -0.33329042792f * w2;
-      ctl.tanh[2] = 0.13281433284f * w2 * w2;
-      ctl.tanh[3] = -0.05160567537f * w2 * w2 * w2;
-      ctl.tanh[4] = 0.01674311422f * (w2 * w2) * (w2 * w2);
-      ctl.tanh[5] = -0.00306706037f * (w2 * w2) * (w2 * w2) * w2;
+      // Up to the cap, cap tanh(x / cap) is a polynomial in the raw product: powers of w = scale / cap go into the
+      // coefficients, where float32 holds them (otherwise every score takes the general way).
+      const float w = opt.scale / opt.cap, cap2 = opt.cap * kLog2e;
+      ctl.cap[0] = w > 1e-3f && w < 1e3f ? 1.0f / w : -1.0f;
+      float power = w * cap2;
+      for (int k = 0; k < 6; ++k, power *= w * w) ctl.cap[1 + k] = tanh_coef(k) * power;
+      ctl.cap[7] = cap2;
+      ctl.cap[8] = w;
     }
     ctl.job = job;
     ctl.opt = opt;

@@ -65,9 +65,10 @@ def attention(q, k, v, first, *, scale=None, cap=0.0, window=0, slopes=None, pre
         err = 128 * 2 * F32 * (qq.abs() @ kk.abs().T) * scale
         if cap > 0:
             x = cap * torch.tanh(x / cap)
-            # the exponential (argument off by 4 roundings, |2 z| <= 40 where it matters), 1 + e, the reciprocal,
-            # the difference: a few roundings of the cap
-            err = err + cap * 96 * F32
+            # up to the cap a polynomial of relative error 6e-7 (10 F32) with about ten roundings; beyond, the
+            # exponential (argument off by 4 roundings, |2 z| <= 40 where it matters), 1 + e, the reciprocal, the
+            # difference: a few roundings of the cap, of which the score is then at least three quarters
+            err = err + 128 * F32 * x.abs()
         if slopes is not None:
             bias = slopes[h].double() * (pos - j).abs()
             x = x - bias

@@ -232,6 +232,14 @@ def test_decode_options(dtype, hq, hkv, opt):
     check_decode(c, q, out, **check)
 
 
+@pytest.mark.parametrize("cap", [1e-4, 0.01, 1.0, 3.0, 500.0, 1e5, 1e20])
+def test_decode_caps(cap):
+    """Caps far below and far above the scores: an all but uniform and an all but plain softmax."""
+    c = pages([700, 33], 2, 16, FP, 35)
+    q = randn(2, 8, 128, dtype=FP, seed=9, scale=3.0)
+    check_decode(c, q, decode(c, q, cap=cap), cap=cap)
+
+
 def test_decode_reads_only_what_is_seen():
     """Tokens outside the window may hold NaN, and their pages may have been given back."""
     c = pages([1000], 2, 16, BF, 41)

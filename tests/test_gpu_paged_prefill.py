@@ -82,6 +82,14 @@ def test_prefill_options(dtype, hq, hkv, opt, workspace):
     check(c, q, cu, prefill(c, q, cu, workspace, **opt), **opt)
 
 
+@pytest.mark.parametrize("cap", [1e-4, 0.01, 1.0, 3.0, 500.0, 1e5, 1e20])
+def test_prefill_caps(cap):
+    """Caps far below and far above the scores: an all but uniform and an all but plain softmax."""
+    c = pages([700, 333], 2, 16, FP, 35)
+    cu, q = starts([150, 300]), randn(450, 8, 128, dtype=FP, seed=9, scale=3.0)
+    check(c, q, cu, prefill(c, q, cu, cap=cap), cap=cap)
+
+
 FEW = [dict(), dict(cap=30.0), dict(window=1), dict(window=100), dict(window=33, cap=50.0), dict(scale=0.3), dict(slopes=True), dict(prefix=True),
        dict(slopes=True, cap=20.0, window=60, prefix=True), dict(window=64, prefix=True)]
 

@@ -148,7 +148,7 @@ def test_norm_rope_arguments(lib):
 
 
 @pytest.mark.parametrize("change, code", [
-    (dict(cap=-1.0), mq.ERR_INVALID_ARG), (dict(cap=float("inf")), mq.ERR_INVALID_ARG), (dict(cap=float("nan")), mq.ERR_INVALID_ARG),
+    (dict(cap=-1.0), mq.ERR_INVALID_ARG), (dict(cap=1e-5), mq.ERR_UNSUPPORTED), (dict(cap=float("inf")), mq.ERR_INVALID_ARG), (dict(cap=float("nan")), mq.ERR_INVALID_ARG),
     (dict(scale=float("nan")), mq.ERR_INVALID_ARG), (dict(scale=float("inf")), mq.ERR_INVALID_ARG), (dict(window=-1), mq.ERR_INVALID_ARG),
     (dict(slopes=A + 2), mq.ERR_MISALIGNED), (dict(prefix_len=A + 1), mq.ERR_MISALIGNED)])
 def test_attention_options(lib, change, code):
