@@ -82,6 +82,7 @@ struct PrefillJob {
   float* part;                                       // [kMaxParts][kPartFloats], null: pieces are whole row tiles
   unsigned* counters;                                // next claim, CTAs that are through, arrivals [kSplitItems]; null: a fixed order
   int max_parts;
+  int tile_rows;                                     // rows of a tile in use: whole tokens (128, or 125 to 127 for groups of 3, 5, 6, 7)
   int q_box;                                         // tokens per tile if the queries come by tiled copies, else 0
   int box_rows;                                      // slots per copy of a page
   int dim_slot, dim_head, dim_page;                  // tensor-map dimension (1..3) of each
@@ -143,6 +144,11 @@ __device__ __forceinline__ bool spin_bar(Control& ctl, int which, uint32_t parit
 __device__ __forceinline__ int token_of(const PrefillJob& job, int row) {
   return job.group == 1 ? row : static_cast<int>(__umulhi(static_cast<unsigned>(row), job.group_inv));
 }
+// Row of a piece that the CTA's row r (tensor-memory lane r % 128 of tile r / 128) holds; -1: none.
+__device__ __forceinline__ int row_at(const PrefillJob& job, const Piece& it, int r) {
+  const int x = (r >> 7) * job.tile_rows + (r & 127);
+  return (r & 127) < job.tile_rows && x < it.rows ? x : -1;
+}
 __device__ __forceinline__ int block_at(const Piece& it, int idx) { return idx < it.n_pre ? idx : it.first + idx - it.n_pre; }
 __device__ __forceinline__ bool token_used(const Piece& it, int j) { return j < it.kv_len && (j >= it.win_lo || j < it.prefix); }
 
@@ -158,12 +164,12 @@ __device__ __forceinline__ Sequence sequence(const PagedView& pv, const AttnOpti
   s.prefix = opt.prefix_len ? min(max(opt.prefix_len[b], 0), s.kv_len) : 0;
   return s;
 }
-__device__ __forceinline__ int row_tiles_of(const PrefillJob& job, const Sequence& s) { return (s.n * job.group + kItemRows - 1) / kItemRows; }
+__device__ __forceinline__ int row_tiles_of(const PrefillJob& job, const Sequence& s) { return (s.n * job.group + 2 * job.tile_rows - 1) / (2 * job.tile_rows); }
 
 // The blocks that row tile rb of a sequence sees.
 __device__ __forceinline__ void set_walk(const PrefillJob& job, const AttnOptions& opt, const Sequence& s, int rb, Piece& it) {
-  it.row0 = rb * kItemRows;
-  it.rows = min(kItemRows, s.n * job.group - it.row0);
+  it.row0 = rb * 2 * job.tile_rows;
+  it.rows = min(2 * job.tile_rows, s.n * job.group - it.row0);
   it.q_first = s.first;
   it.kv_len = s.kv_len;
   it.pos0 = s.kv_len - s.n;
@@ -179,9 +185,9 @@ __device__ __forceinline__ void set_walk(const PrefillJob& job, const AttnOption
   }
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int last = min(it.rows, kTileRows * (i + 1)) - 1;               // last row of the tile
+    const int last = min(it.rows, job.tile_rows * (i + 1)) - 1;           // last row of the tile
     int end = 0;
-    if (last >= kTileRows * i) {
+    if (last >= job.tile_rows * i) {
       const int p = it.pos0 + token_of(job, it.row0 + last);
       end = p >= 0 ? p / kBlock + 1 : 0;
       if (it.win_lo == 0) end = max(end, (it.prefix + kBlock - 1) / kBlock);
@@ -255,7 +261,7 @@ __device__ __forceinline__ Plan make_plan(const PagedView& pv, const AttnOptions
   }
   if (segs == 1) tiles = static_cast<float>(p.items);
   const float mean = blocks / tiles;
-  const float full = fminf(1.0f, static_cast<float>(job.n_tokens) * static_cast<float>(job.group) / (static_cast<float>(p.items) * kItemRows));
+  const float full = fminf(1.0f, static_cast<float>(job.n_tokens) * static_cast<float>(job.group) / (static_cast<float>(p.items) * static_cast<float>(2 * job.tile_rows)));
   float cost = ceilf(tiles * heads / static_cast<float>(grid) - 0.01f) * (mean + (segs == 1 ? 1.5f : 1.5f + 3.0f * full)) + static_cast<float>(size) - mean +
                (segs == 1 ? 0.0f : 2.5f + 1.6f * full * static_cast<float>(segs));
   if (segs > 1 && (whole * segs > job.max_parts || (longest + size - 1) / size < segs)) cost = 1e30f;
@@ -385,12 +391,13 @@ __device__ __forceinline__ void store_rows(const PrefillJob& job, const Piece& i
       for (int k8 = 0; k8 < 4; ++k8) {
         const int r = 8 * k8 + (lane >> 2), u = lane & 3;
         const uint4 x = *reinterpret_cast<const uint4*>(rows_at + r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
-        if (w_row + r >= it.rows) continue;
+        const int mine = row_at(job, it, w_row + r);
+        if (mine < 0) continue;
         if (parts == 1) {
-          const int t = token_of(job, it.row0 + w_row + r), g = it.row0 + w_row + r - t * job.group;
+          const int t = token_of(job, it.row0 + mine), g = it.row0 + mine - t * job.group;
           *reinterpret_cast<uint4*>(job.out.data + (it.q_first + t) * job.out.token + (it.h * job.group + g) * job.out.head + 64 * half + 32 * c4 + 8 * u) = x;
         } else {
-          *reinterpret_cast<uint4*>(piece + (w_row + r) * kHeadDim + 64 * half + 32 * c4 + 16 * part16 + 4 * u) = x;
+          *reinterpret_cast<uint4*>(piece + mine * kHeadDim + 64 * half + 32 * c4 + 16 * part16 + 4 * u) = x;
         }
       }
       __syncwarp();
@@ -571,14 +578,15 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     };
     const int n_blocks = it.idx1 - it.idx0, first = min(max(it.idx1 - it.nb[i], 0), n_blocks);
     // rows behind the last one take its position: they cost no extra mask and are not stored
-    auto position = [&](int r) { return it.pos0 + token_of(job, it.row0 + min(r, it.rows - 1)); };
-    const int my_row = row;
-    const int qpos = position(my_row);
+    auto position = [&](int r) {
+      return it.pos0 + token_of(job, it.row0 + min((r >> 7) * job.tile_rows + min(r & 127, job.tile_rows - 1), it.rows - 1));
+    };
+    const int my_row = row_at(job, it, row), qpos = position(row);
     // tokens all_from .. all_to are seen by every row of the warp
-    const int all_to = position(my_row & ~31), all_from = opt.window > 0 ? position(my_row | 31) - opt.window + 1 : -0x40000000;
-    if (BIAS) slope = my_row < it.rows ? opt.slopes[it.h * job.group + it.row0 + my_row - token_of(job, it.row0 + my_row) * job.group] * kLog2e : 0.0f;
+    const int all_to = position(row & ~31), all_from = opt.window > 0 ? position(row | 31) - opt.window + 1 : -0x40000000;
+    if (BIAS) slope = my_row >= 0 ? opt.slopes[it.h * job.group + it.row0 + my_row - token_of(job, it.row0 + my_row) * job.group] * kLog2e : 0.0f;
     float m_ref = -INFINITY, l = 0.0f;
-    const bool live = my_row < it.rows;
+    const bool live = my_row >= 0;
     bool ok = true;
     for (int n = first; n < n_blocks && ok; ++n) {
       const int j0 = block_at(it, it.idx1 - 1 - n) * kBlock + 64 * half;  // token of this thread's first column
@@ -614,7 +622,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
         for (int c = 0; c < 2; ++c) {
           uint32_t pk[16];
           float csum = masked ? weights(std::true_type{}, c, m_ref, hi, lo, pre, pk) : weights(std::false_type{}, c, m_ref, hi, lo, pre, pk);
-          if (__any_sync(0xffffffffu, (!(csum < kSumLimit) && live) || m_ref == -INFINITY)) {
+          if (__any_sync(0xffffffffu, live && (!(csum < kSumLimit) || m_ref == -INFINITY))) {
             // Rare: the weights add up to more than 2^14, or the row had seen nothing before.  The reference
             // moves to the chunk's largest score, the weights are formed again, what was stored follows.  A row that
             // still sees nothing keeps -inf and weighs its columns, all masked, against 0.
@@ -789,7 +797,8 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     store_rows<BF16>(ctl.job, it, lane_addr + 256 + 128 * i + 64 * half, first < n_blocks, lt == 0.0f, inv, rows_at, 32 * (wp & 7), out_half, ln, piece);
     if (it.n_seg > 1) {
       // ---- the last piece of a row tile to arrive joins all of them, in the order of their tokens ----
-      if (out_half == 0 && 32 * (wp & 7) + ln < it.rows) *reinterpret_cast<float2*>(piece + kItemRows * kHeadDim + 2 * (32 * (wp & 7) + ln)) = make_float2(state.m_ref, lt);
+      const int mine = row_at(ctl.job, it, 32 * (wp & 7) + ln);
+      if (out_half == 0 && mine >= 0) *reinterpret_cast<float2*>(piece + kItemRows * kHeadDim + 2 * mine) = make_float2(state.m_ref, lt);
       __threadfence();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(BAR_PARTS));
@@ -843,8 +852,8 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       if (job.q_box) {
         // whole tokens fill a tile: two tiled copies of 64 channels each; rows behind the sequence's last hold other
         // sequences' queries, whose results are dropped
-        const int tiles = it.rows > kTileRows ? 2 : 1;
-        if (lane == 0) mbar_expect_tx(bar(BAR_QFULL), tiles * kTileBytes);
+        const int tiles = it.rows > job.tile_rows ? 2 : 1;
+        if (lane == 0) mbar_expect_tx(bar(BAR_QFULL), tiles * job.tile_rows * 256);
         __syncwarp();
         if (lane < 2 * tiles) {
           const int tile = lane >> 1, part = lane & 1;
@@ -852,11 +861,11 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
                       it.q_first + token_of(job, it.row0) + tile * job.q_box, bar(BAR_QFULL));
         }
       } else {
-        // any group: 16-byte units by plain loads, rows behind the last zero
+        // strides that the copy engine cannot express: 16-byte units by plain loads, rows that hold nothing zero
         for (int x = lane; x < kItemRows * 16; x += 32) {
-          const int r = x >> 4, u = x & 15, t = token_of(job, it.row0 + r), g = it.row0 + r - t * job.group;
+          const int r = x >> 4, u = x & 15, mine = row_at(job, it, r), t = token_of(job, it.row0 + max(mine, 0)), g = it.row0 + mine - t * job.group;
           uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (r < it.rows) v = *reinterpret_cast<const uint4*>(job.q.data + (it.q_first + t) * job.q.token + (it.h * job.group + g) * job.q.head + 8 * u);
+          if (mine >= 0) v = *reinterpret_cast<const uint4*>(job.q.data + (it.q_first + t) * job.q.token + (it.h * job.group + g) * job.q.head + 8 * u);
           *reinterpret_cast<uint4*>(sQ + (r >> 7) * kTileBytes + (u >> 3) * (kTileBytes / 2) + (r & 127) * 128 + (((u ^ r) & 7) << 4)) = v;
         }
         fence_async_proxy();
@@ -1043,11 +1052,11 @@ bool make_page_map(CUtensorMap* m, const void* base, const PagedView& pv, const 
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Queries (channel, head, token); boxes of 64 channels x the group's heads x the tokens of a tile.  False where the
-// group does not fill a tile with whole tokens or the strides cannot be expressed.
+// Queries (channel, head, token); boxes of 64 channels x the group's heads x the tokens of a tile.  False where the strides
+// cannot be expressed.
 bool make_query_map(CUtensorMap* m, const RowsView& q, int n_tokens, int group) {
   EncodeTiledFn enc = encode_tiled_fn();
-  if (!enc || kTileRows % group != 0) return false;
+  if (!enc) return false;
   const cuuint64_t gdim[3] = {kHeadDim, static_cast<cuuint64_t>(q.n_heads), static_cast<cuuint64_t>(n_tokens)};
   const cuuint64_t gstride[2] = {static_cast<cuuint64_t>(q.head) * 2, static_cast<cuuint64_t>(q.token) * 2};
   const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(kTileRows / group)};
@@ -1057,9 +1066,10 @@ bool make_query_map(CUtensorMap* m, const RowsView& q, int n_tokens, int group) 
              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// row tiles of all sequences, at most: sum of ceil(rows / 256)
+// row tiles of all sequences, at most: sum of ceil(rows / (two tiles' rows))
 long long row_tiles(int batch, int group, int n_tokens) {
-  return (static_cast<long long>(n_tokens) * group + static_cast<long long>(batch) * (kItemRows - 1)) / kItemRows;
+  const int rows = 2 * (kTileRows / group * group);
+  return (static_cast<long long>(n_tokens) * group + static_cast<long long>(batch) * (rows - 1)) / rows;
 }
 
 template <bool BF16, bool CAP, bool BIAS>
@@ -1100,6 +1110,7 @@ cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const i
   job.cu_q = cu_q;
   job.n_tokens = n_tokens;
   job.group = group;
+  job.tile_rows = kTileRows / group * group;
   job.group_inv = group > 1 ? static_cast<unsigned>(((1ull << 32) + group - 1) / group) : 0u;
   long long grid = items;
   if (workspace) {

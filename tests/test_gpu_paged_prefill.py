@@ -4,7 +4,7 @@ import torch
 
 from paper_2506_07533_b200 import binding as mq
 from tests import paged_reference as R
-from tests.test_gpu_paged import BF, FP, ints, pages, randn
+from tests.test_gpu_paged import BF, FP, decode, ints, pages, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -16,7 +16,7 @@ def prefill(c, q, cu, workspace=True, **opt):
     ws = torch.zeros(mq.moqae_paged_prefill_attn_workspace(c, q.shape[1], q.shape[0]), dtype=torch.uint8, device="cuda") if workspace else None
     outs = []
     for _ in range(2):
-        out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+        out = torch.full(tuple(q.shape), 7.0, dtype=q.dtype, device="cuda")
         mq.moqae_paged_prefill_attn(c, q, cu, out, ws, options)
         outs.append(out)
     assert torch.equal(outs[0], outs[1])
@@ -227,6 +227,19 @@ def test_prefill_strided_rows_other_stream_and_graph():
         out.fill_(7.0)
         graph.replay()
         check(c, q, cu, out)
+
+
+@pytest.mark.parametrize("hq, hkv", [(8, 2), (6, 2)])
+def test_prefill_broadcast_queries(hq, hkv):
+    """Queries with a stride of zero (one row for every token, or for every head) are read as they are."""
+    c = pages([300, 40], hkv, 16, BF, 85)
+    cu = starts([100, 20])
+    for q in (randn(1, hq, 128, dtype=BF, seed=1).expand(120, hq, 128), randn(120, 1, 128, dtype=BF, seed=2).expand(120, hq, 128)):
+        for w in (False, True):
+            check(c, q.contiguous(), cu, prefill(c, q, cu, w))
+    c.kv_len.copy_(ints([5, 40]))
+    one = randn(1, hq, 128, dtype=BF, seed=3).expand(2, hq, 128)
+    assert torch.equal(decode(c, one), decode(c, one.contiguous()))
 
 
 def test_pages_interleaved_in_one_buffer_and_by_head():
