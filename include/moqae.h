@@ -496,9 +496,12 @@ int moqae_paged_append(const moqae_paged_cache* cache, const moqae_rope* rope, c
  *   out[b][h] = softmax(x) V  over the tokens it sees, of kv head h / (n_q_heads / n_kv_heads).
  *   q, out rows [batch][n_q_heads][128] in the cache's dtype, n_q_heads / n_kv_heads in {1, .., 8};
  *   options NULL: scale 1/sqrt(128), nothing else.  Tokens that are not seen are not read.
+ *   batch * n_kv_heads at most 2^18.
  *   workspace: moqae_paged_decode_attn_workspace bytes, 16-byte aligned, ZEROED ONCE after it was
- *   allocated (it ends with arrival counters that every completed call leaves at zero).  Calls, and
- *   replays of captured calls, that share a workspace must be ordered after one another.
+ *   allocated (it starts with 1 MiB of counters that every completed call leaves at zero; zero it again
+ *   after a call that ended in MOQAE_ERR_TIMEOUT).  Calls of this and of moqae_paged_prefill_attn, of any
+ *   sizes, can share one buffer that is large enough for each; they, and replays of captured ones, must
+ *   then be ordered after one another.
  */
 int moqae_paged_decode_attn_workspace(const moqae_paged_cache* cache, int32_t n_q_heads, int64_t* out_bytes);
 int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q, const moqae_rows* out,

@@ -37,6 +37,11 @@ struct RopeView {
 
 constexpr int kMaxQueryTokens = 1 << 24;     // of one call, so that its rows and their tiles count in 32 bits
 
+// A workspace of the attention calls starts with this many counters, which every completed call leaves at zero;
+// what follows is plain scratch.  All calls lay it out alike, so calls of any sizes can share one buffer.
+constexpr int kWorkCounters = 1 << 18;
+constexpr long long kWorkCounterBytes = 4ll * kWorkCounters;
+
 struct AttnOptions {
   const float* slopes;
   const int32_t* prefix_len;
@@ -108,11 +113,11 @@ cudaError_t launch_norm_rope(const RopeView& rope, int dtype, const RowsView& q,
 cudaError_t launch_paged_append(const PagedView& pv, const RopeView& rope, const RowsView& q, const RowsView& q_out,
                                 const RowsView& k, const RowsView& v, const int32_t* positions, const int32_t* seq, int n_tokens,
                                 cudaStream_t st);
-long long paged_decode_workspace_bytes(int batch, int n_kv_heads, int group);
+long long paged_decode_workspace_bytes(int group);
 cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
                                 cudaStream_t st);
-bool paged_few_rows(int batch, int group, int n_tokens);
-long long paged_few_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens);
+bool paged_few_rows(int batch, int n_kv_heads, int group, int n_tokens);
+long long paged_few_workspace_bytes();
 cudaError_t launch_paged_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                              const AttnOptions& opt, void* workspace, cudaStream_t st);
 long long paged_prefill_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens);

@@ -183,7 +183,8 @@ int moqae_paged_decode_attn_workspace(const moqae_paged_cache* cache, int32_t n_
   if (rc == MOQAE_OK) rc = check_group(pv, n_q_heads);
   if (rc != MOQAE_OK) return rc;
   if (!out_bytes) return MOQAE_ERR_INVALID_ARG;
-  *out_bytes = moqae::paged_decode_workspace_bytes(pv.batch, pv.n_kv_heads, n_q_heads / pv.n_kv_heads);
+  if (static_cast<int64_t>(pv.batch) * pv.n_kv_heads > moqae::kWorkCounters) return MOQAE_ERR_UNSUPPORTED;
+  *out_bytes = moqae::paged_decode_workspace_bytes(n_q_heads / pv.n_kv_heads);
   return MOQAE_OK;
 }
 
@@ -196,8 +197,8 @@ int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q,
   if (rc != MOQAE_OK) return rc;
   if (!workspace) return MOQAE_ERR_INVALID_ARG;
   if (!aligned(workspace, 16)) return MOQAE_ERR_MISALIGNED;
-  if (workspace_bytes < moqae::paged_decode_workspace_bytes(pv.batch, pv.n_kv_heads, qv.n_heads / pv.n_kv_heads))
-    return MOQAE_ERR_WORKSPACE_TOO_SMALL;
+  if (static_cast<int64_t>(pv.batch) * pv.n_kv_heads > moqae::kWorkCounters) return MOQAE_ERR_UNSUPPORTED;
+  if (workspace_bytes < moqae::paged_decode_workspace_bytes(qv.n_heads / pv.n_kv_heads)) return MOQAE_ERR_WORKSPACE_TOO_SMALL;
   return cuda_rc(moqae::launch_paged_decode(pv, qv, ov, opt, workspace, static_cast<cudaStream_t>(stream)));
 }
 

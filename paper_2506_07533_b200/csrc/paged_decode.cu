@@ -742,10 +742,8 @@ cudaError_t launch_form(PagedView pv, const AttnOptions& opt, const DecodeJob& j
 
 }  // namespace
 
-// partial results of the CTAs' first and last pairs, then one arrival counter per pair
-long long paged_decode_workspace_bytes(int batch, int n_kv_heads, int group) {
-  return (part_bytes(group) + static_cast<long long>(batch) * n_kv_heads * 4 + 15) / 16 * 16;
-}
+// one arrival counter per pair, then partial results of the CTAs' first and last pairs
+long long paged_decode_workspace_bytes(int group) { return kWorkCounterBytes + part_bytes(group); }
 
 cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
                                 cudaStream_t st) {
@@ -754,21 +752,20 @@ cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const Ro
   job.q = q;
   job.out = out;
   job.group = q.n_heads / pv.n_kv_heads;
-  job.part = static_cast<float*>(workspace);
-  job.arrived = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + part_bytes(job.group));
+  job.arrived = static_cast<int*>(workspace);
+  job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
   return launch_form(pv, opt, job, st);
 }
 
 // Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average.  Measured against
 // the large tiles (us, few / large): 8 sequences of 1008 tokens, 4 rows 19.5 / 20.6, 16 rows 26.5 / 21.0; of 8000 tokens, 16
 // rows 68 / 73, 32 rows 106 / 73; lengths from 100 to 4100, 11 rows 31 / 38.
-bool paged_few_rows(int batch, int group, int n_tokens) {
-  return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * batch;
+bool paged_few_rows(int batch, int n_kv_heads, int group, int n_tokens) {
+  return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * batch &&
+         few_sets(batch, group, n_tokens) * n_kv_heads <= kWorkCounters;
 }
 
-long long paged_few_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens) {
-  return (part_bytes(16) + few_sets(batch, group, n_tokens) * n_kv_heads * 4 + 15) / 16 * 16;
-}
+long long paged_few_workspace_bytes() { return kWorkCounterBytes + part_bytes(16); }
 
 cudaError_t launch_paged_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                              const AttnOptions& opt, void* workspace, cudaStream_t st) {
@@ -779,8 +776,8 @@ cudaError_t launch_paged_few(const PagedView& pv, const RowsView& q, const int32
   job.cu_q = cu_q;
   job.n_tokens = n_tokens;
   job.group = q.n_heads / pv.n_kv_heads;
-  job.part = static_cast<float*>(workspace);
-  job.arrived = reinterpret_cast<int*>(static_cast<uint8_t*>(workspace) + part_bytes(16));
+  job.arrived = static_cast<int*>(workspace);
+  job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
   return launch_form(pv, opt, job, st);
 }
 

@@ -1082,8 +1082,7 @@ cudaError_t launch(const PagedView& pv, const AttnOptions& opt, const PrefillJob
   return cudaGetLastError();
 }
 
-constexpr long long kCounterBytes = (2 + kSplitItems) * 4 + 8;      // a multiple of 16
-static_assert(kCounterBytes % 16 == 0, "partial sums start on 16 bytes");
+static_assert(2 + kSplitItems <= kWorkCounters, "counters of a call");
 
 // partial sums that a call can use: row tiles are only cut where there are few
 long long parts_of(long long items) { return items > kSplitItems ? 0 : (items * kMaxSegs < kMaxParts ? items * kMaxSegs : kMaxParts); }
@@ -1092,14 +1091,14 @@ long long parts_of(long long items) { return items > kSplitItems ? 0 : (items * 
 
 // claim counter, CTAs that are through, arrivals per row tile; then the pieces' partial sums
 long long paged_prefill_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens) {
-  if (paged_few_rows(batch, group, n_tokens)) return paged_few_workspace_bytes(batch, n_kv_heads, group, n_tokens);
-  return kCounterBytes + parts_of(row_tiles(batch, group, n_tokens) * n_kv_heads) * kPartFloats * 4;
+  if (paged_few_rows(batch, n_kv_heads, group, n_tokens)) return paged_few_workspace_bytes();
+  return kWorkCounterBytes + parts_of(row_tiles(batch, group, n_tokens) * n_kv_heads) * kPartFloats * 4;
 }
 
 cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                                  const AttnOptions& opt, void* workspace, cudaStream_t st) {
   const int group = q.n_heads / pv.n_kv_heads;
-  if (workspace && paged_few_rows(pv.batch, group, n_tokens)) return launch_paged_few(pv, q, cu_q, n_tokens, out, opt, workspace, st);
+  if (workspace && paged_few_rows(pv.batch, pv.n_kv_heads, group, n_tokens)) return launch_paged_few(pv, q, cu_q, n_tokens, out, opt, workspace, st);
   const long long n_rb = row_tiles(pv.batch, group, n_tokens);
   if (pv.batch <= 0 || n_tokens <= 0 || n_rb == 0) return cudaSuccess;
   const long long items = n_rb * pv.n_kv_heads;
@@ -1117,7 +1116,7 @@ cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const i
     job.counters = static_cast<unsigned*>(workspace);
     job.max_parts = static_cast<int>(parts_of(items));
     if (job.max_parts > 0) {
-      job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kCounterBytes);
+      job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
       grid = items * kMaxSegs;
     }
   }

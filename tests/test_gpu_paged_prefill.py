@@ -201,6 +201,28 @@ def test_prefill_bad_tables():
     assert (prefill(mq.moqae_paged_bind(c.k_pages, c.v_pages, c.block_table[:0], ints([])), q, ints([0])) == 7.0).all()
 
 
+def test_one_workspace_for_all_calls():
+    """One-token calls, calls for few and for many rows, cut and whole row tiles, all in one buffer, in turn and twice."""
+    shapes = [([1, 1, 1], [4000, 20, 333]), ([300, 7, 200], [0, 900, 60]), ([40], [20000]), ([900] * 3, [100] * 3), ([2, 1, 3], [50, 7000, 1])]
+    calls = []
+    for new, past in shapes:
+        c = pages([a + b for a, b in zip(new, past)], 2, 16, BF, 95)
+        q = randn(sum(new), 8, 128, dtype=BF, seed=len(new) + sum(new))
+        size = [mq.moqae_paged_prefill_attn_workspace(c, 8, q.shape[0])]
+        size += [mq.moqae_paged_decode_attn_workspace(c, 8)] if max(new) == 1 else []
+        calls.append((c, q, starts(new), prefill(c, q, starts(new)), decode(c, q) if max(new) == 1 else None, size))
+    ws = torch.zeros(max(max(x[-1]) for x in calls), dtype=torch.uint8, device="cuda")
+    for _ in range(2):
+        for c, q, cu, want, one, _size in calls + calls[::-1]:
+            out = torch.empty_like(q)
+            mq.moqae_paged_prefill_attn(c, q, cu, out, ws)
+            assert torch.equal(out, want)
+            if one is not None:
+                mq.moqae_paged_decode_attn(c, q, out, ws)
+                assert torch.equal(out, one)
+    assert (ws[:1 << 20] == 0).all()                          # the counters are at rest
+
+
 def test_prefill_strided_rows_other_stream_and_graph():
     new, past = [33, 1, 140], [500, 40, 0]
     c = pages([a + b for a, b in zip(new, past)], 2, 16, BF, 81)

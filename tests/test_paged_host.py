@@ -91,6 +91,9 @@ def test_missing_arguments(lib):
     assert lib.moqae_paged_decode_attn_workspace(c, 8, C.byref(n)) == mq.OK and n.value > 0
     assert lib.moqae_paged_decode_attn(c, q, q, None, A, n.value - 1, None) == mq.ERR_WORKSPACE_TOO_SMALL
     assert lib.moqae_paged_decode_attn_workspace(c, 8, None) == bad
+    many = C.byref(cache(batch=(1 << 17) + 1))
+    assert lib.moqae_paged_decode_attn_workspace(many, 8, C.byref(n)) == mq.ERR_UNSUPPORTED
+    assert lib.moqae_paged_decode_attn(many, q, q, None, A, 1 << 40, None) == mq.ERR_UNSUPPORTED
     assert lib.moqae_paged_prefill_attn(c, q, None, 3, q, None, None, 0, None) == bad
     assert lib.moqae_paged_prefill_attn(c, q, A, -3, q, None, None, 0, None) == bad
     assert lib.moqae_paged_prefill_attn(c, q, A, 3, k, None, None, 0, None) == bad
