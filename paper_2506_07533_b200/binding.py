@@ -388,10 +388,23 @@ def moqae_poll_status(cache: Cache) -> int:
 _DTYPE_CODE = {torch.float16: DT_FP16, torch.bfloat16: DT_BF16}
 
 
-# The calls below are made once per layer and generated token, so their host side is kept short: devices are
-# compared as indices, streams are taken as raw handles.
-_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+# The calls below are made once per layer and generated token; their arguments are taken apart in csrc/marshal.cpp.
+_MARSHAL = None
+
+
+def _native():
+    """The marshalling module, bound to the loaded library.  Raises if it has not been built."""
+    global _MARSHAL
+    if _MARSHAL is None:
+        names = ("moqae_norm_rope", "moqae_paged_append", "moqae_paged_decode_attn", "moqae_paged_prefill_attn")
+        addresses = [C.cast(getattr(lib(), n), C.c_void_p).value for n in names]
+        try:
+            from . import _marshal
+        except ImportError as e:
+            raise RuntimeError(f"{_build.MARSHAL} is missing or was built for another torch: run `python -m paper_2506_07533_b200.build --force`") from e
+        _marshal.bind(*addresses)
+        _MARSHAL = _marshal
+    return _MARSHAL
 
 
 def _need(ok: bool, where: str, code: int = ERR_INVALID_ARG):
@@ -403,46 +416,21 @@ def _vector(t, dtype, n, index, where):
     """Address of a contiguous tensor of `n` values on device `index`; None stays None."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.get_device() != index or t.numel() != n or not t.is_contiguous():
-        raise MoqaeError(ERR_INVALID_ARG, where)
+    _need(t.dtype is dtype and t.get_device() == index and t.numel() == n and t.is_contiguous(), where)
     return t.data_ptr()
-
-
-def _call(where, fn, index, *args):
-    """Run a library function on the current stream of device `index`."""
-    if index == _current_device():
-        rc = fn(*args, _raw_stream(index))
-    else:
-        with torch.cuda.device(index):
-            rc = fn(*args, _raw_stream(index))
-    if rc != OK:
-        raise MoqaeError(rc, where)
-
-
-def _rows(t, dtype, index, where, n):
-    """MoqaeRows of a tensor [n, heads, 128] whose rows are contiguous; None stays None."""
-    if t is None:
-        return None
-    shape = t.shape
-    if t.dtype is not dtype or t.get_device() != index or len(shape) != 3 or shape[2] != 128 or shape[0] != n:
-        raise MoqaeError(ERR_INVALID_ARG, where)
-    stride = t.stride()
-    if stride[2] != 1 and t.numel():
-        raise MoqaeError(ERR_INVALID_ARG, where)
-    return MoqaeRows(t.data_ptr(), stride[0], stride[1], shape[1])
-
-
-def _ref(x):
-    return None if x is None else C.byref(x)
 
 
 @dataclass
 class Rope:
     """A moqae_rope and the tensors it points to."""
     view: MoqaeRope
-    dtype: torch.dtype
-    device: int                  # device index, None without tensors
+    code: int                    # dtype of the rows, -1 without weights
+    device: int                  # device index, -1 without tensors
     tensors: tuple
+    address: int = 0
+
+    def __post_init__(self):
+        self.address = C.addressof(self.view)
 
 
 def rope_table(n_positions, rot_dim, base=10000.0, device="cuda"):
@@ -466,22 +454,15 @@ def make_rope(cos_sin, rot_dim, *, interleaved=False, q_weight=None, k_weight=No
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     view = MoqaeRope(ptr(cos_sin), ptr(q_weight), ptr(k_weight), 0 if cos_sin is None else cos_sin.shape[0], int(rot_dim),
                      int(bool(interleaved)), float(eps))
-    return Rope(view, weights[0].dtype if weights else None, given[0].get_device() if given else None, (cos_sin, q_weight, k_weight))
+    return Rope(view, _DTYPE_CODE[weights[0].dtype] if weights else -1, given[0].get_device() if given else -1, (cos_sin, q_weight, k_weight))
 
 
 def moqae_norm_rope(rope: Rope, q, k, positions, q_out=None, k_out=None, status=None):
     """Norm and rotate query rows q [n, heads, 128] and key rows k (either may be None) into q_out / k_out, which
     default to q and k themselves.  positions int32 [n], negative = padding; status int32 [4] or None."""
-    where = "moqae_norm_rope"
-    some = q if q is not None else k
-    _need(some is not None and some.is_cuda and some.dtype in _DTYPE_CODE, where)
-    dtype, index, n = some.dtype, some.get_device(), some.shape[0]
-    _need(rope.dtype in (None, dtype) and rope.device in (None, index), where)
-    a, b = _rows(q, dtype, index, where, n), _rows(k, dtype, index, where, n)
-    c = a if q_out is None else _rows(q_out, dtype, index, where, n)
-    d = b if k_out is None else _rows(k_out, dtype, index, where, n)
-    _call(where, lib().moqae_norm_rope, index, C.byref(rope.view), _DTYPE_CODE[dtype], _ref(a), _ref(b), _ref(c), _ref(d),
-          _vector(positions, torch.int32, n, index, where), n, _vector(status, torch.int32, 4, index, where))
+    rc = (_MARSHAL or _native()).norm_rope(rope.address, rope.code, rope.device, q, k, positions, q_out, k_out, status)
+    if rc:
+        raise MoqaeError(rc, "moqae_norm_rope")
 
 
 @dataclass
@@ -493,9 +474,13 @@ class PagedCache:
     kv_len: torch.Tensor         # int32 [batch]
     status: torch.Tensor         # int32 [4]
     view: MoqaePagedCache
-    dtype: torch.dtype
+    code: int                    # MOQAE_DTYPE_*
     device: int                  # device index
     batch: int
+    address: int = 0
+
+    def __post_init__(self):
+        self.address = C.addressof(self.view)
 
 
 def moqae_paged_bind(k_pages, v_pages, block_table, kv_len, status=None) -> PagedCache:
@@ -515,21 +500,17 @@ def moqae_paged_bind(k_pages, v_pages, block_table, kv_len, status=None) -> Page
                            _vector(kv_len, torch.int32, block_table.shape[0], index, where), _vector(status, torch.int32, 4, index, where),
                            k_pages.shape[0], k_pages.shape[2], k_pages.shape[1], _DTYPE_CODE[k_pages.dtype],
                            block_table.shape[0], block_table.shape[1])
-    return PagedCache(k_pages, v_pages, block_table, kv_len, status, view, k_pages.dtype, index, block_table.shape[0])
+    return PagedCache(k_pages, v_pages, block_table, kv_len, status, view, _DTYPE_CODE[k_pages.dtype], index, block_table.shape[0])
 
 
 def moqae_paged_append(cache: PagedCache, k, v, positions, *, seq=None, rope: Rope = None, q=None, q_out=None):
     """Put key and value rows k, v [n, n_kv_heads, 128] into their pages: token t is token positions[t] (negative =
     padding) of sequence seq[t] (None: sequence t).  With `rope` keys, and queries q into q_out (default: in
     place), are normalised and rotated on the way."""
-    where = "moqae_paged_append"
-    dtype, index, n = cache.dtype, cache.device, k.shape[0]
-    _need(rope is None or (rope.dtype in (None, dtype) and rope.device in (None, index)), where)
-    _need(q is not None or q_out is None, where)
-    a, b, c = _rows(k, dtype, index, where, n), _rows(v, dtype, index, where, n), _rows(q, dtype, index, where, n)
-    d = c if q_out is None else _rows(q_out, dtype, index, where, n)
-    _call(where, lib().moqae_paged_append, index, C.byref(cache.view), None if rope is None else C.byref(rope.view), _ref(a), _ref(b),
-          _ref(c), _ref(d), _vector(positions, torch.int32, n, index, where), _vector(seq, torch.int32, n, index, where), n)
+    r = (0, -1, -1) if rope is None else (rope.address, rope.code, rope.device)
+    rc = (_MARSHAL or _native()).append(cache.address, cache.code, cache.device, *r, k, v, positions, seq, q, q_out)
+    if rc:
+        raise MoqaeError(rc, "moqae_paged_append")
 
 
 @dataclass
@@ -538,6 +519,10 @@ class AttnOptions:
     view: MoqaeAttnOptions
     slopes: torch.Tensor
     prefix_len: torch.Tensor
+    address: int = 0
+
+    def __post_init__(self):
+        self.address = C.addressof(self.view)
 
 
 def make_attn_options(*, scale=0.0, cap=0.0, window=0, slopes=None, prefix_len=None) -> AttnOptions:
@@ -547,19 +532,14 @@ def make_attn_options(*, scale=0.0, cap=0.0, window=0, slopes=None, prefix_len=N
     return AttnOptions(MoqaeAttnOptions(ptr(slopes), ptr(prefix_len), float(scale), float(cap), int(window)), slopes, prefix_len)
 
 
-def _options(options, cache, n_q_heads, where):
+def _options(options, cache, q, where):
     if options is None:
-        return None
-    _vector(options.slopes, torch.float32, n_q_heads, cache.device, where)
-    _vector(options.prefix_len, torch.int32, cache.batch, cache.device, where)
-    return C.byref(options.view)
-
-
-def _space(workspace, index, where):
-    if workspace is None:
-        return None, 0
-    _need(workspace.is_contiguous() and workspace.get_device() == index, where)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        return 0
+    if options.slopes is not None:
+        _vector(options.slopes, torch.float32, q.shape[1], cache.device, where)
+    if options.prefix_len is not None:
+        _vector(options.prefix_len, torch.int32, cache.batch, cache.device, where)
+    return options.address
 
 
 def moqae_paged_decode_attn_workspace(cache: PagedCache, n_q_heads) -> int:
@@ -572,11 +552,9 @@ def moqae_paged_decode_attn(cache: PagedCache, q, out, workspace, options: AttnO
     """Attention of one new token per sequence: q, out [batch, n_q_heads, 128] in the cache's dtype; workspace a
     tensor of moqae_paged_decode_attn_workspace bytes, zeroed once."""
     where = "moqae_paged_decode_attn"
-    dtype, index, n = cache.dtype, cache.device, cache.batch
-    a, b = _rows(q, dtype, index, where, n), _rows(out, dtype, index, where, n)
-    ptr, nbytes = _space(workspace, index, where)
-    _call(where, lib().moqae_paged_decode_attn, index, C.byref(cache.view), C.byref(a), C.byref(b),
-          _options(options, cache, a.n_heads, where), ptr, nbytes)
+    rc = (_MARSHAL or _native()).decode(cache.address, cache.code, cache.device, cache.batch, q, out, workspace, _options(options, cache, q, where))
+    if rc:
+        raise MoqaeError(rc, where)
 
 
 def moqae_paged_prefill_attn_workspace(cache: PagedCache, n_q_heads, n_tokens) -> int:
@@ -590,11 +568,10 @@ def moqae_paged_prefill_attn(cache: PagedCache, q, cu_q, out, workspace=None, op
     """Attention of the last cu_q[b + 1] - cu_q[b] tokens of every sequence: q, out [n_tokens, n_q_heads, 128] in the
     cache's dtype, cu_q int32 [batch + 1]; workspace None, or moqae_paged_prefill_attn_workspace bytes zeroed once."""
     where = "moqae_paged_prefill_attn"
-    dtype, index, n = cache.dtype, cache.device, q.shape[0]
-    a, b = _rows(q, dtype, index, where, n), _rows(out, dtype, index, where, n)
-    ptr, nbytes = _space(workspace, index, where)
-    _call(where, lib().moqae_paged_prefill_attn, index, C.byref(cache.view), C.byref(a),
-          _vector(cu_q, torch.int32, cache.batch + 1, index, where), n, C.byref(b), _options(options, cache, a.n_heads, where), ptr, nbytes)
+    rc = (_MARSHAL or _native()).prefill(cache.address, cache.code, cache.device, cache.batch, q, cu_q, out, workspace,
+                                         _options(options, cache, q, where))
+    if rc:
+        raise MoqaeError(rc, where)
 
 
 def moqae_paged_validate(cache: PagedCache):
