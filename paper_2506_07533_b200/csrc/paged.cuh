@@ -108,6 +108,25 @@ template <typename K> inline cudaError_t allow_shared_memory(K* kernel, size_t b
   return e;
 }
 
+// Launch so that the grid may be set up while the kernel before it on the stream is finishing.  The kernel starts with
+// after_previous() in every thread, before it touches global memory, so the order of the stream holds.  In a loop of
+// small calls this is 0.5 us (norm and rotation of one token, 3.8 -> 3.3) to 2.5 us (decode, 14.5 -> 11.9) of each.
+template <typename... P, typename... A>
+inline cudaError_t launch_early(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t st, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+
 cudaError_t launch_norm_rope(const RopeView& rope, int dtype, const RowsView& q, const RowsView& k, const RowsView& q_out,
                              const RowsView& k_out, const int32_t* positions, int n_tokens, int32_t* status, cudaStream_t st);
 cudaError_t launch_paged_append(const PagedView& pv, const RopeView& rope, const RowsView& q, const RowsView& q_out,

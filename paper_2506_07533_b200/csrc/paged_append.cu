@@ -42,6 +42,7 @@ template <bool BF16> __device__ __forceinline__ uint4 pack8(const float (&x)[8])
 
 template <bool BF16, bool PAGED>
 __global__ void __launch_bounds__(kAppendWarps * 32) norm_rope_kernel(PagedView pv, RopeView rope, RowJob job) {
+  after_previous();
   const int lane = threadIdx.x & 31, sub = lane & (kRowLanes - 1), slot = lane / kRowLanes;
   const long long w = static_cast<long long>(blockIdx.x) * kAppendWarps + (threadIdx.x >> 5);
   const int t = static_cast<int>(w >> job.parts_shift), part = static_cast<int>(w) & ((1 << job.parts_shift) - 1);
@@ -189,9 +190,8 @@ static cudaError_t launch_rows(const PagedView& pv, const RopeView& rope, RowJob
   while ((1 << job.parts_shift) < passes && (static_cast<long long>(job.n_tokens) << job.parts_shift) < wanted) ++job.parts_shift;
   const long long warps = static_cast<long long>(job.n_tokens) << job.parts_shift;
   const unsigned grid = static_cast<unsigned>((warps + kAppendWarps - 1) / kAppendWarps);
-  if (dtype == MOQAE_DTYPE_BF16) norm_rope_kernel<true, PAGED><<<grid, kAppendWarps * 32, 0, st>>>(pv, rope, job);
-  else norm_rope_kernel<false, PAGED><<<grid, kAppendWarps * 32, 0, st>>>(pv, rope, job);
-  return cudaGetLastError();
+  return launch_early(dtype == MOQAE_DTYPE_BF16 ? norm_rope_kernel<true, PAGED> : norm_rope_kernel<false, PAGED>, grid, kAppendWarps * 32, 0, st,
+                      pv, rope, job);
 }
 
 cudaError_t launch_norm_rope(const RopeView& rope, int dtype, const RowsView& q, const RowsView& k, const RowsView& q_out,

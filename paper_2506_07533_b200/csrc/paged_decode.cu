@@ -262,6 +262,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   const uint32_t ring_u = smem_u32(ring);
   auto token_of = [&](int row) { return FORM == kFew16 ? row / job.group : 0; };
 
+  if (threadIdx.x < 2 * kWarps) desc[threadIdx.x].pair = -1;
+  after_previous();
+
   // ---- where the work is: units and sets of every sequence, then this warp's piece ----
   // sequence b, one head: its units; rows that see nothing are zeros (once per launch: `write`)
   auto units_of = [&](int b, int& sets, bool write) -> int {
@@ -310,7 +313,6 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   const long long lo = cta_lo + share(in_cta, warp, kWarps);
   int todo = static_cast<int>(cta_lo + share(in_cta, warp + 1, kWarps) - lo);
 
-  if (threadIdx.x < 2 * kWarps) desc[threadIdx.x].pair = -1;
   __syncthreads();
 
   if (todo > 0) {
@@ -718,8 +720,7 @@ template <bool BF16, int FORM> cudaError_t launch(const PagedView& pv, const Att
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = allow_shared_memory(paged_decode_kernel<BF16, FORM>, decode_smem(FORM, FORM == kOne4 ? 4 : set_rows(FORM)), done);
   if (e != cudaSuccess) return e;
-  paged_decode_kernel<BF16, FORM><<<sm_count_of_current_device(), kWarps * 32, decode_smem(FORM, rows), st>>>(pv, opt, job);
-  return cudaGetLastError();
+  return launch_early(paged_decode_kernel<BF16, FORM>, sm_count_of_current_device(), kWarps * 32, decode_smem(FORM, rows), st, pv, opt, job);
 }
 
 long long part_bytes(int rows) {

@@ -703,6 +703,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
   volatile int* abort_flag = &ctl.abort;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  after_previous();
   // The planning warp has the first piece before the CTA's barriers stand.
   Plan plan;
   Piece it;                                            // (of the planning warp)
@@ -1078,8 +1079,7 @@ cudaError_t launch(const PagedView& pv, const AttnOptions& opt, const PrefillJob
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = allow_shared_memory(paged_prefill_kernel<BF16, CAP, BIAS>, kSmemBytes, done);
   if (e != cudaSuccess) return e;
-  paged_prefill_kernel<BF16, CAP, BIAS><<<static_cast<unsigned>(grid), kThreads, kSmemBytes, st>>>(pv, opt, job, mk, mv, mq);
-  return cudaGetLastError();
+  return launch_early(paged_prefill_kernel<BF16, CAP, BIAS>, static_cast<unsigned>(grid), kThreads, kSmemBytes, st, pv, opt, job, mk, mv, mq);
 }
 
 static_assert(2 + kSplitItems <= kWorkCounters, "counters of a call");
