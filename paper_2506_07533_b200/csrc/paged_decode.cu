@@ -534,11 +534,12 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) p[e] = x[c][e] == -INFINITY ? 0.0f : exp2_fast(x[c][e] - m[c][e & 1]);
-        l[c][0] += p[0] + p[2];
-        l[c][1] += p[1] + p[3];
         uint32_t h0 = float2_to_pair<BF16>(p[0], p[1]), h1 = float2_to_pair<BF16>(p[2], p[3]);
+        const float2 f0 = pair_to_float2<BF16>(h0), f1 = pair_to_float2<BF16>(h1);
+        // the sum of what is multiplied: without the low halves, the rounded weights
+        l[c][0] += FORM == kFew16 ? f0.x + f1.x : p[0] + p[2];
+        l[c][1] += FORM == kFew16 ? f0.y + f1.y : p[1] + p[3];
         if (FORM != kFew16) {
-          const float2 f0 = pair_to_float2<BF16>(h0), f1 = pair_to_float2<BF16>(h1);
           const uint32_t r0 = float2_to_pair<BF16>(p[0] - f0.x, p[1] - f0.y), r1 = float2_to_pair<BF16>(p[2] - f1.x, p[3] - f1.y);
           if (FORM == kOne4 && t4 >= 2) {         // columns 4..7 carry the low halves of queries 0..3
             h0 = r0;

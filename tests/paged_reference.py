@@ -87,8 +87,11 @@ def attention(q, k, v, first, *, scale=None, cap=0.0, window=0, slopes=None, pre
         # rounding of the weights: halves hi + lo are off by u * u; one half by u, and in fp16 by 2^-25 of a
         # reference weight that is at least a half
         weight = weight + (u * u if split_weights else u)
+        # one half: the norm may add the rounded weights p (1 + e), |e| <= u, of any part of the tokens, which moves the
+        # result by -o times the sum of their p e: at most u |o| more (and u u (mass + |o|) from 1 / (1 + that sum))
+        norm_off = 0.0 if split_weights else u * out[:, h].abs() + 2 * u * u * (mass + out[:, h].abs())
         low = 0.0 if split_weights else 2 * SUBNORMAL[dtype] * torch.where(seen, 1.0, 0.0).double() @ vv.abs()
-        tol[:, h] = weight * mass + low + u * out[:, h].abs() * (1 + u) + SUBNORMAL[dtype] + 1e-30
+        tol[:, h] = weight * mass + low + norm_off + u * out[:, h].abs() * (1 + u) + SUBNORMAL[dtype] + 1e-30
     return out, tol
 
 

@@ -251,6 +251,21 @@ def test_prefill_strided_rows_other_stream_and_graph():
         check(c, q, cu, out)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("new", [[300], [3], [1], [2] * 40, [140, 3, 1, 700]])
+def test_a_row_of_one_token_is_its_value(dtype, new):
+    """p v / p with one p, as rounded for the product: v after any rounding of p (an unrounded norm would be off by p's)."""
+    c = pages(new, 2, 16, dtype, 77)
+    cu = starts(new)
+    q = 3 * randn(sum(new), 8, 128, dtype=dtype, seed=78)
+    for workspace in (False, True):
+        out = prefill(c, q, cu, workspace)
+        check(c, q, cu, out)
+        for b, n in enumerate(new):
+            v = R.gather(c.v_pages, c.block_table[b], 1)[0]
+            assert torch.equal(out[cu[b]], v.repeat_interleave(4, 0))
+
+
 @pytest.mark.parametrize("hq, hkv", [(8, 2), (6, 2)])
 def test_prefill_broadcast_queries(hq, hkv):
     """Queries with a stride of zero (one row for every token, or for every head) are read as they are."""
