@@ -24,6 +24,10 @@
 //   Joining.  A warp that has a pair to itself writes the result.  Other pieces meet in shared memory after the
 //   CTA's last tile; a pair that spans CTAs goes through the workspace, and the CTA that arrives last adds the
 //   pieces in the order of their tokens (results do not depend on timing).
+//   Measured.  61 sequences of 1 to 32000 tokens, 32 / 8 heads, bf16: 128 to 136 us for 798 MB (floor 122); 4 of 131000:
+//   320 to 356 us (floor 328 at the rate of a copy, which writes as much as it reads).  Short calls pay about 12 us beside
+//   their bytes: 2 us to find the work, 2 for the first tile, then 2.5 to join inside a CTA, 1.5 for the fence and the
+//   arrival, 2 to join what CTAs share (8 sequences of 1000: 17.4 us, floor 5).
 #include "paged.cuh"
 #include "ptx.cuh"
 
@@ -300,7 +304,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   const long long total = static_cast<long long>(mine) * pv.n_kv_heads;
   const long long pairs = static_cast<long long>(all_sets) * pv.n_kv_heads;
   // A CTA per pair while that is no more than kPairTiles tiles each: with equal lengths no pair then spans CTAs,
-  // which saves the way through the workspace (333 tokens x 8 heads: 8.1 instead of 10.5 us).  Otherwise every
+  // which saves the way through the workspace (8 sequences of 300 tokens x 8 kv heads: 10.1 instead of 12.9 us).  Otherwise every
   // CTA gets at least kMinTiles tiles per warp.
   const int most = static_cast<int>(gridDim.x);
   int ctas = most;

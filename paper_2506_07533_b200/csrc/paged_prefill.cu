@@ -27,6 +27,13 @@
 //   Where the rows alone would leave SMs idle, the blocks of a row tile are cut into up to kMaxSegs pieces,
 //   as many as an estimate of the turns favours; they leave float32 sums in the workspace and the last to arrive
 //   joins them in the order of their tokens (results do not depend on timing).
+//   What bounds it.  A block of 128 tokens takes a CTA about 3450 clocks (8192 tokens, 32 / 8 heads, bf16: 459 us, 1200
+//   TFLOP/s).  A tile's weights take its 8 warps 1790 of them (the exponential unit, shared with the other tile, needs
+//   1024 per tile), from stored weights to the next scores it is 1710: 16 products of 64 clocks, 390 of their latency, the
+//   wait for the other tile's.  With all exponentials left out the period stays, the wait grows: it is the products' turns
+//   that follow one another.  Looked at and slower: scores of 64 columns, so that four chains overlap (a product of N = 64
+//   takes as long as one of 128: 1.45 x the time), an issuing thread per tile (products of the two kinds interleaved: 1.45 x),
+//   no barrier between the two warps of a row (the same time).
 // Every mbarrier wait is bounded; on expiry the CTA records MOQAE_ERR_TIMEOUT, every role stops and the
 // tensor memory is still freed.
 #include <cstring>
