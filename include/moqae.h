@@ -496,7 +496,7 @@ int moqae_paged_append(const moqae_paged_cache* cache, const moqae_rope* rope, c
  *   out[b][h] = softmax(x) V  over the tokens it sees, of kv head h / (n_q_heads / n_kv_heads).
  *   q, out rows [batch][n_q_heads][128] in the cache's dtype, n_q_heads / n_kv_heads in {1, .., 8};
  *   options NULL: scale 1/sqrt(128), nothing else.  Tokens that are not seen are not read.
- *   batch * n_kv_heads at most 2^18.
+ *   batch * n_kv_heads at most 2^18, batch * n_kv_heads * (max_pages * page_size + 32) below 2^35.
  *   workspace: moqae_paged_decode_attn_workspace bytes, 16-byte aligned, ZEROED ONCE after it was
  *   allocated (it starts with 1 MiB of counters that every completed call leaves at zero; zero it again
  *   after a call that ended in MOQAE_ERR_TIMEOUT).  Calls of this and of moqae_paged_prefill_attn, of any
@@ -514,7 +514,9 @@ int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q,
  * tokens: row i of them has position kv_len[b] - (cu_q[b + 1] - cu_q[b]) + i, so sequences do not see
  * one another.  All keys and values have been appended.
  *   q, out rows [n_tokens][n_q_heads][128] in the cache's dtype, n_tokens and batch at most 2^24;
- *   cu_q int32 [batch + 1], not decreasing, 0 <= cu_q <= n_tokens.  Rows of out that belong to no sequence (those behind
+ *   cu_q int32 [batch + 1], not decreasing, 0 <= cu_q <= n_tokens (values outside count as the nearest, a sequence that
+ *   ends before it starts has no tokens; where sequences share rows, so that they bring more than n_tokens together, the call
+ *   has no results and the status becomes MOQAE_ERR_INVALID_ARG).  Rows of out that belong to no sequence (those behind
  *   cu_q[batch], of a padded batch) are left as they were.
  *   Weights are rounded to the cache's dtype before they meet the values, products accumulate in float32.
  *   workspace: NULL, or moqae_paged_prefill_attn_workspace bytes under the rules of

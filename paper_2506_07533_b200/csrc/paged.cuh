@@ -132,14 +132,15 @@ cudaError_t launch_norm_rope(const RopeView& rope, int dtype, const RowsView& q,
 cudaError_t launch_paged_append(const PagedView& pv, const RopeView& rope, const RowsView& q, const RowsView& q_out,
                                 const RowsView& k, const RowsView& v, const int32_t* positions, const int32_t* seq, int n_tokens,
                                 cudaStream_t st);
+bool paged_decode_fits(const PagedView& pv);        // sizes that the kernel's counters and 32-bit sums hold
 long long paged_decode_workspace_bytes(int group);
 cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
                                 cudaStream_t st);
-bool paged_few_rows(int batch, int n_kv_heads, int group, int n_tokens);
+bool paged_few_rows(const PagedView& pv, int group, int n_tokens);
 long long paged_few_workspace_bytes();
 cudaError_t launch_paged_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                              const AttnOptions& opt, void* workspace, cudaStream_t st);
-long long paged_prefill_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens);
+long long paged_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens);
 cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                                  const AttnOptions& opt, void* workspace, cudaStream_t st);
 

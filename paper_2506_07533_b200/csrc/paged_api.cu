@@ -183,7 +183,7 @@ int moqae_paged_decode_attn_workspace(const moqae_paged_cache* cache, int32_t n_
   if (rc == MOQAE_OK) rc = check_group(pv, n_q_heads);
   if (rc != MOQAE_OK) return rc;
   if (!out_bytes) return MOQAE_ERR_INVALID_ARG;
-  if (static_cast<int64_t>(pv.batch) * pv.n_kv_heads > moqae::kWorkCounters) return MOQAE_ERR_UNSUPPORTED;
+  if (!moqae::paged_decode_fits(pv)) return MOQAE_ERR_UNSUPPORTED;
   *out_bytes = moqae::paged_decode_workspace_bytes(n_q_heads / pv.n_kv_heads);
   return MOQAE_OK;
 }
@@ -197,7 +197,7 @@ int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q,
   if (rc != MOQAE_OK) return rc;
   if (!workspace) return MOQAE_ERR_INVALID_ARG;
   if (!aligned(workspace, 16)) return MOQAE_ERR_MISALIGNED;
-  if (static_cast<int64_t>(pv.batch) * pv.n_kv_heads > moqae::kWorkCounters) return MOQAE_ERR_UNSUPPORTED;
+  if (!moqae::paged_decode_fits(pv)) return MOQAE_ERR_UNSUPPORTED;
   if (workspace_bytes < moqae::paged_decode_workspace_bytes(qv.n_heads / pv.n_kv_heads)) return MOQAE_ERR_WORKSPACE_TOO_SMALL;
   return cuda_rc(moqae::launch_paged_decode(pv, qv, ov, opt, workspace, static_cast<cudaStream_t>(stream)));
 }
@@ -209,7 +209,7 @@ int moqae_paged_prefill_attn_workspace(const moqae_paged_cache* cache, int32_t n
   if (rc != MOQAE_OK) return rc;
   if (!out_bytes || n_tokens < 0) return MOQAE_ERR_INVALID_ARG;
   if (n_tokens > moqae::kMaxQueryTokens || pv.batch > moqae::kMaxQueryTokens) return MOQAE_ERR_UNSUPPORTED;
-  *out_bytes = moqae::paged_prefill_workspace_bytes(pv.batch, pv.n_kv_heads, n_q_heads / pv.n_kv_heads, n_tokens);
+  *out_bytes = moqae::paged_prefill_workspace_bytes(pv, n_q_heads / pv.n_kv_heads, n_tokens);
   return MOQAE_OK;
 }
 
@@ -226,7 +226,7 @@ int moqae_paged_prefill_attn(const moqae_paged_cache* cache, const moqae_rows* q
   if (pv.batch > 0 && !cu_q) return MOQAE_ERR_INVALID_ARG;
   if (!aligned(cu_q, 4) || !aligned(workspace, 16)) return MOQAE_ERR_MISALIGNED;
   if (workspace &&
-      workspace_bytes < moqae::paged_prefill_workspace_bytes(pv.batch, pv.n_kv_heads, qv.n_heads / pv.n_kv_heads, n_tokens))
+      workspace_bytes < moqae::paged_prefill_workspace_bytes(pv, qv.n_heads / pv.n_kv_heads, n_tokens))
     return MOQAE_ERR_WORKSPACE_TOO_SMALL;
   const cudaError_t e = moqae::launch_paged_prefill(pv, qv, cu_q, n_tokens, ov, opt, workspace, static_cast<cudaStream_t>(stream));
   return e == cudaErrorNotSupported ? MOQAE_ERR_UNSUPPORTED : cuda_rc(e);

@@ -74,6 +74,7 @@ struct Seen {
   int len, lo, pre;       // pre <= lo
   int n_pre, first, n;    // tiles of the prefix, first tile behind them, number of tiles
   int sets;               // of the sequence
+  int q_n;                // its query tokens
   int row0, rows;         // rows of the set
   int q_first, pos0;      // row of the queries, and position, of the sequence's first query token
   int prefix;             // what every row sees
@@ -87,17 +88,17 @@ __device__ __forceinline__ Seen seen_of(const PagedView& pv, const AttnOptions& 
   int p_first;
   if (FORM == kFew16) {
     s.q_first = min(max(job.cu_q[b], 0), job.n_tokens);
-    const int q_n = min(max(job.cu_q[b + 1], s.q_first), job.n_tokens) - s.q_first;
-    const int rows = q_n * job.group;
+    s.q_n = min(max(job.cu_q[b + 1], s.q_first), job.n_tokens) - s.q_first;
+    const int rows = s.q_n * job.group;
     s.sets = (rows + 15) / 16;
     s.row0 = set * 16;
     s.rows = min(16, rows - s.row0);
-    s.pos0 = kv_len - q_n;
+    s.pos0 = kv_len - s.q_n;
     p_first = s.pos0 + s.row0 / job.group;
     s.len = s.rows > 0 ? max(s.pos0 + (s.row0 + s.rows - 1) / job.group + 1, s.prefix) : 0;
     s.len = max(s.len, 0);
   } else {
-    s.sets = 1;
+    s.sets = s.q_n = 1;
     s.row0 = 0;
     s.rows = job.group;
     s.q_first = b;
@@ -271,12 +272,14 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
 
   // ---- where the work is: units and sets of every sequence, then this warp's piece ----
   // sequence b, one head: its units; rows that see nothing are zeros (once per launch: `write`)
+  int tokens = 0;                                 // query tokens that this lane has counted
   auto units_of = [&](int b, int& sets, bool write) -> int {
     int units = 0;
     sets = 1;
     for (int set = 0; set < sets; ++set) {
       const Seen s = seen_of<FORM>(pv, opt, job, b, set, write && set == 0 && blockIdx.x == 0);
       sets = s.sets;
+      if (FORM == kFew16 && set == 0) tokens += s.q_n;
       units += s.units();
       if (s.n == 0 && write && b % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x))
         for (int h = 0; h < pv.n_kv_heads; ++h)
@@ -289,7 +292,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     return units;
   };
   int mine = 0, first_units = 0, first_sets = 0, all_sets = 0;
-  for (int b = lane; b < pv.batch; b += 32) {
+  for (int b = lane; b < pv.batch && (FORM != kFew16 || tokens <= job.n_tokens); b += 32) {
     int sets;
     const int u = units_of(b, sets, warp == 0);
     mine += u;
@@ -297,6 +300,13 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     if (b < 32) {
       first_units = u;
       first_sets = sets;
+    }
+  }
+  if (FORM == kFew16) {                           // sequences that share rows could have more sets than there are counters
+    tokens = __reduce_add_sync(0xffffffffu, tokens);
+    if (tokens > job.n_tokens) {
+      if (blockIdx.x == 0 && threadIdx.x == 0) paged_status(pv.status, MOQAE_ERR_INVALID_ARG, -1, tokens);
+      return;
     }
   }
   mine = __reduce_add_sync(0xffffffffu, mine);
@@ -735,6 +745,11 @@ long long part_bytes(int rows) {
 
 long long few_sets(int batch, int group, int n_tokens) { return (static_cast<long long>(n_tokens) * group + 15ll * batch) / 16; }
 
+// Units of all heads are counted in 32 bits.
+bool units_fit(const PagedView& pv, long long sets) {
+  return sets * pv.n_kv_heads * (static_cast<long long>(pv.max_pages) * (pv.page_size / kTile) + kPairCost + 1) < (1ll << 31);
+}
+
 cudaError_t launch_form(PagedView pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
   if (pv.n_pages == 0) {                          // copies of no bytes still name an address
     pv.k = pv.v = job.q.data;
@@ -749,6 +764,10 @@ cudaError_t launch_form(PagedView pv, const AttnOptions& opt, const DecodeJob& j
 }  // namespace
 
 // one arrival counter per pair, then partial results of the CTAs' first and last pairs
+bool paged_decode_fits(const PagedView& pv) {
+  return static_cast<long long>(pv.batch) * pv.n_kv_heads <= kWorkCounters && units_fit(pv, pv.batch);
+}
+
 long long paged_decode_workspace_bytes(int group) { return kWorkCounterBytes + part_bytes(group); }
 
 cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
@@ -766,9 +785,10 @@ cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const Ro
 // Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average.  Measured against
 // the large tiles (us, few / large): 8 sequences of 1008 tokens, 4 rows 19.5 / 20.6, 16 rows 26.5 / 21.0; of 8000 tokens, 16
 // rows 68 / 73, 32 rows 106 / 73; lengths from 100 to 4100, 11 rows 31 / 38.
-bool paged_few_rows(int batch, int n_kv_heads, int group, int n_tokens) {
-  return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * batch &&
-         few_sets(batch, group, n_tokens) * n_kv_heads <= kWorkCounters;
+bool paged_few_rows(const PagedView& pv, int group, int n_tokens) {
+  const long long sets = few_sets(pv.batch, group, n_tokens);
+  return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * pv.batch && sets * pv.n_kv_heads <= kWorkCounters &&
+         units_fit(pv, sets);
 }
 
 long long paged_few_workspace_bytes() { return kWorkCounterBytes + part_bytes(16); }

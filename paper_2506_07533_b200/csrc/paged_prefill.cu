@@ -225,9 +225,11 @@ __device__ __forceinline__ Plan make_plan(const PagedView& pv, const AttnOptions
   float blocks = 0.0f;
   p.mine = 0;
   p.seq = Sequence{0, 0, 0, 0};
-  for (int b = lane; b < pv.batch; b += 32) {
+  int tokens = 0;
+  for (int b = lane; b < pv.batch && tokens <= job.n_tokens; b += 32) {
     const Sequence s = sequence(pv, opt, job, b, blockIdx.x == 0);
     const int n = row_tiles_of(job, s);
+    tokens += s.n;
     if (b < 32) {
       p.seq = s;
       p.mine = n;
@@ -244,6 +246,11 @@ __device__ __forceinline__ Plan make_plan(const PagedView& pv, const AttnOptions
     }
     long_blocks = max(long_blocks, max(first.total, last.total));
     blocks += 0.5f * static_cast<float>(n) * static_cast<float>(first.total + last.total);
+  }
+  tokens = warp_sum(tokens);
+  if (tokens > job.n_tokens) {                         // sequences that share rows could have more row tiles than there are counters
+    items = most = 0;
+    if (blockIdx.x == 0 && lane == 0) paged_status(pv.status, MOQAE_ERR_INVALID_ARG, -1, tokens);
   }
   p.items = warp_sum(items);
   p.most = __reduce_max_sync(0xffffffffu, most);
@@ -1101,15 +1108,15 @@ long long parts_of(long long items) { return items > kSplitItems ? 0 : (items * 
 }  // namespace
 
 // claim counter, CTAs that are through, arrivals per row tile; then the pieces' partial sums
-long long paged_prefill_workspace_bytes(int batch, int n_kv_heads, int group, int n_tokens) {
-  if (paged_few_rows(batch, n_kv_heads, group, n_tokens)) return paged_few_workspace_bytes();
-  return kWorkCounterBytes + parts_of(row_tiles(batch, group, n_tokens) * n_kv_heads) * kPartFloats * 4;
+long long paged_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens) {
+  if (paged_few_rows(pv, group, n_tokens)) return paged_few_workspace_bytes();
+  return kWorkCounterBytes + parts_of(row_tiles(pv.batch, group, n_tokens) * pv.n_kv_heads) * kPartFloats * 4;
 }
 
 cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                                  const AttnOptions& opt, void* workspace, cudaStream_t st) {
   const int group = q.n_heads / pv.n_kv_heads;
-  if (workspace && paged_few_rows(pv.batch, pv.n_kv_heads, group, n_tokens)) return launch_paged_few(pv, q, cu_q, n_tokens, out, opt, workspace, st);
+  if (workspace && paged_few_rows(pv, group, n_tokens)) return launch_paged_few(pv, q, cu_q, n_tokens, out, opt, workspace, st);
   const long long n_rb = row_tiles(pv.batch, group, n_tokens);
   if (pv.batch <= 0 || n_tokens <= 0 || n_rb == 0) return cudaSuccess;
   const long long items = n_rb * pv.n_kv_heads;

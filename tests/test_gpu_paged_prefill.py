@@ -201,6 +201,63 @@ def test_prefill_bad_tables():
     assert (prefill(mq.moqae_paged_bind(c.k_pages, c.v_pages, c.block_table[:0], ints([])), q, ints([0])) == 7.0).all()
 
 
+@pytest.mark.parametrize("n, batch", [(700, 40), (60, 40)])      # large tiles, few rows per sequence
+@pytest.mark.parametrize("workspace", [False, True])
+def test_prefill_sequences_that_share_rows(n, batch, workspace):
+    """Offsets that go back and forth: the sequences' tokens would be more than the call has."""
+    c = pages([800] * batch, 8, 16, BF, 91)
+    q = randn(n, 8, 128, dtype=BF, seed=92)
+    out = prefill(c, q, ints([0, n] * (batch // 2) + [0]), workspace)
+    assert mq.moqae_paged_poll_status(c) == mq.ERR_INVALID_ARG and (out == 7.0).all()
+    c.status.zero_()
+    cu = ints([0] * batch + [n])                                # the same buffers serve the next call
+    check(c, q, cu, prefill(c, q, cu, workspace))
+    assert mq.moqae_paged_poll_status(c) == 0
+
+
+def test_sequences_that_share_pages():
+    c = pages([500, 500, 500, 230], 2, 16, FP, 93)
+    c.block_table[1, :20] = c.block_table[0, :20]
+    c.block_table[2] = c.block_table[0]
+    c.block_table[3, :14] = c.block_table[0, :14]
+    cu = starts([200, 180, 500, 9])
+    q = randn(889, 8, 128, dtype=FP, seed=94)
+    check(c, q, cu, prefill(c, q, cu))
+    q1 = randn(4, 8, 128, dtype=FP, seed=95)
+    out = decode(c, q1)
+    for b, n in enumerate(c.kv_len.tolist()):
+        want, tol = R.attention(q1[b:b + 1], R.gather(c.k_pages, c.block_table[b], n), R.gather(c.v_pages, c.block_table[b], n), n - 1)
+        R.close(out[b:b + 1], want, tol)
+
+
+def test_calls_on_two_streams_at_once():
+    """Each with its own workspace: prompts that fill the GPU, steps and few rows side by side."""
+    c = pages([2100, 900, 40, 3000], 8, 16, BF, 96)
+    q, cu = randn(1500, 32, 128, dtype=BF, seed=97), starts([1000, 400, 0, 100])
+    few, cu_few = randn(9, 32, 128, dtype=BF, seed=98), starts([3, 1, 0, 5])
+    step = randn(4, 32, 128, dtype=BF, seed=99)
+    want = [prefill(c, q, cu), prefill(c, few, cu_few), decode(c, step)]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    room = [torch.zeros(max(mq.moqae_paged_prefill_attn_workspace(c, 32, 1500), mq.moqae_paged_prefill_attn_workspace(c, 32, 9)),
+                        dtype=torch.uint8, device="cuda") for _ in streams]
+    outs = [[torch.empty_like(w) for w in want] for _ in streams]
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                for call in range(3):
+                    kind = (call + i + turn) % 3
+                    if kind == 0:
+                        mq.moqae_paged_prefill_attn(c, q, cu, outs[i][0], room[i])
+                    elif kind == 1:
+                        mq.moqae_paged_prefill_attn(c, few, cu_few, outs[i][1], room[i])
+                    else:
+                        mq.moqae_paged_decode_attn(c, step, outs[i][2], room[i])
+    torch.cuda.synchronize()
+    for got in outs:
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_one_workspace_for_all_calls():
     """One-token calls, calls for few and for many rows, cut and whole row tiles, all in one buffer, in turn and twice."""
     shapes = [([1, 1, 1], [4000, 20, 333]), ([300, 7, 200], [0, 900, 60]), ([40], [20000]), ([900] * 3, [100] * 3), ([2, 1, 3], [50, 7000, 1])]

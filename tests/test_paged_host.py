@@ -105,6 +105,20 @@ def test_missing_arguments(lib):
     assert lib.moqae_paged_poll_status(None, None, None) == bad
 
 
+@pytest.mark.parametrize("batch, heads, max_pages, page, code", [
+    (1 << 18, 1, 1, 16, mq.OK), ((1 << 18) + 1, 1, 1, 16, mq.ERR_UNSUPPORTED), (1 << 14, 1, 8192 * 16 - 3, 16, mq.OK),
+    (1 << 14, 1, 8192 * 16, 16, mq.ERR_UNSUPPORTED), (1 << 5, 1, 1 << 22, 256, mq.ERR_UNSUPPORTED), (31, 1, 1 << 22, 256, mq.OK),
+    (4, 8, 1 << 22, 256, mq.ERR_UNSUPPORTED), (3, 8, 1 << 22, 256, mq.OK)])
+def test_decode_sizes_that_its_counters_hold(lib, batch, heads, max_pages, page, code):
+    assert (batch * heads * (max_pages * page // 16 + 2) < 1 << 31 and batch * heads <= 1 << 18) == (code == mq.OK)
+    n = C.c_int64(0)
+    c = cache(batch=batch, n_kv_heads=heads, max_pages=max_pages, page_size=page)
+    assert lib.moqae_paged_decode_attn_workspace(C.byref(c), heads, C.byref(n)) == code
+    if code != mq.OK:
+        q = C.byref(rows(heads))
+        assert lib.moqae_paged_decode_attn(C.byref(c), q, q, None, A, 1 << 40, None) == code
+
+
 @pytest.mark.parametrize("heads, code", [(0, mq.ERR_INVALID_ARG), (-8, mq.ERR_INVALID_ARG), (7, mq.ERR_INVALID_ARG),
                                          (18, mq.ERR_UNSUPPORTED), (32, mq.ERR_UNSUPPORTED)])
 def test_head_counts(lib, heads, code):
