@@ -66,6 +66,10 @@ __device__ __forceinline__ int paged_len(const PagedView& pv, int b, bool report
 __host__ __device__ constexpr float tanh_coef(int k) {
   return k == 0 ? 0.99999940395f : k == 1 ? -0.33329042792f : k == 2 ? 0.13281433284f : k == 3 ? -0.05160567537f : k == 4 ? 0.01674311422f : -0.00306706037f;
 }
+// The same up to 1/2 with four coefficients (5.5e-7).
+__host__ __device__ constexpr float tanh_coef_near(int k) {
+  return k == 0 ? 0.999999463558f : k == 1 ? -0.333263188601f : k == 2 ? 0.131902962923f : -0.0444022081792f;
+}
 __device__ __forceinline__ float tanh_far(float z) {
   float e, r;
   asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(e) : "f"(z * 2.8853900818f));     // 2 log2(e)

@@ -116,7 +116,8 @@ struct Control {
   int abort;
   unsigned ticket;
   int pair_flag[2][8][2];                            // [turn][warps of the same rows][half]
-  float cap[9];                                      // products up to which the polynomial holds; its coefficients; cap in base-2 units; scale / cap
+  float cap[14];                                     // products up to which the polynomial holds; its 6 coefficients; cap in base-2 units;
+                                                     // scale / cap; products up to which 4 coefficients do; those
   PrefillJob job;                                    // the kernel's arguments, for the functions that are not inlined (a
   AttnOptions opt;                                   // reference to a parameter is read through global memory)
 };
@@ -508,17 +509,37 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     const float scale_log2 = opt.scale * kLog2e;
     float slope = 0.0f;
     const volatile float* cap_of = ctl.cap;            // (the constants of the cap stay in shared memory between uses)
-    // Scores of columns 32 c .. 32 c + 31 in base-2 units, up to a factor and a term that `mul` and `add` give
-    // (so that both join the subtraction of the reference); column e is seen if lo < e <= hi or e < pre.
-    auto scores = [&](auto masked, float (&v)[32], int c, int hi, int lo, int pre, float& mul, float& add) {
+    // Scores of columns 32 c .. 32 c + 31 in base-2 units, plus `off`; `mul` and `add` are what is left to be done (one
+    // multiplication and addition where there is neither cap nor bias); column e is seen if lo < e <= hi or e < pre.
+    auto scores = [&](auto masked, float (&v)[32], int c, float off, int hi, int lo, int pre, float& mul, float& add) {
       tmem_ld32(v, s_addr + 32 * c);
       mul = CAP || BIAS ? 1.0f : scale_log2;
-      add = 0.0f;
+      add = CAP || BIAS ? 0.0f : off;
+      // The bias of column e is slope * (e - dist), one step of arithmetic per pair with `off` in it; where tokens behind
+      // the query may be seen it follows by itself.
+      const float dist = static_cast<float>(hi - 32 * c);                 // of column 0
+      const bool behind = BIAS && pre > 0;
+      const float step = BIAS && !behind ? slope : 0.0f, base = BIAS ? fmaf(-step, dist, off) : off;
+      const uint64_t step2 = pack_f2(step, step), base2 = pack_f2(base, base);
+      auto rest = [&](int e) -> uint64_t { return BIAS ? fma_f2(step2, pack_f2(static_cast<float>(e), static_cast<float>(e + 1)), base2) : base2; };
       if (CAP) {
         float big = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 32; ++e) big = fmaxf(big, fabsf(v[e]));
-        if (__all_sync(0xffffffffu, big <= cap_of[0])) {
+        for (int e = 0; e < 32; e += 2) asm("max.abs.f32 %0, %1, %2, %0;\n" : "+f"(big) : "f"(v[e]), "f"(v[e + 1]));
+        const bool near = __all_sync(0xffffffffu, big <= cap_of[9]);
+        if (near) {                                                       // |x / cap| <= 1/2: 5 steps per pair instead of 7
+          uint64_t t[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float x = cap_of[10 + k];
+            t[k] = pack_f2(x, x);
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const uint64_t y = pack_f2(v[e], v[e + 1]), u = mul_f2(y, y);
+            unpack_f2(fma_f2(y, fma_f2(fma_f2(fma_f2(t[3], u, t[2]), u, t[1]), u, t[0]), rest(e)), v[e], v[e + 1]);
+          }
+        } else if (__all_sync(0xffffffffu, big <= cap_of[0])) {
           uint64_t t[6];
 #pragma unroll
           for (int k = 0; k < 6; ++k) {
@@ -528,28 +549,21 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
             const uint64_t y = pack_f2(v[e], v[e + 1]), u = mul_f2(y, y);
-            unpack_f2(mul_f2(y, fma_f2(fma_f2(fma_f2(fma_f2(fma_f2(t[5], u, t[4]), u, t[3]), u, t[2]), u, t[1]), u, t[0])), v[e], v[e + 1]);
+            unpack_f2(fma_f2(y, fma_f2(fma_f2(fma_f2(fma_f2(fma_f2(t[5], u, t[4]), u, t[3]), u, t[2]), u, t[1]), u, t[0]), rest(e)), v[e], v[e + 1]);
           }
         } else {                                                          // some score passes the cap
           const float w = cap_of[8];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = cap_of[7] * tanh_of(v[e] * w);
+          for (int e = 0; e < 32; ++e) v[e] = fmaf(cap_of[7], tanh_of(v[e] * w), fmaf(step, static_cast<float>(e), base));
         }
       } else if (BIAS) {
         const uint64_t scale2 = pack_f2(scale_log2, scale_log2);
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) unpack_f2(mul_f2(pack_f2(v[e], v[e + 1]), scale2), v[e], v[e + 1]);
+        for (int e = 0; e < 32; e += 2) unpack_f2(fma_f2(pack_f2(v[e], v[e + 1]), scale2, rest(e)), v[e], v[e + 1]);
       }
-      if (BIAS) {
-        const float dist = static_cast<float>(hi - 32 * c);               // of column 0
-        if (pre > 0) {                                                    // tokens behind the query may be seen
+      if (behind) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = fmaf(-slope, fabsf(dist - static_cast<float>(e)), v[e]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = fmaf(slope, static_cast<float>(e), v[e]);
-          add = -slope * dist;
-        }
+        for (int e = 0; e < 32; ++e) v[e] = fmaf(-slope, fabsf(dist - static_cast<float>(e)), v[e]);
       }
       if (masked) {
         if (pre <= 0 && opt.window == 0) {                                // the diagonal alone
@@ -566,14 +580,18 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     // weights of a chunk against the reference, packed; their sum
     auto weights = [&](auto masked, int c, float ref, int hi, int lo, int pre, uint32_t (&pk)[16]) -> float {
       float v[32], mul, add;
-      scores(masked, v, c, hi, lo, pre, mul, add);
-      const uint64_t scale2 = pack_f2(mul, mul), negm2 = pack_f2(add - ref, add - ref);
+      scores(masked, v, c, -ref, hi, lo, pre, mul, add);
+      const uint64_t scale2 = pack_f2(mul, mul), negm2 = pack_f2(add, add);
       uint64_t part[2] = {0ull, 0ull};
 #pragma unroll
       for (int e2 = 0; e2 < 16; ++e2) {
         float x0, x1;
-        const uint64_t vv = pack_f2(v[2 * e2], v[2 * e2 + 1]);
-        unpack_f2(CAP || BIAS ? add_f2(vv, negm2) : fma_f2(vv, scale2, negm2), x0, x1);
+        if (CAP || BIAS) {
+          x0 = v[2 * e2];
+          x1 = v[2 * e2 + 1];
+        } else {
+          unpack_f2(fma_f2(pack_f2(v[2 * e2], v[2 * e2 + 1]), scale2, negm2), x0, x1);
+        }
         const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
         pk[e2] = float2_to_pair<BF16>(p0, p1);
         const float2 r = decltype(masked)::value ? pair_to_float2<BF16>(pk[e2]) : make_float2(p0, p1);
@@ -645,7 +663,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
             // moves to the chunk's largest score, the weights are formed again, what was stored follows.  A row that
             // still sees nothing keeps -inf and weighs its columns, all masked, against 0.
             float v[32], mul, add;
-            scores(std::true_type{}, v, c, hi, lo, pre, mul, add);
+            scores(std::true_type{}, v, c, 0.0f, hi, lo, pre, mul, add);
             float top = v[0];
 #pragma unroll
             for (int e = 1; e < 32; ++e) top = fmaxf(top, v[e]);
@@ -749,6 +767,9 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       ctl.cap[0] = w > 1e-3f && w < 1e3f ? 1.0f / w : -1.0f;
       float power = w * cap2;
       for (int k = 0; k < 6; ++k, power *= w * w) ctl.cap[1 + k] = tanh_coef(k) * power;
+      ctl.cap[9] = 0.5f * ctl.cap[0];
+      power = w * cap2;
+      for (int k = 0; k < 4; ++k, power *= w * w) ctl.cap[10 + k] = tanh_coef_near(k) * power;
       ctl.cap[7] = cap2;
       ctl.cap[8] = w;
     }
