@@ -580,9 +580,39 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     // weights of a chunk against the reference, packed; their sum
     auto weights = [&](auto masked, int c, float ref, int hi, int lo, int pre, uint32_t (&pk)[16]) -> float {
       float v[32], mul, add;
+      uint64_t part[2] = {0ull, 0ull};
+      if (CAP && !decltype(masked)::value && !(BIAS && pre > 0)) {
+        // The ordinary chunk under a cap, in one go: polynomial and exponentials of different columns overlap.
+        tmem_ld32(v, s_addr + 32 * c);
+        float big = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) asm("max.abs.f32 %0, %1, %2, %0;\n" : "+f"(big) : "f"(v[e]), "f"(v[e + 1]));
+        if (__all_sync(0xffffffffu, big <= cap_of[9])) {
+          uint64_t t[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float x = cap_of[10 + k];
+            t[k] = pack_f2(x, x);
+          }
+          const float base = BIAS ? fmaf(-slope, static_cast<float>(hi - 32 * c), -ref) : -ref;
+          const uint64_t step2 = pack_f2(slope, slope), base2 = pack_f2(base, base);
+#pragma unroll
+          for (int e2 = 0; e2 < 16; ++e2) {
+            const uint64_t rest = BIAS ? fma_f2(step2, pack_f2(static_cast<float>(2 * e2), static_cast<float>(2 * e2 + 1)), base2) : base2;
+            const uint64_t y = pack_f2(v[2 * e2], v[2 * e2 + 1]), u = mul_f2(y, y);
+            float x0, x1;
+            unpack_f2(fma_f2(y, fma_f2(fma_f2(fma_f2(t[3], u, t[2]), u, t[1]), u, t[0]), rest), x0, x1);
+            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+            pk[e2] = float2_to_pair<BF16>(p0, p1);
+            part[e2 & 1] = add_f2(part[e2 & 1], pack_f2(p0, p1));
+          }
+          float s0, s1;
+          unpack_f2(add_f2(part[0], part[1]), s0, s1);
+          return s0 + s1;
+        }
+      }
       scores(masked, v, c, -ref, hi, lo, pre, mul, add);
       const uint64_t scale2 = pack_f2(mul, mul), negm2 = pack_f2(add, add);
-      uint64_t part[2] = {0ull, 0ull};
 #pragma unroll
       for (int e2 = 0; e2 < 16; ++e2) {
         float x0, x1;
