@@ -509,19 +509,21 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     const float scale_log2 = opt.scale * kLog2e;
     float slope = 0.0f;
     const volatile float* cap_of = ctl.cap;            // (the constants of the cap stay in shared memory between uses)
-    // Scores of columns 32 c .. 32 c + 31 in base-2 units, plus `off`; `mul` and `add` are what is left to be done (one
-    // multiplication and addition where there is neither cap nor bias); column e is seen if lo < e <= hi or e < pre.
+    // Scores of columns 32 c .. 32 c + 31 in base-2 units, plus `off`; `mul` and `add` are what is left to be done (nothing under
+    // a cap, an addition with a bias, else both); column e is seen if lo < e <= hi or e < pre.
     auto scores = [&](auto masked, float (&v)[32], int c, float off, int hi, int lo, int pre, float& mul, float& add) {
       tmem_ld32(v, s_addr + 32 * c);
       mul = CAP || BIAS ? 1.0f : scale_log2;
-      add = CAP || BIAS ? 0.0f : off;
+      add = CAP ? 0.0f : off;
       // The bias of column e is slope * (e - dist), one step of arithmetic per pair with `off` in it; where tokens behind
       // the query may be seen it follows by itself.
       const float dist = static_cast<float>(hi - 32 * c);                 // of column 0
       const bool behind = BIAS && pre > 0;
       const float step = BIAS && !behind ? slope : 0.0f, base = BIAS ? fmaf(-step, dist, off) : off;
-      const uint64_t step2 = pack_f2(step, step), base2 = pack_f2(base, base);
-      auto rest = [&](int e) -> uint64_t { return BIAS ? fma_f2(step2, pack_f2(static_cast<float>(e), static_cast<float>(e + 1)), base2) : base2; };
+      // (column numbers are constants of the instruction here; as packed pairs they would have to be moved to registers)
+      auto rest = [&](int e) -> uint64_t {
+        return BIAS ? pack_f2(fmaf(step, static_cast<float>(e), base), fmaf(step, static_cast<float>(e + 1), base)) : pack_f2(base, base);
+      };
       if (CAP) {
         float big = 0.0f;
 #pragma unroll
@@ -556,12 +558,20 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = fmaf(cap_of[7], tanh_of(v[e] * w), fmaf(step, static_cast<float>(e), base));
         }
-      } else if (BIAS) {
+      } else if (BIAS) {                                                  // (in `rest`, too, it would cost registers that are not there)
         const uint64_t scale2 = pack_f2(scale_log2, scale_log2);
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) unpack_f2(fma_f2(pack_f2(v[e], v[e + 1]), scale2, rest(e)), v[e], v[e + 1]);
+        for (int e = 0; e < 32; e += 2) unpack_f2(mul_f2(pack_f2(v[e], v[e + 1]), scale2), v[e], v[e + 1]);
+        if (pre > 0) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = fmaf(-slope, fabsf(dist - static_cast<float>(e)), v[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = fmaf(slope, static_cast<float>(e), v[e]);
+          add = off - slope * dist;
+        }
       }
-      if (behind) {
+      if (CAP && behind) {
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] = fmaf(-slope, fabsf(dist - static_cast<float>(e)), v[e]);
       }
@@ -582,7 +592,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
       float v[32], mul, add;
       uint64_t part[2] = {0ull, 0ull};
       if (CAP && !decltype(masked)::value && !(BIAS && pre > 0)) {
-        // The ordinary chunk under a cap, in one go: polynomial and exponentials of different columns overlap.
+        // The ordinary chunk under a cap in one go: arithmetic and exponentials of different columns overlap.
         tmem_ld32(v, s_addr + 32 * c);
         float big = 0.0f;
 #pragma unroll
@@ -595,10 +605,10 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
             t[k] = pack_f2(x, x);
           }
           const float base = BIAS ? fmaf(-slope, static_cast<float>(hi - 32 * c), -ref) : -ref;
-          const uint64_t step2 = pack_f2(slope, slope), base2 = pack_f2(base, base);
 #pragma unroll
           for (int e2 = 0; e2 < 16; ++e2) {
-            const uint64_t rest = BIAS ? fma_f2(step2, pack_f2(static_cast<float>(2 * e2), static_cast<float>(2 * e2 + 1)), base2) : base2;
+            const uint64_t rest = BIAS ? pack_f2(fmaf(slope, static_cast<float>(2 * e2), base), fmaf(slope, static_cast<float>(2 * e2 + 1), base))
+                                       : pack_f2(base, base);
             const uint64_t y = pack_f2(v[2 * e2], v[2 * e2 + 1]), u = mul_f2(y, y);
             float x0, x1;
             unpack_f2(fma_f2(y, fma_f2(fma_f2(fma_f2(t[3], u, t[2]), u, t[1]), u, t[0]), rest), x0, x1);
@@ -616,12 +626,8 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 #pragma unroll
       for (int e2 = 0; e2 < 16; ++e2) {
         float x0, x1;
-        if (CAP || BIAS) {
-          x0 = v[2 * e2];
-          x1 = v[2 * e2 + 1];
-        } else {
-          unpack_f2(fma_f2(pack_f2(v[2 * e2], v[2 * e2 + 1]), scale2, negm2), x0, x1);
-        }
+        const uint64_t vv = pack_f2(v[2 * e2], v[2 * e2 + 1]);
+        unpack_f2(CAP ? vv : BIAS ? add_f2(vv, negm2) : fma_f2(vv, scale2, negm2), x0, x1);
         const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
         pk[e2] = float2_to_pair<BF16>(p0, p1);
         const float2 r = decltype(masked)::value ? pair_to_float2<BF16>(pk[e2]) : make_float2(p0, p1);
