@@ -26,8 +26,8 @@
 //   pieces in the order of their tokens (results do not depend on timing).
 //   Measured.  61 sequences of 1 to 32000 tokens, 32 / 8 heads, bf16: 128 to 136 us for 798 MB (floor 122); 4 of 131000:
 //   320 to 356 us (floor 328 at the rate of a copy, which writes as much as it reads).  Short calls pay about 12 us beside
-//   their bytes: 2 us to find the work, 2 for the first tile, then 2.5 to join inside a CTA, 1.5 for the fence and the
-//   arrival, 2 to join what CTAs share (8 sequences of 1000: 17.4 us, floor 5).
+//   their bytes: 2 us to find the work, 2 for the first tile, then 2.5 to join inside a CTA, 1.2 for the fence and the
+//   arrival, 2 to join what CTAs share (8 sequences of 1000: 16.7 us, floor 5).
 #include "paged.cuh"
 #include "ptx.cuh"
 
@@ -180,7 +180,8 @@ template <int FORM> __device__ __forceinline__ int advance(Cursor& c, const Page
 struct Piece {
   int pair;               // set * n_kv_heads + h, or -1
   int starts, ends;       // whether it holds the pair's first and last tile
-  int b, set, n;          // sequence, its set, tiles of the pair
+  int set, n;             // set of the sequence, tiles of the pair
+  int rows, q_first;      // rows of the set, first row of the sequence's queries
   long long unit;         // unit of the pair's first tile
 };
 
@@ -635,9 +636,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
             d.pair = get.flat * pv.n_kv_heads + get.h;
             d.starts = from_start;
             d.ends = last_of_pair;
-            d.b = get.b;
             d.set = get.set;
             d.n = get.s.n;
+            d.rows = get.s.rows;
+            d.q_first = get.s.q_first;
             d.unit = at - get.i;
           }
         }
@@ -658,14 +660,10 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   const int my_pair = lane < 2 * kWarps ? desc[lane].pair : -1;
   const unsigned valid = __ballot_sync(0xffffffffu, my_pair >= 0);
   if (valid == 0) return;
-  // rows of the pair of piece i, and where row r of it goes
-  auto rows_of = [&](int i) -> int {
-    return FORM == kFew16 ? seen_of<FORM>(pv, opt, job, desc[i].b, desc[i].set, false).rows : job.group;
-  };
+  // where row r of the pair of piece i goes
   auto row_of = [&](int i, int r) -> uint16_t* {
     const int h = desc[i].pair % pv.n_kv_heads, row = desc[i].set * kRows + r, t = token_of(row);
-    const int first = FORM == kFew16 ? min(max(job.cu_q[desc[i].b], 0), job.n_tokens) : desc[i].b;
-    return job.out.data + (first + t) * job.out.token + static_cast<long long>(h * job.group + row - t * job.group) * job.out.head;
+    return job.out.data + (desc[i].q_first + t) * job.out.token + static_cast<long long>(h * job.group + row - t * job.group) * job.out.head;
   };
   // Runs of pieces of one pair; a warp takes jobs of two rows of a run.  A run that is not the whole pair goes to the
   // workspace: slot 1 if it holds the pair's first tile (at most one run, the last), slot 0 otherwise (the first).
@@ -677,7 +675,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     const bool starts = desc[first].starts, whole = starts && desc[31 - __clz(run)].ends;
     if (!whole) cross[starts] = first;
     float* joined = job.part + (static_cast<long long>(cta) * 2 + (starts ? 1 : 0)) * piece_floats;
-    const int rows = rows_of(first);
+    const int rows = desc[first].rows;
     for (int r0 = 0; r0 < rows; r0 += 2, ++n_job) {
       if (n_job % kWarps != warp) continue;
       const int r = r0 + (lane >> 4);
@@ -693,19 +691,24 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
 
   // ---- pairs that span CTAs: the CTA that arrives last adds the pieces ----
   auto cta_of = [&](long long unit) -> int {      // largest c with share(total, c, ctas) <= unit
-    int c = static_cast<int>(static_cast<double>(unit) * ctas / static_cast<double>(total));
+    int c = min(static_cast<int>(static_cast<float>(unit) * static_cast<float>(ctas) / static_cast<float>(total)), ctas - 1);
     while (c > 0 && share(total, c, ctas) > unit) --c;
     while (c + 1 < ctas && share(total, c + 1, ctas) <= unit) ++c;
     return c;
   };
+  // (the last two warps speak for the two pairs: they have the fewest rows to join, if any)
+  const int which = kWarps - 1 - warp, speaks_for = which < 2 ? cross[which] : -1;
+  int c0 = 0, c1 = 0;
+  if (speaks_for >= 0) {
+    c0 = cta_of(desc[speaks_for].unit);
+    c1 = cta_of(desc[speaks_for].unit + desc[speaks_for].n - 1);
+  }
   __threadfence();
   __syncthreads();
-  if (warp < 2 && cross[warp] >= 0 && lane == 0) {
-    const Piece& d = desc[cross[warp]];
-    const int c0 = cta_of(d.unit), c1 = cta_of(d.unit + d.n - 1);
-    turn[warp] = static_cast<int>(atomicInc(reinterpret_cast<unsigned*>(job.arrived) + d.pair, static_cast<unsigned>(c1 - c0)));
-    turn[2 + warp] = c0;
-    turn[4 + warp] = c1;
+  if (speaks_for >= 0 && lane == 0) {
+    turn[which] = static_cast<int>(atomicInc(reinterpret_cast<unsigned*>(job.arrived) + desc[speaks_for].pair, static_cast<unsigned>(c1 - c0)));
+    turn[2 + which] = c0;
+    turn[4 + which] = c1;
   }
   __syncthreads();
   n_job = 0;
@@ -715,7 +718,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     const int from = turn[2 + k], to = turn[4 + k];
     if (turn[k] != to - from) continue;
     __threadfence();
-    const int rows = rows_of(cross[k]);
+    const int rows = desc[cross[k]].rows;
     for (int r0 = 0; r0 < rows; r0 += 2, ++n_job) {
       if (n_job % kWarps != warp) continue;
       const int r = r0 + (lane >> 4);
