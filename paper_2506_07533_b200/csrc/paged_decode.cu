@@ -42,7 +42,7 @@ constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kMinTiles = 2;                     // a CTA is worth starting for this many tiles per warp
 constexpr int kPairTiles = 48;                   // up to so many tiles per pair, a CTA takes whole pairs where it can
 constexpr int kPairCost = 1;                     // what a pair costs beside its tiles, in tiles (its queries, its result)
-constexpr int kFewRows = 12;                     // see paged_few_rows
+constexpr int kFewRows = 16;                     // see paged_few_rows
 constexpr float kLag = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -766,11 +766,11 @@ cudaError_t launch_form(PagedView pv, const AttnOptions& opt, const DecodeJob& j
 
 }  // namespace
 
-// one arrival counter per pair, then partial results of the CTAs' first and last pairs
 bool paged_decode_fits(const PagedView& pv) {
   return static_cast<long long>(pv.batch) * pv.n_kv_heads <= kWorkCounters && units_fit(pv, pv.batch);
 }
 
+// one arrival counter per pair, then partial results of the CTAs' first and last pairs
 long long paged_decode_workspace_bytes(int group) { return kWorkCounterBytes + part_bytes(group); }
 
 cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
@@ -785,9 +785,9 @@ cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const Ro
   return launch_form(pv, opt, job, st);
 }
 
-// Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average.  Measured against
-// the large tiles (us, few / large): 8 sequences of 1008 tokens, 4 rows 19.5 / 20.6, 16 rows 26.5 / 21.0; of 8000 tokens, 16
-// rows 68 / 73, 32 rows 106 / 73; lengths from 100 to 4100, 11 rows 31 / 38.
+// Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average, one set of rows.
+// Measured against the large tiles (us, few / large): 8 sequences of 1000 tokens, 4 rows 17.8 / 21.2, 16 rows 22.2 / 21.3, 32
+// rows 27.0 / 21.9; of 8000 tokens, 16 rows 58.9 / 74.7, 32 rows 93.3 / 74.4; 64 of 500 tokens, 16 rows 44.7 / 49.4.
 bool paged_few_rows(const PagedView& pv, int group, int n_tokens) {
   const long long sets = few_sets(pv.batch, group, n_tokens);
   return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * pv.batch && sets * pv.n_kv_heads <= kWorkCounters &&
