@@ -178,18 +178,34 @@ template <int FORM> __device__ __forceinline__ int advance(Cursor& c, const Page
 
 // Which pair a piece in shared memory belongs to.
 struct Piece {
-  int pair;               // set * n_kv_heads + h, or -1
+  int pair, h;            // set * n_kv_heads + h, or -1; h
   int starts, ends;       // whether it holds the pair's first and last tile
   int set, n;             // set of the sequence, tiles of the pair
   int rows, q_first;      // rows of the set, first row of the sequence's queries
   long long unit;         // unit of the pair's first tile
 };
 
-// Half a warp adds row r of n pieces (piece(p): address of the p-th, in the order of their tokens), a lane eight
-// channels, and writes the finished row (out != null) or the joined piece.  r >= rows: it only keeps the other half
-// company.  The first pieces' sums are on their way while the references are compared.
-template <bool BF16, bool REMOTE, typename F>
-__device__ __forceinline__ void join_row(F piece, int n, int rows, int r, int lane, uint16_t* out, float* joined) {
+// The end of a row's joining: the finished row (out != null), or the joined piece.
+template <bool BF16>
+__device__ __forceinline__ void put_row(const float (&acc)[8], float m, float l, int rows, int r, int sub, uint16_t* out, float* joined) {
+  if (out) {
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    *reinterpret_cast<uint4*>(out + 8 * sub) =
+        make_uint4(float2_to_pair<BF16>(acc[0] * inv, acc[1] * inv), float2_to_pair<BF16>(acc[2] * inv, acc[3] * inv),
+                   float2_to_pair<BF16>(acc[4] * inv, acc[5] * inv), float2_to_pair<BF16>(acc[6] * inv, acc[7] * inv));
+  } else {
+    float4* dst = reinterpret_cast<float4*>(joined + r * kHeadDim) + 2 * sub;
+    dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    if (sub == 0) *reinterpret_cast<float2*>(joined + rows * kHeadDim + 2 * r) = make_float2(m, l);
+  }
+}
+
+// Half a warp adds row r of n pieces of the workspace (piece(p): address of the p-th, in the order of their tokens), a
+// lane eight channels, and writes the finished row.  r >= rows: it only keeps the other half company.  The first pieces'
+// sums are on their way while the references are compared.
+template <bool BF16, typename F>
+__device__ __forceinline__ void join_far(F piece, int n, int rows, int r, int lane, uint16_t* out) {
   constexpr int kBatch = 4;
   const int sub = lane & 15;
   const bool act = r < rows;
@@ -201,17 +217,14 @@ __device__ __forceinline__ void join_row(F piece, int n, int rows, int r, int la
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const float4* src = reinterpret_cast<const float4*>(piece(min(p0 + k, n - 1)) + r * kHeadDim) + 2 * sub;
-      v[k][0] = REMOTE ? __ldcg(src) : src[0];
-      v[k][1] = REMOTE ? __ldcg(src + 1) : src[1];
+      v[k][0] = __ldcg(src);
+      v[k][1] = __ldcg(src + 1);
     }
   };
   for (int base = 0; base < n; base += 16) {
     load(base);
     float2 w = make_float2(-INFINITY, 0.0f);
-    if (base + sub < n) {
-      const float2* ml = reinterpret_cast<const float2*>(piece(base + sub) + at_ml);
-      w = REMOTE ? __ldcg(ml) : *ml;
-    }
+    if (base + sub < n) w = __ldcg(reinterpret_cast<const float2*>(piece(base + sub) + at_ml));
     float top = fmaxf(m, w.x);
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -236,18 +249,38 @@ __device__ __forceinline__ void join_row(F piece, int n, int rows, int r, int la
       }
     }
   }
-  if (!act) return;
-  if (out) {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    *reinterpret_cast<uint4*>(out + 8 * sub) =
-        make_uint4(float2_to_pair<BF16>(acc[0] * inv, acc[1] * inv), float2_to_pair<BF16>(acc[2] * inv, acc[3] * inv),
-                   float2_to_pair<BF16>(acc[4] * inv, acc[5] * inv), float2_to_pair<BF16>(acc[6] * inv, acc[7] * inv));
-  } else {
-    float4* dst = reinterpret_cast<float4*>(joined + r * kHeadDim) + 2 * sub;
-    dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-    dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-    if (sub == 0) *reinterpret_cast<float2*>(joined + at_ml) = make_float2(m, l);
+  if (act) put_row<BF16>(acc, m, l, rows, r, sub, out, nullptr);
+}
+
+// The same for pieces in shared memory (bit i of `run`: piece(i)), and where the run is not the whole pair (out == null) the
+// sum goes on as a piece.  They are near enough to be read twice: a pass for the reference, one for the sums.  (The exchange between lanes above costs as much as a dozen pieces do here: jobs of two
+// pieces took 2050 clocks.)
+template <bool BF16, typename P>
+__device__ __forceinline__ void join_near(P piece, unsigned run, int rows, int r, int lane, uint16_t* out, float* joined) {
+  const int sub = lane & 15;
+  const bool act = r < rows;
+  r = act ? r : rows - 1;
+  const int at_ml = rows * kHeadDim + 2 * r;
+  float m = -INFINITY, l = 0.0f, acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (unsigned bits = run; bits; bits &= bits - 1) m = fmaxf(m, piece(__ffs(bits) - 1)[at_ml]);
+#pragma unroll 2
+  for (unsigned bits = run; bits; bits &= bits - 1) {
+    const float* from = piece(__ffs(bits) - 1);
+    const float2 w = *reinterpret_cast<const float2*>(from + at_ml);
+    const float4* x = reinterpret_cast<const float4*>(from + r * kHeadDim) + 2 * sub;
+    const float4 a = x[0], b = x[1];
+    const float f = w.x == -INFINITY ? 0.0f : exp2_fast(w.x - m);
+    l = fmaf(w.y, f, l);
+    acc[0] = fmaf(a.x, f, acc[0]);
+    acc[1] = fmaf(a.y, f, acc[1]);
+    acc[2] = fmaf(a.z, f, acc[2]);
+    acc[3] = fmaf(a.w, f, acc[3]);
+    acc[4] = fmaf(b.x, f, acc[4]);
+    acc[5] = fmaf(b.y, f, acc[5]);
+    acc[6] = fmaf(b.z, f, acc[6]);
+    acc[7] = fmaf(b.w, f, acc[7]);
   }
+  if (act) put_row<BF16>(acc, m, l, rows, r, sub, out, joined);
 }
 
 template <bool BF16, int FORM>
@@ -634,6 +667,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
           if (lane == 0) {
             Piece& d = desc[2 * warp + which];
             d.pair = get.flat * pv.n_kv_heads + get.h;
+            d.h = get.h;
             d.starts = from_start;
             d.ends = last_of_pair;
             d.set = get.set;
@@ -662,32 +696,29 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   if (valid == 0) return;
   // where row r of the pair of piece i goes
   auto row_of = [&](int i, int r) -> uint16_t* {
-    const int h = desc[i].pair % pv.n_kv_heads, row = desc[i].set * kRows + r, t = token_of(row);
+    const int h = desc[i].h, row = desc[i].set * kRows + r, t = token_of(row);
     return job.out.data + (desc[i].q_first + t) * job.out.token + static_cast<long long>(h * job.group + row - t * job.group) * job.out.head;
   };
   // Runs of pieces of one pair; a warp takes jobs of two rows of a run.  A run that is not the whole pair goes to the
   // workspace: slot 1 if it holds the pair's first tile (at most one run, the last), slot 0 otherwise (the first).
-  int n_job = 0, cross[2] = {-1, -1};             // first pieces of the runs that span CTAs
+  int n_job = 0, cross0 = -1, cross1 = -1;        // first pieces of the runs that span CTAs (no array: it would live in local memory)
   for (unsigned rest = valid; rest;) {
     const int first = __ffs(rest) - 1, pair = __shfl_sync(0xffffffffu, my_pair, first);
     const unsigned run = __ballot_sync(0xffffffffu, my_pair == pair);
     rest &= ~run;
     const bool starts = desc[first].starts, whole = starts && desc[31 - __clz(run)].ends;
-    if (!whole) cross[starts] = first;
+    if (!whole && starts) cross1 = first;
+    if (!whole && !starts) cross0 = first;
     float* joined = job.part + (static_cast<long long>(cta) * 2 + (starts ? 1 : 0)) * piece_floats;
     const int rows = desc[first].rows;
     for (int r0 = 0; r0 < rows; r0 += 2, ++n_job) {
       if (n_job % kWarps != warp) continue;
       const int r = r0 + (lane >> 4);
       // (row `rows` of an odd count reads the last one and is not written)
-      join_row<BF16, false>([&](int p) {
-        unsigned bits = run;                      // the p-th piece of the run
-        for (; p > 0; --p) bits &= bits - 1;
-        return piece_at(__ffs(bits) - 1);
-      }, __popc(run), piece_rows, r < rows ? r : piece_rows, lane, whole && r < rows ? row_of(first, r) : nullptr, joined);
+      join_near<BF16>(piece_at, run, piece_rows, r < rows ? r : piece_rows, lane, whole && r < rows ? row_of(first, r) : nullptr, joined);
     }
   }
-  if (cross[0] < 0 && cross[1] < 0) return;
+  if (cross0 < 0 && cross1 < 0) return;
 
   // ---- pairs that span CTAs: the CTA that arrives last adds the pieces ----
   auto cta_of = [&](long long unit) -> int {      // largest c with share(total, c, ctas) <= unit
@@ -697,11 +728,11 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     return c;
   };
   // (the last two warps speak for the two pairs: they have the fewest rows to join, if any)
-  const int which = kWarps - 1 - warp, speaks_for = which < 2 ? cross[which] : -1;
+  const int which = kWarps - 1 - warp, speaks_for = which == 0 ? cross0 : which == 1 ? cross1 : -1;
   int c0 = 0, c1 = 0;
-  if (speaks_for >= 0) {
-    c0 = cta_of(desc[speaks_for].unit);
-    c1 = cta_of(desc[speaks_for].unit + desc[speaks_for].n - 1);
+  if (speaks_for >= 0) {                          // both ends at once, on two lanes
+    c0 = cta_of(desc[speaks_for].unit + (lane == 1 ? desc[speaks_for].n - 1 : 0));
+    c1 = __shfl_sync(0xffffffffu, c0, 1);
   }
   __threadfence();
   __syncthreads();
@@ -714,17 +745,18 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   n_job = 0;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    if (cross[k] < 0) continue;
+    const int piece = k ? cross1 : cross0;
+    if (piece < 0) continue;
     const int from = turn[2 + k], to = turn[4 + k];
     if (turn[k] != to - from) continue;
     __threadfence();
-    const int rows = desc[cross[k]].rows;
+    const int rows = desc[piece].rows;
     for (int r0 = 0; r0 < rows; r0 += 2, ++n_job) {
       if (n_job % kWarps != warp) continue;
       const int r = r0 + (lane >> 4);
-      join_row<BF16, true>([&](int p) -> const float* {
+      join_far<BF16>([&](int p) -> const float* {
         return job.part + (static_cast<long long>(from + p) * 2 + (p == 0 ? 1 : 0)) * piece_floats;
-      }, to - from + 1, piece_rows, r < rows ? r : piece_rows, lane, r < rows ? row_of(cross[k], r) : nullptr, nullptr);
+      }, to - from + 1, piece_rows, r < rows ? r : piece_rows, lane, r < rows ? row_of(piece, r) : nullptr);
     }
   }
 }
