@@ -25,9 +25,9 @@
 //   CTA's last tile; a pair that spans CTAs goes through the workspace, and the CTA that arrives last adds the
 //   pieces in the order of their tokens (results do not depend on timing).
 //   Measured.  61 sequences of 1 to 32000 tokens, 32 / 8 heads, bf16: 128 to 136 us for 798 MB (floor 122); 4 of 131000:
-//   320 to 356 us (floor 328 at the rate of a copy, which writes as much as it reads).  Short calls pay about 12 us beside
-//   their bytes: 2 us to find the work, 2 for the first tile, then 2.5 to join inside a CTA, 1.2 for the fence and the
-//   arrival, 2 to join what CTAs share (8 sequences of 1000: 16.7 us, floor 5).
+//   320 to 356 us (floor 328 at the rate of a copy, which writes as much as it reads).  Short calls pay about 10 us beside
+//   their bytes: 2 us to find the work, 2 for the first tile, 1 to 3 to join inside a CTA, 1 for the fence and the
+//   arrival, 2 to join what CTAs share (8 sequences of 1000: 16.2 us, floor 5; 128 of 300: 38, floor 24).
 #include "paged.cuh"
 #include "ptx.cuh"
 
@@ -254,7 +254,7 @@ __device__ __forceinline__ void join_far(F piece, int n, int rows, int r, int la
 
 // The same for pieces in shared memory (bit i of `run`: piece(i)), and where the run is not the whole pair (out == null) the
 // sum goes on as a piece.  They are near enough to be read twice: a pass for the reference, one for the sums.  (The exchange between lanes above costs as much as a dozen pieces do here: jobs of two
-// pieces took 2050 clocks.)
+// pieces took 2050 clocks instead of 1000.)
 template <bool BF16, typename P>
 __device__ __forceinline__ void join_near(P piece, unsigned run, int rows, int r, int lane, uint16_t* out, float* joined) {
   const int sub = lane & 15;
@@ -701,22 +701,28 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   };
   // Runs of pieces of one pair; a warp takes jobs of two rows of a run.  A run that is not the whole pair goes to the
   // workspace: slot 1 if it holds the pair's first tile (at most one run, the last), slot 0 otherwise (the first).
-  int n_job = 0, cross0 = -1, cross1 = -1;        // first pieces of the runs that span CTAs (no array: it would live in local memory)
-  for (unsigned rest = valid; rest;) {
-    const int first = __ffs(rest) - 1, pair = __shfl_sync(0xffffffffu, my_pair, first);
-    const unsigned run = __ballot_sync(0xffffffffu, my_pair == pair);
-    rest &= ~run;
-    const bool starts = desc[first].starts, whole = starts && desc[31 - __clz(run)].ends;
-    if (!whole && starts) cross1 = first;
-    if (!whole && !starts) cross0 = first;
-    float* joined = job.part + (static_cast<long long>(cta) * 2 + (starts ? 1 : 0)) * piece_floats;
-    const int rows = desc[first].rows;
-    for (int r0 = 0; r0 < rows; r0 += 2, ++n_job) {
-      if (n_job % kWarps != warp) continue;
-      const int r = r0 + (lane >> 4);
-      // (row `rows` of an odd count reads the last one and is not written)
-      join_near<BF16>(piece_at, run, piece_rows, r < rows ? r : piece_rows, lane, whole && r < rows ? row_of(first, r) : nullptr, joined);
-    }
+  // Lane i looks at piece i, so that a warp finds its jobs without walking over all runs.
+  const unsigned run = __match_any_sync(0xffffffffu, my_pair);
+  const bool opens = my_pair >= 0 && (run & ((1u << lane) - 1u)) == 0;          // the first piece of its run
+  const bool starts = opens && desc[lane].starts, whole = starts && desc[31 - __clz(run)].ends;
+  const int cross0 = __ffs(__ballot_sync(0xffffffffu, opens && !whole && !starts)) - 1;    // first pieces of the runs that span CTAs
+  const int cross1 = __ffs(__ballot_sync(0xffffffffu, opens && !whole && starts)) - 1;
+  const int jobs = opens ? (desc[lane].rows + 1) / 2 : 0;
+  int jobs_to = jobs;                             // of pieces 0 .. lane
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, jobs_to, o);
+    if (lane >= o) jobs_to += x;
+  }
+  const int n_jobs = __shfl_sync(0xffffffffu, jobs_to, 31);
+  for (int j = warp; j < n_jobs; j += kWarps) {
+    const int first = __ffs(__ballot_sync(0xffffffffu, jobs_to > j)) - 1;
+    const int r = 2 * (j - __shfl_sync(0xffffffffu, jobs_to - jobs, first)) + (lane >> 4), rows = desc[first].rows;
+    const bool to_out = __shfl_sync(0xffffffffu, whole ? 1 : 0, first) != 0;
+    float* joined = job.part + (static_cast<long long>(cta) * 2 + (desc[first].starts ? 1 : 0)) * piece_floats;
+    // (row `rows` of an odd count reads the last one and is not written)
+    join_near<BF16>(piece_at, __shfl_sync(0xffffffffu, run, first), piece_rows, r < rows ? r : piece_rows, lane,
+                    to_out && r < rows ? row_of(first, r) : nullptr, joined);
   }
   if (cross0 < 0 && cross1 < 0) return;
 
@@ -742,7 +748,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
     turn[4 + which] = c1;
   }
   __syncthreads();
-  n_job = 0;
+  int n_job = 0;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int piece = k ? cross1 : cross0;
