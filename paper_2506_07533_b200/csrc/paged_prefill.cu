@@ -850,12 +850,13 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     const int n_blocks = it.idx1 - it.idx0, first = min(max(it.idx1 - it.nb[i], 0), n_blocks);
     const SoftmaxState state = softmax_blocks<BF16, CAP, BIAS>(ctl, k & 1, tmem, exch, phase);
     phase = state.phase;
+    // A tile without blocks in this piece exchanges nothing (both sums are 0): its warps have not met since they sent out
+    // the rows of the piece before, and the place of the sums may still hold rows of the partner's.
+    const bool worked = first < n_blocks;
     bool ok = state.ok;
-    if (ok) {
-      if (first < n_blocks) {
-        ok = wait_all(BAR_OFULL + i, phase >> 1);
-        phase ^= 2;
-      }
+    if (ok && worked) {
+      ok = wait_all(BAR_OFULL + i, phase >> 1);
+      phase ^= 2;
       exch[lane * 2 + half] = state.l;
       ok = !(meet(ok ? 0 : 2) & 2);
     }
@@ -866,11 +867,14 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     tc_fence_after();
     const int ln = fresh(lane), wp = fresh(warp), out_half = wp >> 3;   // see fresh()
     uint8_t* rows_at = sOut + (2 * (wp & 7) + out_half) * kWarpStage;
-    const float lt = exch[ln * 2] + exch[ln * 2 + 1];
+    float lt = 0.0f;
+    if (worked) {
+      lt = exch[ln * 2] + exch[ln * 2 + 1];
+      pair_sync();                                     // the sums have been read: their place takes rows
+    }
     const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-    pair_sync();                                       // the sums have been read: their place takes rows
     float* piece = job.part + static_cast<long long>(it.part) * kPartFloats;
-    store_rows<BF16>(ctl.job, it, lane_addr + 256 + 128 * i + 64 * half, first < n_blocks, lt == 0.0f, inv, rows_at, 32 * (wp & 7), out_half, ln, piece);
+    store_rows<BF16>(ctl.job, it, lane_addr + 256 + 128 * i + 64 * half, worked, lt == 0.0f, inv, rows_at, 32 * (wp & 7), out_half, ln, piece);
     if (it.n_seg > 1) {
       // ---- the last piece of a row tile to arrive joins all of them, in the order of their tokens ----
       const int mine = row_at(ctl.job, it, 32 * (wp & 7) + ln);
