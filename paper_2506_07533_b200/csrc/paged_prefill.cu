@@ -508,11 +508,26 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     };
     const float scale_log2 = opt.scale * kLog2e;
     float slope = 0.0f;
+    const bool live = row_at(job, it, row) >= 0;
     const volatile float* cap_of = ctl.cap;            // (the constants of the cap stay in shared memory between uses)
+    // What the row does not see.  Under a cap the scores there are taken out of the choice of the polynomial, too, as are
+    // rows that hold nothing: they come from whatever stood in shared memory, and the forms differ in their last bits.
+    auto hide = [&](float (&v)[32], int c, int hi, int lo, int pre, float with) {
+      if (pre <= 0 && opt.window == 0) {                                  // the diagonal alone
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if (32 * c + e > hi) v[e] = with;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          if (!((32 * c + e <= hi && 32 * c + e > lo) || 32 * c + e < pre)) v[e] = with;
+      }
+    };
     // Scores of columns 32 c .. 32 c + 31 in base-2 units, plus `off`; `mul` and `add` are what is left to be done (nothing under
     // a cap, an addition with a bias, else both); column e is seen if lo < e <= hi or e < pre.
     auto scores = [&](auto masked, float (&v)[32], int c, float off, int hi, int lo, int pre, float& mul, float& add) {
       tmem_ld32(v, s_addr + 32 * c);
+      if (CAP && masked) hide(v, c, hi, lo, pre, 0.0f);
       mul = CAP || BIAS ? 1.0f : scale_log2;
       add = CAP ? 0.0f : off;
       // The bias of column e is slope * (e - dist), one step of arithmetic per pair with `off` in it; where tokens behind
@@ -528,7 +543,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
         float big = 0.0f;
 #pragma unroll
         for (int e = 0; e < 32; e += 2) asm("max.abs.f32 %0, %1, %2, %0;\n" : "+f"(big) : "f"(v[e]), "f"(v[e + 1]));
-        const bool near = __all_sync(0xffffffffu, big <= cap_of[9]);
+        const bool near = __all_sync(0xffffffffu, !live || big <= cap_of[9]);
         if (near) {                                                       // |x / cap| <= 1/2: 5 steps per pair instead of 7
           uint64_t t[4];
 #pragma unroll
@@ -541,7 +556,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
             const uint64_t y = pack_f2(v[e], v[e + 1]), u = mul_f2(y, y);
             unpack_f2(fma_f2(y, fma_f2(fma_f2(fma_f2(t[3], u, t[2]), u, t[1]), u, t[0]), rest(e)), v[e], v[e + 1]);
           }
-        } else if (__all_sync(0xffffffffu, big <= cap_of[0])) {
+        } else if (__all_sync(0xffffffffu, !live || big <= cap_of[0])) {
           uint64_t t[6];
 #pragma unroll
           for (int k = 0; k < 6; ++k) {
@@ -575,17 +590,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] = fmaf(-slope, fabsf(dist - static_cast<float>(e)), v[e]);
       }
-      if (masked) {
-        if (pre <= 0 && opt.window == 0) {                                // the diagonal alone
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (32 * c + e > hi) v[e] = -INFINITY;
-        } else {
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            if (!((32 * c + e <= hi && 32 * c + e > lo) || 32 * c + e < pre)) v[e] = -INFINITY;
-        }
-      }
+      if (masked) hide(v, c, hi, lo, pre, -INFINITY);
     };
     // weights of a chunk against the reference, packed; their sum
     auto weights = [&](auto masked, int c, float ref, int hi, int lo, int pre, uint32_t (&pk)[16]) -> float {
@@ -597,7 +602,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
         float big = 0.0f;
 #pragma unroll
         for (int e = 0; e < 32; e += 2) asm("max.abs.f32 %0, %1, %2, %0;\n" : "+f"(big) : "f"(v[e]), "f"(v[e + 1]));
-        if (__all_sync(0xffffffffu, big <= cap_of[9])) {
+        if (__all_sync(0xffffffffu, !live || big <= cap_of[9])) {
           uint64_t t[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -653,12 +658,14 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     auto position = [&](int r) {
       return it.pos0 + token_of(job, it.row0 + min((r >> 7) * job.tile_rows + min(r & 127, job.tile_rows - 1), it.rows - 1));
     };
-    const int my_row = row_at(job, it, row), qpos = position(row);
+    const int qpos = position(row);
     // tokens all_from .. all_to are seen by every row of the warp
     const int all_to = position(row & ~31), all_from = opt.window > 0 ? position(row | 31) - opt.window + 1 : -0x40000000;
-    if (BIAS) slope = my_row >= 0 ? opt.slopes[it.h * job.group + it.row0 + my_row - token_of(job, it.row0 + my_row) * job.group] * kLog2e : 0.0f;
+    if (BIAS) {
+      const int my_row = row_at(job, it, row);
+      slope = my_row >= 0 ? opt.slopes[it.h * job.group + it.row0 + my_row - token_of(job, it.row0 + my_row) * job.group] * kLog2e : 0.0f;
+    }
     float m_ref = -INFINITY, l = 0.0f;
-    const bool live = my_row >= 0;
     bool ok = true;
     for (int n = first; n < n_blocks && ok; ++n) {
       const int j0 = block_at(it, it.idx1 - 1 - n) * kBlock + 64 * half;  // token of this thread's first column
