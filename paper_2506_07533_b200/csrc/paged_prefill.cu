@@ -837,8 +837,8 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     float* exch = reinterpret_cast<float*>(sOut + 2 * pair_id * kWarpStage);   // [32 rows][2 halves], while no rows are staged there
     auto pair_sync = [&]() { asm volatile("bar.sync %0, 64;\n" ::"r"(1 + pair_id) : "memory"); };
     // The two warps of the same rows meet and tell each other whether they are all right (flag 2: a wait ran
-    // out, both leave) and whether a reference has to move (flag 1).  A warp whose wait ran out meets its
-    // partner once more, wherever that is, so that nobody waits at the pair's barrier for good.
+    // out, both leave) and whether a reference has to move (flag 1).  A warp that leaves, because its wait ran out or because there
+    // is no more work, meets its partner once more, wherever that is, so that nobody waits at the pair's barrier for good.
     uint32_t phase = 0;                                // parities: 1 sfull / pfull, 2 ofull, 4 parts / ticket, 8 turn of the flags
     auto meet = [&](int flag) -> int {
       volatile int* f = ctl.pair_flag[phase >> 3][pair_id];
@@ -853,7 +853,10 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       meet(2);
       break;
     }
-    if (it.rows == 0) break;                           // no more work
+    if (it.rows == 0) {                                // no more work
+      meet(0);
+      break;
+    }
     const int n_blocks = it.idx1 - it.idx0, first = min(max(it.idx1 - it.nb[i], 0), n_blocks);
     const SoftmaxState state = softmax_blocks<BF16, CAP, BIAS>(ctl, k & 1, tmem, exch, phase);
     phase = state.phase;
@@ -867,10 +870,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       exch[lane * 2 + half] = state.l;
       ok = !(meet(ok ? 0 : 2) & 2);
     }
-    if (!ok) {
-      if (lane == 0) paged_status(pv.status, MOQAE_ERR_TIMEOUT, static_cast<int>(blockIdx.x), warp);
-      break;
-    }
+    if (!ok) break;
     tc_fence_after();
     const int ln = fresh(lane), wp = fresh(warp), out_half = wp >> 3;   // see fresh()
     uint8_t* rows_at = sOut + (2 * (wp & 7) + out_half) * kWarpStage;
@@ -902,7 +902,6 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       phase ^= 4;
       if (!ok) {
         meet(2);                                       // wherever the partner is, it leaves too
-        if (lane == 0) paged_status(pv.status, MOQAE_ERR_TIMEOUT, static_cast<int>(blockIdx.x), warp);
         break;
       }
       if (*const_cast<volatile unsigned*>(&ctl.ticket) == static_cast<unsigned>(it.n_seg - 1)) {
@@ -1117,6 +1116,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
   }
   tc_fence_before();
   __syncthreads();
+  if (tid == 0 && *abort_flag) paged_status(pv.status, MOQAE_ERR_TIMEOUT, static_cast<int>(blockIdx.x), -1);   // whoever gave up
   if (warp == kIssueWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kTmemCols) : "memory");
 }
