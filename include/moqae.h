@@ -500,7 +500,7 @@ int moqae_paged_append(const moqae_paged_cache* cache, const moqae_rope* rope, c
  *   workspace: moqae_paged_decode_attn_workspace bytes, 16-byte aligned, ZEROED ONCE after it was
  *   allocated (it starts with 1 MiB of counters that every completed call leaves at zero; zero it again
  *   after a call that ended in MOQAE_ERR_TIMEOUT).  Calls of this and of moqae_paged_prefill_attn, of any
- *   sizes, can share one buffer that is large enough for each; they, and replays of captured ones, must
+ *   sizes, can share one buffer that is large enough for the largest; they, and replays of captured ones, must
  *   then be ordered after one another.
  */
 int moqae_paged_decode_attn_workspace(const moqae_paged_cache* cache, int32_t n_q_heads, int64_t* out_bytes);
@@ -521,7 +521,8 @@ int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q,
  *   Weights are rounded to the cache's dtype before they meet the values, products accumulate in float32.
  *   workspace: NULL, or moqae_paged_prefill_attn_workspace bytes under the rules of
  *   moqae_paged_decode_attn; with one, the tokens of few queries over a long context are
- *   shared out among the SMs.  The call encodes the pages' strides for the copy engine and refuses
+ *   shared out among the SMs.  The size for n_tokens and cache->batch is enough for every call of no more tokens and no
+ *   more sequences with the same head counts, and for moqae_paged_decode_attn (85 MB at most).  The call encodes the pages' strides for the copy engine and refuses
  *   strides it cannot express (MOQAE_ERR_UNSUPPORTED).
  */
 int moqae_paged_prefill_attn_workspace(const moqae_paged_cache* cache, int32_t n_q_heads, int32_t n_tokens,

@@ -558,6 +558,7 @@ def moqae_paged_decode_attn(cache: PagedCache, q, out, workspace, options: AttnO
 
 
 def moqae_paged_prefill_attn_workspace(cache: PagedCache, n_q_heads, n_tokens) -> int:
+    """Bytes for every call of up to n_tokens tokens over up to as many sequences as `cache` has, one-token calls included."""
     out = C.c_int64(0)
     _check(lib().moqae_paged_prefill_attn_workspace(C.byref(cache.view), int(n_q_heads), int(n_tokens), C.byref(out)),
            "moqae_paged_prefill_attn_workspace")

@@ -140,6 +140,7 @@ bool paged_decode_fits(const PagedView& pv);        // sizes that the kernel's c
 long long paged_decode_workspace_bytes(int group);
 cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace,
                                 cudaStream_t st);
+constexpr int kFewRows = 16;                 // see paged_few_rows
 bool paged_few_rows(const PagedView& pv, int group, int n_tokens);
 long long paged_few_workspace_bytes();
 cudaError_t launch_paged_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,

@@ -42,7 +42,6 @@ constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kMinTiles = 2;                     // a CTA is worth starting for this many tiles per warp
 constexpr int kPairTiles = 48;                   // up to so many tiles per pair, a CTA takes whole pairs where it can
 constexpr int kPairCost = 1;                     // what a pair costs beside its tiles, in tiles (its queries, its result)
-constexpr int kFewRows = 16;                     // see paged_few_rows
 constexpr float kLag = 8.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 

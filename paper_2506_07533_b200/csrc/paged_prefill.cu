@@ -1175,10 +1175,15 @@ long long parts_of(long long items) { return items > kSplitItems ? 0 : (items * 
 
 }  // namespace
 
-// claim counter, CTAs that are through, arrivals per row tile; then the pieces' partial sums
+// Claim counter, CTAs that are through, arrivals per row tile; then the pieces' partial sums.  Enough for every call of up to
+// n_tokens tokens and pv.batch sequences: a call of more row tiles than are ever cut still asks for the parts that a smaller one
+// would use, so that a buffer sized for the largest call serves them all.
 long long paged_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens) {
-  if (paged_few_rows(pv, group, n_tokens)) return paged_few_workspace_bytes();
-  return kWorkCounterBytes + parts_of(row_tiles(pv.batch, group, n_tokens) * pv.n_kv_heads) * kPartFloats * 4;
+  const long long few = paged_few_workspace_bytes();
+  if (static_cast<long long>(n_tokens) * group <= kFewRows && paged_few_rows(pv, group, n_tokens)) return few;    // few rows however many sequences
+  const long long most = kSplitItems / pv.n_kv_heads, n_rb = row_tiles(pv.batch, group, n_tokens);
+  const long long cut = kWorkCounterBytes + parts_of((n_rb < most ? n_rb : most) * pv.n_kv_heads) * kPartFloats * 4;
+  return cut > few ? cut : few;
 }
 
 cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,

@@ -63,3 +63,21 @@ def test_capped_results_do_not_depend_on_what_nobody_sees(opt, hq):
             check(c, q, cu, out, **opt)
             want = out
         assert torch.equal(out, want), f"{rest}: {int((out != want).sum())} values differ"
+
+
+def test_a_workspace_for_the_largest_call_serves_the_smaller_ones():
+    """Prompts, pieces, few rows and single tokens with one buffer that was sized once, for the most tokens and sequences."""
+    shapes = [([5000], [0]), ([512], [3000]), ([900] * 5, [10] * 5), ([3, 1, 0], [700, 9, 50]), ([1] * 5, [40, 3000, 7, 0, 333]), ([17], [9000])]
+    most = pages([5000] + [0] * 4, 8, 16, BF, 121)
+    ws = torch.zeros(mq.moqae_paged_prefill_attn_workspace(most, 32, 5000), dtype=torch.uint8, device="cuda")
+    for new, past in shapes:
+        c = pages([a + b for a, b in zip(new, past)], 8, 16, BF, 122)
+        cu, q = starts(new), randn(sum(new), 32, 128, dtype=BF, seed=123)
+        out = torch.full_like(q, 7.0)
+        mq.moqae_paged_prefill_attn(c, q, cu, out, ws)
+        check(c, q, cu, out)
+        if set(new) == {1}:
+            one = torch.empty_like(q)
+            mq.moqae_paged_decode_attn(c, q, one, ws)
+            check(c, q, cu, one)
+    assert (ws[:1 << 20] == 0).all()
