@@ -66,13 +66,17 @@ int64_t tokens_of(PyObject* o) {
   return t && t->dim() == 3 && t->size(0) <= INT32_MAX ? t->size(0) : -1;
 }
 
-// The interpreter is free while the library enqueues (as it is under ctypes).
+// The interpreter is free while the library enqueues (as it is under ctypes), and held again however that ends.
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  Unlocked() = default;
+  Unlocked(const Unlocked&) = delete;
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
 template <typename F> int enqueue(F call) {
-  int rc;
-  Py_BEGIN_ALLOW_THREADS
-  rc = call(c10::cuda::getCurrentCUDAStream().stream());
-  Py_END_ALLOW_THREADS
-  return rc;
+  void* stream = c10::cuda::getCurrentCUDAStream().stream();
+  const Unlocked free;
+  return call(stream);
 }
 
 template <typename T> T address(PyObject* o) { return static_cast<T>(PyLong_AsVoidPtr(o)); }
