@@ -29,6 +29,17 @@ def needs_build() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _torch_include() -> str:
+    """The headers of the torch that is imported here, or an empty string where it has none, or none for CUDA."""
+    try:
+        import torch
+    except ImportError:
+        return ""
+    path = os.path.join(os.path.dirname(torch.__file__), "include")
+    needed = (("torch", "csrc", "autograd", "python_variable.h"), ("c10", "cuda", "CUDAStream.h"))
+    return path if all(os.path.exists(os.path.join(path, *n)) for n in needed) else ""
+
+
 def build_marshal(force: bool = False) -> str:
     """The argument marshalling module, against the torch that is imported here."""
     src = os.path.join(CSRC, "marshal.cpp")
@@ -38,9 +49,9 @@ def build_marshal(force: bool = False) -> str:
     import sysconfig
 
     import torch
-    t = os.path.dirname(torch.__file__)
+    t, headers = os.path.dirname(torch.__file__), _torch_include()
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
-    include = [os.path.join(ROOT, "include"), os.path.join(t, "include"), os.path.join(t, "include", "torch", "csrc", "api", "include"),
+    include = [os.path.join(ROOT, "include"), headers, os.path.join(headers, "torch", "csrc", "api", "include"),
                sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
     subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{d}" for d in include], src, "-o", MARSHAL,
@@ -49,9 +60,17 @@ def build_marshal(force: bool = False) -> str:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    build_marshal(force)
-    if not force and not needs_build():
-        return LIB
+    """The C library, which needs nvcc alone, then the Python module, where torch and its headers are there."""
+    if force or needs_build():
+        _build_library(verbose)
+    if _torch_include():
+        build_marshal(force)
+    else:
+        sys.stderr.write(f"torch or its headers are not here: {os.path.basename(MARSHAL)} is left out (the C library does not need it)\n")
+    return LIB
+
+
+def _build_library(verbose: bool) -> None:
     objs = []
     bdir = os.path.join(HERE, "_build")
     os.makedirs(bdir, exist_ok=True)
@@ -73,7 +92,6 @@ def build(force: bool = False, verbose: bool = False) -> str:
             raise RuntimeError(f"nvcc failed on {src}")
     cmd = [_nvcc(), "-shared", "-o", LIB, *objs, "-Xcompiler", "-fPIC", "-cudart", "static"]
     subprocess.check_call(cmd)
-    return LIB
 
 
 if __name__ == "__main__":
