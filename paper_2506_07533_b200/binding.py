@@ -398,10 +398,13 @@ def _native():
     if _MARSHAL is None:
         names = ("moqae_norm_rope", "moqae_paged_append", "moqae_paged_decode_attn", "moqae_paged_prefill_attn")
         addresses = [C.cast(getattr(lib(), n), C.c_void_p).value for n in names]
+        missing = f"{_build.MARSHAL} is missing or was built for another torch: run `python -m paper_2506_07533_b200.build`"
         try:
             from . import _marshal
         except ImportError as e:
-            raise RuntimeError(f"{_build.MARSHAL} is missing or was built for another torch: run `python -m paper_2506_07533_b200.build --force`") from e
+            raise RuntimeError(missing) from e
+        if getattr(_marshal, "built_for", None) != _build.marshal_key():
+            raise RuntimeError(missing)
         _marshal.bind(*addresses)
         _MARSHAL = _marshal
     return _MARSHAL

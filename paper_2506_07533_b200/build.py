@@ -40,12 +40,21 @@ def _torch_include() -> str:
     return path if all(os.path.exists(os.path.join(path, *n)) for n in needed) else ""
 
 
+def marshal_key() -> str:
+    """What the argument marshalling module is built against: layouts of tensors and objects are compiled into it."""
+    import torch
+    return f"torch {torch.__version__}, C++ ABI {int(torch._C._GLIBCXX_USE_CXX11_ABI)}, {sys.implementation.cache_tag}"
+
+
 def build_marshal(force: bool = False) -> str:
-    """The argument marshalling module, against the torch that is imported here."""
+    """The argument marshalling module, against the torch that is imported here; again if it was built against another."""
     src = os.path.join(CSRC, "marshal.cpp")
     deps = [src, os.path.join(ROOT, "include", "moqae.h")]
+    key = marshal_key()
     if not force and os.path.exists(MARSHAL) and all(os.path.getmtime(d) <= os.path.getmtime(MARSHAL) for d in deps):
-        return MARSHAL
+        with open(MARSHAL, "rb") as f:
+            if key.encode() in f.read():
+                return MARSHAL
     import sysconfig
 
     import torch
@@ -53,7 +62,7 @@ def build_marshal(force: bool = False) -> str:
     cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
     include = [os.path.join(ROOT, "include"), headers, os.path.join(headers, "torch", "csrc", "api", "include"),
                sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
-    subprocess.check_call(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+    subprocess.check_call(["g++", f'-DMOQAE_BUILT_FOR="{key}"', "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[f"-I{d}" for d in include], src, "-o", MARSHAL,
                            "-L" + os.path.join(t, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
     return MARSHAL

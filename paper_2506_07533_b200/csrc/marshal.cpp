@@ -202,4 +202,9 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__marshal() { return PyModule_Create(&kModule); }
+// built_for: the torch and Python whose inlined accessors are in here (build.marshal_key()); binding.py compares it with its own.
+PyMODINIT_FUNC PyInit__marshal() {
+  PyObject* m = PyModule_Create(&kModule);
+  if (m && PyModule_AddStringConstant(m, "built_for", MOQAE_BUILT_FOR) != 0) Py_CLEAR(m);
+  return m;
+}

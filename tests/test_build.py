@@ -56,3 +56,27 @@ def test_the_library_needs_no_torch(compilers, monkeypatch, tmp_path, lacks, cap
     assert B.build() == B.LIB and os.path.exists(B.LIB) and not os.path.exists(B.MARSHAL)
     assert compilers and all(is_library(c) for c in compilers)
     assert "_marshal.so is left out" in capsys.readouterr().err
+
+
+def test_the_module_is_built_again_for_another_torch(compilers, monkeypatch):
+    """It holds layouts of torch's objects, so its age alone does not say that it fits."""
+    import torch
+    B.build_marshal()
+    B.build_marshal()
+    assert len(compilers) == 1
+    monkeypatch.setattr(torch, "__version__", "9.9.9")
+    B.build_marshal()
+    B.build_marshal()
+    assert len(compilers) == 2
+
+
+def test_a_module_for_another_torch_is_refused(monkeypatch):
+    from paper_2506_07533_b200 import binding as mq
+    B.build()
+    monkeypatch.setattr(mq, "_MARSHAL", None)
+    assert mq._native().built_for == B.marshal_key()
+    monkeypatch.setattr(mq, "_MARSHAL", None)
+    monkeypatch.setattr(B, "marshal_key", lambda: "torch 9.9.9")
+    with pytest.raises(RuntimeError, match="built for another torch"):
+        mq._native()
+    assert mq._MARSHAL is None
