@@ -19,7 +19,7 @@
 //   Weights of a single token are kept as high + low 16-bit halves, so rounding them costs nothing visible: with a
 //   query group of at most four the low halves ride in the unused columns 4..7, otherwise they take a second
 //   product.  Those of several tokens are rounded to the cache's dtype, as in the large tiles.
-//   Softmax against a reference that moves only when a score exceeds it by 2^kLag (base-2 units): one vote per
+//   Softmax against a reference that moves only when a weight would pass 2^kLag: one vote per
 //   tile instead of a reduction over lanes.
 //   Joining.  A warp that has a pair to itself writes the result.  Other pieces meet in shared memory after the
 //   CTA's last tile; a pair that spans CTAs goes through the workspace, and the CTA that arrives last adds the
@@ -42,7 +42,11 @@ constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kMinTiles = 2;                     // a CTA is worth starting for this many tiles per warp
 constexpr int kPairTiles = 48;                   // up to so many tiles per pair, a CTA takes whole pairs where it can
 constexpr int kPairCost = 1;                     // what a pair costs beside its tiles, in tiles (its queries, its result)
-constexpr float kLag = 8.0f;
+// The reference lies kLead below the largest score so far and moves when a score exceeds it by kLag, in base-2 units: weights below
+// 2^kLag.  In fp16, whose steps end at 2^-24, the lead keeps small weights: each is off by at most 2^-35 of the largest (without
+// it 2^-25, which 131000 tokens behind one large score add up to 0.4 % of that score's weight).
+template <bool BF16> constexpr float kLead = BF16 ? 0.0f : 10.0f;
+template <bool BF16> constexpr float kLag = BF16 ? 8.0f : 15.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // How a launch forms its sets: one token of a group of at most 4 or 8 heads, or up to 16 rows of several tokens.
@@ -555,16 +559,17 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
                                           : j < get.s.len && (j >= get.s.lo || j < get.s.pre);
           x[c][e] = see ? y : -INFINITY;
         }
-        above = above || fmaxf(x[c][0], x[c][2]) > m[c][0] + kLag || fmaxf(x[c][1], x[c][3]) > m[c][1] + kLag;
+        above = above || fmaxf(x[c][0], x[c][2]) > m[c][0] + kLag<BF16> || fmaxf(x[c][1], x[c][3]) > m[c][1] + kLag<BF16>;
       }
       if (__any_sync(0xffffffffu, above)) {
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float t = fmaxf(fmaxf(x[c][e], x[c][2 + e]), m[c][e]);
+            float t = fmaxf(x[c][e], x[c][2 + e]);
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            t = fmaxf(t - kLead<BF16>, m[c][e]);
             const float f = t == -INFINITY ? 0.0f : exp2_fast(m[c][e] - t);
             m[c][e] = t;
             l[c][e] *= f;
