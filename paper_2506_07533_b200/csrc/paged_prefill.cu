@@ -13,8 +13,8 @@
 //   zeroed in shared memory before the product: a weight of zero does not silence a NaN.
 //   Products, softmax and tensor memory as in the prefill attention over the quantised cache (prefill.cu):
 //   S_i = Q_i K^T (M 128, N 128, K 16 steps), two threads per row, P_i written over S_i as 16-bit pairs, O_i += P_i V
-//   with P_i as a tensor-memory operand, a reference that moves only when the weights of 64 columns
-//   would add up to more than 2^14, so O_i is rarely rescaled.  Blocks are walked from the last to the
+//   with P_i as a tensor-memory operand, a reference that moves only when the weights of 32 columns
+//   would add up to more than kSumLimit, so O_i is rarely rescaled.  Blocks are walked from the last to the
 //   first: with a distance bias the largest scores come first (walking forwards moved the reference at every block).  P_i is rounded to the cache's dtype (the
 //   product takes operands of one type), each weight by at most 2^-8 (bf16) or 2^-11, which averages out over the tokens:
 //   with bf16 results, 0.0023 of their norm off instead of the 0.0017 of their own rounding.  Blocks that some row does not
@@ -53,7 +53,12 @@ constexpr int kStages = 2;
 constexpr int kSoftmaxWarps = 16, kIssueWarp = 16, kKeyWarp = 17, kValueWarp = 18, kPlanWarp = 19;
 constexpr int kThreads = 20 * 32;
 constexpr int kTmemCols = 512;
-constexpr float kSumLimit = 16384.0f;                // weights of 64 columns that sum to less cannot overflow fp16
+// The reference moves when the weights of 32 columns add up to more than kSumLimit; it then lies kLead below the largest score
+// (base-2 units), and starts kLead below some score.  fp16 overflows at 65520, and its steps end at 2^-24: the lead keeps small weights,
+// each is off by at most 2^-30 of the weight of a score that the row sees (without it 2^-24: what thousands of tokens beside one
+// large score add up to was lost).  A longer lead moves the reference more often.
+template <bool BF16> constexpr float kSumLimit = BF16 ? 16384.0f : 61440.0f;
+template <bool BF16> constexpr float kLead = BF16 ? 0.0f : 6.0f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr long long kWaitLimit = 1ll << 31;          // about a second
 constexpr long long kPieceWaitLimit = 1ll << 37;     // for what may take as long as a piece: about a minute
@@ -674,8 +679,8 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
       ok = wait_all(BAR_SFULL + i, phase);
       if (ok) tc_fence_after();
       if (ok && n == first) {
-        // The first reference: any score that the row sees will do (its weight is then at most 1 and at least
-        // a half, and larger scores may lead by 2^14).  All rows of the warp see token all_to, if this block
+        // The first reference: any score that the row sees will do (its weight is then between a half and 1, times
+        // 2^kLead, and larger scores may lead by the rest of kSumLimit).  All rows of the warp see token all_to, if this block
         // holds it; both threads of a row read its column, without a word between them.
         const int col = min(all_to - (j0 - 64 * half), kBlock - 1);
         if (col >= 0 && j0 - 64 * half + col >= all_from) {
@@ -685,7 +690,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
           float y = __uint_as_float(raw) * scale_log2;
           if (CAP) y = cap_of[7] * tanh_of(__uint_as_float(raw) * cap_of[8]);
           if (BIAS) y -= slope * static_cast<float>(qpos - (j0 - 64 * half + col));
-          if (y > -1e30f && y < 1e30f) m_ref = ceilf(y);
+          if (y > -1e30f && y < 1e30f) m_ref = ceilf(y) - kLead<BF16>;
         }
         // its partner overwrites a column of the other half only after both have read it
         if (meet(0) & 2) {
@@ -701,8 +706,8 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
         for (int c = 0; c < 2; ++c) {
           uint32_t pk[16];
           float csum = masked ? weights(std::true_type{}, c, m_ref, hi, lo, pre, pk) : weights(std::false_type{}, c, m_ref, hi, lo, pre, pk);
-          if (__any_sync(0xffffffffu, live && (!(csum < kSumLimit) || m_ref == -INFINITY))) {
-            // Rare: the weights add up to more than 2^14, or the row had seen nothing before.  The reference
+          if (__any_sync(0xffffffffu, live && (!(csum < kSumLimit<BF16>) || m_ref == -INFINITY))) {
+            // Rare: the weights add up to more than kSumLimit, or the row had seen nothing before.  The reference
             // moves to the chunk's largest score, the weights are formed again, what was stored follows.  A row that
             // still sees nothing keeps -inf and weighs its columns, all masked, against 0.
             float v[32], mul, add;
@@ -710,7 +715,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
             float top = v[0];
 #pragma unroll
             for (int e = 1; e < 32; ++e) top = fmaxf(top, v[e]);
-            const float m_new = fmaxf(m_ref, ceilf(fmaf(top, mul, add)));  // mul > 0
+            const float m_new = fmaxf(m_ref, ceilf(fmaf(top, mul, add)) - kLead<BF16>);  // mul > 0
             const float corr = m_ref == -INFINITY ? 0.0f : ex2_approx(m_ref - m_new);
             if (c) {
               tmem_st_wait();

@@ -40,3 +40,36 @@ def test_decode_keeps_small_weights(dtype, group, bits):
         tol = tol + 2.0 ** -35 * v.double().abs().sum(0).repeat_interleave(group, 0)
     for b in (0, 1, 30, 63):
         R.close(out[b:b + 1], want, tol, f"sequence {b}")
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("opt", [dict(), dict(cap=30.0), dict(slopes=True), dict(cap=30.0, slopes=True)])
+@pytest.mark.parametrize("bits", [12, 20, 26])
+def test_prefill_keeps_small_weights(dtype, opt, bits):
+    """A token that outweighs everything before it, seen by all rows.  Blocks are walked from the last to the first, so the large score comes
+    first; without a workspace one CTA walks them all."""
+    n, new, hkv, hq = 8000, 40, 2, 8
+    c, q = sink(dtype, n, hkv, hq, 1, bits)
+    q = q.expand(new, hq, 128).contiguous()
+    c.k_pages[-1, :, 15] = 0                                  # the large score moves to the last block: to the token before the new ones
+    at = n - new - 1
+    page, slot = int(c.block_table[0, at // 16]), at % 16
+    c.k_pages[page, :, slot], c.v_pages[page, :, slot] = c.k_pages[0, :, 0], 0
+    c.k_pages[0, :, 0], c.v_pages[0, :, 0] = 0, 100
+    opt = dict(opt)
+    if opt.pop("slopes", False):
+        opt["slopes"] = torch.full((hq,), 1e-4, device="cuda")
+    out = torch.full_like(q, 7.0)
+    mq.moqae_paged_prefill_attn(c, q, ints([0, new]), out, None, mq.make_attn_options(**opt))
+    k, v = rows_of(c, n)
+    want, tol = R.attention(q, k, v, n - new, split_weights=False, **opt)
+    if dtype is FP:                                          # the bound of the definition's file allows 2^-24 of a weight of one
+        used = v.double().abs().sum(0).repeat_interleave(hq // hkv, 0)
+        tol = tol - 2 * R.SUBNORMAL[FP] * seen_sum(v, n, new, hq) + 2.0 ** -30 * used
+    R.close(out, want, tol)
+
+
+def seen_sum(v, n, new, hq):
+    """sum of |v| over the tokens that each of the last `new` queries sees, [new, hq, 128]"""
+    total = v.double().abs().cumsum(0)[n - new:]
+    return total.repeat_interleave(hq // v.shape[1], 1)
