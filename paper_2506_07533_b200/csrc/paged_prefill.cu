@@ -10,7 +10,9 @@
 //   strides); a block is fetched with one tiled copy per page (or per 128 slots of a page) and half of the
 //   channels, page numbers looked up one block ahead.  Rows of a block that no query may use (behind the
 //   sequence, before every window) are not fetched where whole pages are concerned, and their values are
-//   zeroed in shared memory before the product: a weight of zero does not silence a NaN.
+//   zeroed in shared memory before the product: a weight of zero does not silence a NaN.  Under a cap their keys are, too: the
+//   form of the tanh goes by the largest score of 32 columns.  (Zeroing the scores instead: five capped fp16 prompts 471 us,
+//   this way 455.)
 //   Products, softmax and tensor memory as in the prefill attention over the quantised cache (prefill.cu):
 //   S_i = Q_i K^T (M 128, N 128, K 16 steps), two threads per row, P_i written over S_i as 16-bit pairs, O_i += P_i V
 //   with P_i as a tensor-memory operand, a reference that moves only when the weights of 32 columns
@@ -71,11 +73,11 @@ constexpr int kPartFloats = kItemRows * (kHeadDim + 2);   // per piece: sums, th
 constexpr int kWarpStage = 2048;                     // shared memory of a softmax warp on the way to memory
 
 // kfull / vfull: bytes of a block have landed (vfull of an edge block: and its rows are zeroed); vraw: the bytes of
-// an edge block of values; kfree / vfree: the products that read the stage are done; sfull, pfull, ofull as in prefill.cu;
+// an edge block of values; kraw: the same of keys; kfree / vfree: the products that read the stage are done; sfull, pfull, ofull as in prefill.cu;
 // qfull / qfree: the queries of a piece stand in shared memory / are not read any more; ifull / ifree: a piece's
 // description is there / nobody reads it any more; parts, ticket: see the joining of pieces
 enum { BAR_KFULL = 0, BAR_VFULL = kStages, BAR_KFREE = 2 * kStages, BAR_VFREE = 3 * kStages, BAR_SFULL = 4 * kStages,
-       BAR_PFULL = BAR_SFULL + 2, BAR_OFULL = BAR_PFULL + 2, BAR_VRAW = BAR_OFULL + 2, BAR_QFULL, BAR_QFREE, BAR_IFULL,
+       BAR_PFULL = BAR_SFULL + 2, BAR_OFULL = BAR_PFULL + 2, BAR_VRAW = BAR_OFULL + 2, BAR_KRAW, BAR_QFULL, BAR_QFREE, BAR_IFULL,
        BAR_IFREE = BAR_IFULL + 2, BAR_PARTS = BAR_IFREE + 2, BAR_TICKET, BAR_COUNT };
 __host__ __device__ constexpr int arrivals_of(int bar) {
   return bar == BAR_PFULL || bar == BAR_PFULL + 1 ? 8
@@ -516,24 +518,10 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     float slope = 0.0f;
     const bool live = row_at(job, it, row) >= 0;
     const volatile float* cap_of = ctl.cap;            // (the constants of the cap stay in shared memory between uses)
-    // What the row does not see.  Under a cap the scores there are taken out of the choice of the polynomial, too, as are
-    // rows that hold nothing: they come from whatever stood in shared memory, and the forms differ in their last bits.
-    auto hide = [&](float (&v)[32], int c, int hi, int lo, int pre, float with) {
-      if (pre <= 0 && opt.window == 0) {                                  // the diagonal alone
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-          if (32 * c + e > hi) v[e] = with;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 32; ++e)
-          if (!((32 * c + e <= hi && 32 * c + e > lo) || 32 * c + e < pre)) v[e] = with;
-      }
-    };
     // Scores of columns 32 c .. 32 c + 31 in base-2 units, plus `off`; `mul` and `add` are what is left to be done (nothing under
     // a cap, an addition with a bias, else both); column e is seen if lo < e <= hi or e < pre.
     auto scores = [&](auto masked, float (&v)[32], int c, float off, int hi, int lo, int pre, float& mul, float& add) {
       tmem_ld32(v, s_addr + 32 * c);
-      if (CAP && masked) hide(v, c, hi, lo, pre, 0.0f);
       mul = CAP || BIAS ? 1.0f : scale_log2;
       add = CAP ? 0.0f : off;
       // The bias of column e is slope * (e - dist), one step of arithmetic per pair with `off` in it; where tokens behind
@@ -546,6 +534,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
         return BIAS ? pack_f2(fmaf(step, static_cast<float>(e), base), fmaf(step, static_cast<float>(e + 1), base)) : pack_f2(base, base);
       };
       if (CAP) {
+        // (the forms differ in their last bits: rows that hold nothing have no say, and tokens that nobody uses score 0)
         float big = 0.0f;
 #pragma unroll
         for (int e = 0; e < 32; e += 2) asm("max.abs.f32 %0, %1, %2, %0;\n" : "+f"(big) : "f"(v[e]), "f"(v[e + 1]));
@@ -596,7 +585,17 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] = fmaf(-slope, fabsf(dist - static_cast<float>(e)), v[e]);
       }
-      if (masked) hide(v, c, hi, lo, pre, -INFINITY);
+      if (masked) {
+        if (pre <= 0 && opt.window == 0) {                                // the diagonal alone
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (32 * c + e > hi) v[e] = -INFINITY;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (!((32 * c + e <= hi && 32 * c + e > lo) || 32 * c + e < pre)) v[e] = -INFINITY;
+        }
+      }
     };
     // weights of a chunk against the reference, packed; their sum
     auto weights = [&](auto masked, int c, float ref, int hi, int lo, int pre, uint32_t (&pk)[16]) -> float {
@@ -1004,8 +1003,9 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
           break;
         }
         const int j0 = block_at(it, it.idx1 - 1 - n) * kBlock;
-        const bool edge = is_v && (j0 + kBlock > it.kv_len || (j0 < it.win_lo && j0 + kBlock > it.prefix));
-        const uint32_t full = bar((is_v ? BAR_VFULL : BAR_KFULL) + st), landed = edge ? bar(BAR_VRAW) : full;
+        const bool edge = (is_v || CAP) && (j0 + kBlock > it.kv_len || (j0 < it.win_lo && j0 + kBlock > it.prefix));
+        const int raw = is_v ? BAR_VRAW : BAR_KRAW;
+        const uint32_t full = bar((is_v ? BAR_VFULL : BAR_KFULL) + st), landed = edge ? bar(raw) : full;
         const unsigned need = __ballot_sync(0xffffffffu, page >= 0);
         if (lane == 0) mbar_expect_tx(landed, __popc(need) * job.box_rows * 256);
         __syncwarp();
@@ -1020,7 +1020,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
           tma_load_4d(d + kTileBytes / 2, map, 64, y, z, w, landed);      // channels 64..127
         }
         if (edge) {
-          if (!wait_all(BAR_VRAW, n_raw++)) {
+          if (!wait_all(raw, n_raw++)) {
             ok = false;
             break;
           }
