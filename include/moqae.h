@@ -518,7 +518,8 @@ int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q,
  *   ends before it starts has no tokens; where sequences share rows, so that they bring more than n_tokens together, the call
  *   has no results and the status becomes MOQAE_ERR_INVALID_ARG).  Rows of out that belong to no sequence (those behind
  *   cu_q[batch], of a padded batch) are left as they were.
- *   Weights are rounded to the cache's dtype before they meet the values, products accumulate in float32.
+ *   Weights are rounded to the cache's dtype before they meet the values (small ones in fp16 by up to 2^-28 of the weight of
+ *   a score that the row sees), products accumulate in float32.
  *   workspace: NULL, or moqae_paged_prefill_attn_workspace bytes under the rules of
  *   moqae_paged_decode_attn; with one, the tokens of few queries over a long context are
  *   shared out among the SMs.  The size for n_tokens and cache->batch is enough for every call of no more tokens and no

@@ -351,8 +351,9 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   const long long total = static_cast<long long>(mine) * pv.n_kv_heads;
   const long long pairs = static_cast<long long>(all_sets) * pv.n_kv_heads;
   // A CTA per pair while that is no more than kPairTiles tiles each: with equal lengths no pair then spans CTAs,
-  // which saves the way through the workspace (8 sequences of 300 tokens x 8 kv heads: 10.1 instead of 12.9 us).  Otherwise every
-  // CTA gets at least kMinTiles tiles per warp.
+  // which saves the way through the workspace.  Otherwise every CTA gets at least kMinTiles tiles per warp.  Measured with a limit of
+  // 8 / 24 / 48 / 96 tiles (us, timer steps of 2): 64 pairs of 19 tiles 16.4 / 14.3 / 14.3 / 14.3, 128 pairs of 19 18.4 / 16.4 / 16.4 / 16.4, of 44
+  // 24.6 / 24.6 / 20.5 / 20.5, of 63 28.7 / 28.7 / 28.7 / 24.6; 2 or 8 pairs of 44 14.3 / 14.3 / 16.4 / 16.4, of 63 14.3 / 14.3 / 14.3 / 20.5.
   const int most = static_cast<int>(gridDim.x);
   int ctas = most;
   if (total <= static_cast<long long>(most) * kWarps * kMinTiles) ctas = static_cast<int>((total + kWarps * kMinTiles - 1) / (kWarps * kMinTiles));
@@ -828,8 +829,13 @@ cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const Ro
 }
 
 // Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average, one set of rows.
-// Measured against the large tiles (us, few / large): 8 sequences of 1000 tokens, 4 rows 17.8 / 21.2, 16 rows 22.2 / 21.3, 32
-// rows 27.0 / 21.9; of 8000 tokens, 16 rows 58.9 / 74.7, 32 rows 93.3 / 74.4; 64 of 500 tokens, 16 rows 44.7 / 49.4.
+// Measured against the large tiles (us, few / large; 32 / 8 heads, bf16, workspace).  Even batches: 8 sequences of 500 tokens with 4
+// new ones each 20.5 / 22.6, of 8000 71.7 / 81.9; 64 of 500 with 1 to 4 45 to 49 / 57 to 59, of 8000 350 / 480; 40 / 40 heads, 16 of 2000
+// with 16 139 / 174.  With 32 rows per sequence the large tiles win (8 of 8000: 93.3 / 74.4).
+// Only the mean is known here (the lengths are on the device), and every set of a long sequence streams that sequence's tokens again.
+// One sequence of 190 new tokens beside 63 single ones: all over 32000 tokens 2207 / 1890, over 8000 596 / 487, single ones of 300
+// to 32000 and 8000 934 / 1028; the worst found is 190 over 32000 beside 63 of 300, 993 / 512.  A bound on how uneven a batch
+// may be would send the even batches of the same size to the slower side, so there is none.
 bool paged_few_rows(const PagedView& pv, int group, int n_tokens) {
   const long long sets = few_sets(pv.batch, group, n_tokens);
   return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * pv.batch && sets * pv.n_kv_heads <= kWorkCounters &&

@@ -7,7 +7,7 @@
 //   r / group, head r % group), so a group shares every key block and a few tokens fill a tile.  A CTA
 //   owns 256 consecutive rows (two tiles of 128) and walks the blocks of 128 tokens that some row sees.
 //   Pages.  The pages are a four-dimensional tensor map (channel, slot, head, page in the order of their
-//   strides); a block is fetched with one tiled copy per page (or per 128 slots of a page) and half of the
+//   strides); a block is fetched with one tiled copy per page (or per 64 slots of a page) and half of the
 //   channels, page numbers looked up one block ahead.  Rows of a block that no query may use (behind the
 //   sequence, before every window) are not fetched where whole pages are concerned, and their values are
 //   zeroed in shared memory before the product: a weight of zero does not silence a NaN.  Under a cap their keys are, too: the
@@ -18,7 +18,7 @@
 //   with P_i as a tensor-memory operand, a reference that moves only when the weights of 32 columns
 //   would add up to more than kSumLimit, so O_i is rarely rescaled.  Blocks are walked from the last to the
 //   first: with a distance bias the largest scores come first (walking forwards moved the reference at every block).  P_i is rounded to the cache's dtype (the
-//   product takes operands of one type), each weight by at most 2^-8 (bf16) or 2^-11, which averages out over the tokens:
+//   product takes operands of one type), each weight by at most 2^-8 (bf16) or 2^-11 (small ones: see kLead), which averages out over the tokens:
 //   with bf16 results, 0.0023 of their norm off instead of the 0.0017 of their own rounding.  Blocks that some row does not
 //   see whole add up the rounded weights: a row of one token is then exact, rows of up to 128 are 0.0019 to 0.0020 off instead
 //   of 0.0021 to 0.0023.  The other blocks add up the exact ones, as many tokens gain nothing from it (2 to 8 % of the time).
@@ -29,13 +29,13 @@
 //   Where the rows alone would leave SMs idle, the blocks of a row tile are cut into up to kMaxSegs pieces,
 //   as many as an estimate of the turns favours; they leave float32 sums in the workspace and the last to arrive
 //   joins them in the order of their tokens (results do not depend on timing).
-//   What bounds it.  A block of 128 tokens takes a CTA about 3450 clocks (8192 tokens, 32 / 8 heads, bf16: 459 us, 1200
-//   TFLOP/s).  A tile's weights take its 8 warps 1790 of them (the exponential unit, shared with the other tile, needs
-//   1024 per tile), from stored weights to the next scores it is 1710: 16 products of 64 clocks, 390 of their latency, the
-//   wait for the other tile's.  With all exponentials left out the period stays, the wait grows: it is the products' turns
-//   that follow one another.  Looked at and slower: scores of 64 columns, so that four chains overlap (a product of N = 64
-//   takes as long as one of 128: 1.45 x the time), an issuing thread per tile (products of the two kinds interleaved: 1.45 x),
-//   no barrier between the two warps of a row (the same time).
+//   What bounds it.  A block of 128 tokens takes a CTA about 3450 clocks (8192 tokens, 32 / 8 heads, bf16: 457 us, 1200
+//   TFLOP/s), of which the products are 2048 (the tensor pipe is busy half of the time): a tile's own chain is as long as that.  Its
+//   weights take its 8 warps 1790 clocks, from stored weights to the next scores it is 1710 (16 products of 64 clocks, 390 of
+//   their latency, the wait for the other tile's), and with two tiles tensor memory is full.  It is not the exponential unit: with two
+//   integer operations in the place of every exponential the same prompt takes 492 us.  Looked at and slower: scores of 64 columns, so that four
+//   chains overlap (a product of N = 64 takes as long as one of 128: 1.45 x the time), an issuing thread per tile (products of the
+//   two kinds interleaved: 1.45 x), no barrier between the two warps of a row (the same time).
 // Every mbarrier wait is bounded; on expiry the CTA records MOQAE_ERR_TIMEOUT, every role stops and the
 // tensor memory is still freed.
 #include <cstring>
@@ -68,7 +68,10 @@ constexpr long long kPieceWaitLimit = 1ll << 37;     // for what may take as lon
 constexpr int kMaxSegs = 32;
 constexpr int kMinSegBlocks = 2;                     // a piece of a cut row tile is at least this many blocks
 constexpr int kMaxParts = 640;                       // partial sums that the workspace holds (of 130 KiB)
-constexpr long long kSplitItems = 512;               // more row tiles than this are never cut
+// More row tiles than this are never cut.  (Nor are most calls near it: 640 parts are one per row tile.  So a long context beside many
+// short prompts is walked by one CTA per row tile: 64 tokens over 32000 take 86 us alone, 490 beside 55 prompts of 20 tokens, where
+// the limit does not apply, and 496 beside 69, where it does.)
+constexpr long long kSplitItems = 512;
 constexpr int kPartFloats = kItemRows * (kHeadDim + 2);   // per piece: sums, then (reference, weight sum) per row
 constexpr int kWarpStage = 2048;                     // shared memory of a softmax warp on the way to memory
 
