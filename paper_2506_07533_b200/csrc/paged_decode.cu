@@ -18,7 +18,9 @@
 //   form needs no operand expansion and no accumulator outside registers.
 //   Weights of a single token are kept as high + low 16-bit halves, so rounding them costs nothing visible: with a
 //   query group of at most four the low halves ride in the unused columns 4..7, otherwise they take a second
-//   product.  Those of several tokens are rounded to the cache's dtype, as in the large tiles.
+//   product.  Those of several tokens are rounded to the cache's dtype, as in the large tiles: bf16 results 0.0022 of their norm
+//   off instead of the 0.0017 of their own rounding.  (Their low halves as well: 2 to 5 % more time, 8 sequences of 1 to 8 tokens
+//   24.1 instead of 23.6 us, 64 of 8000 with 4 365 instead of 353.)
 //   Softmax against a reference that moves only when a weight would pass 2^kLag: one vote per
 //   tile instead of a reduction over lanes.
 //   Joining.  A warp that has a pair to itself writes the result.  Other pieces meet in shared memory after the
