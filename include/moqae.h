@@ -523,8 +523,8 @@ int moqae_paged_decode_attn(const moqae_paged_cache* cache, const moqae_rows* q,
  *   workspace: NULL, or moqae_paged_prefill_attn_workspace bytes under the rules of
  *   moqae_paged_decode_attn; with one, the tokens of few queries over a long context are
  *   shared out among the SMs.  The size for n_tokens and cache->batch is enough for every call of no more tokens and no
- *   more sequences with the same head counts, and for moqae_paged_decode_attn (85 MB at most).  The call encodes the pages' strides for the copy engine and refuses
- *   strides it cannot express (MOQAE_ERR_UNSUPPORTED).
+ *   more sequences with the same head counts, and for moqae_paged_decode_attn (87 MB at most).
+ *   The call encodes the pages' strides for the copy engine and refuses strides it cannot express (MOQAE_ERR_UNSUPPORTED).
  */
 int moqae_paged_prefill_attn_workspace(const moqae_paged_cache* cache, int32_t n_q_heads, int32_t n_tokens,
                                        int64_t* out_bytes);
