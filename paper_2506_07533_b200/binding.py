@@ -532,7 +532,8 @@ def make_attn_options(*, scale=0.0, cap=0.0, window=0, slopes=None, prefix_len=N
     """Options of the paged attention calls: scale (<= 0: 1/sqrt(128)), tanh cap of the scores (0: none), sliding
     window (0: none), slopes float32 [n_q_heads] of the distance bias, prefix_len int32 [batch]."""
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    return AttnOptions(MoqaeAttnOptions(ptr(slopes), ptr(prefix_len), float(scale), float(cap), int(window)), slopes, prefix_len)
+    window = max(min(int(window), 1 << 30), -1)              # no sequence is longer; numbers past 32 bits would lose their upper ones
+    return AttnOptions(MoqaeAttnOptions(ptr(slopes), ptr(prefix_len), float(scale), float(cap), window), slopes, prefix_len)
 
 
 def _options(options, cache, q, where):
