@@ -545,6 +545,104 @@ int moqae_paged_validate(const moqae_paged_cache* cache, void* stream, int32_t* 
 /* Synchronous read of a paged cache's status word (MOQAE_OK where the cache has none).  Waits for `stream`. */
 int moqae_paged_poll_status(const moqae_paged_cache* cache, void* stream, int32_t* out_status);
 
+/* ------------------------------------------------------------------------------------------------
+ * Paged 4-bit cache: the pages of ragged batches held in 4 bits, for sequences that grow token by token (a chunk of the
+ * quantised cache is complete before it is quantised, Section 3.2, and all sequences there have one length).
+ * (No counterpart in the paper.)
+ *
+ *   row    128 channels are four groups of 32.  A group keeps z, the largest fp16 value not above its smallest element
+ *          (-0 as +0), s, the smallest fp16 value not below (largest element - z) / 15 (a float32 quotient), and per element x the whole
+ *          number nearest to (x - z) * r, r the float32 value nearest to 1 / s, halves to even (0 where s = 0): the rule of
+ *          moqae_quantize_kv.  The element then stands for z + s * code.  Elements are finite and at most 65504 in magnitude.
+ *   tile   16 consecutive tokens of one kv head, 2560 bytes: keys and values, 64 code bytes and four scales and zeros each per token.
+ *          Byte positions, for token t of the tile and channel c, g = c / 32; the even channel of a pair is in the low four bits:
+ *            key code    64 t + 16 ((c % 32) / 8) + 4 g + (c % 8) / 2        key scale    1024 + 16 t + 2 g     zero  8 further
+ *            value code  1280 + 512 (u / 4) + 32 r + 8 (u % 4) + 2 g + (c % 4) / 2,  u = (c % 32) / 4,  r = 8 (t / 8) + 4 (t % 2) + (t % 8) / 2
+ *            value scale 2304 + 32 (t / 2) + 4 g + 2 (t % 2)                  zero  16 further
+ *   page   page_size (16, 32, 64, 128 or 256) consecutive tokens: for every kv head page_size / 16 tiles after one another, tile
+ *          i of head h of page p at pages + p * page_stride + h * head_stride + 2560 i.  The strides count bytes, are positive multiples of 16.
+ *   block_table, kv_len, status and the limits on sizes are those of moqae_paged_cache, and so is what unused rows may hold.
+ *   dtype  of the rows that the calls take and give.
+ */
+typedef struct moqae_paged4_cache {
+  void* pages;
+  int64_t page_stride, head_stride;
+  const int32_t* block_table;  /* [batch][max_pages] */
+  const int32_t* kv_len;       /* [batch] */
+  int32_t* status;             /* int32[4] or NULL */
+  int32_t n_pages;
+  int32_t page_size;
+  int32_t n_kv_heads;
+  int32_t dtype;               /* MOQAE_DTYPE_* */
+  int32_t batch;
+  int32_t max_pages;           /* entries per row of block_table */
+} moqae_paged4_cache;
+
+/* The free pages of a cache: ring[(first + i) % n_pages], i = 0 .. free - 1.  state = int32[4]: first, free, 0, 0. */
+typedef struct moqae_page_pool {
+  int32_t* ring;               /* [n_pages] */
+  int32_t* state;
+  int32_t n_pages;
+} moqae_page_pool;
+
+/*
+ * The tables of a step from the tokens that its sequences bring, for either kind of pages.  Sequence b has past_len[b] tokens,
+ * all of them in pages of its row of block_table, and gets n_new[b] more (n_new < 0: it loses its last -n_new, at most all of them):
+ *   block_table   the entries of its new pages are written, pages taken from the front of the pool in the order of sequences and entries;
+ *   kv_len[b]     = max(past_len[b] + n_new[b], 0);
+ *   pool          pages that hold none of its tokens any more go to the end, in the same order (their entries stay as they were); they can be
+ *                 taken from the next call on;
+ *   cu_q          int32 [batch + 1]: the rows of sequence b are cu_q[b] .. cu_q[b + 1] - 1, max(n_new[b], 0) of them;
+ *   positions, seq  int32 [n_rows]: position and sequence of every row, -1 behind the last (the padding of the other calls).
+ *   past_len may be kv_len, and state (NULL: pool->state), the pool's state before the call, may be pool->state; the third word of
+ *   pool->state must be 0.  Nothing else may overlap.  n_rows and batch at most 2^24.
+ *   Found on the device and recorded in status (int32[4] or NULL), with tables and pool as they were, kv_len = past_len, cu_q zero and
+ *   positions and seq -1: MOQAE_ERR_POOL_FULL, not enough free pages (details: pages wanted, pages free); MOQAE_ERR_CORRUPT_TABLE, a length below 0
+ *   or above max_pages * page_size before or after (details: sequence, -1), or a state that cannot be (-1, -1);
+ *   MOQAE_ERR_INVALID_ARG, more tokens than n_rows (-1, tokens).  A page number outside 0 .. n_pages - 1 that is moved is recorded
+ *   as MOQAE_ERR_CORRUPT_TABLE (sequence, entry) and moved all the same: no call follows it.
+ */
+int moqae_paged_plan(const int32_t* past_len, const int32_t* n_new, int32_t batch, int32_t page_size, int32_t max_pages,
+                     int32_t* block_table, int32_t* kv_len, const moqae_page_pool* pool, const int32_t* state, int32_t* cu_q,
+                     int32_t* positions, int32_t* seq, int32_t n_rows, int32_t* status, void* stream);
+
+/*
+ * moqae_paged_append into a 4-bit cache: keys (after norm and rotation, in float32) and values are quantised into their tiles, queries
+ * go to q_out.  Arguments and refusals are those of moqae_paged_append.
+ */
+int moqae_paged4_append(const moqae_paged4_cache* cache, const moqae_rope* rope, const moqae_rows* k, const moqae_rows* v,
+                        const moqae_rows* q, const moqae_rows* q_out, const int32_t* positions, const int32_t* seq,
+                        int32_t n_tokens, void* stream);
+
+/*
+ * Rows of a 4-bit cache as the values they stand for, rounded to dtype: row t of k_out, v_out (one of them may be NULL) is token
+ * positions[t] of sequence seq[t] (NULL: sequence t); kv_len is not read.  A token with a negative position, or whose sequence, position
+ * or page does not exist (status: MOQAE_ERR_CORRUPT_TABLE with token and position), leaves its output rows as they were.
+ */
+int moqae_paged4_read(const moqae_paged4_cache* cache, const moqae_rows* k_out, const moqae_rows* v_out, const int32_t* positions,
+                      const int32_t* seq, int32_t n_tokens, void* stream);
+
+/*
+ * moqae_paged_decode_attn over a 4-bit cache; workspaces (their size, use and sharing) are alike, and can be shared with the calls
+ * over 16-bit pages.  Queries are finite, below 2^40 in magnitude.  Weights are rounded to fp16, their products with a value's scale
+ * once more; sums are float32.
+ */
+int moqae_paged4_decode_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int64_t* out_bytes);
+int moqae_paged4_decode_attn(const moqae_paged4_cache* cache, const moqae_rows* q, const moqae_rows* out,
+                             const moqae_attn_options* options, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * moqae_paged_prefill_attn over a 4-bit cache, with the domain of queries of moqae_paged4_decode_attn.  The workspace is required.
+ */
+int moqae_paged4_prefill_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int32_t n_tokens, int64_t* out_bytes);
+int moqae_paged4_prefill_attn(const moqae_paged4_cache* cache, const moqae_rows* q, const int32_t* cu_q, int32_t n_tokens,
+                              const moqae_rows* out, const moqae_attn_options* options, void* workspace,
+                              int64_t workspace_bytes, void* stream);
+
+/* moqae_paged_validate and moqae_paged_poll_status of a 4-bit cache. */
+int moqae_paged4_validate(const moqae_paged4_cache* cache, void* stream, int32_t* bad_seq, int32_t* bad_entry);
+int moqae_paged4_poll_status(const moqae_paged4_cache* cache, void* stream, int32_t* out_status);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,7 +31,9 @@ EXPORTS = ["moqae_version", "moqae_last_cuda_error", "moqae_error_string", "moqa
            "moqae_validate_tables", "moqae_validate_tables_host", "moqae_decode_attn_step",
            "moqae_norm_rope", "moqae_paged_append", "moqae_paged_decode_attn_workspace", "moqae_paged_decode_attn",
            "moqae_paged_prefill_attn_workspace", "moqae_paged_prefill_attn", "moqae_paged_validate_host",
-           "moqae_paged_validate", "moqae_paged_poll_status"]
+           "moqae_paged_validate", "moqae_paged_poll_status", "moqae_paged_plan", "moqae_paged4_append", "moqae_paged4_read",
+           "moqae_paged4_decode_attn_workspace", "moqae_paged4_decode_attn", "moqae_paged4_prefill_attn_workspace",
+           "moqae_paged4_prefill_attn", "moqae_paged4_validate", "moqae_paged4_poll_status"]
 
 
 class MoqaeConfig(C.Structure):
@@ -55,6 +57,16 @@ class MoqaePagedCache(C.Structure):
                 ("block_table", C.c_void_p), ("kv_len", C.c_void_p), ("status", C.c_void_p), ("n_pages", C.c_int32),
                 ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("dtype", C.c_int32), ("batch", C.c_int32),
                 ("max_pages", C.c_int32)]
+
+
+class MoqaePaged4Cache(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("block_table", C.c_void_p),
+                ("kv_len", C.c_void_p), ("status", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("n_kv_heads", C.c_int32), ("dtype", C.c_int32), ("batch", C.c_int32), ("max_pages", C.c_int32)]
+
+
+class MoqaePagePool(C.Structure):
+    _fields_ = [("ring", C.c_void_p), ("state", C.c_void_p), ("n_pages", C.c_int32)]
 
 
 class MoqaeRows(C.Structure):
@@ -147,6 +159,18 @@ def lib() -> C.CDLL:
                                                 C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         L.moqae_paged_validate.argtypes = [pc, C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         L.moqae_paged_poll_status.argtypes = [pc, C.c_void_p, C.POINTER(C.c_int32)]
+        L.moqae_paged_plan.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                       C.POINTER(MoqaePagePool), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32,
+                                       C.c_void_p, C.c_void_p]
+        pc4 = C.POINTER(MoqaePaged4Cache)
+        L.moqae_paged4_append.argtypes = [pc4, C.POINTER(MoqaeRope), rows, rows, rows, rows, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        L.moqae_paged4_read.argtypes = [pc4, rows, rows, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        L.moqae_paged4_decode_attn_workspace.argtypes = [pc4, C.c_int32, C.POINTER(C.c_int64)]
+        L.moqae_paged4_decode_attn.argtypes = [pc4, rows, rows, opts, C.c_void_p, C.c_int64, C.c_void_p]
+        L.moqae_paged4_prefill_attn_workspace.argtypes = [pc4, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
+        L.moqae_paged4_prefill_attn.argtypes = [pc4, rows, C.c_void_p, C.c_int32, rows, opts, C.c_void_p, C.c_int64, C.c_void_p]
+        L.moqae_paged4_validate.argtypes = [pc4, C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+        L.moqae_paged4_poll_status.argtypes = [pc4, C.c_void_p, C.POINTER(C.c_int32)]
         for name in EXPORTS:
             if name not in ("moqae_error_string",):
                 getattr(L, name).restype = C.c_int
@@ -396,7 +420,8 @@ def _native():
     """The marshalling module, bound to the loaded library.  Raises if it has not been built."""
     global _MARSHAL
     if _MARSHAL is None:
-        names = ("moqae_norm_rope", "moqae_paged_append", "moqae_paged_decode_attn", "moqae_paged_prefill_attn")
+        names = ("moqae_norm_rope", "moqae_paged_append", "moqae_paged_decode_attn", "moqae_paged_prefill_attn", "moqae_paged_plan",
+                 "moqae_paged4_append", "moqae_paged4_read", "moqae_paged4_decode_attn", "moqae_paged4_prefill_attn")
         addresses = [C.cast(getattr(lib(), n), C.c_void_p).value for n in names]
         missing = f"{_build.MARSHAL} is missing or was built for another torch: run `python -m paper_2506_07533_b200.build`"
         try:
@@ -405,7 +430,8 @@ def _native():
             raise RuntimeError(missing) from e
         if getattr(_marshal, "built_for", None) != _build.marshal_key():
             raise RuntimeError(missing)
-        _marshal.bind(*addresses)
+        _marshal.bind(*addresses[:4])
+        _marshal.bind4(*addresses[4:])
         _MARSHAL = _marshal
     return _MARSHAL
 
@@ -579,11 +605,13 @@ def moqae_paged_prefill_attn(cache: PagedCache, q, cu_q, out, workspace=None, op
         raise MoqaeError(rc, where)
 
 
-def moqae_paged_validate(cache: PagedCache):
-    """(code, bad_seq, bad_entry): OK, or ERR_CORRUPT_TABLE with the first offending table entry (-1: the length)."""
+def moqae_paged_validate(cache):
+    """(code, bad_seq, bad_entry): OK, or ERR_CORRUPT_TABLE with the first offending table entry (-1: the length).  Of
+    a PagedCache or a Paged4Cache."""
     b, e = C.c_int32(-1), C.c_int32(-1)
+    call = lib().moqae_paged4_validate if isinstance(cache, Paged4Cache) else lib().moqae_paged_validate
     with torch.cuda.device(cache.device):
-        rc = lib().moqae_paged_validate(C.byref(cache.view), torch.cuda.current_stream().cuda_stream, C.byref(b), C.byref(e))
+        rc = call(C.byref(cache.view), torch.cuda.current_stream().cuda_stream, C.byref(b), C.byref(e))
     if rc not in (OK, ERR_CORRUPT_TABLE):
         raise MoqaeError(rc, "moqae_paged_validate")
     return rc, int(b.value), int(e.value)
@@ -600,9 +628,124 @@ def moqae_paged_validate_host(block_table, kv_len, n_pages, page_size):
     return rc, int(b.value), int(e.value)
 
 
-def moqae_paged_poll_status(cache: PagedCache) -> int:
+def moqae_paged_poll_status(cache) -> int:
+    """MOQAE_OK or the first device-side error of a PagedCache or a Paged4Cache."""
     out = C.c_int32(0)
+    call = lib().moqae_paged4_poll_status if isinstance(cache, Paged4Cache) else lib().moqae_paged_poll_status
     with torch.cuda.device(cache.device):
-        _check(lib().moqae_paged_poll_status(C.byref(cache.view), torch.cuda.current_stream().cuda_stream, C.byref(out)),
-               "moqae_paged_poll_status")
+        _check(call(C.byref(cache.view), torch.cuda.current_stream().cuda_stream, C.byref(out)), "moqae_paged_poll_status")
     return int(out.value)
+
+
+# ---- plan of a step -------------------------------------------------------------------------------
+
+@dataclass
+class PagePool:
+    """The free pages of a cache: ring[(first + i) % n], i < free, of page numbers.  state int32 [4]: first, free, 0, 0."""
+    ring: torch.Tensor           # int32 [n_pages]
+    state: torch.Tensor          # int32 [4]
+
+
+def make_page_pool(n_pages, device="cuda") -> PagePool:
+    """A pool that holds the pages 0 .. n_pages - 1."""
+    return PagePool(torch.arange(n_pages, dtype=torch.int32, device=device), torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device=device))
+
+
+def moqae_paged_plan(cache, pool: PagePool, n_new, cu_q, positions, seq, *, past_len=None, pool_state=None):
+    """Block table and lengths of a step of `cache` (PagedCache or Paged4Cache), pages taken from and given back to `pool`.
+    n_new int32 [batch]: tokens that each sequence gets (negative: loses).  Written: cache.block_table, cache.kv_len, cu_q int32
+    [batch + 1], positions and seq int32 [rows] (-1 behind the last row).  past_len, the lengths before, and pool_state, the
+    pool's state before, default to cache.kv_len and pool.state.  Errors are recorded in cache.status."""
+    rc = (_MARSHAL or _native()).plan(cache.device, cache.batch, cache.block_table.shape[1], cache.view.page_size, cache.block_table,
+                                      cache.kv_len, cache.status, pool.ring, pool.state, n_new, past_len, pool_state, cu_q, positions, seq)
+    if rc:
+        raise MoqaeError(rc, "moqae_paged_plan")
+
+
+# ---- paged 4-bit cache ----------------------------------------------------------------------------
+
+TOKEN_BYTES4 = 160               # of a token and kv head
+
+
+@dataclass
+class Paged4Cache:
+    """The tensors of a paged 4-bit cache and the C view handed to the library."""
+    pages: torch.Tensor          # uint8 [n_pages, n_kv_heads, page_size * 160], any strides of whole pages and heads
+    block_table: torch.Tensor    # int32 [batch, max_pages]
+    kv_len: torch.Tensor         # int32 [batch]
+    status: torch.Tensor         # int32 [4]
+    view: MoqaePaged4Cache
+    code: int                    # MOQAE_DTYPE_* of rows
+    device: int                  # device index
+    batch: int
+    address: int = 0
+
+    def __post_init__(self):
+        self.address = C.addressof(self.view)
+
+
+def moqae_paged4_bind(pages, block_table, kv_len, dtype, status=None) -> Paged4Cache:
+    """A paged 4-bit cache over the caller's tensors.  pages uint8 [n_pages, n_kv_heads, page_size * 160] (contents need not be
+    initialised); block_table int32 [batch, max_pages]; kv_len int32 [batch]; dtype of the rows that the calls take and give.
+    The contents of all of them may change between calls."""
+    where = "moqae_paged4_bind"
+    _need(pages.is_cuda and pages.dtype == torch.uint8 and pages.dim() == 3 and pages.shape[2] % TOKEN_BYTES4 == 0, where)
+    _need(pages.stride(2) == 1 and dtype in _DTYPE_CODE, where)
+    index = pages.get_device()
+    _need(block_table.dim() == 2 and block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.get_device() == index, where)
+    if status is None:
+        status = torch.zeros(4, dtype=torch.int32, device=pages.device)
+    view = MoqaePaged4Cache(pages.data_ptr(), pages.stride(0), pages.stride(1), block_table.data_ptr(),
+                            _vector(kv_len, torch.int32, block_table.shape[0], index, where), _vector(status, torch.int32, 4, index, where),
+                            pages.shape[0], pages.shape[2] // TOKEN_BYTES4, pages.shape[1], _DTYPE_CODE[dtype], block_table.shape[0],
+                            block_table.shape[1])
+    return Paged4Cache(pages, block_table, kv_len, status, view, _DTYPE_CODE[dtype], index, block_table.shape[0])
+
+
+def moqae_paged4_append(cache: Paged4Cache, k, v, positions, *, seq=None, rope: Rope = None, q=None, q_out=None):
+    """moqae_paged_append into a 4-bit cache: keys (normalised and rotated with `rope`) and values are quantised on their way."""
+    r = (0, -1, -1) if rope is None else (rope.address, rope.code, rope.device)
+    rc = (_MARSHAL or _native()).append4(cache.address, cache.code, cache.device, *r, k, v, positions, seq, q, q_out)
+    if rc:
+        raise MoqaeError(rc, "moqae_paged4_append")
+
+
+def moqae_paged4_read(cache: Paged4Cache, k_out, v_out, positions, *, seq=None):
+    """Keys and values of tokens positions[t] (negative: left out) of sequences seq[t] (None: sequence t) as the values they
+    stand for, into rows k_out, v_out [n, n_kv_heads, 128] (one of them may be None)."""
+    rc = (_MARSHAL or _native()).read4(cache.address, cache.code, cache.device, k_out, v_out, positions, seq)
+    if rc:
+        raise MoqaeError(rc, "moqae_paged4_read")
+
+
+def moqae_paged4_decode_attn_workspace(cache: Paged4Cache, n_q_heads) -> int:
+    out = C.c_int64(0)
+    _check(lib().moqae_paged4_decode_attn_workspace(C.byref(cache.view), int(n_q_heads), C.byref(out)), "moqae_paged4_decode_attn_workspace")
+    return int(out.value)
+
+
+def moqae_paged4_decode_attn(cache: Paged4Cache, q, out, workspace, options: AttnOptions = None):
+    """Attention of one new token per sequence: q, out [batch, n_q_heads, 128] in the cache's dtype; workspace a
+    tensor of moqae_paged4_decode_attn_workspace bytes, zeroed once."""
+    where = "moqae_paged4_decode_attn"
+    rc = (_MARSHAL or _native()).decode4(cache.address, cache.code, cache.device, cache.batch, q, out, workspace, _options(options, cache, q, where))
+    if rc:
+        raise MoqaeError(rc, where)
+
+
+def moqae_paged4_prefill_attn_workspace(cache: Paged4Cache, n_q_heads, n_tokens) -> int:
+    """Bytes for every call of up to n_tokens tokens over up to as many sequences as `cache` has, one-token calls included."""
+    out = C.c_int64(0)
+    _check(lib().moqae_paged4_prefill_attn_workspace(C.byref(cache.view), int(n_q_heads), int(n_tokens), C.byref(out)),
+           "moqae_paged4_prefill_attn_workspace")
+    return int(out.value)
+
+
+def moqae_paged4_prefill_attn(cache: Paged4Cache, q, cu_q, out, workspace, options: AttnOptions = None):
+    """Attention of the last cu_q[b + 1] - cu_q[b] tokens of every sequence: q, out [n_tokens, n_q_heads, 128] in the
+    cache's dtype, cu_q int32 [batch + 1]; workspace of moqae_paged4_prefill_attn_workspace bytes, zeroed once."""
+    where = "moqae_paged4_prefill_attn"
+    rc = (_MARSHAL or _native()).prefill4(cache.address, cache.code, cache.device, cache.batch, q, cu_q, out, workspace,
+                                          _options(options, cache, q, where))
+    if rc:
+        raise MoqaeError(rc, where)

@@ -14,6 +14,11 @@ decltype(&moqae_norm_rope) g_norm_rope = nullptr;
 decltype(&moqae_paged_append) g_append = nullptr;
 decltype(&moqae_paged_decode_attn) g_decode = nullptr;
 decltype(&moqae_paged_prefill_attn) g_prefill = nullptr;
+decltype(&moqae_paged_plan) g_plan = nullptr;
+decltype(&moqae_paged4_append) g_append4 = nullptr;
+decltype(&moqae_paged4_read) g_read4 = nullptr;
+decltype(&moqae_paged4_decode_attn) g_decode4 = nullptr;
+decltype(&moqae_paged4_prefill_attn) g_prefill4 = nullptr;
 
 // What the tensors of a call have to agree on.
 struct Kind {
@@ -92,12 +97,23 @@ template <typename F> PyObject* guarded(F call) {
   }
 }
 
+template <typename F> void set(F& f, PyObject* o) { f = reinterpret_cast<F>(PyLong_AsVoidPtr(o)); }
+
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 4) return PyErr_Format(PyExc_TypeError, "bind takes 4 addresses");
-  g_norm_rope = reinterpret_cast<decltype(g_norm_rope)>(PyLong_AsVoidPtr(a[0]));
-  g_append = reinterpret_cast<decltype(g_append)>(PyLong_AsVoidPtr(a[1]));
-  g_decode = reinterpret_cast<decltype(g_decode)>(PyLong_AsVoidPtr(a[2]));
-  g_prefill = reinterpret_cast<decltype(g_prefill)>(PyLong_AsVoidPtr(a[3]));
+  set(g_norm_rope, a[0]);
+  set(g_append, a[1]);
+  set(g_decode, a[2]);
+  set(g_prefill, a[3]);
+  Py_RETURN_NONE;
+}
+PyObject* bind4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) return PyErr_Format(PyExc_TypeError, "bind4 takes 5 addresses");
+  set(g_plan, a[0]);
+  set(g_append4, a[1]);
+  set(g_read4, a[2]);
+  set(g_decode4, a[3]);
+  set(g_prefill4, a[4]);
   Py_RETURN_NONE;
 }
 
@@ -129,7 +145,7 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
 }
 
 // append(cache, dtype, device, rope or 0, rope dtype or -1, rope device or -1, k, v, positions, seq, q, q_out)
-PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+template <typename C, typename F> PyObject* append_to(F g, PyObject* const* a, Py_ssize_t n_args) {
   if (n_args != 12) return PyErr_Format(PyExc_TypeError, "append takes 12 arguments");
   return guarded([&]() -> int {
     const int dtype = static_cast<int>(PyLong_AsLong(a[1]));
@@ -144,16 +160,18 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         !rows(a[11], kind, n, &r[3], &p[3]) || !ints(a[8], kind, n, &positions) || !ints(a[9], kind, n, &seq) || (!p[2] && p[3]))
       return MOQAE_ERR_INVALID_ARG;
     const c10::cuda::CUDAGuard guard(static_cast<c10::DeviceIndex>(kind.device));
-    const moqae_paged_cache* cache = address<const moqae_paged_cache*>(a[0]);
+    const C* cache = address<const C*>(a[0]);
     const moqae_rope* rope = address<const moqae_rope*>(a[3]);
     return enqueue([&](void* stream) {
-      return g_append(cache, rope, p[0], p[1], p[2], p[3] ? p[3] : p[2], positions, seq, static_cast<int32_t>(n), stream);
+      return g(cache, rope, p[0], p[1], p[2], p[3] ? p[3] : p[2], positions, seq, static_cast<int32_t>(n), stream);
     });
   });
 }
+PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) { return append_to<moqae_paged_cache>(g_append, a, n); }
+PyObject* append4(PyObject*, PyObject* const* a, Py_ssize_t n) { return append_to<moqae_paged4_cache>(g_append4, a, n); }
 
 // decode(cache, dtype, device, batch, q, out, workspace, options or 0)
-PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+template <typename C, typename F> PyObject* decode_over(F g, PyObject* const* a, Py_ssize_t n_args) {
   if (n_args != 8) return PyErr_Format(PyExc_TypeError, "decode takes 8 arguments");
   return guarded([&]() -> int {
     const Kind kind{scalar_of(static_cast<int>(PyLong_AsLong(a[1]))), static_cast<int>(PyLong_AsLong(a[2]))};
@@ -164,14 +182,16 @@ PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     int64_t bytes;
     if (!rows(a[4], kind, n, &r[0], &p[0]) || !rows(a[5], kind, n, &r[1], &p[1]) || !space(a[6], kind, &ws, &bytes)) return MOQAE_ERR_INVALID_ARG;
     const c10::cuda::CUDAGuard guard(static_cast<c10::DeviceIndex>(kind.device));
-    const moqae_paged_cache* cache = address<const moqae_paged_cache*>(a[0]);
+    const C* cache = address<const C*>(a[0]);
     const moqae_attn_options* options = address<const moqae_attn_options*>(a[7]);
-    return enqueue([&](void* stream) { return g_decode(cache, p[0], p[1], options, ws, bytes, stream); });
+    return enqueue([&](void* stream) { return g(cache, p[0], p[1], options, ws, bytes, stream); });
   });
 }
+PyObject* decode(PyObject*, PyObject* const* a, Py_ssize_t n) { return decode_over<moqae_paged_cache>(g_decode, a, n); }
+PyObject* decode4(PyObject*, PyObject* const* a, Py_ssize_t n) { return decode_over<moqae_paged4_cache>(g_decode4, a, n); }
 
 // prefill(cache, dtype, device, batch, q, cu_q, out, workspace, options or 0)
-PyObject* prefill(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+template <typename C, typename F> PyObject* prefill_over(F g, PyObject* const* a, Py_ssize_t n_args) {
   if (n_args != 9) return PyErr_Format(PyExc_TypeError, "prefill takes 9 arguments");
   return guarded([&]() -> int {
     const Kind kind{scalar_of(static_cast<int>(PyLong_AsLong(a[1]))), static_cast<int>(PyLong_AsLong(a[2]))};
@@ -185,18 +205,69 @@ PyObject* prefill(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         !space(a[7], kind, &ws, &bytes))
       return MOQAE_ERR_INVALID_ARG;
     const c10::cuda::CUDAGuard guard(static_cast<c10::DeviceIndex>(kind.device));
-    const moqae_paged_cache* cache = address<const moqae_paged_cache*>(a[0]);
+    const C* cache = address<const C*>(a[0]);
     const moqae_attn_options* options = address<const moqae_attn_options*>(a[8]);
-    return enqueue([&](void* stream) { return g_prefill(cache, p[0], cu_q, static_cast<int32_t>(n), p[1], options, ws, bytes, stream); });
+    return enqueue([&](void* stream) { return g(cache, p[0], cu_q, static_cast<int32_t>(n), p[1], options, ws, bytes, stream); });
+  });
+}
+PyObject* prefill(PyObject*, PyObject* const* a, Py_ssize_t n) { return prefill_over<moqae_paged_cache>(g_prefill, a, n); }
+PyObject* prefill4(PyObject*, PyObject* const* a, Py_ssize_t n) { return prefill_over<moqae_paged4_cache>(g_prefill4, a, n); }
+
+// read4(cache, dtype, device, k_out, v_out, positions, seq)
+PyObject* read4(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 7) return PyErr_Format(PyExc_TypeError, "read4 takes 7 arguments");
+  return guarded([&]() -> int {
+    const Kind kind{scalar_of(static_cast<int>(PyLong_AsLong(a[1]))), static_cast<int>(PyLong_AsLong(a[2]))};
+    const int64_t n = tokens_of(a[3] != Py_None ? a[3] : a[4]);
+    moqae_rows r[2];
+    const moqae_rows* p[2];
+    const int32_t *positions, *seq;
+    if (n < 0 || !rows(a[3], kind, n, &r[0], &p[0]) || !rows(a[4], kind, n, &r[1], &p[1]) || !ints(a[5], kind, n, &positions) ||
+        !ints(a[6], kind, n, &seq))
+      return MOQAE_ERR_INVALID_ARG;
+    const c10::cuda::CUDAGuard guard(static_cast<c10::DeviceIndex>(kind.device));
+    const moqae_paged4_cache* cache = address<const moqae_paged4_cache*>(a[0]);
+    return enqueue([&](void* stream) { return g_read4(cache, p[0], p[1], positions, seq, static_cast<int32_t>(n), stream); });
+  });
+}
+
+// plan(device, batch, max_pages, page_size, block_table, kv_len, status, ring, state, n_new, past_len, pool_state, cu_q, positions, seq)
+PyObject* plan(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+  if (n_args != 15) return PyErr_Format(PyExc_TypeError, "plan takes 15 arguments");
+  return guarded([&]() -> int {
+    const Kind kind{at::kInt, static_cast<int>(PyLong_AsLong(a[0]))};
+    const int64_t batch = PyLong_AsLong(a[1]), max_pages = PyLong_AsLong(a[2]), page_size = PyLong_AsLong(a[3]);
+    const at::Tensor *ring = tensor(a[7]), *rows_of = tensor(a[13]);
+    if (!ring || !rows_of || ring->numel() > INT32_MAX || rows_of->numel() > INT32_MAX) return MOQAE_ERR_INVALID_ARG;
+    const int64_t n_pages = ring->numel(), n_rows = rows_of->numel();
+    const int32_t *table, *kv_len, *status, *ring_at, *state, *n_new, *past, *before, *cu_q, *positions, *seq;
+    if (!ints(a[4], kind, batch * max_pages, &table) || !ints(a[5], kind, batch, &kv_len) || !ints(a[6], kind, 4, &status) ||
+        !ints(a[7], kind, n_pages, &ring_at) || !ints(a[8], kind, 4, &state) || !ints(a[9], kind, batch, &n_new) ||
+        !ints(a[10], kind, batch, &past) || !ints(a[11], kind, 4, &before) || !ints(a[12], kind, batch + 1, &cu_q) ||
+        !ints(a[13], kind, n_rows, &positions) || !ints(a[14], kind, n_rows, &seq))
+      return MOQAE_ERR_INVALID_ARG;
+    const c10::cuda::CUDAGuard guard(static_cast<c10::DeviceIndex>(kind.device));
+    const moqae_page_pool pool{const_cast<int32_t*>(ring_at), const_cast<int32_t*>(state), static_cast<int32_t>(n_pages)};
+    return enqueue([&](void* stream) {
+      return g_plan(past ? past : kv_len, n_new, static_cast<int32_t>(batch), static_cast<int32_t>(page_size), static_cast<int32_t>(max_pages),
+                    const_cast<int32_t*>(table), const_cast<int32_t*>(kv_len), &pool, before, const_cast<int32_t*>(cu_q),
+                    const_cast<int32_t*>(positions), const_cast<int32_t*>(seq), static_cast<int32_t>(n_rows), const_cast<int32_t*>(status), stream);
+    });
   });
 }
 
 PyMethodDef kMethods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind)), METH_FASTCALL, "addresses of the C functions"},
+    {"bind4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(bind4)), METH_FASTCALL, "those of the plan and of 4-bit pages"},
     {"norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(norm_rope)), METH_FASTCALL, nullptr},
     {"append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(append)), METH_FASTCALL, nullptr},
     {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(decode)), METH_FASTCALL, nullptr},
     {"prefill", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(prefill)), METH_FASTCALL, nullptr},
+    {"plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(plan)), METH_FASTCALL, nullptr},
+    {"append4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(append4)), METH_FASTCALL, nullptr},
+    {"read4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(read4)), METH_FASTCALL, nullptr},
+    {"decode4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(decode4)), METH_FASTCALL, nullptr},
+    {"prefill4", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(prefill4)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

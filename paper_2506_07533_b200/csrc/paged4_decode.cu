@@ -1,0 +1,506 @@
+// Attention of one new token per sequence over a paged 4-bit cache (moqae_paged4_decode_attn), and of a few
+// (moqae_paged4_prefill_attn where the sequences bring so few rows that the large tiles would be empty).
+//
+// Mathematics.  A cached key is k^ = z + s code per group of 32 channels, so for a query row q
+//   q.k^_j = sum_g s_jg (q_g . code_jg) + z_jg (sum of q_g),     o_c = sum_j (p_j s_jg) code_jc + sum_j p_j z_jg:
+// the codes go to the tensor cores as they are, as the small fp16 numbers code 2^-24 and (where they stand four bits higher)
+// code 2^-20, one logic instruction per register of two; scales and zeros are a few values per token.
+//
+//   Work, tiles, pieces and their joining are those of the 16-bit pages (paged_split.cuh); a tile of 16 tokens of one kv
+//   head is 2560 bytes in one place, fetched with one bulk copy by the warp that works on it.
+//   Products, on mma.sync m16n8k16.  S^T = codes q^T: per group two products whose sums meet the tokens' scales in registers, and one for the
+//   zeros of all groups, with the sums of the queries' groups as high + low halves.  O^T += codes^T (p s)^T: weights become fp16, turn by movmatrix, and
+//   meet a group's value scales as packed pairs; one more product sums what the zeros give and, in a row of ones, the weights.
+//   Queries are scaled by a power of two to at most 16, so that bf16 rows and small ones keep their bits in fp16 (2^-24 of the largest).
+//   Signs.  Codes are never negative, and a sum of many that the zeros then cancel loses what the mean over a long context leaves (the
+//   tensor cores cut off the bits below 2^-23 of a running sum: 131000 tokens were off by 0.004 of their norm instead of the 0.0017 of
+//   rounding to bf16, 32000 in one warp by 0.011).  So every second token has 15 - code (the same instruction) with the weight -p, and the zeros become the
+//   middles of the ranges, mid = z + 7.5 s: with sums over even and odd tokens
+//     sum p (z + s code) = [sum_even p s code - sum_odd p s (15 - code)] + sum p mid - 7.5 (sum_even p s - sum_odd p s),
+//   and none of the three grows with the number of tokens as they do not cancel one another.
+//   Weights.  p and p s are rounded to fp16, mid too: a result is off by about 2^-11 of the codes' size, 5e-4 of its norm, beside the 0.1 of holding
+//   the cache in 4 bits.  The largest weight is kept near 2^15 / (largest scale), so that small ones do not vanish below
+//   fp16's steps; the sum of the weights is that of the rounded ones.
+#include "paged4.cuh"
+#include "paged_split.cuh"
+#include "ptx.cuh"
+
+namespace moqae {
+
+namespace {
+
+__host__ __device__ constexpr int warps_of(int form) { return form == kFew16 ? 8 : 16; }
+__host__ __device__ constexpr int stages4_of(int form) { return form == kFew16 ? 4 : 3; }
+constexpr int kMinTiles4 = 2, kPairTiles4 = 96;
+// Weights of a row are 2^(score - reference), at most 2^top: the reference lies top - kLag below the largest score so far and moves when
+// a score passes it by top.  top is 15, less where value scales above 1 would take p s out of fp16.
+constexpr float kLag = 3.0f;
+constexpr float kTop = 15.0f;
+constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;     // codes in bits 0..3 and 4..7 of both halves
+constexpr uint32_t kOddLow = 0x000f0000u, kOddHigh = 0x00f00000u;   // turn those of the second token to 15 - code
+constexpr uint32_t kOddSign = 0x80000000u;                      // the second token's sign
+
+// d = a b + 0, d += a b: fp16 operands whatever the dtype of queries and results
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
+__device__ __forceinline__ void mma_more(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];\n" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void ldsm2(uint32_t& r0, uint32_t& r1, uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];\n" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// z + 7.5 s, the second token's negated
+__device__ __forceinline__ uint32_t mid2(uint32_t s, uint32_t z) {
+  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&s), __float2half2_rn(7.5f), *reinterpret_cast<const __half2*>(&z));
+  return *reinterpret_cast<const uint32_t*>(&r) ^ kOddSign;
+}
+__device__ __forceinline__ float low_half(uint32_t u) { return __low2float(*reinterpret_cast<const __half2*>(&u)); }
+__device__ __forceinline__ float high_half(uint32_t u) { return __high2float(*reinterpret_cast<const __half2*>(&u)); }
+
+template <bool BF16, int FORM>
+__global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(PagedView pv, AttnOptions opt, DecodeJob job) {
+  constexpr int kRows = set_rows(FORM), kCols = kRows / 8, kStages = stages4_of(FORM), kWarps = warps_of(FORM);
+  extern __shared__ __align__(128) uint8_t smem[];
+  // [warps][stages] tiles; the piece each warp may leave behind at the start of its range (the one at its end goes into
+  // its ring, which is empty by then); barriers of the stages; descriptors
+  const int piece_rows = FORM == kFew16 ? kRows : job.group;
+  const int piece_floats = piece_floats_of(piece_rows);
+  float* head_piece = reinterpret_cast<float*>(smem + kWarps * kStages * kTileBytes4);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(head_piece + kWarps * piece_floats);
+  Piece* desc = reinterpret_cast<Piece*>(bars + kWarps * kStages);                  // [2 * kWarps]
+  int* turn = reinterpret_cast<int*>(desc + 2 * kWarps);                            // see join_pieces
+  volatile int* failed = turn + 6;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t4 = lane & 3;
+  uint8_t* ring = smem + warp * kStages * kTileBytes4;
+  const uint32_t ring_u = smem_u32(ring), bar_u = smem_u32(bars + warp * kStages);
+  auto token_of = [&](int row) { return token_in_sequence<FORM>(job, row); };
+
+  if (threadIdx.x < 2 * kWarps) desc[threadIdx.x].pair = -1;
+  if (threadIdx.x == 0) *failed = 0;
+  if (lane == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(bar_u + 8 * i, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  after_previous();
+
+  Part part;
+  if (!share_work<FORM, kWarps, kMinTiles4, kPairTiles4>(pv, opt, job, warp, lane, part)) return;
+  __syncthreads();
+
+  if (part.todo > 0) {
+    long long at;                                 // unit of the tile that is worked on
+    Cursor put = find_first<FORM>(pv, opt, job, lane, part, at);   // next tile to copy
+    int todo = part.todo;
+    Cursor get = put;                             // next tile to work on
+    int to_put = todo;
+    auto page_of = [&](const Cursor& c) -> int {
+      if (c.b >= pv.batch) return -1;
+      return pv.table[static_cast<long long>(c.b) * pv.max_pages + ((tile_of(c.s, c.i) * kTile) >> pv.page_shift)];
+    };
+    int page = page_of(put);
+    // copy of the next tile into stage st; a tile without a page is all zeros
+    auto copy_tile = [&](int st) {
+      const int t0 = tile_of(put.s, put.i) * kTile;
+      const uint32_t dst = ring_u + st * kTileBytes4;
+      if (page >= 0 && page < pv.n_pages) {
+        if (lane == 0) {
+          mbar_expect_tx(bar_u + 8 * st, kTileBytes4);
+          bulk_load(dst, tile4(pv, page, put.h, t0 & (pv.page_size - 1)), kTileBytes4, bar_u + 8 * st);
+        }
+      } else {
+        if (lane == 0) paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, put.b, t0 >> pv.page_shift);
+        for (int i = lane; i < kTileBytes4 / 16; i += 32) *reinterpret_cast<uint4*>(ring + st * kTileBytes4 + 16 * i) = make_uint4(0, 0, 0, 0);
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_u + 8 * st);
+      }
+      to_put -= advance<FORM>(put, pv, opt, job);
+      page = to_put > 0 ? page_of(put) : -1;
+    };
+#pragma unroll
+    for (int st = 0; st < kStages - 1; ++st)
+      if (to_put > 0) copy_tile(st);
+
+    const bool shaped = opt.cap > 0.0f;
+    const float by_cap = shaped ? 1.0f / opt.cap : 0.0f;
+    uint32_t qf[kCols][4][2][2], qz[kCols][2];    // fragments of the queries; sums of their groups
+    float factor[kCols][2], slope[kCols][2], m[kCols][2], o[kCols][4][2][4], zo[kCols][4];
+    int pos[kCols][2];                            // positions of this lane's columns 8 c + 2 t4, + 1
+    float top = kTop;
+    uint32_t most = 0;                            // largest scale that `top` allows, in both halves
+    bool from_start = false, fresh = true;        // the next tile opens a pair
+    int stage = 0;
+    uint32_t parity = 0;
+    while (todo > 0) {
+      if (to_put > 0) copy_tile(stage + kStages - 1 >= kStages ? stage - 1 : stage + kStages - 1);
+      if (fresh) {
+        fresh = false;
+        from_start = get.i == 0;
+        top = kTop;
+        most = 0x3c003c00u;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+          // ---- queries: lane (g, t4) takes channels 8 t4 .. 8 t4 + 7 of every group of row 8 c + g ----
+          const int r = 8 * c + g, t = token_of(get.s.row0 + r);
+          const bool real = r < get.s.rows;
+          const uint16_t* src = job.q.data + 8 * t4;
+          if (real) src += (get.s.q_first + t) * job.q.token + (get.h * job.group + get.s.row0 + r - t * job.group) * job.q.head;
+          uint4 raw[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) raw[i] = real ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0, 0, 0, 0);
+          float big = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = pair_to_float2<BF16>(w[e]);
+              big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+            }
+          }
+          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+          const uint32_t ex = max(__float_as_uint(big) >> 23, 4u);        // 2^(ex - 127) <= largest
+          const float up = __uint_as_float((257u - ex) << 23), down = __uint_as_float((ex - 3u) << 23);   // 2^(130 - ex) and its inverse
+          float sums[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 f = pair_to_float2<BF16>(w[e]);
+              x[2 * e] = f.x * up;
+              x[2 * e + 1] = f.y * up;
+            }
+            // channel e of a word of codes stands in its bits 4 e: pairs (e, e + 4), odd ones 16 times too large
+            qf[c][i][0][0] = float2_to_pair<false>(x[0], x[4]);
+            qf[c][i][0][1] = float2_to_pair<false>(x[1] * 0.0625f, x[5] * 0.0625f);
+            qf[c][i][1][0] = float2_to_pair<false>(x[2], x[6]);
+            qf[c][i][1][1] = float2_to_pair<false>(x[3] * 0.0625f, x[7] * 0.0625f);
+            sums[i] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+            sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], 1);
+            sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], 2);
+          }
+          // zeros are columns 4..7 of a token's scales and zeros: lanes t4 = 2, 3
+          const float s0 = t4 == 2 ? sums[0] : t4 == 3 ? sums[2] : 0.0f, s1 = t4 == 2 ? sums[1] : t4 == 3 ? sums[3] : 0.0f;
+          qz[c][0] = float2_to_pair<false>(s0, s1);
+          qz[c][1] = float2_to_pair<false>(s0 - low_half(qz[c][0]), s1 - high_half(qz[c][0]));
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int rr = min(8 * c + 2 * t4 + e, get.s.rows - 1), tt = token_of(get.s.row0 + rr);
+            factor[c][e] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e)) * 16777216.0f * opt.scale * (shaped ? by_cap : kLog2e);
+            pos[c][e] = get.s.pos0 + tt;
+            slope[c][e] = opt.slopes && 8 * c + 2 * t4 + e < get.s.rows ? opt.slopes[get.h * job.group + get.s.row0 + rr - tt * job.group] * kLog2e : 0.0f;
+            m[c][e] = -INFINITY;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            zo[c][i] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][i][0][e] = o[c][i][1][e] = 0.0f;
+          }
+        }
+      }
+      if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar_u + 8 * stage, parity))) {
+        if (lane == 0) *failed = 1;
+        break;
+      }
+      const uint32_t tile = ring_u + stage * kTileBytes4;
+      const int t0 = tile_of(get.s, get.i) * kTile;
+      if (t0 + kTile > get.s.len || (t0 < get.s.lo && t0 + kTile > get.s.pre)) {
+        // what no row may use can hold anything: its scales and zeros become 0
+        const int j = t0 + lane;
+        if (lane < kTile && !(j < get.s.len && (j >= get.s.lo || j < get.s.pre))) {
+          uint8_t* tp = ring + stage * kTileBytes4;
+          *reinterpret_cast<uint4*>(tp + kKeyMeta4 + 16 * lane) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t*>(tp + kValueMeta4 + 32 * (lane >> 1))[2 * i + (lane & 1)] = 0;
+        }
+        fence_async_smem();
+        __syncwarp();
+      }
+
+      // ---- scores ----
+      float x[kCols][4];
+      {
+        const uint4 k0 = lds128(tile + 64 * g + 16 * t4), k1 = lds128(tile + 64 * (g + 8) + 16 * t4);
+        const uint2 c0 = lds64(tile + kKeyMeta4 + 16 * g), c1 = lds64(tile + kKeyMeta4 + 16 * (g + 8));
+        uint32_t z0, z1;
+        ldsm2(z0, z1, tile + kKeyMeta4 + 16 * (lane & 15));
+        const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+        const float s0[4] = {low_half(c0.x), high_half(c0.x), low_half(c0.y), high_half(c0.y)};
+        const float s1[4] = {low_half(c1.x), high_half(c1.x), low_half(c1.y), high_half(c1.y)};
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+          float acc[4];
+          mma_first(acc, z0, z1, z0, z1, qz[c][0], qz[c][1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[c][e] = acc[e] * 5.9604645e-8f;     // 2^-24, as the codes have it
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t a = w0[i], b = w1[i], a8 = a >> 8, b8 = b >> 8;
+#pragma unroll
+          for (int c = 0; c < kCols; ++c) {
+            float acc[4];
+            mma_first(acc, a & kLow, b & kLow, a & kHigh, b & kHigh, qf[c][i][0][0], qf[c][i][0][1]);
+            mma_more(acc, a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, qf[c][i][1][0], qf[c][i][1][1]);
+            x[c][0] = fmaf(acc[0], s0[i], x[c][0]);
+            x[c][1] = fmaf(acc[1], s0[i], x[c][1]);
+            x[c][2] = fmaf(acc[2], s1[i], x[c][2]);
+            x[c][3] = fmaf(acc[3], s1[i], x[c][3]);
+          }
+        }
+      }
+      // value scales and zeros: pairs of tokens (2 t4, 2 t4 + 1), (2 t4 + 8, 2 t4 + 9)
+      const uint32_t vm = tile + kValueMeta4 + 32 * t4;
+      const uint32_t vs0 = lds32(vm + 4 * (g & 3)), vs1 = lds32(vm + 128 + 4 * (g & 3));     // scales of group g % 4
+      const uint32_t vz0 = lds32(vm + 16 + 4 * (g & 3)), vz1 = lds32(vm + 144 + 4 * (g & 3));
+      bool above;
+      {
+        const __half2 big = __hmax2(*reinterpret_cast<const __half2*>(&vs0), *reinterpret_cast<const __half2*>(&vs1));
+        above = !__hble2(big, *reinterpret_cast<const __half2*>(&most));
+      }
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int j = t0 + g + 8 * (e >> 1);
+          float y = x[c][e] * factor[c][e & 1];
+          if (shaped) y = opt.cap * kLog2e * tanh_of(y);
+          const int p = pos[c][e & 1];
+          if (opt.slopes) y = fmaf(-slope[c][e & 1], fabsf(static_cast<float>(p - j)), y);
+          const bool see = FORM == kFew16 ? (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix
+                                          : j < get.s.len && (j >= get.s.lo || j < get.s.pre);
+          x[c][e] = see ? y : -INFINITY;
+        }
+        above = above || fmaxf(x[c][0], x[c][2]) > m[c][0] + top || fmaxf(x[c][1], x[c][3]) > m[c][1] + top;
+      }
+      if (__any_sync(0xffffffffu, above)) {
+        float sm = fmaxf(fmaxf(low_half(vs0), high_half(vs0)), fmaxf(low_half(vs1), high_half(vs1)));   // largest value scale of the tile
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) sm = fmaxf(sm, __shfl_xor_sync(0xffffffffu, sm, d));
+        float lower = 0.0f;
+        const int up = static_cast<int>((__float_as_uint(sm) + 0x007fffffu) >> 23) - 127;     // sm <= 2^up
+        if (static_cast<float>(up) > kTop - top) {
+          lower = static_cast<float>(up) - (kTop - top);
+          top -= lower;
+          const uint32_t h = static_cast<uint32_t>(min(up, 15) + 15) << 10;
+          most = h | (h << 16);
+        }
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float t = fmaxf(x[c][e], x[c][2 + e]);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            t = fmaxf(t - (top - kLag), m[c][e] + lower);
+            const float f = t == -INFINITY ? 0.0f : exp2_fast(m[c][e] - t);
+            m[c][e] = t;
+            zo[c][e] *= f;
+            zo[c][2 + e] *= f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              o[c][i][0][e] *= f;
+              o[c][i][0][2 + e] *= f;
+              o[c][i][1][e] *= f;
+              o[c][i][1][2 + e] *= f;
+            }
+          }
+      }
+      uint32_t b0[kCols], b1[kCols];
+      // rows 0..3: scales, 4..7: middles, 8: ones, with the signs of the weights
+      const uint32_t a0 = g < 4 ? vs0 : mid2(vs0, vz0), a1 = g < 4 ? vs1 : mid2(vs1, vz1), ones = g == 0 ? 0xbc003c00u : 0u;
+#pragma unroll
+      for (int c = 0; c < kCols; ++c) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = x[c][e] == -INFINITY ? 0.0f : exp2_fast(x[c][e] - m[c][e & 1]);
+        b0[c] = transpose8(float2_to_pair<false>(p[0], p[1])) ^ kOddSign;
+        b1[c] = transpose8(float2_to_pair<false>(p[2], p[3])) ^ kOddSign;
+        mma_more(zo[c], a0, ones, a1, ones, b0[c], b1[c]);
+      }
+      // ---- values ----
+      {
+        const uint4 v0 = lds128(vm), v1 = lds128(vm + 128);
+        const uint32_t s0[4] = {v0.x, v0.y, v0.z, v0.w}, s1[4] = {v1.x, v1.y, v1.z, v1.w};
+        const uint32_t vc = tile + kValueCodes4 + 512 * (g >> 2) + 32 * t4 + 8 * (g & 3);
+        const uint2 a = lds64(vc), b = lds64(vc + 128), d = lds64(vc + 256), e = lds64(vc + 384);   // tokens 2 t4, + 1, + 8, + 9
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t p0 = __byte_perm(i < 2 ? a.x : a.y, i < 2 ? b.x : b.y, (i & 1) ? 0x7632 : 0x5410), q0 = p0 >> 8;
+          const uint32_t p1 = __byte_perm(i < 2 ? d.x : d.y, i < 2 ? e.x : e.y, (i & 1) ? 0x7632 : 0x5410), q1 = p1 >> 8;
+#pragma unroll
+          for (int c = 0; c < kCols; ++c) {
+            const uint32_t w0 = mul2(b0[c], s0[i]), w1 = mul2(b1[c], s1[i]);
+            mma_more(o[c][i][0], (p0 & kLow) ^ kOddLow, (p0 & kHigh) ^ kOddHigh, (p1 & kLow) ^ kOddLow, (p1 & kHigh) ^ kOddHigh, w0, w1);
+            mma_more(o[c][i][1], (q0 & kLow) ^ kOddLow, (q0 & kHigh) ^ kOddHigh, (q1 & kLow) ^ kOddLow, (q1 & kHigh) ^ kOddHigh, w0, w1);
+          }
+        }
+      }
+      __syncwarp();                               // the stage may be filled again
+      if (++stage == kStages) {
+        stage = 0;
+        parity ^= 1;
+      }
+
+      const bool last_of_pair = get.i + 1 == get.s.n, last_of_all = todo <= (last_of_pair ? 1 + kPairCost : 1);
+      if (last_of_pair || last_of_all) {
+        // lane (g, t4): rows 8 c + 2 t4 + e, channels 32 i + 4 g + 2 j + half; the middles' sums in lanes 4 + i, the scales' in i, the weights' in 0
+        const bool whole = from_start && last_of_pair;
+        const int which = from_start ? 1 : 0;
+        float* dst = which ? reinterpret_cast<float*>(ring) : head_piece + warp * piece_floats;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+          float l[2], inv[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            l[e] = __shfl_sync(0xffffffffu, zo[c][2 + e], t4);
+            inv[e] = !whole ? 1.0f : l[e] == 0.0f ? 0.0f : 1.0f / l[e];
+          }
+          const int r = 8 * c + g, t = token_of(get.s.row0 + r);
+          uint16_t* row = job.out.data + (get.s.q_first + t) * job.out.token + (get.h * job.group + get.s.row0 + r - t * job.group) * job.out.head;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v[2][4];                        // [row][channel 2 j + half]
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float z = fmaf(-7.5f, __shfl_sync(0xffffffffu, zo[c][e], 4 * i + t4), __shfl_sync(0xffffffffu, zo[c][e], 4 * (4 + i) + t4));
+              v[e][0] = fmaf(o[c][i][0][e], 16777216.0f, z) * inv[e];
+              v[e][1] = fmaf(o[c][i][0][2 + e], 1048576.0f, z) * inv[e];
+              v[e][2] = fmaf(o[c][i][1][e], 16777216.0f, z) * inv[e];
+              v[e][3] = fmaf(o[c][i][1][2 + e], 1048576.0f, z) * inv[e];
+            }
+            if (whole) {
+              uint32_t w[4];                      // lane (g, t4) then has row 8 c + g, channels 32 i + 8 t4 + k and + k + 4
+#pragma unroll
+              for (int k = 0; k < 4; ++k) w[k] = transpose8(float2_to_pair<BF16>(v[0][k], v[1][k]));
+              if (r < get.s.rows)
+                *reinterpret_cast<uint4*>(row + 32 * i + 8 * t4) = make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410),
+                                                                            __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
+            } else {
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (8 * c + 2 * t4 + e < piece_rows)
+                  *reinterpret_cast<float4*>(dst + (8 * c + 2 * t4 + e) * kHeadDim + 32 * i + 4 * g) = make_float4(v[e][0], v[e][1], v[e][2], v[e][3]);
+            }
+          }
+          if (!whole && g == 0)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (8 * c + 2 * t4 + e < piece_rows) *reinterpret_cast<float2*>(dst + piece_rows * kHeadDim + 2 * (8 * c + 2 * t4 + e)) = make_float2(m[c][e], l[e]);
+        }
+        if (!whole && lane == 0) {
+          Piece& d = desc[2 * warp + which];
+          d.pair = get.flat * pv.n_kv_heads + get.h;
+          d.h = get.h;
+          d.starts = from_start;
+          d.ends = last_of_pair;
+          d.set = get.set;
+          d.n = get.s.n;
+          d.rows = get.s.rows;
+          d.q_first = get.s.q_first;
+          d.unit = at - get.i;
+        }
+        fresh = true;
+      }
+      const int passed = advance<FORM>(get, pv, opt, job);
+      todo -= passed;
+      at += passed;
+    }
+  }
+  __syncthreads();
+  if (*failed) {                                  // a copy did not come: what is still under way may land before the CTA leaves
+    if (threadIdx.x == 0) paged_status(pv.status, MOQAE_ERR_TIMEOUT, static_cast<int>(blockIdx.x), -1);
+    const long long since = clock64();
+    while (clock64() - since < (1 << 20)) {
+    }
+    return;
+  }
+
+  auto piece_at = [&](int i) -> const float* {
+    return (i & 1) ? reinterpret_cast<const float*>(smem + (i >> 1) * kStages * kTileBytes4) : head_piece + (i >> 1) * piece_floats;
+  };
+  join_pieces<BF16, FORM, kWarps>(job, part, desc, turn, piece_rows, piece_floats, warp, lane, piece_at);
+}
+
+size_t smem4(int form, int rows) {
+  const int warps = warps_of(form), stages = stages4_of(form);
+  return static_cast<size_t>(warps) * stages * (kTileBytes4 + 8) + static_cast<size_t>(warps) * piece_floats_of(rows) * 4 + 2 * warps * sizeof(Piece) + 32;
+}
+
+template <bool BF16, int FORM> cudaError_t launch4(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
+  static_assert(stages4_of(FORM) * kTileBytes4 >= piece_floats_of(set_rows(FORM)) * 4, "a piece fits the ring");
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = allow_shared_memory(paged4_decode_kernel<BF16, FORM>, smem4(FORM, set_rows(FORM)), done);
+  if (e != cudaSuccess) return e;
+  return launch_early(paged4_decode_kernel<BF16, FORM>, sm_count_of_current_device(), warps_of(FORM) * 32, smem4(FORM, FORM == kFew16 ? 16 : job.group), st, pv, opt, job);
+}
+
+}  // namespace
+
+bool paged4_decode_fits(const PagedView& pv) {
+  return static_cast<long long>(pv.batch) * pv.n_kv_heads <= kWorkCounters && units_fit(pv, pv.batch);
+}
+
+long long paged4_decode_workspace_bytes(int group) { return kWorkCounterBytes + part_bytes(group); }
+
+cudaError_t launch_paged4_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace, cudaStream_t st) {
+  if (pv.batch <= 0) return cudaSuccess;
+  DecodeJob job{};
+  job.q = q;
+  job.out = out;
+  job.group = q.n_heads / pv.n_kv_heads;
+  job.arrived = static_cast<int*>(workspace);
+  job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
+  return pv.dtype == MOQAE_DTYPE_BF16 ? launch4<true, kOne8>(pv, opt, job, st) : launch4<false, kOne8>(pv, opt, job, st);
+}
+
+bool paged4_prefill_fits(const PagedView& pv, int group, int n_tokens) {
+  const long long sets = few_sets(pv.batch, group, n_tokens);
+  return sets * pv.n_kv_heads <= kWorkCounters && units_fit(pv, sets);
+}
+
+long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens) { return kWorkCounterBytes + part_bytes(16); }
+
+cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
+                                  const AttnOptions& opt, void* workspace, cudaStream_t st) {
+  if (pv.batch <= 0 || n_tokens <= 0) return cudaSuccess;
+  DecodeJob job{};
+  job.q = q;
+  job.out = out;
+  job.cu_q = cu_q;
+  job.n_tokens = n_tokens;
+  job.group = q.n_heads / pv.n_kv_heads;
+  job.arrived = static_cast<int*>(workspace);
+  job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
+  return pv.dtype == MOQAE_DTYPE_BF16 ? launch4<true, kFew16>(pv, opt, job, st) : launch4<false, kFew16>(pv, opt, job, st);
+}
+
+}  // namespace moqae

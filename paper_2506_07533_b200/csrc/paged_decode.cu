@@ -30,7 +30,7 @@
 //   320 to 356 us (floor 328 at the rate of a copy, which writes as much as it reads).  Short calls pay about 10 us beside
 //   their bytes: 2 us to find the work, 2 for the first tile, 1 to 3 to join inside a CTA, 1 for the fence and the
 //   arrival, 2 to join what CTAs share (8 sequences of 1000: 16.2 us, floor 5; 128 of 300: 38, floor 24).
-#include "paged.cuh"
+#include "paged_split.cuh"
 #include "ptx.cuh"
 
 namespace moqae {
@@ -38,255 +38,24 @@ namespace moqae {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kTile = 16;                        // tokens per tile
 constexpr int kTileBytes = kTile * 256;          // of keys, and of values
 constexpr int kStageBytes = 2 * kTileBytes;
 constexpr int kMinTiles = 2;                     // a CTA is worth starting for this many tiles per warp
 constexpr int kPairTiles = 48;                   // up to so many tiles per pair, a CTA takes whole pairs where it can
-constexpr int kPairCost = 1;                     // what a pair costs beside its tiles, in tiles (its queries, its result)
 // The reference lies kLead below the largest score so far and moves when a score exceeds it by kLag, in base-2 units: weights below
 // 2^kLag.  In fp16, whose steps end at 2^-24, the lead keeps small weights: each is off by at most 2^-35 of the largest (without
 // it 2^-25, which 131000 tokens behind one large score add up to 0.4 % of that score's weight).
 template <bool BF16> constexpr float kLead = BF16 ? 0.0f : 10.0f;
 template <bool BF16> constexpr float kLag = BF16 ? 8.0f : 15.0f;
-constexpr float kLog2e = 1.4426950408889634f;
 
-// How a launch forms its sets: one token of a group of at most 4 or 8 heads, or up to 16 rows of several tokens.
-enum { kOne4, kOne8, kFew16 };
-__host__ __device__ constexpr int set_rows(int form) { return form == kFew16 ? 16 : 8; }
 // tiles in flight or in use per warp (the pieces of 16 rows take the room of the third)
 __host__ __device__ constexpr int stages_of(int form) { return form == kFew16 ? 2 : 3; }
-
-// A piece: the sums of a pair's tiles, float [rows][128], then (reference, weight sum) per row.
-__host__ __device__ constexpr int piece_floats_of(int rows) { return (rows * (kHeadDim + 2) + 3) / 4 * 4; }
-
-// total * i / n for i <= n < 256
-__device__ __forceinline__ long long share(long long total, int i, int n) {
-  if (total < (1ll << 23)) return static_cast<unsigned>(total) * static_cast<unsigned>(i) / static_cast<unsigned>(n);
-  return total * i / n;
-}
-
-struct DecodeJob {
-  RowsView q, out;
-  const int32_t* cu_q;    // null: one token per sequence
-  int n_tokens, group;
-  float* part;            // [ctas][2] pieces
-  int* arrived;           // [sets][n_kv_heads]
-};
-
-// A set of rows and the tiles that they see: tokens [lo, len) and [0, pre).
-struct Seen {
-  int len, lo, pre;       // pre <= lo
-  int n_pre, first, n;    // tiles of the prefix, first tile behind them, number of tiles
-  int sets;               // of the sequence
-  int q_n;                // its query tokens
-  int row0, rows;         // rows of the set
-  int q_first, pos0;      // row of the queries, and position, of the sequence's first query token
-  int prefix;             // what every row sees
-  __device__ __forceinline__ int units() const { return n > 0 ? n + kPairCost : 0; }
-};
-template <int FORM>
-__device__ __forceinline__ Seen seen_of(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, int b, int set, bool report) {
-  Seen s;
-  const int kv_len = paged_len(pv, b, report);
-  s.prefix = opt.prefix_len ? min(max(opt.prefix_len[b], 0), kv_len) : 0;
-  int p_first;
-  if (FORM == kFew16) {
-    s.q_first = min(max(job.cu_q[b], 0), job.n_tokens);
-    s.q_n = min(max(job.cu_q[b + 1], s.q_first), job.n_tokens) - s.q_first;
-    const int rows = s.q_n * job.group;
-    s.sets = (rows + 15) / 16;
-    s.row0 = set * 16;
-    s.rows = min(16, rows - s.row0);
-    s.pos0 = kv_len - s.q_n;
-    p_first = s.pos0 + s.row0 / job.group;
-    s.len = s.rows > 0 ? max(s.pos0 + (s.row0 + s.rows - 1) / job.group + 1, s.prefix) : 0;
-    s.len = max(s.len, 0);
-  } else {
-    s.sets = s.q_n = 1;
-    s.row0 = 0;
-    s.rows = job.group;
-    s.q_first = b;
-    s.pos0 = p_first = kv_len - 1;
-    s.len = kv_len;
-  }
-  s.lo = opt.window > 0 ? max(0, p_first + 1 - opt.window) : 0;
-  s.pre = min(s.prefix, s.len);
-  if (s.pre >= s.lo) s.lo = s.pre = 0;
-  s.n_pre = (s.pre + kTile - 1) / kTile;
-  s.first = max(s.lo / kTile, s.n_pre);
-  s.n = s.n_pre + max(0, (s.len + kTile - 1) / kTile - s.first);
-  return s;
-}
-__device__ __forceinline__ int tile_of(const Seen& s, int i) { return i < s.n_pre ? i : s.first + i - s.n_pre; }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool fetch) {
   asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(fetch ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory"); }
-
-__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];\n"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(x));
-  return r;
-}
-template <bool BF16> __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if (BF16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
-  return r;
-}
-
-// A position in the order of all tiles: tile i of set `set` of sequence b, head h.  Work is shared out in units: a pair
-// is kPairCost units without a tile, then one unit per tile.
-struct Cursor {
-  int b, set, h, i;
-  int flat;               // sets before this one, of all sequences
-  Seen s;
-};
-// To the next tile; returns the units that this passes.
-template <int FORM> __device__ __forceinline__ int advance(Cursor& c, const PagedView& pv, const AttnOptions& opt, const DecodeJob& job) {
-  if (++c.i < c.s.n) return 1;
-  c.i = 0;
-  if (++c.h < pv.n_kv_heads) return 1 + kPairCost;
-  c.h = 0;
-  do {
-    ++c.flat;
-    if (++c.set >= c.s.sets) {
-      c.set = 0;
-      do {
-        if (++c.b >= pv.batch) return 1 + kPairCost;
-        c.s = seen_of<FORM>(pv, opt, job, c.b, 0, false);
-      } while (c.s.sets == 0);
-    } else {
-      c.s = seen_of<FORM>(pv, opt, job, c.b, c.set, false);
-    }
-  } while (c.s.n == 0);
-  return 1 + kPairCost;
-}
-
-// Which pair a piece in shared memory belongs to.
-struct Piece {
-  int pair, h;            // set * n_kv_heads + h, or -1; h
-  int starts, ends;       // whether it holds the pair's first and last tile
-  int set, n;             // set of the sequence, tiles of the pair
-  int rows, q_first;      // rows of the set, first row of the sequence's queries
-  long long unit;         // unit of the pair's first tile
-};
-
-// The end of a row's joining: the finished row (out != null), or the joined piece.
-template <bool BF16>
-__device__ __forceinline__ void put_row(const float (&acc)[8], float m, float l, int rows, int r, int sub, uint16_t* out, float* joined) {
-  if (out) {
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    *reinterpret_cast<uint4*>(out + 8 * sub) =
-        make_uint4(float2_to_pair<BF16>(acc[0] * inv, acc[1] * inv), float2_to_pair<BF16>(acc[2] * inv, acc[3] * inv),
-                   float2_to_pair<BF16>(acc[4] * inv, acc[5] * inv), float2_to_pair<BF16>(acc[6] * inv, acc[7] * inv));
-  } else {
-    float4* dst = reinterpret_cast<float4*>(joined + r * kHeadDim) + 2 * sub;
-    dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-    dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-    if (sub == 0) *reinterpret_cast<float2*>(joined + rows * kHeadDim + 2 * r) = make_float2(m, l);
-  }
-}
-
-// Half a warp adds row r of n pieces of the workspace (piece(p): address of the p-th, in the order of their tokens), a
-// lane eight channels, and writes the finished row.  r >= rows: it only keeps the other half company.  The first pieces'
-// sums are on their way while the references are compared.
-template <bool BF16, typename F>
-__device__ __forceinline__ void join_far(F piece, int n, int rows, int r, int lane, uint16_t* out) {
-  constexpr int kBatch = 4;
-  const int sub = lane & 15;
-  const bool act = r < rows;
-  r = act ? r : rows - 1;
-  const int at_ml = rows * kHeadDim + 2 * r;
-  float m = -INFINITY, l = 0.0f, acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  float4 v[kBatch][2];
-  auto load = [&](int p0) {
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const float4* src = reinterpret_cast<const float4*>(piece(min(p0 + k, n - 1)) + r * kHeadDim) + 2 * sub;
-      v[k][0] = __ldcg(src);
-      v[k][1] = __ldcg(src + 1);
-    }
-  };
-  for (int base = 0; base < n; base += 16) {
-    load(base);
-    float2 w = make_float2(-INFINITY, 0.0f);
-    if (base + sub < n) w = __ldcg(reinterpret_cast<const float2*>(piece(base + sub) + at_ml));
-    float top = fmaxf(m, w.x);
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const float f = w.x == -INFINITY ? 0.0f : exp2_fast(w.x - top), old = m == -INFINITY ? 0.0f : exp2_fast(m - top);
-    float fl = w.y * f;
-#pragma unroll
-    for (int o = 8; o > 0; o >>= 1) fl += __shfl_xor_sync(0xffffffffu, fl, o);
-    l = l * old + fl;
-    m = top;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= old;
-    const int many = min(16, n - base);
-    for (int p0 = 0; p0 < many; p0 += kBatch) {
-      if (p0) load(base + p0);
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const float fp = __shfl_sync(0xffffffffu, f, p0 + k, 16);          // 0 behind the last piece
-        const float* x = reinterpret_cast<const float*>(v[k]);
-        if (p0 + k < many)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) acc[e] = fmaf(x[e], fp, acc[e]);
-      }
-    }
-  }
-  if (act) put_row<BF16>(acc, m, l, rows, r, sub, out, nullptr);
-}
-
-// The same for pieces in shared memory (bit i of `run`: piece(i)), and where the run is not the whole pair (out == null) the
-// sum goes on as a piece.  They are near enough to be read twice: a pass for the reference, one for the sums.  (The exchange between lanes above costs as much as a dozen pieces do here: jobs of two
-// pieces took 2050 clocks instead of 1000.)
-template <bool BF16, typename P>
-__device__ __forceinline__ void join_near(P piece, unsigned run, int rows, int r, int lane, uint16_t* out, float* joined) {
-  const int sub = lane & 15;
-  const bool act = r < rows;
-  r = act ? r : rows - 1;
-  const int at_ml = rows * kHeadDim + 2 * r;
-  float m = -INFINITY, l = 0.0f, acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (unsigned bits = run; bits; bits &= bits - 1) m = fmaxf(m, piece(__ffs(bits) - 1)[at_ml]);
-#pragma unroll 2
-  for (unsigned bits = run; bits; bits &= bits - 1) {
-    const float* from = piece(__ffs(bits) - 1);
-    const float2 w = *reinterpret_cast<const float2*>(from + at_ml);
-    const float4* x = reinterpret_cast<const float4*>(from + r * kHeadDim) + 2 * sub;
-    const float4 a = x[0], b = x[1];
-    const float f = w.x == -INFINITY ? 0.0f : exp2_fast(w.x - m);
-    l = fmaf(w.y, f, l);
-    acc[0] = fmaf(a.x, f, acc[0]);
-    acc[1] = fmaf(a.y, f, acc[1]);
-    acc[2] = fmaf(a.z, f, acc[2]);
-    acc[3] = fmaf(a.w, f, acc[3]);
-    acc[4] = fmaf(b.x, f, acc[4]);
-    acc[5] = fmaf(b.y, f, acc[5]);
-    acc[6] = fmaf(b.z, f, acc[6]);
-    acc[7] = fmaf(b.w, f, acc[7]);
-  }
-  if (act) put_row<BF16>(acc, m, l, rows, r, sub, out, joined);
-}
 
 template <bool BF16, int FORM>
 __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView pv, AttnOptions opt, DecodeJob job) {
@@ -304,118 +73,23 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   const int g = lane >> 2, t4 = lane & 3;
   uint8_t* ring = smem + warp * kStages * kStageBytes;
   const uint32_t ring_u = smem_u32(ring);
-  auto token_of = [&](int row) { return FORM == kFew16 ? row / job.group : 0; };
+  auto token_of = [&](int row) { return token_in_sequence<FORM>(job, row); };
 
   if (threadIdx.x < 2 * kWarps) desc[threadIdx.x].pair = -1;
   after_previous();
 
-  // ---- where the work is: units and sets of every sequence, then this warp's piece ----
-  // sequence b, one head: its units; rows that see nothing are zeros (once per launch: `write`)
-  int tokens = 0;                                 // query tokens that this lane has counted
-  auto units_of = [&](int b, int& sets, bool write) -> int {
-    int units = 0;
-    sets = 1;
-    for (int set = 0; set < sets; ++set) {
-      const Seen s = seen_of<FORM>(pv, opt, job, b, set, write && set == 0 && blockIdx.x == 0);
-      sets = s.sets;
-      if (FORM == kFew16 && set == 0) tokens += s.q_n;
-      units += s.units();
-      if (s.n == 0 && write && b % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x))
-        for (int h = 0; h < pv.n_kv_heads; ++h)
-          for (int r = 0; r < s.rows; ++r) {
-            const int t = token_of(s.row0 + r);
-            uint16_t* row = job.out.data + (s.q_first + t) * job.out.token + (h * job.group + s.row0 + r - t * job.group) * job.out.head;
-            for (int c = 0; c < kHeadDim; c += 8) *reinterpret_cast<uint4*>(row + c) = make_uint4(0, 0, 0, 0);
-          }
-    }
-    return units;
-  };
-  int mine = 0, first_units = 0, first_sets = 0, all_sets = 0;
-  for (int b = lane; b < pv.batch && (FORM != kFew16 || tokens <= job.n_tokens); b += 32) {
-    int sets;
-    const int u = units_of(b, sets, warp == 0);
-    mine += u;
-    all_sets += sets;
-    if (b < 32) {
-      first_units = u;
-      first_sets = sets;
-    }
-  }
-  if (FORM == kFew16) {                           // sequences that share rows could have more sets than there are counters
-    tokens = __reduce_add_sync(0xffffffffu, tokens);
-    if (tokens > job.n_tokens) {
-      if (blockIdx.x == 0 && threadIdx.x == 0) paged_status(pv.status, MOQAE_ERR_INVALID_ARG, -1, tokens);
-      return;
-    }
-  }
-  mine = __reduce_add_sync(0xffffffffu, mine);
-  all_sets = __reduce_add_sync(0xffffffffu, all_sets);
-  const long long total = static_cast<long long>(mine) * pv.n_kv_heads;
-  const long long pairs = static_cast<long long>(all_sets) * pv.n_kv_heads;
-  // A CTA per pair while that is no more than kPairTiles tiles each: with equal lengths no pair then spans CTAs,
-  // which saves the way through the workspace.  Otherwise every CTA gets at least kMinTiles tiles per warp.  Measured with a limit of
-  // 8 / 24 / 48 / 96 tiles (us, timer steps of 2): 64 pairs of 19 tiles 16.4 / 14.3 / 14.3 / 14.3, 128 pairs of 19 18.4 / 16.4 / 16.4 / 16.4, of 44
-  // 24.6 / 24.6 / 20.5 / 20.5, of 63 28.7 / 28.7 / 28.7 / 24.6; 2 or 8 pairs of 44 14.3 / 14.3 / 16.4 / 16.4, of 63 14.3 / 14.3 / 14.3 / 20.5.
-  const int most = static_cast<int>(gridDim.x);
-  int ctas = most;
-  if (total <= static_cast<long long>(most) * kWarps * kMinTiles) ctas = static_cast<int>((total + kWarps * kMinTiles - 1) / (kWarps * kMinTiles));
-  if (pairs <= most && total <= pairs * (kPairTiles + kPairCost) && total >= pairs) ctas = static_cast<int>(pairs);
-  const int cta = static_cast<int>(blockIdx.x);
-  if (cta >= ctas) return;
-  const long long cta_lo = share(total, cta, ctas), cta_hi = share(total, cta + 1, ctas);
-  const int in_cta = static_cast<int>(cta_hi - cta_lo);
-  const long long lo = cta_lo + share(in_cta, warp, kWarps);
-  int todo = static_cast<int>(cta_lo + share(in_cta, warp + 1, kWarps) - lo);
+  // ---- where the work is.  Measured with a limit of 8 / 24 / 48 / 96 tiles per pair (us, timer steps of 2): 64 pairs of 19 tiles
+  // 16.4 / 14.3 / 14.3 / 14.3, 128 pairs of 19 18.4 / 16.4 / 16.4 / 16.4, of 44 24.6 / 24.6 / 20.5 / 20.5, of 63 28.7 / 28.7 / 28.7 / 24.6;
+  // 2 or 8 pairs of 44 14.3 / 14.3 / 16.4 / 16.4, of 63 14.3 / 14.3 / 14.3 / 20.5. ----
+  Part part;
+  if (!share_work<FORM, kWarps, kMinTiles, kPairTiles>(pv, opt, job, warp, lane, part)) return;
 
   __syncthreads();
 
-  if (todo > 0) {
-    // ---- the pair that holds unit `lo` ----
-    Cursor put;                                   // next tile to copy
-    long long at = lo;                            // unit of the tile that is worked on
-    {
-      int before = 0, sets_before = 0;            // of one head
-      put.b = 0;
-      for (int base = 0; base < pv.batch; base += 32) {
-        const int b = base + lane;
-        int n = first_units, sets = first_sets;
-        if (base > 0) n = b < pv.batch ? units_of(b, sets, false) : (sets = 0);
-        int inc = n, sinc = sets;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int x = __shfl_up_sync(0xffffffffu, inc, o), y = __shfl_up_sync(0xffffffffu, sinc, o);
-          if (lane >= o) {
-            inc += x;
-            sinc += y;
-          }
-        }
-        const unsigned hit = __ballot_sync(0xffffffffu, static_cast<long long>(before + inc) * pv.n_kv_heads > lo);
-        if (hit) {
-          const int l = __ffs(hit) - 1;
-          put.b = base + l;
-          before += __shfl_sync(0xffffffffu, inc - n, l);
-          sets_before += __shfl_sync(0xffffffffu, sinc - sets, l);
-          break;
-        }
-        before += __shfl_sync(0xffffffffu, inc, 31);
-        sets_before += __shfl_sync(0xffffffffu, sinc, 31);
-      }
-      int off = static_cast<int>(lo - static_cast<long long>(before) * pv.n_kv_heads);
-      put.set = 0;
-      put.s = seen_of<FORM>(pv, opt, job, put.b, 0, false);
-      while (off >= put.s.units() * pv.n_kv_heads) {
-        off -= put.s.units() * pv.n_kv_heads;
-        put.s = seen_of<FORM>(pv, opt, job, put.b, ++put.set, false);
-      }
-      put.flat = sets_before + put.set;
-      put.h = off / put.s.units();
-      put.i = off - put.h * put.s.units() - kPairCost;
-      if (put.i < 0) {                            // the piece opens with units that hold no tile
-        todo += put.i;
-        at -= put.i;
-        put.i = 0;
-      }
-    }
+  if (part.todo > 0) {
+    long long at;                                 // unit of the tile that is worked on
+    Cursor put = find_first<FORM>(pv, opt, job, lane, part, at);   // next tile to copy
+    int todo = part.todo;
     Cursor get = put;                             // next tile to work on
     int to_put = todo;
     auto page_of = [&](const Cursor& c) -> int {
@@ -698,80 +372,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
   auto piece_at = [&](int i) -> const float* {
     return (i & 1) ? reinterpret_cast<const float*>(smem + (i >> 1) * kStages * kStageBytes) : head_piece + (i >> 1) * piece_floats;
   };
-  const int my_pair = lane < 2 * kWarps ? desc[lane].pair : -1;
-  const unsigned valid = __ballot_sync(0xffffffffu, my_pair >= 0);
-  if (valid == 0) return;
-  // where row r of the pair of piece i goes
-  auto row_of = [&](int i, int r) -> uint16_t* {
-    const int h = desc[i].h, row = desc[i].set * kRows + r, t = token_of(row);
-    return job.out.data + (desc[i].q_first + t) * job.out.token + static_cast<long long>(h * job.group + row - t * job.group) * job.out.head;
-  };
-  // Runs of pieces of one pair; a warp takes jobs of two rows of a run.  A run that is not the whole pair goes to the
-  // workspace: slot 1 if it holds the pair's first tile (at most one run, the last), slot 0 otherwise (the first).
-  // Lane i looks at piece i, so that a warp finds its jobs without walking over all runs.
-  const unsigned run = __match_any_sync(0xffffffffu, my_pair);
-  const bool opens = my_pair >= 0 && (run & ((1u << lane) - 1u)) == 0;          // the first piece of its run
-  const bool starts = opens && desc[lane].starts, whole = starts && desc[31 - __clz(run)].ends;
-  const int cross0 = __ffs(__ballot_sync(0xffffffffu, opens && !whole && !starts)) - 1;    // first pieces of the runs that span CTAs
-  const int cross1 = __ffs(__ballot_sync(0xffffffffu, opens && !whole && starts)) - 1;
-  const int jobs = opens ? (desc[lane].rows + 1) / 2 : 0;
-  int jobs_to = jobs;                             // of pieces 0 .. lane
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, jobs_to, o);
-    if (lane >= o) jobs_to += x;
-  }
-  const int n_jobs = __shfl_sync(0xffffffffu, jobs_to, 31);
-  for (int j = warp; j < n_jobs; j += kWarps) {
-    const int first = __ffs(__ballot_sync(0xffffffffu, jobs_to > j)) - 1;
-    const int r = 2 * (j - __shfl_sync(0xffffffffu, jobs_to - jobs, first)) + (lane >> 4), rows = desc[first].rows;
-    const bool to_out = __shfl_sync(0xffffffffu, whole ? 1 : 0, first) != 0;
-    float* joined = job.part + (static_cast<long long>(cta) * 2 + (desc[first].starts ? 1 : 0)) * piece_floats;
-    // (row `rows` of an odd count reads the last one and is not written)
-    join_near<BF16>(piece_at, __shfl_sync(0xffffffffu, run, first), piece_rows, r < rows ? r : piece_rows, lane,
-                    to_out && r < rows ? row_of(first, r) : nullptr, joined);
-  }
-  if (cross0 < 0 && cross1 < 0) return;
-
-  // ---- pairs that span CTAs: the CTA that arrives last adds the pieces ----
-  auto cta_of = [&](long long unit) -> int {      // largest c with share(total, c, ctas) <= unit
-    int c = min(static_cast<int>(static_cast<float>(unit) * static_cast<float>(ctas) / static_cast<float>(total)), ctas - 1);
-    while (c > 0 && share(total, c, ctas) > unit) --c;
-    while (c + 1 < ctas && share(total, c + 1, ctas) <= unit) ++c;
-    return c;
-  };
-  // (the last two warps speak for the two pairs: they have the fewest rows to join, if any)
-  const int which = kWarps - 1 - warp, speaks_for = which == 0 ? cross0 : which == 1 ? cross1 : -1;
-  int c0 = 0, c1 = 0;
-  if (speaks_for >= 0) {                          // both ends at once, on two lanes
-    c0 = cta_of(desc[speaks_for].unit + (lane == 1 ? desc[speaks_for].n - 1 : 0));
-    c1 = __shfl_sync(0xffffffffu, c0, 1);
-  }
-  __threadfence();
-  __syncthreads();
-  if (speaks_for >= 0 && lane == 0) {
-    turn[which] = static_cast<int>(atomicInc(reinterpret_cast<unsigned*>(job.arrived) + desc[speaks_for].pair, static_cast<unsigned>(c1 - c0)));
-    turn[2 + which] = c0;
-    turn[4 + which] = c1;
-  }
-  __syncthreads();
-  int n_job = 0;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int piece = k ? cross1 : cross0;
-    if (piece < 0) continue;
-    const int from = turn[2 + k], to = turn[4 + k];
-    if (turn[k] != to - from) continue;
-    __threadfence();
-    const int rows = desc[piece].rows;
-    for (int r0 = 0; r0 < rows; r0 += 2, ++n_job) {
-      if (n_job % kWarps != warp) continue;
-      const int r = r0 + (lane >> 4);
-      join_far<BF16>([&](int p) -> const float* {
-        return job.part + (static_cast<long long>(from + p) * 2 + (p == 0 ? 1 : 0)) * piece_floats;
-      }, to - from + 1, piece_rows, r < rows ? r : piece_rows, lane, r < rows ? row_of(piece, r) : nullptr);
-    }
-  }
+  join_pieces<BF16, FORM, kWarps>(job, part, desc, turn, piece_rows, piece_floats, warp, lane, piece_at);
 }
 
 size_t decode_smem(int form, int rows) {
@@ -784,18 +385,6 @@ template <bool BF16, int FORM> cudaError_t launch(const PagedView& pv, const Att
   cudaError_t e = allow_shared_memory(paged_decode_kernel<BF16, FORM>, decode_smem(FORM, FORM == kOne4 ? 4 : set_rows(FORM)), done);
   if (e != cudaSuccess) return e;
   return launch_early(paged_decode_kernel<BF16, FORM>, sm_count_of_current_device(), kWarps * 32, decode_smem(FORM, rows), st, pv, opt, job);
-}
-
-long long part_bytes(int rows) {
-  const long long n = 2ll * sm_count_of_current_device() * piece_floats_of(rows) * 4;
-  return (n + 15) / 16 * 16;
-}
-
-long long few_sets(int batch, int group, int n_tokens) { return (static_cast<long long>(n_tokens) * group + 15ll * batch) / 16; }
-
-// Units of all heads are counted in 32 bits.
-bool units_fit(const PagedView& pv, long long sets) {
-  return sets * pv.n_kv_heads * (static_cast<long long>(pv.max_pages) * (pv.page_size / kTile) + kPairCost + 1) < (1ll << 31);
 }
 
 cudaError_t launch_form(PagedView pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
