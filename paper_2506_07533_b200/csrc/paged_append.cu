@@ -30,7 +30,7 @@ constexpr int kRowsPerPass = 32 / kRowLanes;    // rows a warp handles at a time
 constexpr int kAppendWarps = 4;
 
 struct RowJob {
-  RowsView q, k, v, q_out, k_out, v_out;        // k_out: not into pages; v_out: of paged4_read_kernel alone
+  RowsView q, k, v, q_out, k_out;               // k_out: only without pages
   const int32_t* positions;
   const int32_t* seq;
   int32_t* status;
@@ -285,7 +285,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) norm_rope_kernel(PagedView 
 
 // Rows of 4-bit pages as the 16-bit values nearest to what they stand for.  Eight lanes a row again: of a key a lane takes two units of 8
 // channels, of a value four channels of each group.
-template <bool BF16> __global__ void __launch_bounds__(kAppendWarps * 32) paged4_read_kernel(PagedView pv, RowJob job) {
+template <bool BF16> __global__ void __launch_bounds__(kAppendWarps * 32) paged4_read_kernel(PagedView pv, RowJob job, RowsView v_out) {
   after_previous();
   const int lane = threadIdx.x & 31, sub = lane & (kRowLanes - 1), slot = lane / kRowLanes;
   const long long w = static_cast<long long>(blockIdx.x) * kAppendWarps + (threadIdx.x >> 5);
@@ -301,7 +301,7 @@ template <bool BF16> __global__ void __launch_bounds__(kAppendWarps * 32) paged4
     return;
   }
   const int at = pos & (pv.page_size - 1), tt = at & 15;
-  const int n_k = job.k_out.n_heads, n_rows = n_k + job.v_out.n_heads;
+  const int n_k = job.k_out.n_heads, n_rows = n_k + v_out.n_heads;
   for (int r = part * kRowsPerPass + slot; r < n_rows; r += kRowsPerPass << job.parts_shift) {
     const bool is_v = r >= n_k;
     const int h = is_v ? r - n_k : r;
@@ -324,7 +324,7 @@ template <bool BF16> __global__ void __launch_bounds__(kAppendWarps * 32) paged4
       const uint2 code = *reinterpret_cast<const uint2*>(tile + kValueCodes4 + 512 * (sub >> 2) + 32 * value_row4(tt) + 8 * (sub & 3));
       const uint4 s4 = *reinterpret_cast<const uint4*>(tile + kValueMeta4 + 32 * (tt >> 1)), z4 = *reinterpret_cast<const uint4*>(tile + kValueMeta4 + 32 * (tt >> 1) + 16);
       const uint32_t sw[4] = {s4.x, s4.y, s4.z, s4.w}, zw[4] = {z4.x, z4.y, z4.z, z4.w};
-      uint16_t* dst = job.v_out.data + t * job.v_out.token + h * job.v_out.head;
+      uint16_t* dst = v_out.data + t * v_out.token + h * v_out.head;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const float sc = (tt & 1) ? hi_f<false>(sw[g]) : lo_f<false>(sw[g]), z = (tt & 1) ? hi_f<false>(zw[g]) : lo_f<false>(zw[g]);
@@ -387,12 +387,12 @@ cudaError_t launch_paged4_append(const PagedView& pv, const RopeView& rope, cons
 cudaError_t launch_paged4_read(const PagedView& pv, const RowsView& k_out, const RowsView& v_out, const int32_t* positions, const int32_t* seq,
                                int n_tokens, cudaStream_t st) {
   RowJob job{};
-  job.k_out = k_out; job.v_out = v_out;
+  job.k_out = k_out;
   job.positions = positions; job.seq = seq; job.status = pv.status; job.n_tokens = n_tokens;
   const int n_rows = k_out.n_heads + v_out.n_heads;
   if (n_tokens <= 0 || n_rows <= 0) return cudaSuccess;
   const unsigned grid = share_rows(job, n_rows);
-  return launch_early(pv.dtype == MOQAE_DTYPE_BF16 ? paged4_read_kernel<true> : paged4_read_kernel<false>, grid, kAppendWarps * 32, 0, st, pv, job);
+  return launch_early(pv.dtype == MOQAE_DTYPE_BF16 ? paged4_read_kernel<true> : paged4_read_kernel<false>, grid, kAppendWarps * 32, 0, st, pv, job, v_out);
 }
 
 }  // namespace moqae
