@@ -7,14 +7,14 @@
 // code 2^-20, one logic instruction per register of two; scales and zeros are a few values per token.
 //
 //   Work, tiles, pieces and their joining are those of the 16-bit pages (paged_split.cuh); a tile of 16 tokens of one kv
-//   head is 2560 bytes in one place, fetched with one bulk copy by the warp that works on it.
+//   head is 2560 bytes in one place, fetched with one bulk copy by the warp that works on it, two at a time.
 //   Products, on mma.sync m16n8k16.  S^T = codes q^T: per group two products whose sums meet the tokens' scales in registers, and one for the
 //   zeros of all groups, with the sums of the queries' groups as high + low halves.  O^T += codes^T (p s)^T: weights become fp16, turn by movmatrix, and
 //   meet a group's value scales as packed pairs; one more product sums what the zeros give and, in a row of ones, the weights.
 //   Queries are scaled by a power of two to at most 16, so that bf16 rows and small ones keep their bits in fp16 (2^-24 of the largest).
 //   Signs.  Codes are never negative, and a sum of many that the zeros then cancel loses what the mean over a long context leaves (the
 //   tensor cores cut off the bits below 2^-23 of a running sum: 131000 tokens were off by 0.004 of their norm instead of the 0.0017 of
-//   rounding to bf16, 32000 in one warp by 0.011).  So every second token has 15 - code (the same instruction) with the weight -p, and the zeros become the
+//   rounding to bf16, 32000 in one warp by 0.011).  So every second token has 15 - code with the weight -p, and the zeros become the
 //   middles of the ranges, mid = z + 7.5 s: with sums over even and odd tokens
 //     sum p (z + s code) = [sum_even p s code - sum_odd p s (15 - code)] + sum p mid - 7.5 (sum_even p s - sum_odd p s),
 //   and none of the three grows with the number of tokens as they do not cancel one another.
@@ -29,15 +29,17 @@ namespace moqae {
 
 namespace {
 
-__host__ __device__ constexpr int warps_of(int form) { return form == kFew16 ? 8 : 16; }
-__host__ __device__ constexpr int stages4_of(int form) { return form == kFew16 ? 4 : 3; }
+// Warps of a CTA (the most that registers and pieces leave room for) and stages of a warp's ring, of two tiles each.
+__host__ __device__ constexpr int warps_of(int form) { return form == kFew16Q ? 8 : form == kOne8Q ? 12 : 16; }
+__host__ __device__ constexpr int stages4_of(int form) { return form == kFew16Q ? 3 : 2; }
+constexpr int kStageBytes4 = 2 * kTileBytes4;
 constexpr int kMinTiles4 = 2, kPairTiles4 = 96;
 // Weights of a row are 2^(score - reference), at most 2^top: the reference lies top - kLag below the largest score so far and moves when
 // a score passes it by top.  top is 15, less where value scales above 1 would take p s out of fp16.
 constexpr float kLag = 3.0f;
 constexpr float kTop = 15.0f;
+constexpr float kNothing = -1e30f;                // reference of a row that has seen nothing
 constexpr uint32_t kLow = 0x000f000fu, kHigh = 0x00f000f0u;     // codes in bits 0..3 and 4..7 of both halves
-constexpr uint32_t kOddLow = 0x000f0000u, kOddHigh = 0x00f00000u;   // turn those of the second token to 15 - code
 constexpr uint32_t kOddSign = 0x80000000u;                      // the second token's sign
 
 // d = a b + 0, d += a b: fp16 operands whatever the dtype of queries and results
@@ -85,17 +87,18 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
   extern __shared__ __align__(128) uint8_t smem[];
   // [warps][stages] tiles; the piece each warp may leave behind at the start of its range (the one at its end goes into
   // its ring, which is empty by then); barriers of the stages; descriptors
-  const int piece_rows = FORM == kFew16 ? kRows : job.group;
+  const int piece_rows = FORM == kFew16Q ? kRows : job.group;
   const int piece_floats = piece_floats_of(piece_rows);
-  float* head_piece = reinterpret_cast<float*>(smem + kWarps * kStages * kTileBytes4);
+  float* head_piece = reinterpret_cast<float*>(smem + kWarps * kStages * kStageBytes4);
   uint64_t* bars = reinterpret_cast<uint64_t*>(head_piece + kWarps * piece_floats);
   Piece* desc = reinterpret_cast<Piece*>(bars + kWarps * kStages);                  // [2 * kWarps]
   int* turn = reinterpret_cast<int*>(desc + 2 * kWarps);                            // see join_pieces
   volatile int* failed = turn + 6;
+  Cursor* cursors = reinterpret_cast<Cursor*>(turn + 8);                            // [2 * kWarps]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t4 = lane & 3;
-  uint8_t* ring = smem + warp * kStages * kTileBytes4;
+  uint8_t* ring = smem + warp * kStages * kStageBytes4;
   const uint32_t ring_u = smem_u32(ring), bar_u = smem_u32(bars + warp * kStages);
   auto token_of = [&](int row) { return token_in_sequence<FORM>(job, row); };
 
@@ -112,131 +115,168 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
   __syncthreads();
 
   if (part.todo > 0) {
-    long long at;                                 // unit of the tile that is worked on
-    Cursor put = find_first<FORM>(pv, opt, job, lane, part, at);   // next tile to copy
-    int todo = part.todo;
-    Cursor get = put;                             // next tile to work on
-    int to_put = todo;
-    auto page_of = [&](const Cursor& c) -> int {
-      if (c.b >= pv.batch) return -1;
-      return pv.table[static_cast<long long>(c.b) * pv.max_pages + ((tile_of(c.s, c.i) * kTile) >> pv.page_shift)];
+    long long at;                                 // unit of the pair's tile that is worked on first
+    {
+      const Cursor first = find_first<FORM>(pv, opt, job, lane, part, at);
+      if (lane == 0) cursors[2 * warp] = cursors[2 * warp + 1] = first;
+    }
+    __syncwarp();
+    // Two walks over the warp's tiles: `put` copies them, `get` works on them.  What a tile needs of its pair is in registers, the rest
+    // in shared memory (lane 0 takes it to the next pair).
+    Cursor &put = cursors[2 * warp], &get = cursors[2 * warp + 1];
+    int todo = part.todo, to_put = part.todo;
+    int put_i, put_left, put_pre, put_first;      // index of the next tile in the pair's walk, tiles left; the walk: see tile_of
+    const int32_t* put_row;                       // the sequence's pages
+    const uint8_t* put_head;                      // the head's part of page 0
+    int at_token, page;                           // of lanes 0 and 1: first token of the next tile and of the one behind it, and their pages
+    auto look_up = [&]() {
+      const int i = put_i + (lane & 1);
+      at_token = (i < put_pre ? i : put_first + i - put_pre) * kTile;
+      page = (lane & 1) < put_left ? put_row[at_token >> pv.page_shift] : 0;
     };
-    int page = page_of(put);
-    // copy of the next tile into stage st; a tile without a page is all zeros
-    auto copy_tile = [&](int st) {
-      const int t0 = tile_of(put.s, put.i) * kTile;
-      const uint32_t dst = ring_u + st * kTileBytes4;
-      if (page >= 0 && page < pv.n_pages) {
-        if (lane == 0) {
-          mbar_expect_tx(bar_u + 8 * st, kTileBytes4);
-          bulk_load(dst, tile4(pv, page, put.h, t0 & (pv.page_size - 1)), kTileBytes4, bar_u + 8 * st);
-        }
-      } else {
-        if (lane == 0) paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, put.b, t0 >> pv.page_shift);
-        for (int i = lane; i < kTileBytes4 / 16; i += 32) *reinterpret_cast<uint4*>(ring + st * kTileBytes4 + 16 * i) = make_uint4(0, 0, 0, 0);
+    auto open_put = [&]() {
+      put_i = put.i;
+      put_left = min(put.s.n - put.i, to_put);
+      put_pre = put.s.n_pre;
+      put_first = put.s.first;
+      put_row = pv.table + static_cast<long long>(put.b) * pv.max_pages;
+      put_head = reinterpret_cast<const uint8_t*>(pv.k) + put.h * pv.k_head;
+      to_put -= put_left + pair_cost(FORM);
+      look_up();
+    };
+    open_put();
+    __syncwarp();
+    // copy of the next two tiles of the pair (or its last) into stage st; a tile without a page is all zeros
+    auto copy_tiles = [&](int st) {
+      if (put_left <= 0) return;
+      const int count = min(put_left, 2);
+      const uint32_t bar = bar_u + 8 * st;
+      const bool mine = lane < count, good = page >= 0 && page < pv.n_pages;
+      const unsigned bad = __ballot_sync(0xffffffffu, mine && !good);
+      if (bad) {
+        if (mine && !good) paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, put.b, at_token >> pv.page_shift);
+        for (int k = 0; k < 2; ++k)
+          for (int i = lane; i < kTileBytes4 / 16 && (bad >> k & 1u); i += 32)
+            *reinterpret_cast<uint4*>(ring + st * kStageBytes4 + k * kTileBytes4 + 16 * i) = make_uint4(0, 0, 0, 0);
         fence_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar_u + 8 * st);
       }
-      to_put -= advance<FORM>(put, pv, opt, job);
-      page = to_put > 0 ? page_of(put) : -1;
+      if (lane == 0) mbar_expect_tx(bar, (count - __popc(bad)) * kTileBytes4);
+      __syncwarp();
+      if (mine && good)
+        bulk_load(ring_u + st * kStageBytes4 + lane * kTileBytes4, put_head + page * pv.k_page + (at_token & (pv.page_size - 1)) * kTokenBytes4,
+                  kTileBytes4, bar);
+      put_left -= count;
+      put_i += count;
+      if (put_left > 0) {
+        look_up();
+      } else if (to_put > 0) {
+        __syncwarp();
+        if (lane == 0) next_pair<FORM>(put, pv, opt, job);
+        __syncwarp();
+        open_put();
+      }
     };
 #pragma unroll
-    for (int st = 0; st < kStages - 1; ++st)
-      if (to_put > 0) copy_tile(st);
+    for (int st = 0; st < kStages - 1; ++st) copy_tiles(st);
 
-    const bool shaped = opt.cap > 0.0f;
+    const bool shaped = opt.cap > 0.0f, plain = !shaped && !opt.slopes;
     const float by_cap = shaped ? 1.0f / opt.cap : 0.0f;
-    uint32_t qf[kCols][4][2][2], qz[kCols][2];    // fragments of the queries; sums of their groups
-    float factor[kCols][2], slope[kCols][2], m[kCols][2], o[kCols][4][2][4], zo[kCols][4];
-    int pos[kCols][2];                            // positions of this lane's columns 8 c + 2 t4, + 1
-    float top = kTop;
-    uint32_t most = 0;                            // largest scale that `top` allows, in both halves
-    bool from_start = false, fresh = true;        // the next tile opens a pair
     int stage = 0;
     uint32_t parity = 0;
     while (todo > 0) {
-      if (to_put > 0) copy_tile(stage + kStages - 1 >= kStages ? stage - 1 : stage + kStages - 1);
-      if (fresh) {
-        fresh = false;
-        from_start = get.i == 0;
-        top = kTop;
-        most = 0x3c003c00u;
+      // ---- a pair: the tiles of it that are the warp's ----
+      const int n_here = min(get.s.n - get.i, todo);
+      const bool from_start = get.i == 0, last_of_pair = get.i + n_here == get.s.n;
+      uint32_t qf[kCols][4][2][2], qz[kCols][2];  // fragments of the queries; sums of their groups
+      float factor[kCols][2], m[kCols][2], o[kCols][4][2][4], zo[kCols][4];
+      float top = kTop;
+      uint32_t most = 0x3c003c00u;                // largest scale that `top` allows, in both halves
+      // the tile that starts at t0 is seen whole by every row if full_lo <= t0 and t0 + 16 <= full_hi, or t0 + 16 <= full_pre
+      int full_lo = get.s.lo, full_hi = get.s.len;
+      const int full_pre = FORM == kFew16Q ? get.s.prefix : get.s.pre;
+      const int n_pre = get.s.n_pre, behind = get.s.first - n_pre;
+      if (FORM == kFew16Q) {
+        full_hi = get.s.pos0 + token_of(get.s.row0) + 1;
+        full_lo = opt.window > 0 ? get.s.pos0 + token_of(get.s.row0 + get.s.rows - 1) - opt.window + 1 : 0;
+      }
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) {
-          // ---- queries: lane (g, t4) takes channels 8 t4 .. 8 t4 + 7 of every group of row 8 c + g ----
-          const int r = 8 * c + g, t = token_of(get.s.row0 + r);
-          const bool real = r < get.s.rows;
-          const uint16_t* src = job.q.data + 8 * t4;
-          if (real) src += (get.s.q_first + t) * job.q.token + (get.h * job.group + get.s.row0 + r - t * job.group) * job.q.head;
-          uint4 raw[4];
+      for (int c = 0; c < kCols; ++c) {
+        // ---- queries: lane (g, t4) takes channels 8 t4 .. 8 t4 + 7 of every group of row 8 c + g ----
+        const int r = 8 * c + g, t = token_of(get.s.row0 + r);
+        const bool real = r < get.s.rows;
+        const uint16_t* src = job.q.data + 8 * t4;
+        if (real) src += (get.s.q_first + t) * job.q.token + (get.h * job.group + get.s.row0 + r - t * job.group) * job.q.head;
+        uint4 raw[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) raw[i] = real ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0, 0, 0, 0);
-          float big = 0.0f;
+        for (int i = 0; i < 4; ++i) raw[i] = real ? *reinterpret_cast<const uint4*>(src + 32 * i) : make_uint4(0, 0, 0, 0);
+        float big = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = pair_to_float2<BF16>(w[e]);
-              big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
-            }
-          }
-          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-          const uint32_t ex = max(__float_as_uint(big) >> 23, 4u);        // 2^(ex - 127) <= largest
-          const float up = __uint_as_float((257u - ex) << 23), down = __uint_as_float((ex - 3u) << 23);   // 2^(130 - ex) and its inverse
-          float sums[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = pair_to_float2<BF16>(w[e]);
-              x[2 * e] = f.x * up;
-              x[2 * e + 1] = f.y * up;
-            }
-            // channel e of a word of codes stands in its bits 4 e: pairs (e, e + 4), odd ones 16 times too large
-            qf[c][i][0][0] = float2_to_pair<false>(x[0], x[4]);
-            qf[c][i][0][1] = float2_to_pair<false>(x[1] * 0.0625f, x[5] * 0.0625f);
-            qf[c][i][1][0] = float2_to_pair<false>(x[2], x[6]);
-            qf[c][i][1][1] = float2_to_pair<false>(x[3] * 0.0625f, x[7] * 0.0625f);
-            sums[i] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-            sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], 1);
-            sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], 2);
-          }
-          // zeros are columns 4..7 of a token's scales and zeros: lanes t4 = 2, 3
-          const float s0 = t4 == 2 ? sums[0] : t4 == 3 ? sums[2] : 0.0f, s1 = t4 == 2 ? sums[1] : t4 == 3 ? sums[3] : 0.0f;
-          qz[c][0] = float2_to_pair<false>(s0, s1);
-          qz[c][1] = float2_to_pair<false>(s0 - low_half(qz[c][0]), s1 - high_half(qz[c][0]));
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int rr = min(8 * c + 2 * t4 + e, get.s.rows - 1), tt = token_of(get.s.row0 + rr);
-            factor[c][e] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e)) * 16777216.0f * opt.scale * (shaped ? by_cap : kLog2e);
-            pos[c][e] = get.s.pos0 + tt;
-            slope[c][e] = opt.slopes && 8 * c + 2 * t4 + e < get.s.rows ? opt.slopes[get.h * job.group + get.s.row0 + rr - tt * job.group] * kLog2e : 0.0f;
-            m[c][e] = -INFINITY;
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            zo[c][i] = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[c][i][0][e] = o[c][i][1][e] = 0.0f;
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = pair_to_float2<BF16>(w[e]);
+            big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
           }
         }
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const uint32_t ex = max(__float_as_uint(big) >> 23, 4u);        // 2^(ex - 127) <= largest
+        const float up = __uint_as_float((257u - ex) << 23), down = __uint_as_float((ex - 3u) << 23);   // 2^(130 - ex) and its inverse
+        float sums[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float2 f = pair_to_float2<BF16>(w[e]);
+            x[2 * e] = f.x * up;
+            x[2 * e + 1] = f.y * up;
+          }
+          // channel e of a word of codes stands in its bits 4 e: pairs (e, e + 4), odd ones 16 times too large
+          qf[c][i][0][0] = float2_to_pair<false>(x[0], x[4]);
+          qf[c][i][0][1] = float2_to_pair<false>(x[1] * 0.0625f, x[5] * 0.0625f);
+          qf[c][i][1][0] = float2_to_pair<false>(x[2], x[6]);
+          qf[c][i][1][1] = float2_to_pair<false>(x[3] * 0.0625f, x[7] * 0.0625f);
+          sums[i] = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+          sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], 1);
+          sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], 2);
+        }
+        // zeros are columns 4..7 of a token's scales and zeros: lanes t4 = 2, 3
+        const float s0 = t4 == 2 ? sums[0] : t4 == 3 ? sums[2] : 0.0f, s1 = t4 == 2 ? sums[1] : t4 == 3 ? sums[3] : 0.0f;
+        qz[c][0] = float2_to_pair<false>(s0, s1);
+        qz[c][1] = float2_to_pair<false>(s0 - low_half(qz[c][0]), s1 - high_half(qz[c][0]));
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          factor[c][e] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e)) * 16777216.0f * opt.scale * (shaped ? by_cap : kLog2e);
+          m[c][e] = kNothing;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          zo[c][i] = 0.0f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[c][i][0][e] = o[c][i][1][e] = 0.0f;
+        }
       }
-      if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar_u + 8 * stage, parity))) {
-        if (lane == 0) *failed = 1;
-        break;
-      }
-      const uint32_t tile = ring_u + stage * kTileBytes4;
-      const int t0 = tile_of(get.s, get.i) * kTile;
-      if (t0 + kTile > get.s.len || (t0 < get.s.lo && t0 + kTile > get.s.pre)) {
+
+      int index = get.i;                          // of the tile in the walk
+      const int end = index + n_here;
+      while (index < end) {
+      copy_tiles(stage == 0 ? kStages - 1 : stage - 1);
+      if (!mbar_try_wait(bar_u + 8 * stage, parity) && !*failed && !mbar_wait_bounded(bar_u + 8 * stage, parity)) *failed = 1;
+      __syncwarp();
+      const uint32_t stage_at = ring_u + stage * kStageBytes4;
+#pragma unroll 1
+      for (uint32_t tile = stage_at; tile < stage_at + kStageBytes4 && index < end; tile += kTileBytes4, ++index) {
+      const int t0 = (index < n_pre ? index : index + behind) * kTile;
+      const bool edge = !((t0 >= full_lo && t0 + kTile <= full_hi) || t0 + kTile <= full_pre);
+      if (edge) {
         // what no row may use can hold anything: its scales and zeros become 0
         const int j = t0 + lane;
         if (lane < kTile && !(j < get.s.len && (j >= get.s.lo || j < get.s.pre))) {
-          uint8_t* tp = ring + stage * kTileBytes4;
+          uint8_t* tp = ring + (tile - ring_u);
           *reinterpret_cast<uint4*>(tp + kKeyMeta4 + 16 * lane) = make_uint4(0, 0, 0, 0);
 #pragma unroll
           for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t*>(tp + kValueMeta4 + 32 * (lane >> 1))[2 * i + (lane & 1)] = 0;
@@ -286,20 +326,30 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         const __half2 big = __hmax2(*reinterpret_cast<const __half2*>(&vs0), *reinterpret_cast<const __half2*>(&vs1));
         above = !__hble2(big, *reinterpret_cast<const __half2*>(&most));
       }
+      if (!plain || edge) {                       // otherwise x times factor is the score
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = t0 + g + 8 * (e >> 1);
+            const int rr = min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1), tt = token_of(get.s.row0 + rr), p = get.s.pos0 + tt;
+            if (!plain) {
+              float y = x[c][e] * factor[c][e & 1];
+              if (shaped) y = opt.cap * kLog2e * tanh_of(y);
+              if (opt.slopes) y = fmaf(-kLog2e * opt.slopes[get.h * job.group + get.s.row0 + rr - tt * job.group], fabsf(static_cast<float>(p - j)), y);
+              x[c][e] = y;
+            }
+            const bool see = FORM == kFew16Q ? (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix
+                                            : j < get.s.len && (j >= get.s.lo || j < get.s.pre);
+            if (!see) x[c][e] = -INFINITY;
+          }
+      }
+      float r[kCols][4];                          // scores above the reference
 #pragma unroll
       for (int c = 0; c < kCols; ++c) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int j = t0 + g + 8 * (e >> 1);
-          float y = x[c][e] * factor[c][e & 1];
-          if (shaped) y = opt.cap * kLog2e * tanh_of(y);
-          const int p = pos[c][e & 1];
-          if (opt.slopes) y = fmaf(-slope[c][e & 1], fabsf(static_cast<float>(p - j)), y);
-          const bool see = FORM == kFew16 ? (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix
-                                          : j < get.s.len && (j >= get.s.lo || j < get.s.pre);
-          x[c][e] = see ? y : -INFINITY;
-        }
-        above = above || fmaxf(x[c][0], x[c][2]) > m[c][0] + top || fmaxf(x[c][1], x[c][3]) > m[c][1] + top;
+        for (int e = 0; e < 4; ++e) r[c][e] = fmaf(x[c][e], plain ? factor[c][e & 1] : 1.0f, -m[c][e & 1]);
+        above = above || fmaxf(fmaxf(r[c][0], r[c][1]), fmaxf(r[c][2], r[c][3])) > top;
       }
       if (__any_sync(0xffffffffu, above)) {
         float sm = fmaxf(fmaxf(low_half(vs0), high_half(vs0)), fmaxf(low_half(vs1), high_half(vs1)));   // largest value scale of the tile
@@ -317,12 +367,15 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         for (int c = 0; c < kCols; ++c)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float t = fmaxf(x[c][e], x[c][2 + e]);
+            const float f0 = plain ? factor[c][e] : 1.0f;
+            float t = fmaxf(x[c][e] * f0, x[c][2 + e] * f0);
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
             t = fmaxf(t - (top - kLag), m[c][e] + lower);
-            const float f = t == -INFINITY ? 0.0f : exp2_fast(m[c][e] - t);
+            const float f = exp2_fast(m[c][e] - t);
             m[c][e] = t;
+            r[c][e] = fmaf(x[c][e], f0, -t);
+            r[c][2 + e] = fmaf(x[c][2 + e], f0, -t);
             zo[c][e] *= f;
             zo[c][2 + e] *= f;
 #pragma unroll
@@ -339,11 +392,8 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
       const uint32_t a0 = g < 4 ? vs0 : mid2(vs0, vz0), a1 = g < 4 ? vs1 : mid2(vs1, vz1), ones = g == 0 ? 0xbc003c00u : 0u;
 #pragma unroll
       for (int c = 0; c < kCols; ++c) {
-        float p[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = x[c][e] == -INFINITY ? 0.0f : exp2_fast(x[c][e] - m[c][e & 1]);
-        b0[c] = transpose8(float2_to_pair<false>(p[0], p[1])) ^ kOddSign;
-        b1[c] = transpose8(float2_to_pair<false>(p[2], p[3])) ^ kOddSign;
+        b0[c] = transpose8(float2_to_pair<false>(exp2_fast(r[c][0]), exp2_fast(r[c][1]))) ^ kOddSign;
+        b1[c] = transpose8(float2_to_pair<false>(exp2_fast(r[c][2]), exp2_fast(r[c][3]))) ^ kOddSign;
         mma_more(zo[c], a0, ones, a1, ones, b0[c], b1[c]);
       }
       // ---- values ----
@@ -351,7 +401,10 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         const uint4 v0 = lds128(vm), v1 = lds128(vm + 128);
         const uint32_t s0[4] = {v0.x, v0.y, v0.z, v0.w}, s1[4] = {v1.x, v1.y, v1.z, v1.w};
         const uint32_t vc = tile + kValueCodes4 + 512 * (g >> 2) + 32 * t4 + 8 * (g & 3);
-        const uint2 a = lds64(vc), b = lds64(vc + 128), d = lds64(vc + 256), e = lds64(vc + 384);   // tokens 2 t4, + 1, + 8, + 9
+        const uint2 a = lds64(vc), d = lds64(vc + 256);          // tokens 2 t4, + 8
+        uint2 b = lds64(vc + 128), e = lds64(vc + 384);          // tokens 2 t4 + 1, + 9: 15 - code
+        b = make_uint2(~b.x, ~b.y);
+        e = make_uint2(~e.x, ~e.y);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const uint32_t p0 = __byte_perm(i < 2 ? a.x : a.y, i < 2 ? b.x : b.y, (i & 1) ? 0x7632 : 0x5410), q0 = p0 >> 8;
@@ -359,19 +412,19 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
 #pragma unroll
           for (int c = 0; c < kCols; ++c) {
             const uint32_t w0 = mul2(b0[c], s0[i]), w1 = mul2(b1[c], s1[i]);
-            mma_more(o[c][i][0], (p0 & kLow) ^ kOddLow, (p0 & kHigh) ^ kOddHigh, (p1 & kLow) ^ kOddLow, (p1 & kHigh) ^ kOddHigh, w0, w1);
-            mma_more(o[c][i][1], (q0 & kLow) ^ kOddLow, (q0 & kHigh) ^ kOddHigh, (q1 & kLow) ^ kOddLow, (q1 & kHigh) ^ kOddHigh, w0, w1);
+            mma_more(o[c][i][0], p0 & kLow, p0 & kHigh, p1 & kLow, p1 & kHigh, w0, w1);
+            mma_more(o[c][i][1], q0 & kLow, q0 & kHigh, q1 & kLow, q1 & kHigh, w0, w1);
           }
         }
+      }
       }
       __syncwarp();                               // the stage may be filled again
       if (++stage == kStages) {
         stage = 0;
         parity ^= 1;
       }
-
-      const bool last_of_pair = get.i + 1 == get.s.n, last_of_all = todo <= (last_of_pair ? 1 + kPairCost : 1);
-      if (last_of_pair || last_of_all) {
+      }
+      {
         // lane (g, t4): rows 8 c + 2 t4 + e, channels 32 i + 4 g + 2 j + half; the middles' sums in lanes 4 + i, the scales' in i, the weights' in 0
         const bool whole = from_start && last_of_pair;
         const int which = from_start ? 1 : 0;
@@ -428,11 +481,14 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
           d.q_first = get.s.q_first;
           d.unit = at - get.i;
         }
-        fresh = true;
       }
-      const int passed = advance<FORM>(get, pv, opt, job);
-      todo -= passed;
-      at += passed;
+      at += n_here + pair_cost(FORM);
+      todo -= n_here + pair_cost(FORM);
+      __syncwarp();
+      if (todo > 0) {
+        if (lane == 0) next_pair<FORM>(get, pv, opt, job);
+        __syncwarp();
+      }
     }
   }
   __syncthreads();
@@ -445,28 +501,28 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
   }
 
   auto piece_at = [&](int i) -> const float* {
-    return (i & 1) ? reinterpret_cast<const float*>(smem + (i >> 1) * kStages * kTileBytes4) : head_piece + (i >> 1) * piece_floats;
+    return (i & 1) ? reinterpret_cast<const float*>(smem + (i >> 1) * kStages * kStageBytes4) : head_piece + (i >> 1) * piece_floats;
   };
   join_pieces<BF16, FORM, kWarps>(job, part, desc, turn, piece_rows, piece_floats, warp, lane, piece_at);
 }
 
 size_t smem4(int form, int rows) {
   const int warps = warps_of(form), stages = stages4_of(form);
-  return static_cast<size_t>(warps) * stages * (kTileBytes4 + 8) + static_cast<size_t>(warps) * piece_floats_of(rows) * 4 + 2 * warps * sizeof(Piece) + 32;
+  return static_cast<size_t>(warps) * stages * (kStageBytes4 + 8) + static_cast<size_t>(warps) * piece_floats_of(rows) * 4 + 2 * warps * (sizeof(Piece) + sizeof(Cursor)) + 32;
 }
 
 template <bool BF16, int FORM> cudaError_t launch4(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
-  static_assert(stages4_of(FORM) * kTileBytes4 >= piece_floats_of(set_rows(FORM)) * 4, "a piece fits the ring");
+  static_assert(stages4_of(FORM) * kStageBytes4 >= piece_floats_of(set_rows(FORM)) * 4, "a piece fits the ring");
   static std::atomic<unsigned long long> done{0};
-  cudaError_t e = allow_shared_memory(paged4_decode_kernel<BF16, FORM>, smem4(FORM, set_rows(FORM)), done);
+  cudaError_t e = allow_shared_memory(paged4_decode_kernel<BF16, FORM>, smem4(FORM, FORM == kOne4Q ? 4 : set_rows(FORM)), done);
   if (e != cudaSuccess) return e;
-  return launch_early(paged4_decode_kernel<BF16, FORM>, sm_count_of_current_device(), warps_of(FORM) * 32, smem4(FORM, FORM == kFew16 ? 16 : job.group), st, pv, opt, job);
+  return launch_early(paged4_decode_kernel<BF16, FORM>, sm_count_of_current_device(), warps_of(FORM) * 32, smem4(FORM, FORM == kFew16Q ? 16 : job.group), st, pv, opt, job);
 }
 
 }  // namespace
 
 bool paged4_decode_fits(const PagedView& pv) {
-  return static_cast<long long>(pv.batch) * pv.n_kv_heads <= kWorkCounters && units_fit(pv, pv.batch);
+  return static_cast<long long>(pv.batch) * pv.n_kv_heads <= kWorkCounters && units_fit(pv, pv.batch, kOne8Q);
 }
 
 long long paged4_decode_workspace_bytes(int group) { return kWorkCounterBytes + part_bytes(group); }
@@ -479,12 +535,14 @@ cudaError_t launch_paged4_decode(const PagedView& pv, const RowsView& q, const R
   job.group = q.n_heads / pv.n_kv_heads;
   job.arrived = static_cast<int*>(workspace);
   job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
-  return pv.dtype == MOQAE_DTYPE_BF16 ? launch4<true, kOne8>(pv, opt, job, st) : launch4<false, kOne8>(pv, opt, job, st);
+  const bool bf16 = pv.dtype == MOQAE_DTYPE_BF16;
+  if (job.group <= 4) return bf16 ? launch4<true, kOne4Q>(pv, opt, job, st) : launch4<false, kOne4Q>(pv, opt, job, st);
+  return bf16 ? launch4<true, kOne8Q>(pv, opt, job, st) : launch4<false, kOne8Q>(pv, opt, job, st);
 }
 
 bool paged4_prefill_fits(const PagedView& pv, int group, int n_tokens) {
   const long long sets = few_sets(pv.batch, group, n_tokens);
-  return sets * pv.n_kv_heads <= kWorkCounters && units_fit(pv, sets);
+  return sets * pv.n_kv_heads <= kWorkCounters && units_fit(pv, sets, kFew16Q);
 }
 
 long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens) { return kWorkCounterBytes + part_bytes(16); }
@@ -500,7 +558,7 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   job.group = q.n_heads / pv.n_kv_heads;
   job.arrived = static_cast<int*>(workspace);
   job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
-  return pv.dtype == MOQAE_DTYPE_BF16 ? launch4<true, kFew16>(pv, opt, job, st) : launch4<false, kFew16>(pv, opt, job, st);
+  return pv.dtype == MOQAE_DTYPE_BF16 ? launch4<true, kFew16Q>(pv, opt, job, st) : launch4<false, kFew16Q>(pv, opt, job, st);
 }
 
 }  // namespace moqae

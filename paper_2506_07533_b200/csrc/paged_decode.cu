@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
             qn_h = 0;
             ++qn_b;
           }
-          if (todo > get.s.n - get.i + kPairCost) load_ahead();   // otherwise this is the warp's last pair
+          if (todo > get.s.n - get.i + pair_cost(FORM)) load_ahead();   // otherwise this is the warp's last pair
         } else if (!first_pair) {
           load_rows(get);
         }
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(kWarps * 32, 1) paged_decode_kernel(PagedView 
       __syncwarp();                               // the stage may be filled again
       stage = stage + 1 == kStages ? 0 : stage + 1;
 
-      const bool last_of_pair = get.i + 1 == get.s.n, last_of_all = todo <= (last_of_pair ? 1 + kPairCost : 1);
+      const bool last_of_pair = get.i + 1 == get.s.n, last_of_all = todo <= (last_of_pair ? 1 + pair_cost(FORM) : 1);
       if (last_of_pair || last_of_all) {
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
@@ -401,7 +401,7 @@ cudaError_t launch_form(PagedView pv, const AttnOptions& opt, const DecodeJob& j
 }  // namespace
 
 bool paged_decode_fits(const PagedView& pv) {
-  return static_cast<long long>(pv.batch) * pv.n_kv_heads <= kWorkCounters && units_fit(pv, pv.batch);
+  return static_cast<long long>(pv.batch) * pv.n_kv_heads <= kWorkCounters && units_fit(pv, pv.batch, kOne8);
 }
 
 // one arrival counter per pair, then partial results of the CTAs' first and last pairs
@@ -430,7 +430,7 @@ cudaError_t launch_paged_decode(const PagedView& pv, const RowsView& q, const Ro
 bool paged_few_rows(const PagedView& pv, int group, int n_tokens) {
   const long long sets = few_sets(pv.batch, group, n_tokens);
   return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * pv.batch && sets * pv.n_kv_heads <= kWorkCounters &&
-         units_fit(pv, sets);
+         units_fit(pv, sets, kFew16);
 }
 
 long long paged_few_workspace_bytes() { return kWorkCounterBytes + part_bytes(16); }

@@ -10,12 +10,15 @@ namespace moqae {
 namespace {
 
 constexpr int kTile = 16;                        // tokens per tile
-constexpr int kPairCost = 1;                     // what a pair costs beside its tiles, in tiles (its queries, its result)
 constexpr float kLog2e = 1.4426950408889634f;
 
-// How a launch forms its sets: one token of a group of at most 4 or 8 heads, or up to 16 rows of several tokens.
-enum { kOne4, kOne8, kFew16 };
-__host__ __device__ constexpr int set_rows(int form) { return form == kFew16 ? 16 : 8; }
+// How a launch forms its sets: one token of a group of at most 4 or 8 heads, or up to 16 rows of several tokens; over 16-bit
+// or 4-bit pages.
+enum { kOne4, kOne8, kFew16, kOne4Q, kOne8Q, kFew16Q };
+__host__ __device__ constexpr bool several(int form) { return form == kFew16 || form == kFew16Q; }
+__host__ __device__ constexpr int set_rows(int form) { return several(form) ? 16 : 8; }
+// What a pair costs beside its tiles, in tiles (its queries, its result).
+__host__ __device__ constexpr int pair_cost(int form) { return form < kOne4Q ? 1 : 3; }
 
 // A piece: the sums of a pair's tiles, float [rows][128], then (reference, weight sum) per row.
 __host__ __device__ constexpr int piece_floats_of(int rows) { return (rows * (kHeadDim + 2) + 3) / 4 * 4; }
@@ -43,7 +46,7 @@ struct Seen {
   int row0, rows;         // rows of the set
   int q_first, pos0;      // row of the queries, and position, of the sequence's first query token
   int prefix;             // what every row sees
-  __device__ __forceinline__ int units() const { return n > 0 ? n + kPairCost : 0; }
+  template <int FORM> __device__ __forceinline__ int units() const { return n > 0 ? n + pair_cost(FORM) : 0; }
 };
 template <int FORM>
 __device__ __forceinline__ Seen seen_of(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, int b, int set, bool report) {
@@ -51,7 +54,7 @@ __device__ __forceinline__ Seen seen_of(const PagedView& pv, const AttnOptions& 
   const int kv_len = paged_len(pv, b, report);
   s.prefix = opt.prefix_len ? min(max(opt.prefix_len[b], 0), kv_len) : 0;
   int p_first;
-  if (FORM == kFew16) {
+  if (several(FORM)) {
     s.q_first = min(max(job.cu_q[b], 0), job.n_tokens);
     s.q_n = min(max(job.cu_q[b + 1], s.q_first), job.n_tokens) - s.q_first;
     const int rows = s.q_n * job.group;
@@ -108,31 +111,35 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // A position in the order of all tiles: tile i of set `set` of sequence b, head h.  Work is shared out in units: a pair
-// is kPairCost units without a tile, then one unit per tile.
+// is pair_cost units without a tile, then one unit per tile.
 struct Cursor {
   int b, set, h, i;
   int flat;               // sets before this one, of all sequences
   Seen s;
 };
-// To the next tile; returns the units that this passes.
-template <int FORM> __device__ __forceinline__ int advance(Cursor& c, const PagedView& pv, const AttnOptions& opt, const DecodeJob& job) {
-  if (++c.i < c.s.n) return 1;
+// To the first tile of the next pair; its b is the batch if there is none.
+template <int FORM> __device__ __forceinline__ void next_pair(Cursor& c, const PagedView& pv, const AttnOptions& opt, const DecodeJob& job) {
   c.i = 0;
-  if (++c.h < pv.n_kv_heads) return 1 + kPairCost;
+  if (++c.h < pv.n_kv_heads) return;
   c.h = 0;
   do {
     ++c.flat;
     if (++c.set >= c.s.sets) {
       c.set = 0;
       do {
-        if (++c.b >= pv.batch) return 1 + kPairCost;
+        if (++c.b >= pv.batch) return;
         c.s = seen_of<FORM>(pv, opt, job, c.b, 0, false);
       } while (c.s.sets == 0);
     } else {
       c.s = seen_of<FORM>(pv, opt, job, c.b, c.set, false);
     }
   } while (c.s.n == 0);
-  return 1 + kPairCost;
+}
+// To the next tile; returns the units that this passes.
+template <int FORM> __device__ __forceinline__ int advance(Cursor& c, const PagedView& pv, const AttnOptions& opt, const DecodeJob& job) {
+  if (++c.i < c.s.n) return 1;
+  next_pair<FORM>(c, pv, opt, job);
+  return 1 + pair_cost(FORM);
 }
 
 // Which pair a piece in shared memory belongs to.
@@ -243,7 +250,7 @@ __device__ __forceinline__ void join_near(P piece, unsigned run, int rows, int r
 }
 
 // Row of the set's tokens that row `row` of a sequence belongs to.
-template <int FORM> __device__ __forceinline__ int token_in_sequence(const DecodeJob& job, int row) { return FORM == kFew16 ? row / job.group : 0; }
+template <int FORM> __device__ __forceinline__ int token_in_sequence(const DecodeJob& job, int row) { return several(FORM) ? row / job.group : 0; }
 
 // Sequence b, one head: its units and sets; rows that see nothing are zeros (once per launch: `write`).  `tokens` counts query tokens.
 template <int FORM>
@@ -253,8 +260,8 @@ __device__ __forceinline__ int units_of(const PagedView& pv, const AttnOptions& 
   for (int set = 0; set < sets; ++set) {
     const Seen s = seen_of<FORM>(pv, opt, job, b, set, write && set == 0 && blockIdx.x == 0);
     sets = s.sets;
-    if (FORM == kFew16 && set == 0) tokens += s.q_n;
-    units += s.units();
+    if (several(FORM) && set == 0) tokens += s.q_n;
+    units += s.units<FORM>();
     if (s.n == 0 && write && b % static_cast<int>(gridDim.x) == static_cast<int>(blockIdx.x))
       for (int h = 0; h < pv.n_kv_heads; ++h)
         for (int r = 0; r < s.rows; ++r) {
@@ -282,7 +289,7 @@ __device__ __forceinline__ bool share_work(const PagedView& pv, const AttnOption
   int tokens = 0;                                 // query tokens that this lane has counted
   int mine = 0, all_sets = 0;
   part.first_units = part.first_sets = 0;
-  for (int b = lane; b < pv.batch && (FORM != kFew16 || tokens <= job.n_tokens); b += 32) {
+  for (int b = lane; b < pv.batch && (!several(FORM) || tokens <= job.n_tokens); b += 32) {
     int sets;
     const int u = units_of<FORM>(pv, opt, job, b, sets, tokens, warp == 0);
     mine += u;
@@ -292,7 +299,7 @@ __device__ __forceinline__ bool share_work(const PagedView& pv, const AttnOption
       part.first_sets = sets;
     }
   }
-  if (FORM == kFew16) {                           // sequences that share rows could have more sets than there are counters
+  if (several(FORM)) {                           // sequences that share rows could have more sets than there are counters
     tokens = __reduce_add_sync(0xffffffffu, tokens);
     if (tokens > job.n_tokens) {
       if (blockIdx.x == 0 && threadIdx.x == 0) paged_status(pv.status, MOQAE_ERR_INVALID_ARG, -1, tokens);
@@ -306,7 +313,7 @@ __device__ __forceinline__ bool share_work(const PagedView& pv, const AttnOption
   const int most = static_cast<int>(gridDim.x);
   part.ctas = most;
   if (part.total <= static_cast<long long>(most) * WARPS * MIN_TILES) part.ctas = static_cast<int>((part.total + WARPS * MIN_TILES - 1) / (WARPS * MIN_TILES));
-  if (pairs <= most && part.total <= pairs * (PAIR_TILES + kPairCost) && part.total >= pairs) part.ctas = static_cast<int>(pairs);
+  if (pairs <= most && part.total <= pairs * (PAIR_TILES + pair_cost(FORM)) && part.total >= pairs) part.ctas = static_cast<int>(pairs);
   const int cta = static_cast<int>(blockIdx.x);
   if (cta >= part.ctas) return false;
   const long long cta_lo = share(part.total, cta, part.ctas), cta_hi = share(part.total, cta + 1, part.ctas);
@@ -352,13 +359,13 @@ __device__ __forceinline__ Cursor find_first(const PagedView& pv, const AttnOpti
   int off = static_cast<int>(lo - static_cast<long long>(before) * pv.n_kv_heads);
   put.set = 0;
   put.s = seen_of<FORM>(pv, opt, job, put.b, 0, false);
-  while (off >= put.s.units() * pv.n_kv_heads) {
-    off -= put.s.units() * pv.n_kv_heads;
+  while (off >= put.s.units<FORM>() * pv.n_kv_heads) {
+    off -= put.s.units<FORM>() * pv.n_kv_heads;
     put.s = seen_of<FORM>(pv, opt, job, put.b, ++put.set, false);
   }
   put.flat = sets_before + put.set;
-  put.h = off / put.s.units();
-  put.i = off - put.h * put.s.units() - kPairCost;
+  put.h = off / put.s.units<FORM>();
+  put.i = off - put.h * put.s.units<FORM>() - pair_cost(FORM);
   if (put.i < 0) {                            // the piece opens with units that hold no tile
     part.todo += put.i;
     at -= put.i;
@@ -461,8 +468,8 @@ inline long long part_bytes(int rows) {
 inline long long few_sets(int batch, int group, int n_tokens) { return (static_cast<long long>(n_tokens) * group + 15ll * batch) / 16; }
 
 // Units of all heads are counted in 32 bits.
-inline bool units_fit(const PagedView& pv, long long sets) {
-  return sets * pv.n_kv_heads * (static_cast<long long>(pv.max_pages) * (pv.page_size / kTile) + kPairCost + 1) < (1ll << 31);
+inline bool units_fit(const PagedView& pv, long long sets, int form) {
+  return sets * pv.n_kv_heads * (static_cast<long long>(pv.max_pages) * (pv.page_size / kTile) + pair_cost(form) + 1) < (1ll << 31);
 }
 
 }  // namespace
