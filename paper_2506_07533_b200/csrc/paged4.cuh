@@ -49,7 +49,10 @@ cudaError_t launch_paged4_read(const PagedView& pv, const RowsView& k_out, const
 bool paged4_decode_fits(const PagedView& pv);
 long long paged4_decode_workspace_bytes(int group);
 cudaError_t launch_paged4_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace, cudaStream_t st);
-bool paged4_prefill_fits(const PagedView& pv, int group, int n_tokens);
+bool paged4_few_rows(const PagedView& pv, int group, int n_tokens);
+long long paged4_few_workspace_bytes();
+cudaError_t launch_paged4_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
+                              const AttnOptions& opt, void* workspace, cudaStream_t st);
 long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens);
 cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                                   const AttnOptions& opt, void* workspace, cudaStream_t st);

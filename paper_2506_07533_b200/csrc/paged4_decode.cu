@@ -540,15 +540,17 @@ cudaError_t launch_paged4_decode(const PagedView& pv, const RowsView& q, const R
   return bf16 ? launch4<true, kOne8Q>(pv, opt, job, st) : launch4<false, kOne8Q>(pv, opt, job, st);
 }
 
-bool paged4_prefill_fits(const PagedView& pv, int group, int n_tokens) {
+// Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average (see paged_few_rows).
+bool paged4_few_rows(const PagedView& pv, int group, int n_tokens) {
   const long long sets = few_sets(pv.batch, group, n_tokens);
-  return sets * pv.n_kv_heads <= kWorkCounters && units_fit(pv, sets, kFew16Q);
+  return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * pv.batch && sets * pv.n_kv_heads <= kWorkCounters &&
+         units_fit(pv, sets, kFew16Q);
 }
 
-long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens) { return kWorkCounterBytes + part_bytes(16); }
+long long paged4_few_workspace_bytes() { return kWorkCounterBytes + part_bytes(16); }
 
-cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
-                                  const AttnOptions& opt, void* workspace, cudaStream_t st) {
+cudaError_t launch_paged4_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
+                              const AttnOptions& opt, void* workspace, cudaStream_t st) {
   if (pv.batch <= 0 || n_tokens <= 0) return cudaSuccess;
   DecodeJob job{};
   job.q = q;

@@ -404,7 +404,6 @@ int moqae_paged4_prefill_attn_workspace(const moqae_paged4_cache* cache, int32_t
   if (rc != MOQAE_OK) return rc;
   if (!out_bytes || n_tokens < 0) return MOQAE_ERR_INVALID_ARG;
   if (n_tokens > moqae::kMaxQueryTokens || pv.batch > moqae::kMaxQueryTokens) return MOQAE_ERR_UNSUPPORTED;
-  if (!moqae::paged4_prefill_fits(pv, n_q_heads / pv.n_kv_heads, n_tokens)) return MOQAE_ERR_UNSUPPORTED;
   *out_bytes = moqae::paged4_prefill_workspace_bytes(pv, n_q_heads / pv.n_kv_heads, n_tokens);
   return MOQAE_OK;
 }
@@ -422,9 +421,9 @@ int moqae_paged4_prefill_attn(const moqae_paged4_cache* cache, const moqae_rows*
   if ((pv.batch > 0 && !cu_q) || !workspace) return MOQAE_ERR_INVALID_ARG;
   if (!aligned(cu_q, 4) || !aligned(workspace, 16)) return MOQAE_ERR_MISALIGNED;
   const int group = qv.n_heads / pv.n_kv_heads;
-  if (!moqae::paged4_prefill_fits(pv, group, n_tokens)) return MOQAE_ERR_UNSUPPORTED;
   if (workspace_bytes < moqae::paged4_prefill_workspace_bytes(pv, group, n_tokens)) return MOQAE_ERR_WORKSPACE_TOO_SMALL;
-  return cuda_rc(moqae::launch_paged4_prefill(pv, qv, cu_q, n_tokens, ov, opt, workspace, static_cast<cudaStream_t>(stream)));
+  const cudaError_t e = moqae::launch_paged4_prefill(pv, qv, cu_q, n_tokens, ov, opt, workspace, static_cast<cudaStream_t>(stream));
+  return e == cudaErrorNotSupported ? MOQAE_ERR_UNSUPPORTED : cuda_rc(e);
 }
 
 }  // extern "C"
