@@ -553,7 +553,7 @@ int moqae_paged_poll_status(const moqae_paged_cache* cache, void* stream, int32_
  *   row    128 channels are four groups of 32.  A group keeps z, the largest fp16 value not above its smallest element
  *          (-0 as +0), s, the smallest fp16 value not below (largest element - z) / 15 (a float32 quotient), and per element x the whole
  *          number nearest to (x - z) * r, r the float32 value nearest to 1 / s, halves to even (0 where s = 0): the rule of
- *          moqae_quantize_kv.  The element then stands for z + s * code.  Elements are finite and at most 65504 in magnitude.
+ *          moqae_quantize_kv.  The element then stands for z + s * code.  Elements are finite and below 32752 in magnitude.
  *   tile   16 consecutive tokens of one kv head, 2560 bytes: keys and values, 64 code bytes and four scales and zeros each per token.
  *          Byte positions, for token t of the tile and channel c, g = c / 32; the even channel of a pair is in the low four bits:
  *            key code    64 t + 16 ((c % 32) / 8) + 4 g + (c % 8) / 2        key scale    1024 + 16 t + 2 g     zero  8 further
@@ -632,9 +632,15 @@ int moqae_paged4_decode_attn(const moqae_paged4_cache* cache, const moqae_rows* 
                              const moqae_attn_options* options, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * moqae_paged_prefill_attn over a 4-bit cache, with the domain of queries of moqae_paged4_decode_attn.  The workspace is required.
+ * moqae_paged_prefill_attn over a 4-bit cache.  Keys, values and queries meet in fp16 (queries are finite, at most 65504 in
+ * magnitude), each element of a key or value rounded once, z + s * code; weights are rounded to fp16; sums are float32.
+ *   workspace: required; *out_bytes is enough for every call of no more tokens and no more sequences with the same head counts, and
+ *   for moqae_paged4_decode_attn.  It holds, among other things, the sequences' blocks expanded to 16 bits, as many as 1 GiB takes; *least_bytes (may
+ *   be NULL) leaves these out, and any size between is used as far as it goes: sequences that find no room are expanded inside the attention
+ *   kernel, which computes the same more slowly.  Only the first 1 MiB has to be zeroed, once, as that of moqae_paged_decode_attn.
  */
-int moqae_paged4_prefill_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int32_t n_tokens, int64_t* out_bytes);
+int moqae_paged4_prefill_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int32_t n_tokens, int64_t* out_bytes,
+                                        int64_t* least_bytes);
 int moqae_paged4_prefill_attn(const moqae_paged4_cache* cache, const moqae_rows* q, const int32_t* cu_q, int32_t n_tokens,
                               const moqae_rows* out, const moqae_attn_options* options, void* workspace,
                               int64_t workspace_bytes, void* stream);

@@ -167,7 +167,7 @@ def lib() -> C.CDLL:
         L.moqae_paged4_read.argtypes = [pc4, rows, rows, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
         L.moqae_paged4_decode_attn_workspace.argtypes = [pc4, C.c_int32, C.POINTER(C.c_int64)]
         L.moqae_paged4_decode_attn.argtypes = [pc4, rows, rows, opts, C.c_void_p, C.c_int64, C.c_void_p]
-        L.moqae_paged4_prefill_attn_workspace.argtypes = [pc4, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]
+        L.moqae_paged4_prefill_attn_workspace.argtypes = [pc4, C.c_int32, C.c_int32, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]
         L.moqae_paged4_prefill_attn.argtypes = [pc4, rows, C.c_void_p, C.c_int32, rows, opts, C.c_void_p, C.c_int64, C.c_void_p]
         L.moqae_paged4_validate.argtypes = [pc4, C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         L.moqae_paged4_poll_status.argtypes = [pc4, C.c_void_p, C.POINTER(C.c_int32)]
@@ -733,12 +733,13 @@ def moqae_paged4_decode_attn(cache: Paged4Cache, q, out, workspace, options: Att
         raise MoqaeError(rc, where)
 
 
-def moqae_paged4_prefill_attn_workspace(cache: Paged4Cache, n_q_heads, n_tokens) -> int:
-    """Bytes for every call of up to n_tokens tokens over up to as many sequences as `cache` has, one-token calls included."""
-    out = C.c_int64(0)
-    _check(lib().moqae_paged4_prefill_attn_workspace(C.byref(cache.view), int(n_q_heads), int(n_tokens), C.byref(out)),
+def moqae_paged4_prefill_attn_workspace(cache: Paged4Cache, n_q_heads, n_tokens, *, least=False) -> int:
+    """Bytes for every call of up to n_tokens tokens over up to as many sequences as `cache` has, one-token calls included.
+    They hold the sequences' blocks at 16 bits, as far as 1 GiB goes; least=True leaves these out (slower calls)."""
+    out, low = C.c_int64(0), C.c_int64(0)
+    _check(lib().moqae_paged4_prefill_attn_workspace(C.byref(cache.view), int(n_q_heads), int(n_tokens), C.byref(out), C.byref(low)),
            "moqae_paged4_prefill_attn_workspace")
-    return int(out.value)
+    return int(low.value if least else out.value)
 
 
 def moqae_paged4_prefill_attn(cache: Paged4Cache, q, cu_q, out, workspace, options: AttnOptions = None):

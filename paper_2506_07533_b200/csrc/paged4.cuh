@@ -53,8 +53,9 @@ bool paged4_few_rows(const PagedView& pv, int group, int n_tokens);
 long long paged4_few_workspace_bytes();
 cudaError_t launch_paged4_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
                               const AttnOptions& opt, void* workspace, cudaStream_t st);
+long long paged4_prefill_least_bytes(const PagedView& pv, int group, int n_tokens);     // without room for expanded blocks
 long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens);
 cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
-                                  const AttnOptions& opt, void* workspace, cudaStream_t st);
+                                  const AttnOptions& opt, void* workspace, long long workspace_bytes, cudaStream_t st);
 
 }  // namespace moqae

@@ -1,61 +1,204 @@
 // moqae_paged4_prefill_attn: launches over 4-bit pages.  Few rows per sequence go to the streaming kernel (paged4_decode.cu), the others to the
-// large tiles (paged_prefill.cuh), behind a pass that brings the queries into fp16 and into the order of the channels there.
-//   A query is read once and written once: 16300 tokens of 32 heads, 267 MB, about 45 us of the 1.8 ms that follow.
+// large tiles (paged_prefill.cuh), behind a pass that brings queries into fp16 and keys and values out of their codes.
+//   Expanding once costs 672 bytes per token and kv head and one reading of 512; inside the large tiles every row tile would
+//   expand the blocks that it sees again (see Four there).  The workspace holds kExpandBytes of expanded blocks at most, sequences beyond that are
+//   expanded inside.
 #include "paged_prefill.cuh"
 
 namespace moqae {
 
 namespace {
 
-constexpr int kQueryThreads = 256;
+constexpr int kExpandThreads = 256, kExpandWarps = kExpandThreads / 32;
+constexpr long long kExpandBytes = 1ll << 30;
+constexpr int kMaxExpanded = 1 << 20;              // blocks
+constexpr int kBlockTiles = kBlock / kTileTokens4;
 
-// Unit i (8 channels) of row i / 16: channels 0, 4, 1, 5, 2, 6, 3, 7 of it, in fp16.
-template <bool BF16> __global__ void __launch_bounds__(kQueryThreads) query4_kernel(RowsView q, uint16_t* to, long long units) {
+struct ExpandJob {
+  RowsView q;
+  const int32_t* cu_q;
+  uint16_t* q16;                                   // [n_tokens][heads][128], channels in column4's order
+  uint16_t* k16;                                   // [blocks][kv heads][128 tokens][128], channels in column4's order
+  uint16_t* v16;
+  int32_t* first;                                  // [batch]: a sequence's first block, -1: not expanded
+  long long q_units;                               // of 8 channels
+  int n_tokens, blocks;                            // rows of q; room for blocks
+};
+
+// Blocks are dealt out in the order of the sequences that bring tokens, until one has no room; a warp takes a tile of 16 tokens of one head.
+template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand4_kernel(PagedView pv, AttnOptions opt, ExpandJob job) {
+  __shared__ int block_to[kExpandThreads + 1], warp_sum[kExpandWarps];      // blocks in front of a sequence
+  __shared__ int len_of[kExpandThreads], lo_of[kExpandThreads], pre_of[kExpandThreads];   // tokens, and which of them some row sees: [lo, len) and [0, pre)
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int r8 = lane & 7, u = lane >> 3;
   after_previous();
-  for (long long i = static_cast<long long>(blockIdx.x) * kQueryThreads + threadIdx.x; i < units; i += static_cast<long long>(gridDim.x) * kQueryThreads) {
-    const long long row = i >> 4, t = row / q.n_heads;
-    const int u = static_cast<int>(i & 15), h = static_cast<int>(row - t * q.n_heads);
-    const uint4 x = *reinterpret_cast<const uint4*>(q.data + t * q.token + h * q.head + 8 * u);
+  int before = 0;
+  for (int base = 0; base < pv.batch; base += kExpandThreads) {
+    const int b = base + tid;
+    int need = 0, len = 0, lo = 0, pre = 0;
+    if (b < pv.batch) {
+      const int from = min(max(job.cu_q[b], 0), job.n_tokens), n = min(max(job.cu_q[b + 1], from), job.n_tokens) - from;
+      len = paged_len(pv, b, false);
+      need = n > 0 ? min((len + kBlock - 1) / kBlock, kMaxExpanded + 1) : 0;
+      lo = opt.window > 0 ? max(0, len - n - opt.window + 1) : 0;
+      pre = opt.prefix_len ? min(max(opt.prefix_len[b], 0), len) : 0;
+    }
+    int sum = need;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, sum, o);
+      if (lane >= o) sum += x;
+    }
+    __syncthreads();                               // the turn before is done with the arrays
+    if (lane == 31) warp_sum[warp] = sum;
+    __syncthreads();
+    int in_front = before;
+#pragma unroll
+    for (int w = 0; w < kExpandWarps; ++w) {
+      const int x = warp_sum[w];
+      if (w < warp) in_front += x;
+      before += x;
+    }
+    before = min(before, kMaxExpanded + 1);
+    block_to[tid] = in_front + sum - need;
+    len_of[tid] = len;
+    lo_of[tid] = lo;
+    pre_of[tid] = pre;
+    if (tid == kExpandThreads - 1) block_to[kExpandThreads] = in_front + sum;
+    if (blockIdx.x == 0 && b < pv.batch) job.first[b] = need > 0 && in_front + sum <= job.blocks ? in_front + sum - need : -1;
+    __syncthreads();
+    const int from = block_to[0], to = min(block_to[kExpandThreads], job.blocks);
+    const long long units = to > from ? static_cast<long long>(to - from) * kBlockTiles * pv.n_kv_heads : 0;
+    for (long long x = static_cast<long long>(blockIdx.x) * kExpandWarps + warp; x < units; x += static_cast<long long>(gridDim.x) * kExpandWarps) {
+      const int t = static_cast<int>(x / pv.n_kv_heads), h = static_cast<int>(x - static_cast<long long>(t) * pv.n_kv_heads);
+      const int block = from + t / kBlockTiles;
+      int i = 0, hi = kExpandThreads;              // the sequence: block_to[i] <= block < block_to[i + 1]
+      while (hi - i > 1) {
+        const int mid = (i + hi) >> 1;
+        if (block_to[mid] <= block) i = mid;
+        else hi = mid;
+      }
+      const int in_seq = block - block_to[i], j0 = (in_seq * kBlockTiles + t % kBlockTiles) * kTileTokens4;
+      if (block_to[i + 1] > job.blocks || !((in_seq + 1) * kBlock > lo_of[i] || in_seq * kBlock < pre_of[i])) continue;
+      const uint8_t* tile = nullptr;
+      if (j0 < len_of[i]) {
+        const int page = pv.table[static_cast<long long>(base + i) * pv.max_pages + (j0 >> pv.page_shift)];
+        if (page >= 0 && page < pv.n_pages) tile = tile4(pv, page, h, j0 & (pv.page_size - 1));
+        else if (lane == 0) paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, base + i, j0 >> pv.page_shift);
+      }
+      Raw4 raw[4];                                 // keys, values of tokens 0..7, of 8..15
+#pragma unroll
+      for (int k = 0; k < 4; ++k) raw[k].code = raw[k].s = raw[k].z = make_uint4(0, 0, 0, 0);
+      if (tile) {
+        load4<false>(raw[0], tile, r8, u);
+        load4<false>(raw[1], tile, r8 + 8, u);
+        load4<true>(raw[2], tile, r8, u);
+        load4<true>(raw[3], tile, r8 + 8, u);
+      }
+      const long long row0 = (static_cast<long long>(block) * pv.n_kv_heads + h) * kBlock + (j0 & (kBlock - 1));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int at = r8 + 8 * (k & 1), j = j0 + at;
+        const bool used = j < len_of[i] && (j >= lo_of[i] || j < pre_of[i]);
+        uint4* dst = reinterpret_cast<uint4*>((k < 2 ? job.k16 : job.v16) + (row0 + at) * kHeadDim) + u;
+        auto put = [&](int g, const uint4& unit) { dst[4 * g] = unit; };
+        if (k < 2) expand4<false>(raw[k], used, at, put);
+        else expand4<true>(raw[k], used, at, put);
+      }
+    }
+  }
+  // queries: unit i is channels 8 (i % 16) .. + 7 of row i / 16
+  for (long long i = static_cast<long long>(blockIdx.x) * kExpandThreads + tid; i < job.q_units; i += static_cast<long long>(gridDim.x) * kExpandThreads) {
+    const long long row = i >> 4, t = row / job.q.n_heads;
+    const int c = static_cast<int>(i & 15), h = static_cast<int>(row - t * job.q.n_heads);
+    const uint4 x = *reinterpret_cast<const uint4*>(job.q.data + t * job.q.token + h * job.q.head + 8 * c);
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t f[4];                                     // pairs (2 i, 2 i + 1)
+    uint32_t f[4];                                 // pairs (2 k, 2 k + 1)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float2 v = pair_to_float2<BF16>(w[k]);
       f[k] = BF16 ? float2_to_pair<false>(v.x, v.y) : w[k];
     }
-    reinterpret_cast<uint4*>(to)[i] = make_uint4(__byte_perm(f[0], f[2], 0x5410), __byte_perm(f[0], f[2], 0x7632), __byte_perm(f[1], f[3], 0x5410),
-                                                 __byte_perm(f[1], f[3], 0x7632));
+    reinterpret_cast<uint4*>(job.q16)[i] = make_uint4(__byte_perm(f[0], f[2], 0x5410), __byte_perm(f[0], f[2], 0x7632), __byte_perm(f[1], f[3], 0x5410),
+                                                      __byte_perm(f[1], f[3], 0x7632));
   }
+}
+
+// The workspace behind what the large tiles need: queries, a number per sequence, blocks.
+struct Layout {
+  long long queries, first, blocks;                // offsets
+  long long block_bytes;                           // of keys and values
+};
+Layout layout_of(const PagedView& pv, int group, int n_tokens) {
+  Layout l;
+  l.queries = tiles_workspace_bytes(pv, group, n_tokens);
+  l.first = l.queries + static_cast<long long>(n_tokens) * group * pv.n_kv_heads * kHeadDim * 2;
+  l.blocks = l.first + (4ll * pv.batch + 255) / 256 * 256;
+  l.block_bytes = 2ll * pv.n_kv_heads * kBlock * kHeadDim * 2;
+  return l;
 }
 
 }  // namespace
 
-// What the large tiles need, or the streaming kernel, and the queries.
+// What every call needs, and room for the blocks of the longest sequences that the tables allow, up to kExpandBytes.
+long long paged4_prefill_least_bytes(const PagedView& pv, int group, int n_tokens) {
+  const long long few = paged4_few_workspace_bytes(), tiles = layout_of(pv, group, n_tokens).blocks;
+  return tiles > few ? tiles : few;
+}
 long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens) {
-  const long long few = paged4_few_workspace_bytes(), cut = tiles_workspace_bytes(pv, group, n_tokens);
-  return (cut > few ? cut : few) + static_cast<long long>(n_tokens) * group * pv.n_kv_heads * kHeadDim * 2;
+  const Layout l = layout_of(pv, group, n_tokens);
+  const long long a_sequence = (static_cast<long long>(pv.max_pages) * pv.page_size + kBlock - 1) / kBlock, room = kExpandBytes / l.block_bytes;
+  const long long all = a_sequence * pv.batch;
+  return paged4_prefill_least_bytes(pv, group, n_tokens) + (all < room ? all : room) * l.block_bytes;
 }
 
 cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
-                                  const AttnOptions& opt, void* workspace, cudaStream_t st) {
+                                  const AttnOptions& opt, void* workspace, long long workspace_bytes, cudaStream_t st) {
   if (pv.batch <= 0 || n_tokens <= 0) return cudaSuccess;
   const int group = q.n_heads / pv.n_kv_heads;
   if (paged4_few_rows(pv, group, n_tokens)) return launch_paged4_few(pv, q, cu_q, n_tokens, out, opt, workspace, st);
+  const Layout l = layout_of(pv, group, n_tokens);
+  uint8_t* space = static_cast<uint8_t*>(workspace);
+  const long long room = (workspace_bytes - l.blocks) / l.block_bytes;
+  ExpandJob ex{};
+  ex.q = q;
+  ex.cu_q = cu_q;
+  ex.q16 = reinterpret_cast<uint16_t*>(space + l.queries);
+  ex.first = reinterpret_cast<int32_t*>(space + l.first);
+  ex.blocks = static_cast<int>(room < kMaxExpanded ? room : kMaxExpanded);
+  ex.k16 = reinterpret_cast<uint16_t*>(space + l.blocks);
+  ex.v16 = ex.k16 + static_cast<long long>(ex.blocks) * pv.n_kv_heads * kBlock * kHeadDim;
+  ex.q_units = static_cast<long long>(n_tokens) * q.n_heads * 16;
+  ex.n_tokens = n_tokens;
+
   RowsView q16{};
-  q16.data = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(workspace) + tiles_workspace_bytes(pv, group, n_tokens));
+  q16.data = ex.q16;
   q16.token = static_cast<long long>(q.n_heads) * kHeadDim;
   q16.head = kHeadDim;
   q16.n_heads = q.n_heads;
   PrefillJob job;
   long long grid;
   if (!make_job(job, grid, pv, q16, cu_q, n_tokens, out, workspace)) return cudaErrorInvalidConfiguration;
-  CUtensorMap mq;
-  if (!make_query_map(&mq, q16, n_tokens, group)) return cudaErrorNotSupported;
+  job.expanded = ex.first;
   job.q_box = kTileRows / group;
-  const long long units = static_cast<long long>(n_tokens) * q.n_heads * 16, ctas = (units + kQueryThreads - 1) / kQueryThreads, most = 16ll * sm_count_of_current_device();
-  const unsigned q_grid = static_cast<unsigned>(ctas < most ? ctas : most);
-  const cudaError_t e = launch_early(pv.dtype == MOQAE_DTYPE_BF16 ? query4_kernel<true> : query4_kernel<false>, q_grid, kQueryThreads, 0, st, q, q16.data, units);
-  return e != cudaSuccess ? e : launch_shaped<true>(pv, opt, job, mq, mq, mq, grid, st);
+  job.box_rows = 64;
+  job.dim_slot = 1;
+  job.dim_head = 2;
+  job.dim_page = 3;
+  PagedView blocks = pv;                           // the expanded blocks as pages of 128 tokens
+  blocks.page_size = kBlock;
+  blocks.n_pages = ex.blocks;
+  const long long stride[3] = {kHeadDim, kBlock * kHeadDim, static_cast<long long>(pv.n_kv_heads) * kBlock * kHeadDim};
+  const int order[3] = {0, 1, 2};
+  CUtensorMap mk, mv, mq;
+  const void* kb = ex.blocks > 0 ? ex.k16 : ex.q16;  // without room no block is ever named
+  const void* vb = ex.blocks > 0 ? ex.v16 : ex.q16;
+  if (!make_query_map(&mq, q16, n_tokens, group) || !make_page_map(&mk, kb, blocks, stride, order, job.box_rows) ||
+      !make_page_map(&mv, vb, blocks, stride, order, job.box_rows))
+    return cudaErrorNotSupported;
+  const unsigned expand_grid = 4u * sm_count_of_current_device();
+  const cudaError_t e = launch_early(pv.dtype == MOQAE_DTYPE_BF16 ? expand4_kernel<true> : expand4_kernel<false>, expand_grid, kExpandThreads, 0, st, pv, opt, ex);
+  return e != cudaSuccess ? e : launch_shaped<true>(pv, opt, job, mk, mv, mq, grid, st);
 }
 
 }  // namespace moqae

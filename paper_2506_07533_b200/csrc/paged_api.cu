@@ -397,7 +397,8 @@ int moqae_paged4_decode_attn(const moqae_paged4_cache* cache, const moqae_rows* 
   return cuda_rc(moqae::launch_paged4_decode(pv, qv, ov, opt, workspace, static_cast<cudaStream_t>(stream)));
 }
 
-int moqae_paged4_prefill_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int32_t n_tokens, int64_t* out_bytes) {
+int moqae_paged4_prefill_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int32_t n_tokens, int64_t* out_bytes,
+                                        int64_t* least_bytes) {
   PagedView pv;
   int rc = check_pages(cache, &pv);
   if (rc == MOQAE_OK) rc = check_group(pv, n_q_heads);
@@ -405,6 +406,7 @@ int moqae_paged4_prefill_attn_workspace(const moqae_paged4_cache* cache, int32_t
   if (!out_bytes || n_tokens < 0) return MOQAE_ERR_INVALID_ARG;
   if (n_tokens > moqae::kMaxQueryTokens || pv.batch > moqae::kMaxQueryTokens) return MOQAE_ERR_UNSUPPORTED;
   *out_bytes = moqae::paged4_prefill_workspace_bytes(pv, n_q_heads / pv.n_kv_heads, n_tokens);
+  if (least_bytes) *least_bytes = moqae::paged4_prefill_least_bytes(pv, n_q_heads / pv.n_kv_heads, n_tokens);
   return MOQAE_OK;
 }
 
@@ -421,8 +423,8 @@ int moqae_paged4_prefill_attn(const moqae_paged4_cache* cache, const moqae_rows*
   if ((pv.batch > 0 && !cu_q) || !workspace) return MOQAE_ERR_INVALID_ARG;
   if (!aligned(cu_q, 4) || !aligned(workspace, 16)) return MOQAE_ERR_MISALIGNED;
   const int group = qv.n_heads / pv.n_kv_heads;
-  if (workspace_bytes < moqae::paged4_prefill_workspace_bytes(pv, group, n_tokens)) return MOQAE_ERR_WORKSPACE_TOO_SMALL;
-  const cudaError_t e = moqae::launch_paged4_prefill(pv, qv, cu_q, n_tokens, ov, opt, workspace, static_cast<cudaStream_t>(stream));
+  if (workspace_bytes < moqae::paged4_prefill_least_bytes(pv, group, n_tokens)) return MOQAE_ERR_WORKSPACE_TOO_SMALL;
+  const cudaError_t e = moqae::launch_paged4_prefill(pv, qv, cu_q, n_tokens, ov, opt, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
   return e == cudaErrorNotSupported ? MOQAE_ERR_UNSUPPORTED : cuda_rc(e);
 }
 

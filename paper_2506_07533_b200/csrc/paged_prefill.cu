@@ -3,28 +3,6 @@
 
 namespace moqae {
 
-namespace {
-
-// (channel, slot, head, page) with the last three in the order of their strides; boxes of 64 channels x rows slots
-bool make_page_map(CUtensorMap* m, const void* base, const PagedView& pv, const long long stride[3], const int order[3], int rows) {
-  EncodeTiledFn enc = encode_tiled_fn();
-  if (!enc) return false;
-  const cuuint64_t size[3] = {static_cast<cuuint64_t>(pv.page_size), static_cast<cuuint64_t>(pv.n_kv_heads),
-                              static_cast<cuuint64_t>(pv.n_pages > 0 ? pv.n_pages : 1)};
-  cuuint64_t gdim[4] = {kHeadDim, 0, 0, 0}, gstride[3];
-  cuuint32_t box[4] = {64, 1, 1, 1};
-  const cuuint32_t estr[4] = {1, 1, 1, 1};
-  for (int d = 0; d < 3; ++d) {
-    gdim[d + 1] = size[order[d]];
-    gstride[d] = static_cast<cuuint64_t>(stride[order[d]]) * 2;
-    if (order[d] == 0) box[d + 1] = static_cast<cuuint32_t>(rows);
-  }
-  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-}  // namespace
-
 long long paged_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens) {
   const long long few = paged_few_workspace_bytes();
   if (static_cast<long long>(n_tokens) * group <= kFewRows && paged_few_rows(pv, group, n_tokens)) return few;    // few rows however many sequences

@@ -110,6 +110,7 @@ struct PrefillJob {
   int q_box;                                         // tokens per tile if the queries come by tiled copies, else 0
   int box_rows;                                      // slots per copy of a page
   int dim_slot, dim_head, dim_page;                  // tensor-map dimension (1..3) of each
+  const int32_t* expanded;                           // 4-bit pages: first expanded block of each sequence, -1: it has none
 };
 
 // A piece of work: rows row0 .. row0 + rows - 1 of (sequence b, head h), blocks [idx0, idx1) of their walk.
@@ -782,19 +783,20 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     return {m_ref, l, phase, ok ? 1 : 0};
 }
 
-// Four.  Over 4-bit pages the two fetching warps bring keys and values out of their codes: a lane takes 16 bytes of codes of a
-// token, 8 tokens x 4 units of the warp at a time, and stores four units of 8 channels, z + s code in fp16, into the swizzled operand (a
+// Four.  4-bit pages are expanded to fp16 blocks in the workspace by a pass in front (expand4_kernel in paged4_prefill.cu), as far as there is room, and
+// arrive like 16-bit pages of 128 tokens.  Sequences that do not fit are expanded here, by the two fetching warps: a lane takes 16
+// bytes of codes of a token, 8 tokens x 4 units of the warp at a time, and stores four units of 8 channels, z + s code in fp16, into the swizzled operand (a
 // quarter warp: 8 rows, one unit each, all banks).  A pair of codes costs a logic instruction (1024 + c, or 1024 + 16 c, as fp16 bits), one that takes the
-// 1024 away exactly, and a fused multiply-add, so an element is rounded once.  Four steps are under way to hide
-// the trip to L2; the lines of the next block are prefetched there.  All operands are fp16 whatever the dtype of the results: bf16 queries come
-// converted, and in the channels' order, from a pass in front (query4_kernel).
+// 1024 away exactly, and a fused multiply-add, so an element is rounded once, and alike on both ways.  Four steps are under way to hide
+// the trip to L2; the lines of the next block are prefetched there.  Expanding inside takes a block 8700 clocks instead of 3450 (512 tokens over 32100: 796
+// instead of 330 us): 1250 instructions of each of the two warps.  All operands are fp16 whatever the dtype of the
+// results: queries come converted, and in the channels' order, from the same pass.
 struct Raw4 {
   uint4 code, s, z;                                    // keys: scales and zeros in s alone
 };
 
-// One step: 8 tokens x 128 channels.  dst: the operand's row of this lane, unit offsets a0, a1 (see the caller).
-template <bool IS_V>
-__device__ __forceinline__ void expand4(const Raw4& x, bool used, int t, uint8_t* dst, int a0, int a1) {
+// A lane's part of one step of 8 tokens x 128 channels; put(g, unit): channels 32 g + 8 u .. + 7 (in column4's order) of its token.
+template <bool IS_V, typename F> __device__ __forceinline__ void expand4(const Raw4& x, bool used, int t, F put) {
   uint32_t s2[4], z2[4];                               // both halves alike
   if (IS_V) {
     const uint32_t pick = (t & 1) ? 0x3232u : 0x1010u, s[4] = {x.s.x, x.s.y, x.s.z, x.s.w}, z[4] = {x.z.x, x.z.y, x.z.z, x.z.w};
@@ -833,7 +835,19 @@ __device__ __forceinline__ void expand4(const Raw4& x, bool used, int t, uint8_t
       const __half2 v = __hfma2(c, *reinterpret_cast<const __half2*>(&s2[g]), *reinterpret_cast<const __half2*>(&z2[g]));
       r[k] = *reinterpret_cast<const uint32_t*>(&v);
     }
-    *reinterpret_cast<uint4*>(dst + (g >> 1) * (kTileBytes / 2) + ((g & 1) ? a1 : a0)) = make_uint4(r[0], r[1], r[2], r[3]);
+    put(g, make_uint4(r[0], r[1], r[2], r[3]));
+  }
+}
+
+// What a lane takes of its token t of a tile: unit u of the codes, scales and zeros.
+template <bool IS_V> __device__ __forceinline__ void load4(Raw4& x, const uint8_t* tile, int t, int u) {
+  if (IS_V) {
+    x.code = *reinterpret_cast<const uint4*>(tile + kValueCodes4 + 512 * (u >> 1) + 16 * (u & 1) + 32 * value_row4(t));
+    x.s = *reinterpret_cast<const uint4*>(tile + kValueMeta4 + 32 * (t >> 1));
+    x.z = *reinterpret_cast<const uint4*>(tile + kValueMeta4 + 32 * (t >> 1) + 16);
+  } else {
+    x.code = *reinterpret_cast<const uint4*>(tile + 64 * t + 16 * u);
+    x.s = *reinterpret_cast<const uint4*>(tile + kKeyMeta4 + 16 * t);
   }
 }
 
@@ -1038,100 +1052,6 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     }
     // the last CTA to find no more work leaves the counters at zero
     if (job.counters && lane == 0 && atomicInc(job.counters + 1, gridDim.x - 1) == gridDim.x - 1) atomicExch(job.counters, 0u);
-  } else if (Q4 && warp > kIssueWarp) {
-    // ================= expand: key blocks (one warp) and value blocks (another) =================
-    auto expand = [&](auto which) {
-      constexpr bool IS_V = decltype(which)::value;
-      constexpr int kDepth = 4, kSteps = kBlock / 8;     // steps under way; of a block
-      const int r8 = lane & 7, u = lane >> 3;
-      const int a0 = (u ^ r8) << 4, a1 = ((4 + u) ^ r8) << 4;
-      const int code_at = IS_V ? kValueCodes4 + 512 * (u >> 1) + 16 * (u & 1) : 16 * u;
-      int g = 0;                                          // blocks of all pieces
-      for (int k = 0;; ++k) {
-        if (!wait_all(BAR_IFULL + (k & 1), k >> 1, kPieceWaitLimit)) break;
-        const Piece& it = ctl.piece[k & 1];
-        if (it.rows == 0) break;
-        const int n_blocks = it.idx1 - it.idx0, idx1 = it.idx1;
-        const uint8_t* head = reinterpret_cast<const uint8_t*>(pv.k) + it.h * pv.k_head;
-        const int32_t* table = pv.table + static_cast<long long>(it.b) * pv.max_pages;
-        // lane l < 8: page of tile l of block n; -1: not needed, or there is none
-        auto pages_of = [&](int n) -> int {
-          if (n >= n_blocks || lane >= 8) return -1;
-          const int j = block_at(it, idx1 - 1 - n) * kBlock + kTileTokens4 * lane;
-          if (j >= it.kv_len || !(j + kTileTokens4 > it.win_lo || j < it.prefix)) return -1;
-          const int page = table[j >> pv.page_shift];
-          if (page >= 0 && page < pv.n_pages) {
-            const uint8_t* tile = head + page * pv.k_page + (j & (pv.page_size - 1)) * kTokenBytes4 + (IS_V ? kValueCodes4 : 0);
-#pragma unroll
-            for (int i = 0; i < 10; ++i) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(tile + 128 * i));
-            return page;
-          }
-          paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, it.b, j >> pv.page_shift);
-          return -1;
-        };
-        int page = pages_of(0), next = pages_of(1);
-        int load_n = 0, load_s = 0;                       // the step that is loaded next
-        int load_j = n_blocks > 0 ? block_at(it, idx1 - 1) * kBlock : 0;
-        Raw4 ring[kDepth];
-        auto load = [&](Raw4& x) {
-          const int p = __shfl_sync(0xffffffffu, page, load_s >> 1);
-          x.code = x.s = x.z = make_uint4(0, 0, 0, 0);
-          if (p >= 0) {
-            const int j = load_j + 8 * load_s + r8, t = j & (kTileTokens4 - 1);
-            const uint8_t* tile = head + p * pv.k_page + (((j & (pv.page_size - 1)) >> 4) * kTileBytes4);
-            x.code = *reinterpret_cast<const uint4*>(tile + code_at + (IS_V ? 32 * value_row4(t) : 64 * t));
-            if (IS_V) {
-              x.s = *reinterpret_cast<const uint4*>(tile + kValueMeta4 + 32 * (t >> 1));
-              x.z = *reinterpret_cast<const uint4*>(tile + kValueMeta4 + 32 * (t >> 1) + 16);
-            } else {
-              x.s = *reinterpret_cast<const uint4*>(tile + kKeyMeta4 + 16 * t);
-            }
-          }
-          if (++load_s == kSteps) {
-            load_s = 0;
-            page = next;
-            ++load_n;
-            if (load_n < n_blocks) load_j = block_at(it, idx1 - 1 - load_n) * kBlock;
-            next = pages_of(load_n + 1);
-          }
-        };
-#pragma unroll
-        for (int i = 0; i < kDepth; ++i) load(ring[i]);
-        bool ok = true;
-        for (int n = 0; n < n_blocks; ++n, ++g) {
-          const int st = g % kStages;
-          if (g >= kStages && !wait_all((IS_V ? BAR_VFREE : BAR_KFREE) + st, g / kStages - 1)) {
-            ok = false;
-            break;
-          }
-          const int j0 = block_at(it, idx1 - 1 - n) * kBlock;
-          const bool edge = j0 + kBlock > it.kv_len || (j0 < it.win_lo && j0 + kBlock > it.prefix);
-          uint8_t* dst = (IS_V ? sV : sK) + st * kTileBytes + r8 * 128;
-#pragma unroll 1
-          for (int s0 = 0; s0 < kSteps; s0 += kDepth) {
-#pragma unroll
-            for (int i = 0; i < kDepth; ++i) {
-              const int j = j0 + 8 * (s0 + i) + r8;
-              expand4<IS_V>(ring[i], !edge || token_used(it, j), j, dst + (s0 + i) * 1024, a0, a1);
-              load(ring[i]);
-            }
-          }
-          fence_async_proxy();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar((IS_V ? BAR_VFULL : BAR_KFULL) + st));
-        }
-        if (!ok) break;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(BAR_IFREE + (k & 1)));
-      }
-    };
-    if (warp == kValueWarp) expand(std::true_type{});
-    else expand(std::false_type{});
-    if (*abort_flag) {                                    // copies of queries under way still land in this CTA's memory: let them
-      const long long t0 = clock64();
-      while (clock64() - t0 < (1 << 17)) {
-      }
-    }
   } else if (warp > kIssueWarp) {
     // ================= fetch: key blocks (one warp) and value blocks (another) =================
     const bool is_v = warp == kValueWarp;
@@ -1139,16 +1059,15 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     const int boxes = kBlock / job.box_rows;
     int n_raw = 0, g = 0;                               // edge blocks, blocks of all pieces
     bool ok = true;
-    for (int k = 0;; ++k) {
-      if (!wait_all(BAR_IFULL + (k & 1), k >> 1, kPieceWaitLimit)) break;
-      const Piece it = ctl.piece[k & 1];
-      if (it.rows == 0) break;
+    // by tiled copies; of 4-bit pages: the sequence's blocks from `first16` on, which a pass in front has expanded
+    auto copy_blocks = [&](const Piece& it, int first16) {
       const int n_blocks = it.idx1 - it.idx0;
       auto box_token = [&](int n) { return block_at(it, it.idx1 - 1 - n) * kBlock + lane * job.box_rows; };
       auto look_up = [&](int n) -> int {                // page of this lane's box, -1: not needed
         if (n >= n_blocks || lane >= boxes) return -1;
         const int j = box_token(n);
         if (j >= it.kv_len || !(j + job.box_rows > it.win_lo || j < it.prefix)) return -1;
+        if (Q4) return first16 + j / kBlock;
         const int page = pv.table[static_cast<long long>(it.b) * pv.max_pages + (j >> pv.page_shift)];
         if (page >= 0 && page < pv.n_pages) return page;
         paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, it.b, j >> pv.page_shift);
@@ -1171,7 +1090,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
         __syncwarp();
         uint8_t* dst = (is_v ? sV : sK) + st * kTileBytes;
         if (page >= 0) {
-          const int slot = box_token(n) & (pv.page_size - 1);
+          const int slot = box_token(n) & (Q4 ? kBlock - 1 : pv.page_size - 1);
           const int y = job.dim_slot == 1 ? slot : (job.dim_head == 1 ? it.h : page);
           const int z = job.dim_slot == 2 ? slot : (job.dim_head == 2 ? it.h : page);
           const int w = job.dim_slot == 3 ? slot : (job.dim_head == 3 ? it.h : page);
@@ -1198,6 +1117,86 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
         }
         page = next;
       }
+    };
+    // out of their codes
+    auto expand_blocks = [&](auto which, const Piece& it) {
+      constexpr bool IS_V = decltype(which)::value;
+      constexpr int kDepth = 4, kSteps = kBlock / 8;     // steps under way; of a block
+      const int r8 = lane & 7, u = lane >> 3;
+      const int a0 = (u ^ r8) << 4, a1 = ((4 + u) ^ r8) << 4;
+      const int n_blocks = it.idx1 - it.idx0, idx1 = it.idx1;
+      const uint8_t* head = reinterpret_cast<const uint8_t*>(pv.k) + it.h * pv.k_head;
+      const int32_t* table = pv.table + static_cast<long long>(it.b) * pv.max_pages;
+      // lane l < 8: page of tile l of block n; -1: not needed, or there is none
+      auto pages_of = [&](int n) -> int {
+        if (n >= n_blocks || lane >= 8) return -1;
+        const int j = block_at(it, idx1 - 1 - n) * kBlock + kTileTokens4 * lane;
+        if (j >= it.kv_len || !(j + kTileTokens4 > it.win_lo || j < it.prefix)) return -1;
+        const int page = table[j >> pv.page_shift];
+        if (page >= 0 && page < pv.n_pages) {
+          const uint8_t* tile = head + page * pv.k_page + (j & (pv.page_size - 1)) * kTokenBytes4 + (IS_V ? kValueCodes4 : 0);
+#pragma unroll
+          for (int i = 0; i < 10; ++i) asm volatile("prefetch.global.L2 [%0];\n" ::"l"(tile + 128 * i));
+          return page;
+        }
+        paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, it.b, j >> pv.page_shift);
+        return -1;
+      };
+      int page = pages_of(0), next = pages_of(1);
+      int load_n = 0, load_s = 0;                       // the step that is loaded next
+      int load_j = n_blocks > 0 ? block_at(it, idx1 - 1) * kBlock : 0;
+      Raw4 ring[kDepth];
+      auto load = [&](Raw4& x) {
+        const int p = __shfl_sync(0xffffffffu, page, load_s >> 1);
+        x.code = x.s = x.z = make_uint4(0, 0, 0, 0);
+        if (p >= 0) {
+          const int j = load_j + 8 * load_s + r8, t = j & (kTileTokens4 - 1);
+          const uint8_t* tile = head + p * pv.k_page + (((j & (pv.page_size - 1)) >> 4) * kTileBytes4);
+          load4<IS_V>(x, tile, t, u);
+        }
+        if (++load_s == kSteps) {
+          load_s = 0;
+          page = next;
+          ++load_n;
+          if (load_n < n_blocks) load_j = block_at(it, idx1 - 1 - load_n) * kBlock;
+          next = pages_of(load_n + 1);
+        }
+      };
+#pragma unroll
+      for (int i = 0; i < kDepth; ++i) load(ring[i]);
+      for (int n = 0; n < n_blocks; ++n, ++g) {
+        const int st = g % kStages;
+        if (g >= kStages && !wait_all((IS_V ? BAR_VFREE : BAR_KFREE) + st, g / kStages - 1)) {
+          ok = false;
+          break;
+        }
+        const int j0 = block_at(it, idx1 - 1 - n) * kBlock;
+        const bool edge = j0 + kBlock > it.kv_len || (j0 < it.win_lo && j0 + kBlock > it.prefix);
+        uint8_t* dst = (IS_V ? sV : sK) + st * kTileBytes + r8 * 128;
+#pragma unroll 1
+        for (int s0 = 0; s0 < kSteps; s0 += kDepth) {
+#pragma unroll
+          for (int i = 0; i < kDepth; ++i) {
+            const int j = j0 + 8 * (s0 + i) + r8;
+            expand4<IS_V>(ring[i], !edge || token_used(it, j), j, [&](int c, const uint4& unit) {
+              *reinterpret_cast<uint4*>(dst + (s0 + i) * 1024 + (c >> 1) * (kTileBytes / 2) + ((c & 1) ? a1 : a0)) = unit;
+            });
+            load(ring[i]);
+          }
+        }
+        fence_async_proxy();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar((IS_V ? BAR_VFULL : BAR_KFULL) + st));
+      }
+    };
+    for (int k = 0;; ++k) {
+      if (!wait_all(BAR_IFULL + (k & 1), k >> 1, kPieceWaitLimit)) break;
+      const Piece it = ctl.piece[k & 1];
+      if (it.rows == 0) break;
+      const int first16 = Q4 ? job.expanded[it.b] : 0;
+      if (!Q4 || first16 >= 0) copy_blocks(it, first16);
+      else if (is_v) expand_blocks(std::true_type{}, it);
+      else expand_blocks(std::false_type{}, it);
       if (!ok) break;
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(BAR_IFREE + (k & 1)));
@@ -1285,6 +1284,24 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
   if (tid == 0 && *abort_flag) paged_status(pv.status, MOQAE_ERR_TIMEOUT, static_cast<int>(blockIdx.x), -1);   // whoever gave up
   if (warp == kIssueWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kTmemCols) : "memory");
+}
+
+// (channel, slot, head, page) with the last three in the order of their strides; boxes of 64 channels x rows slots
+bool make_page_map(CUtensorMap* m, const void* base, const PagedView& pv, const long long stride[3], const int order[3], int rows) {
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return false;
+  const cuuint64_t size[3] = {static_cast<cuuint64_t>(pv.page_size), static_cast<cuuint64_t>(pv.n_kv_heads),
+                              static_cast<cuuint64_t>(pv.n_pages > 0 ? pv.n_pages : 1)};
+  cuuint64_t gdim[4] = {kHeadDim, 0, 0, 0}, gstride[3];
+  cuuint32_t box[4] = {64, 1, 1, 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  for (int d = 0; d < 3; ++d) {
+    gdim[d + 1] = size[order[d]];
+    gstride[d] = static_cast<cuuint64_t>(stride[order[d]]) * 2;
+    if (order[d] == 0) box[d + 1] = static_cast<cuuint32_t>(rows);
+  }
+  return enc(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // Queries (channel, head, token); boxes of 64 channels x the group's heads x the tokens of a tile.  False where the strides

@@ -384,9 +384,15 @@ def test_prefill(dtype, case, shaping):
     q = randn(gen, n + 3, hq + 2, 128, dtype=dtype)[:, 1:hq + 1]
     out = torch.full((n + 3, hq, 128), 9.0, dtype=dtype, device="cuda")
     cu = torch.tensor([0] + new, dtype=torch.int32).cumsum(0).to(torch.int32).cuda()
-    work = space(mq.moqae_paged4_prefill_attn_workspace(cache, hq, n + 3))
+    size, least = (mq.moqae_paged4_prefill_attn_workspace(cache, hq, n + 3, least=x) for x in (False, True))
+    work = space(size)
     for _ in range(2):
         mq.moqae_paged4_prefill_attn(cache, q, cu, out, work, opt)
+    # without room for expanded blocks, and with room for some sequences, the same bits
+    for part in (least, least + (size - least) // 2):
+        small, again = space(part), torch.full_like(out, 9.0)
+        mq.moqae_paged4_prefill_attn(cache, q, cu, again, small, opt)
+        assert (again == out).all() and (small[:1 << 20] == 0).all(), part
     assert (out[n:] == 9).all()                           # rows behind the last sequence
     rest = {k: v for k, v in shaping.items() if k in ("scale", "cap", "window")}
     check(cache, q[:n], new, out[:n], slopes, prefix, **rest)

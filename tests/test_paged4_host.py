@@ -58,7 +58,7 @@ def test_bad_caches_are_refused_by_every_call(lib, change, code):
     assert lib.moqae_paged4_decode_attn(c, q, q, None, A, 1 << 40, None) == code
     assert lib.moqae_paged4_prefill_attn(c, q, A, 3, q, None, A, 1 << 40, None) == code
     assert lib.moqae_paged4_decode_attn_workspace(c, 8, C.byref(n)) == code
-    assert lib.moqae_paged4_prefill_attn_workspace(c, 8, 3, C.byref(n)) == code
+    assert lib.moqae_paged4_prefill_attn_workspace(c, 8, 3, C.byref(n), None) == code
 
 
 def test_missing_arguments(lib):
@@ -106,6 +106,27 @@ def test_batches_that_the_counters_cannot_hold(lib):
     n = C.c_int64(0)
     assert lib.moqae_paged4_decode_attn_workspace(C.byref(cache(batch=1 << 18)), 8, C.byref(n)) == mq.ERR_UNSUPPORTED
     assert lib.moqae_paged4_decode_attn_workspace(C.byref(cache(batch=100000, max_pages=60000)), 8, C.byref(n)) == mq.ERR_UNSUPPORTED
+
+
+def test_workspaces_serve_every_smaller_call(lib):
+    def sizes(batch, tokens, heads=8, **kw):
+        n, low = C.c_int64(0), C.c_int64(0)
+        assert lib.moqae_paged4_prefill_attn_workspace(C.byref(cache(batch=batch, **kw)), heads, tokens, C.byref(n), C.byref(low)) == 0
+        one = C.c_int64(0)
+        assert lib.moqae_paged4_decode_attn_workspace(C.byref(cache(batch=batch, **kw)), heads, C.byref(one)) == 0
+        assert (1 << 20) < one.value <= low.value <= n.value
+        return low.value, n.value
+    for kw in (dict(), dict(max_pages=8192), dict(n_kv_heads=1, page_stride=2560), dict(max_pages=0)):
+        shape = [(b, t) for b in (1, 2, 3, 40, 300) for t in (1, 2, 15, 64, 300, 5000, 40000)]
+        got = {s: sizes(*s, **kw) for s in shape}
+        for b, t in shape:
+            for c, u in shape:
+                if c >= b and u >= t:
+                    assert got[c, u][0] >= got[b, t][0] and got[c, u][1] >= got[b, t][1], (b, t, c, u)
+    assert sizes(1000, 8, max_pages=8192)[1] - sizes(1000, 8, max_pages=8192)[0] <= 1 << 30
+    n = C.c_int64(0)
+    assert lib.moqae_paged4_prefill_attn_workspace(C.byref(cache()), 8, 3, None, None) == mq.ERR_INVALID_ARG
+    assert lib.moqae_paged4_prefill_attn_workspace(C.byref(cache()), 8, -1, C.byref(n), None) == mq.ERR_INVALID_ARG
 
 
 def plan(lib, **kw):
