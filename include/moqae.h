@@ -595,11 +595,11 @@ typedef struct moqae_page_pool {
  *   cu_q          int32 [batch + 1]: the rows of sequence b are cu_q[b] .. cu_q[b + 1] - 1, max(n_new[b], 0) of them;
  *   positions, seq  int32 [n_rows]: position and sequence of every row, -1 behind the last (the padding of the other calls).
  *   past_len may be kv_len, and state (NULL: pool->state), the pool's state before the call, may be pool->state; the third word of
- *   pool->state must be 0.  Nothing else may overlap.  n_rows and batch at most 2^24.
+ *   pool->state must be 0.  Nothing else may overlap.  n_rows, batch and pool->n_pages at most 2^24.
  *   Found on the device and recorded in status (int32[4] or NULL), with tables and pool as they were, kv_len = past_len, cu_q zero and
- *   positions and seq -1: MOQAE_ERR_POOL_FULL, not enough free pages (details: pages wanted, pages free); MOQAE_ERR_CORRUPT_TABLE, a length below 0
+ *   positions and seq -1: MOQAE_ERR_POOL_FULL, not enough free pages (details: pages wanted, or more than there are; pages free); MOQAE_ERR_CORRUPT_TABLE, a length below 0
  *   or above max_pages * page_size before or after (details: sequence, -1), or a state that cannot be (-1, -1);
- *   MOQAE_ERR_INVALID_ARG, more tokens than n_rows (-1, tokens).  A page number outside 0 .. n_pages - 1 that is moved is recorded
+ *   MOQAE_ERR_INVALID_ARG, more tokens than n_rows (-1, tokens, or more than n_rows).  A page number outside 0 .. n_pages - 1 that is moved is recorded
  *   as MOQAE_ERR_CORRUPT_TABLE (sequence, entry) and moved all the same: no call follows it.
  */
 int moqae_paged_plan(const int32_t* past_len, const int32_t* n_new, int32_t batch, int32_t page_size, int32_t max_pages,

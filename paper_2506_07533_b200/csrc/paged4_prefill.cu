@@ -1,5 +1,5 @@
 // moqae_paged4_prefill_attn: launches over 4-bit pages.  Few rows per sequence go to the streaming kernel (paged4_decode.cu), the others to the
-// large tiles (paged_prefill.cuh), behind a pass that brings queries into fp16 and keys and values out of their codes.
+// large tiles (paged_prefill.cuh), behind a pass that brings keys and values out of their codes and bf16 queries into fp16.
 //   Expanding once costs 672 bytes per token and kv head and one reading of 512; inside the large tiles every row tile would
 //   expand the blocks that it sees again (see Four there).  The workspace holds kExpandBytes of expanded blocks at most, sequences beyond that are
 //   expanded inside.
@@ -17,11 +17,10 @@ constexpr int kBlockTiles = kBlock / kTileTokens4;
 struct ExpandJob {
   RowsView q;
   const int32_t* cu_q;
-  uint16_t* q16;                                   // [n_tokens][heads][128], channels in column4's order
-  uint16_t* k16;                                   // [blocks][kv heads][128 tokens][128], channels in column4's order
+  uint16_t* q16;                                   // [n_tokens][heads][128]; null: the queries are fp16
+  uint16_t* k16;                                   // [blocks][kv heads][128 tokens][128]
   uint16_t* v16;
   int32_t* first;                                  // [batch]: a sequence's first block, -1: not expanded
-  long long q_units;                               // of 8 channels
   int n_tokens, blocks;                            // rows of q; room for blocks
 };
 
@@ -68,9 +67,10 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
     if (blockIdx.x == 0 && b < pv.batch) job.first[b] = need > 0 && in_front + sum <= job.blocks ? in_front + sum - need : -1;
     __syncthreads();
     const int from = block_to[0], to = min(block_to[kExpandThreads], job.blocks);
-    const long long units = to > from ? static_cast<long long>(to - from) * kBlockTiles * pv.n_kv_heads : 0;
-    for (long long x = static_cast<long long>(blockIdx.x) * kExpandWarps + warp; x < units; x += static_cast<long long>(gridDim.x) * kExpandWarps) {
-      const int t = static_cast<int>(x / pv.n_kv_heads), h = static_cast<int>(x - static_cast<long long>(t) * pv.n_kv_heads);
+    const int tiles = max(to - from, 0) * kBlockTiles, n_warps = static_cast<int>(gridDim.x) * kExpandWarps;
+    const int step_t = n_warps / pv.n_kv_heads, step_h = n_warps - step_t * pv.n_kv_heads, id = static_cast<int>(blockIdx.x) * kExpandWarps + warp;
+    int h = id % pv.n_kv_heads;
+    for (int t = id / pv.n_kv_heads; t < tiles; t += step_t + (h + step_h >= pv.n_kv_heads), h = h + step_h >= pv.n_kv_heads ? h + step_h - pv.n_kv_heads : h + step_h) {
       const int block = from + t / kBlockTiles;
       int i = 0, hi = kExpandThreads;              // the sequence: block_to[i] <= block < block_to[i + 1]
       while (hi - i > 1) {
@@ -107,20 +107,27 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
       }
     }
   }
-  // queries: unit i is channels 8 (i % 16) .. + 7 of row i / 16
-  for (long long i = static_cast<long long>(blockIdx.x) * kExpandThreads + tid; i < job.q_units; i += static_cast<long long>(gridDim.x) * kExpandThreads) {
-    const long long row = i >> 4, t = row / job.q.n_heads;
-    const int c = static_cast<int>(i & 15), h = static_cast<int>(row - t * job.q.n_heads);
+  if (!BF16) return;
+  // queries: half a warp takes a row
+  const int n_rows = static_cast<int>(gridDim.x) * (kExpandThreads / 16), id = static_cast<int>(blockIdx.x) * (kExpandThreads / 16) + (tid >> 4), c = tid & 15;
+  const int step_t = n_rows / job.q.n_heads, step_h = n_rows - step_t * job.q.n_heads;
+  int h = id % job.q.n_heads;
+  for (int t = id / job.q.n_heads; t < job.n_tokens;) {
     const uint4 x = *reinterpret_cast<const uint4*>(job.q.data + t * job.q.token + h * job.q.head + 8 * c);
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t f[4];                                 // pairs (2 k, 2 k + 1)
+    uint32_t f[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float2 v = pair_to_float2<BF16>(w[k]);
-      f[k] = BF16 ? float2_to_pair<false>(v.x, v.y) : w[k];
+      f[k] = float2_to_pair<false>(v.x, v.y);
     }
-    reinterpret_cast<uint4*>(job.q16)[i] = make_uint4(__byte_perm(f[0], f[2], 0x5410), __byte_perm(f[0], f[2], 0x7632), __byte_perm(f[1], f[3], 0x5410),
-                                                      __byte_perm(f[1], f[3], 0x7632));
+    *reinterpret_cast<uint4*>(job.q16 + (static_cast<long long>(t) * job.q.n_heads + h) * kHeadDim + 8 * c) = make_uint4(f[0], f[1], f[2], f[3]);
+    t += step_t;
+    h += step_h;
+    if (h >= job.q.n_heads) {
+      h -= job.q.n_heads;
+      ++t;
+    }
   }
 }
 
@@ -132,7 +139,7 @@ struct Layout {
 Layout layout_of(const PagedView& pv, int group, int n_tokens) {
   Layout l;
   l.queries = tiles_workspace_bytes(pv, group, n_tokens);
-  l.first = l.queries + static_cast<long long>(n_tokens) * group * pv.n_kv_heads * kHeadDim * 2;
+  l.first = l.queries + (pv.dtype == MOQAE_DTYPE_BF16 ? static_cast<long long>(n_tokens) * group * pv.n_kv_heads * kHeadDim * 2 : 0);
   l.blocks = l.first + (4ll * pv.batch + 255) / 256 * 256;
   l.block_bytes = 2ll * pv.n_kv_heads * kBlock * kHeadDim * 2;
   return l;
@@ -168,19 +175,19 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   ex.blocks = static_cast<int>(room < kMaxExpanded ? room : kMaxExpanded);
   ex.k16 = reinterpret_cast<uint16_t*>(space + l.blocks);
   ex.v16 = ex.k16 + static_cast<long long>(ex.blocks) * pv.n_kv_heads * kBlock * kHeadDim;
-  ex.q_units = static_cast<long long>(n_tokens) * q.n_heads * 16;
   ex.n_tokens = n_tokens;
 
-  RowsView q16{};
-  q16.data = ex.q16;
-  q16.token = static_cast<long long>(q.n_heads) * kHeadDim;
-  q16.head = kHeadDim;
-  q16.n_heads = q.n_heads;
+  const bool bf16 = pv.dtype == MOQAE_DTYPE_BF16;
+  RowsView q16 = q;
+  if (bf16) {
+    q16.data = ex.q16;
+    q16.token = static_cast<long long>(q.n_heads) * kHeadDim;
+    q16.head = kHeadDim;
+  }
   PrefillJob job;
   long long grid;
   if (!make_job(job, grid, pv, q16, cu_q, n_tokens, out, workspace)) return cudaErrorInvalidConfiguration;
   job.expanded = ex.first;
-  job.q_box = kTileRows / group;
   job.box_rows = 64;
   job.dim_slot = 1;
   job.dim_head = 2;
@@ -191,13 +198,13 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   const long long stride[3] = {kHeadDim, kBlock * kHeadDim, static_cast<long long>(pv.n_kv_heads) * kBlock * kHeadDim};
   const int order[3] = {0, 1, 2};
   CUtensorMap mk, mv, mq;
-  const void* kb = ex.blocks > 0 ? ex.k16 : ex.q16;  // without room no block is ever named
-  const void* vb = ex.blocks > 0 ? ex.v16 : ex.q16;
-  if (!make_query_map(&mq, q16, n_tokens, group) || !make_page_map(&mk, kb, blocks, stride, order, job.box_rows) ||
-      !make_page_map(&mv, vb, blocks, stride, order, job.box_rows))
-    return cudaErrorNotSupported;
+  const void* kb = ex.blocks > 0 ? ex.k16 : workspace;   // without room no block is ever named
+  const void* vb = ex.blocks > 0 ? ex.v16 : workspace;
+  if (!make_page_map(&mk, kb, blocks, stride, order, job.box_rows) || !make_page_map(&mv, vb, blocks, stride, order, job.box_rows)) return cudaErrorNotSupported;
+  if (make_query_map(&mq, q16, n_tokens, group)) job.q_box = kTileRows / group;
+  else mq = mk;
   const unsigned expand_grid = 4u * sm_count_of_current_device();
-  const cudaError_t e = launch_early(pv.dtype == MOQAE_DTYPE_BF16 ? expand4_kernel<true> : expand4_kernel<false>, expand_grid, kExpandThreads, 0, st, pv, opt, ex);
+  const cudaError_t e = launch_early(bf16 ? expand4_kernel<true> : expand4_kernel<false>, expand_grid, kExpandThreads, 0, st, pv, opt, ex);
   return e != cudaSuccess ? e : launch_shaped<true>(pv, opt, job, mk, mv, mq, grid, st);
 }
 

@@ -340,7 +340,7 @@ int moqae_paged_plan(const int32_t* past_len, const int32_t* n_new, int32_t batc
   int shift = 4;
   while (shift < 8 && (1 << shift) != page_size) ++shift;
   if ((1 << shift) != page_size || static_cast<int64_t>(max_pages) * page_size > (1ll << 30)) return MOQAE_ERR_UNSUPPORTED;
-  if (n_rows > moqae::kMaxQueryTokens || batch > moqae::kMaxQueryTokens || pool->n_pages > (1 << 30)) return MOQAE_ERR_UNSUPPORTED;
+  if (n_rows > moqae::kMaxQueryTokens || batch > moqae::kMaxQueryTokens || pool->n_pages > moqae::kMaxQueryTokens) return MOQAE_ERR_UNSUPPORTED;
   if (!pool->state || (pool->n_pages > 0 && !pool->ring) || !cu_q || (n_rows > 0 && (!positions || !seq))) return MOQAE_ERR_INVALID_ARG;
   if (batch > 0 && (!past_len || !n_new || !kv_len || (max_pages > 0 && !block_table))) return MOQAE_ERR_INVALID_ARG;
   if (!aligned(past_len, 4) || !aligned(n_new, 4) || !aligned(block_table, 4) || !aligned(kv_len, 4) || !aligned(pool->ring, 4) ||

@@ -51,12 +51,20 @@ template <bool BF16> __device__ __forceinline__ uint4 pack8(const float (&x)[8])
                     float2_to_pair<BF16>(x[6], x[7]));
 }
 
-// Eight codes, the first in the lowest bits.
+// (x - zero) * inv as codes behind the bits of kMagic, two at a time: one packed addition, one packed fused multiply-add.
+__device__ __forceinline__ void encode_two(float x0, float x1, uint64_t negz2, uint64_t inv2, uint32_t& u0, uint32_t& u1) {
+  uint64_t d2, r2;
+  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(d2) : "l"(pack_f2(x0, x1)), "l"(negz2));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(r2) : "l"(d2), "l"(inv2), "l"(pack_f2(kMagic, kMagic)));
+  asm("mov.b64 {%0, %1}, %2;\n" : "=r"(u0), "=r"(u1) : "l"(r2));
+}
+// Eight codes, the first in the lowest bits.  (What stands above a code's four bits is a multiple of 2^22: it leaves the low 16.)
 __device__ __forceinline__ uint32_t codes8(const float (&x)[8], float zero, float inv) {
+  const uint64_t negz2 = pack_f2(-zero, -zero), inv2 = pack_f2(inv, inv);
   uint32_t u[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(__fmaf_rn(__fsub_rn(x[i], zero), inv, kMagic)) & 15u;
-  return pack4<4>(u[0], u[1], u[2], u[3]) | (pack4<4>(u[4], u[5], u[6], u[7]) << 16);
+  for (int i = 0; i < 8; i += 2) encode_two(x[i], x[i + 1], negz2, inv2, u[i], u[i + 1]);
+  return __byte_perm(pack4<4>(u[0], u[1], u[2], u[3]), pack4<4>(u[4], u[5], u[6], u[7]), 0x5410);
 }
 
 // A key row of a 4-bit page: units u0 and u1 (8 channels each, float32) of lane `sub` of the row's eight lanes (`mask`).  `at`: the
@@ -116,17 +124,17 @@ template <bool BF16> __device__ __forceinline__ void put_value4(uint8_t* tile, i
     uint32_t u[4];
     encode2<BF16>(w[g].x, pack_f2(-z, -z), pack_f2(r, r), u[0], u[1]);
     encode2<BF16>(w[g].y, pack_f2(-z, -z), pack_f2(r, r), u[2], u[3]);
-    half[g] = pack4<4>(u[0] & 15u, u[1] & 15u, u[2] & 15u, u[3] & 15u);
+    half[g] = pack4<4>(u[0], u[1], u[2], u[3]);
   }
   *reinterpret_cast<uint2*>(tile + kValueCodes4 + 512 * (sub >> 2) + 32 * value_row4(t) + 8 * (sub & 3)) =
-      make_uint2(half[0] | (half[1] << 16), half[2] | (half[3] << 16));
+      make_uint2(__byte_perm(half[0], half[1], 0x5410), __byte_perm(half[2], half[3], 0x5410));
 }
 
 // Where the rows go: to rows, to 16-bit pages, to 4-bit pages.
 enum { kToRows, kToPages, kToPages4 };
 
 template <bool BF16, int DEST>
-__global__ void __launch_bounds__(kAppendWarps * 32) norm_rope_kernel(PagedView pv, RopeView rope, RowJob job) {
+__global__ void __launch_bounds__(kAppendWarps * 32, DEST == kToPages4 ? 6 : 1) norm_rope_kernel(PagedView pv, RopeView rope, RowJob job) {
   constexpr bool PAGED = DEST != kToRows, FOUR = DEST == kToPages4;
   __shared__ __align__(16) float2 exchange[FOUR ? kAppendWarps * kRowsPerPass * 20 : 1];        // units' extremes, groups' parameters of a key row
   after_previous();

@@ -3,7 +3,7 @@
 // Mathematics: three running sums over the sequences (new tokens, pages taken, pages given back), then every row of the
 // step finds its sequence by bisection in the first, every page its sequence and entry in the others.  A few
 // kilobytes at most are moved, so the call is bound by its launch and the trips to memory that depend on each other:
-// lengths, sums, look-up, store.  One launch therefore: all CTAs form the sums of the whole batch, 256 sequences at a time
+// lengths, sums, store (the first free pages travel beside the lengths).  One launch therefore: all CTAs form the sums of the whole batch, 256 sequences at a time
 // (nothing to wait for but the lengths), and share out rows and pages; what may be read and written in place (lengths, the pool's
 // state) is written by the CTA that comes last, when all have read it.  A batch that is refused is found in a first pass
 // over the lengths, before anything is written.
@@ -15,6 +15,7 @@ namespace {
 
 constexpr int kPlanThreads = 256, kPlanWarps = kPlanThreads / 32;
 constexpr int kRowsPerCta = 2048;                // rows that a CTA is worth starting for
+constexpr int kBatch = 4;
 
 struct Sums {
   int tokens, take, give;
@@ -22,14 +23,19 @@ struct Sums {
 
 // What sequence b brings: its length before and after, and pages.
 struct Change {
-  int past, total, grow, have, want;             // have, want: pages before and after
+  int given, past, total, grow, have, want;      // given: past_len as it is; have, want: pages before and after
   bool good;
 };
+// (What a batch that is refused asks for is cut off just above what could be granted, so that a warp's sums stay in 32 bits.)
+__device__ __forceinline__ Sums sums_of(const Change& c, const PlanJob& job, const PoolView& pool) {
+  return Sums{min(c.grow, job.n_rows + 1), min(max(c.want - c.have, 0), pool.n_pages + 1), min(max(c.have - c.want, 0), pool.n_pages + 1)};
+}
 __device__ __forceinline__ Change change_of(const PlanJob& job, int b) {
-  Change c{0, 0, 0, 0, 0, true};
+  Change c{0, 0, 0, 0, 0, 0, true};
   if (b >= job.batch) return c;
   const long long most = static_cast<long long>(job.max_pages) << job.page_shift;
   const long long past = job.past[b], total = max(past + job.n_new[b], 0ll);
+  c.given = job.past[b];
   c.good = past >= 0 && past <= most && total <= most;
   if (!c.good) return c;
   const int page = 1 << job.page_shift;
@@ -39,6 +45,16 @@ __device__ __forceinline__ Change change_of(const PlanJob& job, int b) {
   c.have = (c.past + page - 1) >> job.page_shift;
   c.want = (c.total + page - 1) >> job.page_shift;
   return c;
+}
+
+// Sums over the lanes up to this one.
+__device__ __forceinline__ Sums scan(Sums s, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int x = __shfl_up_sync(0xffffffffu, s.tokens, o), y = __shfl_up_sync(0xffffffffu, s.take, o), z = __shfl_up_sync(0xffffffffu, s.give, o);
+    if (lane >= o) s = Sums{s.tokens + x, s.take + y, s.give + z};
+  }
+  return s;
 }
 
 // largest i with sums[i] <= x (sums not decreasing, sums[0] <= x < sums[n])
@@ -65,36 +81,61 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(PlanJob job, P
   Change mine = change_of(job, tid);
   __syncthreads();
 
-  // ---- does it all fit? ----
-  long long tokens = 0, take = 0, give = 0;
-  for (int b = tid; b < job.batch; b += kPlanThreads) {
-    const Change c = b == tid ? mine : change_of(job, b);
-    if (!c.good) atomicMin(&bad_seq, b);
-    tokens += c.grow;
-    take += max(c.want - c.have, 0);
-    give += max(c.have - c.want, 0);
+  // ---- does it all fit? (the sums of up to 256 sequences, which one turn holds, come out of the turn) ----
+  Sums own = sums_of(mine, job, pool), to_here = scan(own, lane);
+  if (!mine.good) atomicMin(&bad_seq, tid);
+  if (lane == 31) {
+    warp_sum[0][warp] = to_here.tokens;
+    warp_sum[1][warp] = to_here.take;
+    warp_sum[2][warp] = to_here.give;
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    tokens += __shfl_xor_sync(0xffffffffu, tokens, o);
-    take += __shfl_xor_sync(0xffffffffu, take, o);
-    give += __shfl_xor_sync(0xffffffffu, give, o);
-  }
-  if (lane == 0) {
-    all_tokens[warp] = tokens;
-    all_take[warp] = take;
-    all_give[warp] = give;
-  }
+  // the page that this thread takes first, if it takes any, travels meanwhile
+  const int first = static_cast<int>(blockIdx.x) * kPlanThreads + tid, step = static_cast<int>(gridDim.x) * kPlanThreads;
+  auto place = [&](int n) -> int {               // n < 2 n_pages behind the first free page
+    const long long at = static_cast<long long>(head) + n;
+    return static_cast<int>(at >= pool.n_pages ? at - pool.n_pages : at);
+  };
+  const bool sound = head >= 0 && head < max(pool.n_pages, 1) && n_free >= 0 && n_free <= pool.n_pages;
+  const int ahead = sound && first < n_free ? pool.ring[place(first)] : -1;
   __syncthreads();
-  tokens = take = give = 0;
+  long long tokens = 0, take = 0, give = 0;
 #pragma unroll
   for (int w = 0; w < kPlanWarps; ++w) {
-    tokens += all_tokens[w];
-    take += all_take[w];
-    give += all_give[w];
+    tokens += warp_sum[0][w];
+    take += warp_sum[1][w];
+    give += warp_sum[2][w];
+  }
+  if (job.batch > kPlanThreads) {
+    long long more_tokens = 0, more_take = 0, more_give = 0;
+    for (int b = tid + kPlanThreads; b < job.batch; b += kPlanThreads) {
+      const Change c = change_of(job, b);
+      if (!c.good) atomicMin(&bad_seq, b);
+      const Sums s = sums_of(c, job, pool);
+      more_tokens += s.tokens;
+      more_take += s.take;
+      more_give += s.give;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      more_tokens += __shfl_xor_sync(0xffffffffu, more_tokens, o);
+      more_take += __shfl_xor_sync(0xffffffffu, more_take, o);
+      more_give += __shfl_xor_sync(0xffffffffu, more_give, o);
+    }
+    if (lane == 0) {
+      all_tokens[warp] = more_tokens;
+      all_take[warp] = more_take;
+      all_give[warp] = more_give;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kPlanWarps; ++w) {
+      tokens += all_tokens[w];
+      take += all_take[w];
+      give += all_give[w];
+    }
   }
   int code = MOQAE_OK, d0 = -1, d1 = -1;
-  if (head < 0 || head >= max(pool.n_pages, 1) || n_free < 0 || n_free > pool.n_pages || give > pool.n_pages - n_free) {
+  if (!sound || give > pool.n_pages - n_free) {
     code = MOQAE_ERR_CORRUPT_TABLE;
   } else if (bad_seq != 0x7fffffff) {
     code = MOQAE_ERR_CORRUPT_TABLE;
@@ -108,7 +149,6 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(PlanJob job, P
     d1 = n_free;
   }
   const bool go = code == MOQAE_OK;
-  const int first = static_cast<int>(blockIdx.x) * kPlanThreads + tid, step = static_cast<int>(gridDim.x) * kPlanThreads;
   if (blockIdx.x == 0 && tid == 0) {
     if (!go) paged_status(job.status, code, d0, d1);
     job.cu_q[0] = 0;
@@ -118,26 +158,19 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(PlanJob job, P
   Sums before{0, 0, 0};
   for (int base = 0; base < job.batch; base += kPlanThreads) {
     const int b = base + tid;
-    const Change c = base == 0 ? mine : change_of(job, b);
-    Sums s{c.grow, max(c.want - c.have, 0), max(c.have - c.want, 0)};
-    if (!go) s = Sums{0, 0, 0};
-    const Sums own = s;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, s.tokens, o), y = __shfl_up_sync(0xffffffffu, s.take, o), z = __shfl_up_sync(0xffffffffu, s.give, o);
-      if (lane >= o) {
-        s.tokens += x;
-        s.take += y;
-        s.give += z;
+    Change c = mine;
+    if (base > 0) {
+      c = change_of(job, b);
+      own = sums_of(c, job, pool);
+      to_here = scan(own, lane);
+      __syncthreads();                           // the turn before is done with the arrays
+      if (lane == 31) {
+        warp_sum[0][warp] = to_here.tokens;
+        warp_sum[1][warp] = to_here.take;
+        warp_sum[2][warp] = to_here.give;
       }
+      __syncthreads();
     }
-    __syncthreads();                             // the turn before is done with the arrays
-    if (lane == 31) {
-      warp_sum[0][warp] = s.tokens;
-      warp_sum[1][warp] = s.take;
-      warp_sum[2][warp] = s.give;
-    }
-    __syncthreads();
     Sums in_front = before;
 #pragma unroll
     for (int w = 0; w < kPlanWarps; ++w) {
@@ -145,9 +178,9 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(PlanJob job, P
       if (w < warp) in_front = Sums{in_front.tokens + v.tokens, in_front.take + v.take, in_front.give + v.give};
       before = Sums{before.tokens + v.tokens, before.take + v.take, before.give + v.give};
     }
-    tokens_to[tid] = in_front.tokens + s.tokens - own.tokens;
-    take_to[tid] = in_front.take + s.take - own.take;
-    give_to[tid] = in_front.give + s.give - own.give;
+    tokens_to[tid] = in_front.tokens + to_here.tokens - own.tokens;
+    take_to[tid] = in_front.take + to_here.take - own.take;
+    give_to[tid] = in_front.give + to_here.give - own.give;
     past_of[tid] = c.past;
     have_of[tid] = c.have;
     want_of[tid] = c.want;
@@ -156,27 +189,48 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(PlanJob job, P
       take_to[kPlanThreads] = before.take;
       give_to[kPlanThreads] = before.give;
     }
-    if (blockIdx.x == 0 && b < job.batch) job.cu_q[b + 1] = in_front.tokens + s.tokens;
+    if (blockIdx.x == 0 && b < job.batch) job.cu_q[b + 1] = go ? in_front.tokens + to_here.tokens : 0;
     __syncthreads();
+    if (!go) continue;
     for (int r = tokens_to[0] + first; r < tokens_to[kPlanThreads]; r += step) {
       const int i = find_in(tokens_to, kPlanThreads, r);
       job.positions[r] = past_of[i] + r - tokens_to[i];
       job.seq[r] = base + i;
     }
-    auto place = [&](int n) -> int {             // n < 2 n_pages behind the first free page
-      const long long at = static_cast<long long>(head) + n;
-      return static_cast<int>(at >= pool.n_pages ? at - pool.n_pages : at);
-    };
-    for (int k = take_to[0] + first; k < take_to[kPlanThreads]; k += step) {
-      const int i = find_in(take_to, kPlanThreads, k), entry = have_of[i] + k - take_to[i], page = pool.ring[place(k)];
-      if (page < 0 || page >= pool.n_pages) paged_status(job.status, MOQAE_ERR_CORRUPT_TABLE, base + i, entry);
-      job.table[static_cast<long long>(base + i) * job.max_pages + entry] = page;
+    // pages: kBatch at a time, so that their trips overlap
+    for (int k0 = take_to[0] + first; k0 < take_to[kPlanThreads]; k0 += kBatch * step) {
+      int page[kBatch];
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        const int k = k0 + e * step;
+        page[e] = k == first ? ahead : k < take_to[kPlanThreads] ? pool.ring[place(k)] : 0;
+      }
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        const int k = k0 + e * step;
+        if (k >= take_to[kPlanThreads]) break;
+        const int i = find_in(take_to, kPlanThreads, k), entry = have_of[i] + k - take_to[i];
+        if (page[e] < 0 || page[e] >= pool.n_pages) paged_status(job.status, MOQAE_ERR_CORRUPT_TABLE, base + i, entry);
+        job.table[static_cast<long long>(base + i) * job.max_pages + entry] = page[e];
+      }
     }
-    for (int k = give_to[0] + first; k < give_to[kPlanThreads]; k += step) {
-      const int i = find_in(give_to, kPlanThreads, k), entry = want_of[i] + k - give_to[i];
-      const int page = job.table[static_cast<long long>(base + i) * job.max_pages + entry];
-      if (page < 0 || page >= pool.n_pages) paged_status(job.status, MOQAE_ERR_CORRUPT_TABLE, base + i, entry);
-      pool.ring[place(n_free + k)] = page;       // behind the free ones: never one that this call takes
+    for (int k0 = give_to[0] + first; k0 < give_to[kPlanThreads]; k0 += kBatch * step) {
+      int page[kBatch];
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        const int k = min(k0 + e * step, give_to[kPlanThreads] - 1), i = find_in(give_to, kPlanThreads, k);
+        page[e] = job.table[static_cast<long long>(base + i) * job.max_pages + want_of[i] + k - give_to[i]];
+      }
+#pragma unroll
+      for (int e = 0; e < kBatch; ++e) {
+        const int k = k0 + e * step;
+        if (k >= give_to[kPlanThreads]) break;
+        if (page[e] < 0 || page[e] >= pool.n_pages) {
+          const int i = find_in(give_to, kPlanThreads, k);
+          paged_status(job.status, MOQAE_ERR_CORRUPT_TABLE, base + i, want_of[i] + k - give_to[i]);
+        }
+        pool.ring[place(n_free + k)] = page[e];  // behind the free ones: never one that this call takes
+      }
     }
   }
   for (int r = (go ? static_cast<int>(tokens) : 0) + first; r < job.n_rows; r += step) job.positions[r] = job.seq[r] = -1;
@@ -191,7 +245,8 @@ __global__ void __launch_bounds__(kPlanThreads) paged_plan_kernel(PlanJob job, P
     __syncthreads();
     if (!last) return;
   }
-  for (int b = tid; b < job.batch; b += kPlanThreads) {
+  if (tid < job.batch) job.kv_len[tid] = go ? mine.total : mine.given;
+  for (int b = tid + kPlanThreads; b < job.batch; b += kPlanThreads) {
     const int past = job.past[b];
     job.kv_len[b] = go ? max(past + job.n_new[b], 0) : past;
   }

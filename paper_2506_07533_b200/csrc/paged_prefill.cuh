@@ -384,14 +384,10 @@ __device__ __forceinline__ bool find_piece(const PagedView& pv, const AttnOption
   return true;
 }
 
-// 4-bit pages: eight neighbouring channels stand in the operands in the order 0, 4, 1, 5, 2, 6, 3, 7 (a logic instruction brings codes
-// out of a word in pairs (i, i + 4)): column of channel c.
-__host__ __device__ constexpr int column4(int c) { return (c & ~7) | (2 * (c & 3)) | ((c >> 2) & 1); }
-
 // A softmax warp's 32 rows x 64 columns of O on their way out: results, or the float32 sums of a piece.  They leave through
 // shared memory, 64 bytes of a row at a time, so that a store covers whole sectors of eight rows (a thread storing
 // its own row took 32 half-sectors per instruction, 3 us for the 64 KiB of a CTA).
-template <bool BF16, bool Q4>
+template <bool BF16>
 __device__ __forceinline__ void store_rows(const PrefillJob& job, const Piece& it, uint32_t o_addr, bool has_sums, bool nothing, float inv,
                                         uint8_t* rows_at, int w_row, int half, int lane, float* piece) {
 #pragma unroll 1
@@ -411,18 +407,17 @@ __device__ __forceinline__ void store_rows(const PrefillJob& job, const Piece& i
 #pragma unroll
     for (int part16 = 0; part16 < 2; ++part16) {
       if (part16 >= parts) break;
-      auto ch = [&](int c) -> float { return v[Q4 ? column4(c) : c]; };
       if (parts == 1) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *reinterpret_cast<uint4*>(rows_at + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) =
-              make_uint4(float2_to_pair<BF16>(ch(8 * e) * inv, ch(8 * e + 1) * inv), float2_to_pair<BF16>(ch(8 * e + 2) * inv, ch(8 * e + 3) * inv),
-                         float2_to_pair<BF16>(ch(8 * e + 4) * inv, ch(8 * e + 5) * inv), float2_to_pair<BF16>(ch(8 * e + 6) * inv, ch(8 * e + 7) * inv));
+              make_uint4(float2_to_pair<BF16>(v[8 * e] * inv, v[8 * e + 1] * inv), float2_to_pair<BF16>(v[8 * e + 2] * inv, v[8 * e + 3] * inv),
+                         float2_to_pair<BF16>(v[8 * e + 4] * inv, v[8 * e + 5] * inv), float2_to_pair<BF16>(v[8 * e + 6] * inv, v[8 * e + 7] * inv));
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           *reinterpret_cast<float4*>(rows_at + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) =
-              make_float4(ch(16 * part16 + 4 * e), ch(16 * part16 + 4 * e + 1), ch(16 * part16 + 4 * e + 2), ch(16 * part16 + 4 * e + 3));
+              make_float4(v[16 * part16 + 4 * e], v[16 * part16 + 4 * e + 1], v[16 * part16 + 4 * e + 2], v[16 * part16 + 4 * e + 3]);
       }
       __syncwarp();
 #pragma unroll
@@ -790,12 +785,12 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 // 1024 away exactly, and a fused multiply-add, so an element is rounded once, and alike on both ways.  Four steps are under way to hide
 // the trip to L2; the lines of the next block are prefetched there.  Expanding inside takes a block 8700 clocks instead of 3450 (512 tokens over 32100: 796
 // instead of 330 us): 1250 instructions of each of the two warps.  All operands are fp16 whatever the dtype of the
-// results: queries come converted, and in the channels' order, from the same pass.
+// results: bf16 queries come converted from the same pass.
 struct Raw4 {
   uint4 code, s, z;                                    // keys: scales and zeros in s alone
 };
 
-// A lane's part of one step of 8 tokens x 128 channels; put(g, unit): channels 32 g + 8 u .. + 7 (in column4's order) of its token.
+// A lane's part of one step of 8 tokens x 128 channels; put(g, unit): channels 32 g + 8 u .. + 7 of its token.
 template <bool IS_V, typename F> __device__ __forceinline__ void expand4(const Raw4& x, bool used, int t, F put) {
   uint32_t s2[4], z2[4];                               // both halves alike
   if (IS_V) {
@@ -835,7 +830,8 @@ template <bool IS_V, typename F> __device__ __forceinline__ void expand4(const R
       const __half2 v = __hfma2(c, *reinterpret_cast<const __half2*>(&s2[g]), *reinterpret_cast<const __half2*>(&z2[g]));
       r[k] = *reinterpret_cast<const uint32_t*>(&v);
     }
-    put(g, make_uint4(r[0], r[1], r[2], r[3]));
+    // pairs of channels (k, k + 4) become neighbours
+    put(g, make_uint4(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410), __byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632)));
   }
 }
 
@@ -966,7 +962,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     }
     const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
     float* piece = job.part + static_cast<long long>(it.part) * kPartFloats;
-    store_rows<BF16, Q4>(ctl.job, it, lane_addr + 256 + 128 * i + 64 * half, worked, lt == 0.0f, inv, rows_at, 32 * (wp & 7), out_half, ln, piece);
+    store_rows<BF16>(ctl.job, it, lane_addr + 256 + 128 * i + 64 * half, worked, lt == 0.0f, inv, rows_at, 32 * (wp & 7), out_half, ln, piece);
     if (it.n_seg > 1) {
       // ---- the last piece of a row tile to arrive joins all of them, in the order of their tokens ----
       const int mine = row_at(ctl.job, it, 32 * (wp & 7) + ln);

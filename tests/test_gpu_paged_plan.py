@@ -133,6 +133,27 @@ def test_refusals_on_the_device():
     both(rng, n_pages=12, past=[10, 0, 20], n_new=[1, (1 << 31) - 1, 1], rows=100, **common)
 
 
+def test_sums_past_32_bits_are_refused():
+    """Sequences that each bring 2^29 tokens: their sums, and those of their pages, must not wrap into something that fits."""
+    batch, page, width = 70, 16, 1 << 25
+    cache = mq.moqae_paged4_bind(torch.empty(9, 1, 2560, dtype=torch.uint8, device="cuda"), torch.empty(batch, 0, dtype=torch.int32, device="cuda"),
+                                 ints([0] * batch), torch.float16)
+    table = torch.zeros(4, dtype=torch.int32, device="cuda")          # never read or written: the batch is refused
+    pool = mq.make_page_pool(9)
+    cu, pos, seq = ints([5] * (batch + 1)), ints([5] * 8), ints([5] * 8)
+    L, C = mq.lib(), mq.C
+    view = mq.MoqaePagePool(pool.ring.data_ptr(), pool.state.data_ptr(), 9)
+    for grow in (1 << 29, 1 << 27):
+        cache.status.zero_()
+        new = ints([grow] * batch)
+        assert L.moqae_paged_plan(cache.kv_len.data_ptr(), new.data_ptr(), batch, page, width, table.data_ptr(), cache.kv_len.data_ptr(), C.byref(view), None,
+                                  cu.data_ptr(), pos.data_ptr(), seq.data_ptr(), 8, cache.status.data_ptr(),
+                                  torch.cuda.current_stream().cuda_stream) == 0
+        code, _, tokens, _ = cache.status.tolist()
+        assert code == mq.ERR_INVALID_ARG and tokens > 8 and cache.kv_len.tolist() == [0] * batch
+        assert cu.tolist() == [0] * (batch + 1) and pos.tolist() == [-1] * 8 and pool.state.tolist() == [0, 9, 0, 0]
+
+
 def test_a_state_that_cannot_be_and_a_page_that_does_not_exist():
     cache = mq.moqae_paged4_bind(torch.empty(4, 1, 2560, dtype=torch.uint8, device="cuda"), ints([[0, 99]]), ints([20]), torch.float16)
     for state in ([4, 1, 0, 0], [-1, 1, 0, 0], [0, 5, 0, 0], [0, -1, 0, 0], [0, 4, 0, 0]):       # the last: two pages in use, none missing

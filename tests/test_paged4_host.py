@@ -142,7 +142,7 @@ def plan(lib, **kw):
     (dict(pool=False), mq.ERR_INVALID_ARG), (dict(batch=-1), mq.ERR_INVALID_ARG), (dict(width=-1), mq.ERR_INVALID_ARG),
     (dict(rows=-1), mq.ERR_INVALID_ARG), (dict(n_pages=-1), mq.ERR_INVALID_ARG), (dict(page=24), mq.ERR_UNSUPPORTED),
     (dict(page=512), mq.ERR_UNSUPPORTED), (dict(page=0), mq.ERR_UNSUPPORTED), (dict(width=(1 << 26) + 1), mq.ERR_UNSUPPORTED),
-    (dict(rows=(1 << 24) + 1), mq.ERR_UNSUPPORTED), (dict(batch=(1 << 24) + 1), mq.ERR_UNSUPPORTED), (dict(n_pages=(1 << 30) + 1), mq.ERR_UNSUPPORTED),
+    (dict(rows=(1 << 24) + 1), mq.ERR_UNSUPPORTED), (dict(batch=(1 << 24) + 1), mq.ERR_UNSUPPORTED), (dict(n_pages=(1 << 24) + 1), mq.ERR_UNSUPPORTED),
     (dict(past=None), mq.ERR_INVALID_ARG), (dict(n_new=None), mq.ERR_INVALID_ARG), (dict(table=None), mq.ERR_INVALID_ARG),
     (dict(kv_len=None), mq.ERR_INVALID_ARG), (dict(ring=None), mq.ERR_INVALID_ARG), (dict(state=None), mq.ERR_INVALID_ARG),
     (dict(cu=None), mq.ERR_INVALID_ARG), (dict(pos=None), mq.ERR_INVALID_ARG), (dict(seq=None), mq.ERR_INVALID_ARG),
