@@ -33,7 +33,9 @@ namespace {
 __host__ __device__ constexpr int warps_of(int form) { return form == kFew16Q ? 8 : form == kOne8Q ? 12 : 16; }
 __host__ __device__ constexpr int stages4_of(int form) { return form == kFew16Q ? 3 : 2; }
 constexpr int kStageBytes4 = 2 * kTileBytes4;
-constexpr int kMinTiles4 = 2, kPairTiles4 = 96;
+// See share_work.  Measured with least tiles per warp / most per pair of 1 / 12, 1 / 24, 2 / 48, 2 / 96, 4 / 160 (us): 8 pairs of 21 tiles 12.2 / 10.2 / 10.2 / 10.2 / 10.2,
+// of 63 12.8 / 13.0 / 13.3 / 13.5 / 13.4, of 157 13.4 / 13.6 / 13.8 / 13.7 / 18.7; 64 pairs of 63 13.2 / 13.2 / 13.4 / 13.5 / 13.6; 256 of 4 11.2 / 11.2 / 11.4 / 11.5 / 13.4.
+constexpr int kMinTiles4 = 1, kPairTiles4 = 24;
 // Weights of a row are 2^(score - reference), at most 2^top: the reference lies top - kLag below the largest score so far and moves when
 // a score passes it by top.  top is 15, less where value scales above 1 would take p s out of fp16.
 constexpr float kLag = 3.0f;
@@ -66,9 +68,6 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   asm volatile("ld.shared.u32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ void ldsm2(uint32_t& r0, uint32_t& r1, uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x2.shared.b16 {%0, %1}, [%2];\n" : "=r"(r0), "=r"(r1) : "r"(addr) : "memory");
-}
 __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
@@ -81,7 +80,8 @@ __device__ __forceinline__ uint32_t mid2(uint32_t s, uint32_t z) {
 __device__ __forceinline__ float low_half(uint32_t u) { return __low2float(*reinterpret_cast<const __half2*>(&u)); }
 __device__ __forceinline__ float high_half(uint32_t u) { return __high2float(*reinterpret_cast<const __half2*>(&u)); }
 
-template <bool BF16, int FORM>
+// SHAPED: scores have a cap or a distance bias
+template <bool BF16, int FORM, bool SHAPED>
 __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(PagedView pv, AttnOptions opt, DecodeJob job) {
   constexpr int kRows = set_rows(FORM), kCols = kRows / 8, kStages = stages4_of(FORM), kWarps = warps_of(FORM);
   extern __shared__ __align__(128) uint8_t smem[];
@@ -125,18 +125,20 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
     // in shared memory (lane 0 takes it to the next pair).
     Cursor &put = cursors[2 * warp], &get = cursors[2 * warp + 1];
     int todo = part.todo, to_put = part.todo;
+    // Within a pair the tiles are walked backwards: under a distance bias the largest scores then come first (the reference would move with
+    // nearly every tile the other way: 32 sequences of 4000, 40 heads, 194 us).
     int put_i, put_left, put_pre, put_first;      // index of the next tile in the pair's walk, tiles left; the walk: see tile_of
     const int32_t* put_row;                       // the sequence's pages
     const uint8_t* put_head;                      // the head's part of page 0
-    int at_token, page;                           // of lanes 0 and 1: first token of the next tile and of the one behind it, and their pages
+    int at_token, page;                           // of lanes 0 and 1: first token of the next tile and of the one after it, and their pages
     auto look_up = [&]() {
-      const int i = put_i + (lane & 1);
+      const int i = put_i - (lane & 1);
       at_token = (i < put_pre ? i : put_first + i - put_pre) * kTile;
       page = (lane & 1) < put_left ? put_row[at_token >> pv.page_shift] : 0;
     };
     auto open_put = [&]() {
-      put_i = put.i;
       put_left = min(put.s.n - put.i, to_put);
+      put_i = put.i + put_left - 1;
       put_pre = put.s.n_pre;
       put_first = put.s.first;
       put_row = pv.table + static_cast<long long>(put.b) * pv.max_pages;
@@ -167,7 +169,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         bulk_load(ring_u + st * kStageBytes4 + lane * kTileBytes4, put_head + page * pv.k_page + (at_token & (pv.page_size - 1)) * kTokenBytes4,
                   kTileBytes4, bar);
       put_left -= count;
-      put_i += count;
+      put_i -= count;
       if (put_left > 0) {
         look_up();
       } else if (to_put > 0) {
@@ -180,8 +182,8 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
 #pragma unroll
     for (int st = 0; st < kStages - 1; ++st) copy_tiles(st);
 
-    const bool shaped = opt.cap > 0.0f, plain = !shaped && !opt.slopes;
-    const float by_cap = shaped ? 1.0f / opt.cap : 0.0f;
+    const bool capped = SHAPED && opt.cap > 0.0f;
+    const float to_score = opt.scale * (capped ? 1.0f / opt.cap : kLog2e);
     int stage = 0;
     uint32_t parity = 0;
     while (todo > 0) {
@@ -189,7 +191,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
       const int n_here = min(get.s.n - get.i, todo);
       const bool from_start = get.i == 0, last_of_pair = get.i + n_here == get.s.n;
       uint32_t qf[kCols][4][2][2], qz[kCols][2];  // fragments of the queries; sums of their groups
-      float factor[kCols][2], m[kCols][2], o[kCols][4][2][4], zo[kCols][4];
+      float factor[kCols][2], slope[kCols][2], m[kCols][2], o[kCols][4][2][4], zo[kCols][4];
       float top = kTop;
       uint32_t most = 0x3c003c00u;                // largest scale that `top` allows, in both halves
       // the tile that starts at t0 is seen whole by every row if full_lo <= t0 and t0 + 16 <= full_hi, or t0 + 16 <= full_pre
@@ -250,8 +252,12 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         qz[c][1] = float2_to_pair<false>(s0 - low_half(qz[c][0]), s1 - high_half(qz[c][0]));
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          factor[c][e] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e)) * 16777216.0f * opt.scale * (shaped ? by_cap : kLog2e);
+          factor[c][e] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e)) * 16777216.0f * to_score;
           m[c][e] = kNothing;
+          if (SHAPED) {
+            const int rr = min(8 * c + 2 * t4 + e, get.s.rows - 1), head = get.s.row0 + rr - token_of(get.s.row0 + rr) * job.group;
+            slope[c][e] = opt.slopes ? -kLog2e * opt.slopes[get.h * job.group + head] : 0.0f;
+          }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -261,15 +267,15 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         }
       }
 
-      int index = get.i;                          // of the tile in the walk
-      const int end = index + n_here;
-      while (index < end) {
+      const int begin = get.i;
+      int index = begin + n_here - 1;             // of the tile in the walk
+      while (index >= begin) {
       copy_tiles(stage == 0 ? kStages - 1 : stage - 1);
       if (!mbar_try_wait(bar_u + 8 * stage, parity) && !*failed && !mbar_wait_bounded(bar_u + 8 * stage, parity)) *failed = 1;
       __syncwarp();
       const uint32_t stage_at = ring_u + stage * kStageBytes4;
 #pragma unroll 1
-      for (uint32_t tile = stage_at; tile < stage_at + kStageBytes4 && index < end; tile += kTileBytes4, ++index) {
+      for (uint32_t tile = stage_at; tile < stage_at + kStageBytes4 && index >= begin; tile += kTileBytes4, --index) {
       const int t0 = (index < n_pre ? index : index + behind) * kTile;
       const bool edge = !((t0 >= full_lo && t0 + kTile <= full_hi) || t0 + kTile <= full_pre);
       if (edge) {
@@ -290,15 +296,15 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
       {
         const uint4 k0 = lds128(tile + 64 * g + 16 * t4), k1 = lds128(tile + 64 * (g + 8) + 16 * t4);
         const uint2 c0 = lds64(tile + kKeyMeta4 + 16 * g), c1 = lds64(tile + kKeyMeta4 + 16 * (g + 8));
-        uint32_t z0, z1;
-        ldsm2(z0, z1, tile + kKeyMeta4 + 16 * (lane & 15));
+        uint32_t zm[4];                           // scales and zeros of tokens 0..7, 8..15, and once more
+        ldsm4(zm, tile + kKeyMeta4 + 16 * (lane & 15));
         const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
         const float s0[4] = {low_half(c0.x), high_half(c0.x), low_half(c0.y), high_half(c0.y)};
         const float s1[4] = {low_half(c1.x), high_half(c1.x), low_half(c1.y), high_half(c1.y)};
 #pragma unroll
         for (int c = 0; c < kCols; ++c) {
           float acc[4];
-          mma_first(acc, z0, z1, z0, z1, qz[c][0], qz[c][1]);
+          mma_first(acc, zm[0], zm[1], zm[2], zm[3], qz[c][0], qz[c][1]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) x[c][e] = acc[e] * 5.9604645e-8f;     // 2^-24, as the codes have it
         }
@@ -326,21 +332,53 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         const __half2 big = __hmax2(*reinterpret_cast<const __half2*>(&vs0), *reinterpret_cast<const __half2*>(&vs1));
         above = !__hble2(big, *reinterpret_cast<const __half2*>(&most));
       }
-      if (!plain || edge) {                       // otherwise x times factor is the score
+      if (SHAPED) {                               // otherwise x times factor is the score
+        float far = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[c][e] *= factor[c][e & 1];
+            far = fmaxf(far, fabsf(x[c][e]));
+          }
+        if (capped) {
+          const float cap2 = opt.cap * kLog2e;
+          if (__any_sync(0xffffffffu, far > 1.0f)) {
+#pragma unroll
+            for (int c = 0; c < kCols; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[c][e] = cap2 * tanh_of(x[c][e]);
+          } else {                                // no score passes the cap
+#pragma unroll
+            for (int c = 0; c < kCols; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float z = x[c][e], u = z * z;
+                x[c][e] = cap2 * z * fmaf(fmaf(fmaf(fmaf(fmaf(tanh_coef(5), u, tanh_coef(4)), u, tanh_coef(3)), u, tanh_coef(2)), u, tanh_coef(1)), u, tanh_coef(0));
+              }
+          }
+        }
+        if (opt.slopes) {
+#pragma unroll
+          for (int c = 0; c < kCols; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int p = FORM == kFew16Q ? get.s.pos0 + token_of(get.s.row0 + min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1)) : get.s.pos0;
+              x[c][e] = fmaf(slope[c][e & 1], fabsf(static_cast<float>(p - (t0 + g + 8 * (e >> 1)))), x[c][e]);
+            }
+        }
+      }
+      if (edge) {
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int j = t0 + g + 8 * (e >> 1);
-            const int rr = min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1), tt = token_of(get.s.row0 + rr), p = get.s.pos0 + tt;
-            if (!plain) {
-              float y = x[c][e] * factor[c][e & 1];
-              if (shaped) y = opt.cap * kLog2e * tanh_of(y);
-              if (opt.slopes) y = fmaf(-kLog2e * opt.slopes[get.h * job.group + get.s.row0 + rr - tt * job.group], fabsf(static_cast<float>(p - j)), y);
-              x[c][e] = y;
+            bool see = j < get.s.len && (j >= get.s.lo || j < get.s.pre);
+            if (FORM == kFew16Q) {
+              const int p = get.s.pos0 + token_of(get.s.row0 + min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1));
+              see = (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix;
             }
-            const bool see = FORM == kFew16Q ? (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix
-                                            : j < get.s.len && (j >= get.s.lo || j < get.s.pre);
             if (!see) x[c][e] = -INFINITY;
           }
       }
@@ -348,7 +386,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
 #pragma unroll
       for (int c = 0; c < kCols; ++c) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[c][e] = fmaf(x[c][e], plain ? factor[c][e & 1] : 1.0f, -m[c][e & 1]);
+        for (int e = 0; e < 4; ++e) r[c][e] = SHAPED ? x[c][e] - m[c][e & 1] : fmaf(x[c][e], factor[c][e & 1], -m[c][e & 1]);
         above = above || fmaxf(fmaxf(r[c][0], r[c][1]), fmaxf(r[c][2], r[c][3])) > top;
       }
       if (__any_sync(0xffffffffu, above)) {
@@ -367,7 +405,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         for (int c = 0; c < kCols; ++c)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float f0 = plain ? factor[c][e] : 1.0f;
+            const float f0 = SHAPED ? 1.0f : factor[c][e];
             float t = fmaxf(x[c][e] * f0, x[c][2 + e] * f0);
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
@@ -511,12 +549,18 @@ size_t smem4(int form, int rows) {
   return static_cast<size_t>(warps) * stages * (kStageBytes4 + 8) + static_cast<size_t>(warps) * piece_floats_of(rows) * 4 + 2 * warps * (sizeof(Piece) + sizeof(Cursor)) + 32;
 }
 
-template <bool BF16, int FORM> cudaError_t launch4(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
+template <bool BF16, int FORM, bool SHAPED> cudaError_t launch4(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
   static_assert(stages4_of(FORM) * kStageBytes4 >= piece_floats_of(set_rows(FORM)) * 4, "a piece fits the ring");
   static std::atomic<unsigned long long> done{0};
-  cudaError_t e = allow_shared_memory(paged4_decode_kernel<BF16, FORM>, smem4(FORM, FORM == kOne4Q ? 4 : set_rows(FORM)), done);
+  cudaError_t e = allow_shared_memory(paged4_decode_kernel<BF16, FORM, SHAPED>, smem4(FORM, FORM == kOne4Q ? 4 : set_rows(FORM)), done);
   if (e != cudaSuccess) return e;
-  return launch_early(paged4_decode_kernel<BF16, FORM>, sm_count_of_current_device(), warps_of(FORM) * 32, smem4(FORM, FORM == kFew16Q ? 16 : job.group), st, pv, opt, job);
+  return launch_early(paged4_decode_kernel<BF16, FORM, SHAPED>, sm_count_of_current_device(), warps_of(FORM) * 32, smem4(FORM, FORM == kFew16Q ? 16 : job.group), st, pv, opt, job);
+}
+
+template <int FORM> cudaError_t launch_shaped4(const PagedView& pv, const AttnOptions& opt, const DecodeJob& job, cudaStream_t st) {
+  const bool bf16 = pv.dtype == MOQAE_DTYPE_BF16;
+  if (opt.cap > 0.0f || opt.slopes) return bf16 ? launch4<true, FORM, true>(pv, opt, job, st) : launch4<false, FORM, true>(pv, opt, job, st);
+  return bf16 ? launch4<true, FORM, false>(pv, opt, job, st) : launch4<false, FORM, false>(pv, opt, job, st);
 }
 
 }  // namespace
@@ -535,9 +579,7 @@ cudaError_t launch_paged4_decode(const PagedView& pv, const RowsView& q, const R
   job.group = q.n_heads / pv.n_kv_heads;
   job.arrived = static_cast<int*>(workspace);
   job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
-  const bool bf16 = pv.dtype == MOQAE_DTYPE_BF16;
-  if (job.group <= 4) return bf16 ? launch4<true, kOne4Q>(pv, opt, job, st) : launch4<false, kOne4Q>(pv, opt, job, st);
-  return bf16 ? launch4<true, kOne8Q>(pv, opt, job, st) : launch4<false, kOne8Q>(pv, opt, job, st);
+  return job.group <= 4 ? launch_shaped4<kOne4Q>(pv, opt, job, st) : launch_shaped4<kOne8Q>(pv, opt, job, st);
 }
 
 // Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average (see paged_few_rows).
@@ -560,7 +602,7 @@ cudaError_t launch_paged4_few(const PagedView& pv, const RowsView& q, const int3
   job.group = q.n_heads / pv.n_kv_heads;
   job.arrived = static_cast<int*>(workspace);
   job.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kWorkCounterBytes);
-  return pv.dtype == MOQAE_DTYPE_BF16 ? launch4<true, kFew16Q>(pv, opt, job, st) : launch4<false, kFew16Q>(pv, opt, job, st);
+  return launch_shaped4<kFew16Q>(pv, opt, job, st);
 }
 
 }  // namespace moqae
