@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoqae.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")      # Python module: tensors in, C ABI structs out
 SOURCES = ["api.cu", "route.cu", "quantize.cu", "decode.cu", "decode_mma.cu", "decode_static.cu", "prefill.cu", "project.cu",
-           "paged_api.cu", "paged_append.cu", "paged_decode.cu", "paged_prefill.cu", "paged_plan.cu", "paged4_decode.cu", "paged4_prefill.cu"]
+           "paged_api.cu", "paged_append.cu", "paged_decode.cu", "paged_prefill.cu", "paged_plan.cu", "paged4_append.cu", "paged4_decode.cu", "paged4_prefill.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr"]
 
