@@ -49,10 +49,11 @@ cudaError_t launch_paged4_read(const PagedView& pv, const RowsView& k_out, const
 bool paged4_decode_fits(const PagedView& pv);
 long long paged4_decode_workspace_bytes(int group);
 cudaError_t launch_paged4_decode(const PagedView& pv, const RowsView& q, const RowsView& out, const AttnOptions& opt, void* workspace, cudaStream_t st);
-bool paged4_few_rows(const PagedView& pv, int group, int n_tokens);
+bool paged4_few_fits(const PagedView& pv, int group, int n_tokens, int max_rows);
 long long paged4_few_workspace_bytes();
+// max_rows > 0: sequences of more rows (tokens times heads of a group) are left to another kernel
 cudaError_t launch_paged4_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
-                              const AttnOptions& opt, void* workspace, cudaStream_t st);
+                              const AttnOptions& opt, void* workspace, int max_rows, cudaStream_t st);
 long long paged4_prefill_least_bytes(const PagedView& pv, int group, int n_tokens);     // without room for expanded blocks
 long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens);
 cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,

@@ -583,19 +583,21 @@ cudaError_t launch_paged4_decode(const PagedView& pv, const RowsView& q, const R
   return job.group <= 4 ? launch_shaped4<kOne4Q>(pv, opt, job, st) : launch_shaped4<kOne8Q>(pv, opt, job, st);
 }
 
-// Several tokens per sequence by the same kernel: up to kFewRows rows per sequence and head on average (see paged_few_rows).
-bool paged4_few_rows(const PagedView& pv, int group, int n_tokens) {
-  const long long sets = few_sets(pv.batch, group, n_tokens);
-  return static_cast<long long>(n_tokens) * group <= static_cast<long long>(kFewRows) * pv.batch && sets * pv.n_kv_heads <= kWorkCounters &&
-         units_fit(pv, sets, kFew16Q);
+// Several tokens per sequence by the same kernel, in sets of 16 rows.
+bool paged4_few_fits(const PagedView& pv, int group, int n_tokens, int max_rows) {
+  long long sets = few_sets(pv.batch, group, n_tokens);
+  const long long most = static_cast<long long>(pv.batch) * ((max_rows + 15) / 16);
+  if (max_rows > 0 && most < sets) sets = most;
+  return sets * pv.n_kv_heads <= kWorkCounters && units_fit(pv, sets, kFew16Q);
 }
 
 long long paged4_few_workspace_bytes() { return kWorkCounterBytes + part_bytes(16); }
 
 cudaError_t launch_paged4_few(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
-                              const AttnOptions& opt, void* workspace, cudaStream_t st) {
+                              const AttnOptions& opt, void* workspace, int max_rows, cudaStream_t st) {
   if (pv.batch <= 0 || n_tokens <= 0) return cudaSuccess;
   DecodeJob job{};
+  job.max_rows = max_rows;
   job.q = q;
   job.out = out;
   job.cu_q = cu_q;

@@ -1,4 +1,4 @@
-// moqae_paged4_prefill_attn: launches over 4-bit pages.  Few rows per sequence go to the streaming kernel (paged4_decode.cu), the others to the
+// moqae_paged4_prefill_attn: launches over 4-bit pages.  Sequences of few rows go to the streaming kernel (paged4_decode.cu), the others to the
 // large tiles (paged_prefill.cuh), behind a pass that brings keys and values out of their codes and bf16 queries into fp16.
 //   Expanding once costs 672 bytes per token and kv head and one reading of 512; inside the large tiles every row tile would
 //   expand the blocks that it sees again (see Four there).  The workspace holds kExpandBytes of expanded blocks at most, sequences beyond that are
@@ -12,6 +12,11 @@ namespace {
 constexpr int kExpandThreads = 256, kExpandWarps = kExpandThreads / 32;
 constexpr long long kExpandBytes = 1ll << 30;
 constexpr int kMaxExpanded = 1 << 20;              // blocks
+// Rows (tokens times heads of a group) of a sequence up to which the streaming kernel is faster, although it streams the sequence once per
+// 16 rows: it reads a third of the bytes, and expands nothing.  Streaming / large tiles, us: one sequence of 32000 tokens, 32 / 8 heads, with 32 rows 39 / 90,
+// 64 62 / 90, 96 84 / 99, 128 106 / 100; 8 of 2000 with 64 40 / 55, 96 53 / 57, 128 66 / 60; 64 of 2000 with 96 293 / 295; 8 of 8000, 40 / 40 heads, with
+// 64 450 / 804, 96 667 / 842, 128 884 / 838.
+constexpr int kFewRows4 = 96;
 constexpr int kBlockTiles = kBlock / kTileTokens4;
 
 struct ExpandJob {
@@ -22,6 +27,7 @@ struct ExpandJob {
   uint16_t* v16;
   int32_t* first;                                  // [batch]: a sequence's first block, -1: not expanded
   int n_tokens, blocks;                            // rows of q; room for blocks
+  int group, few_rows;                             // sequences of at most few_rows rows are the streaming kernel's
 };
 
 // Blocks are dealt out in the order of the sequences that bring tokens, until one has no room; a warp takes a tile of 16 tokens of one head.
@@ -38,7 +44,7 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
     if (b < pv.batch) {
       const int from = min(max(job.cu_q[b], 0), job.n_tokens), n = min(max(job.cu_q[b + 1], from), job.n_tokens) - from;
       len = paged_len(pv, b, false);
-      need = n > 0 ? min((len + kBlock - 1) / kBlock, kMaxExpanded + 1) : 0;
+      need = n * job.group > job.few_rows ? min((len + kBlock - 1) / kBlock, kMaxExpanded + 1) : 0;
       lo = opt.window > 0 ? max(0, len - n - opt.window + 1) : 0;
       pre = opt.prefix_len ? min(max(opt.prefix_len[b], 0), len) : 0;
     }
@@ -163,7 +169,17 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
                                   const AttnOptions& opt, void* workspace, long long workspace_bytes, cudaStream_t st) {
   if (pv.batch <= 0 || n_tokens <= 0) return cudaSuccess;
   const int group = q.n_heads / pv.n_kv_heads;
-  if (paged4_few_rows(pv, group, n_tokens)) return launch_paged4_few(pv, q, cu_q, n_tokens, out, opt, workspace, st);
+  // Who takes which sequence is decided on the device, by its rows; the host only knows their sum.  Where all of them have few, or 16 on average, the
+  // streaming kernel takes the call alone (the large tiles would cost two launches, 6 us, to find nothing), as the large tiles do where there is one
+  // sequence.  Otherwise both run: one piece of a prompt beside 63 single tokens expands and tiles that one sequence only.
+  const long long rows = static_cast<long long>(n_tokens) * group;
+  if ((rows <= kFewRows4 || rows <= static_cast<long long>(kFewRows) * pv.batch) && paged4_few_fits(pv, group, n_tokens, 0))
+    return launch_paged4_few(pv, q, cu_q, n_tokens, out, opt, workspace, 0, st);
+  const int few_rows = pv.batch > 1 && paged4_few_fits(pv, group, n_tokens, kFewRows4) ? kFewRows4 : 0;
+  if (few_rows > 0) {
+    const cudaError_t e = launch_paged4_few(pv, q, cu_q, n_tokens, out, opt, workspace, few_rows, st);
+    if (e != cudaSuccess) return e;
+  }
   const Layout l = layout_of(pv, group, n_tokens);
   uint8_t* space = static_cast<uint8_t*>(workspace);
   const long long room = (workspace_bytes - l.blocks) / l.block_bytes;
@@ -176,6 +192,8 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   ex.k16 = reinterpret_cast<uint16_t*>(space + l.blocks);
   ex.v16 = ex.k16 + static_cast<long long>(ex.blocks) * pv.n_kv_heads * kBlock * kHeadDim;
   ex.n_tokens = n_tokens;
+  ex.group = group;
+  ex.few_rows = few_rows;
 
   const bool bf16 = pv.dtype == MOQAE_DTYPE_BF16;
   RowsView q16 = q;
@@ -188,6 +206,7 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   long long grid;
   if (!make_job(job, grid, pv, q16, cu_q, n_tokens, out, workspace)) return cudaErrorInvalidConfiguration;
   job.expanded = ex.first;
+  job.few_rows = few_rows;
   job.box_rows = 64;
   job.dim_slot = 1;
   job.dim_head = 2;

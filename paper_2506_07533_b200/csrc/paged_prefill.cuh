@@ -111,6 +111,7 @@ struct PrefillJob {
   int box_rows;                                      // slots per copy of a page
   int dim_slot, dim_head, dim_page;                  // tensor-map dimension (1..3) of each
   const int32_t* expanded;                           // 4-bit pages: first expanded block of each sequence, -1: it has none
+  int few_rows;                                      // 4-bit pages: sequences of at most so many rows are the streaming kernel's
 };
 
 // A piece of work: rows row0 .. row0 + rows - 1 of (sequence b, head h), blocks [idx0, idx1) of their walk.
@@ -190,7 +191,10 @@ __device__ __forceinline__ Sequence sequence(const PagedView& pv, const AttnOpti
   s.prefix = opt.prefix_len ? min(max(opt.prefix_len[b], 0), s.kv_len) : 0;
   return s;
 }
-__device__ __forceinline__ int row_tiles_of(const PrefillJob& job, const Sequence& s) { return (s.n * job.group + 2 * job.tile_rows - 1) / (2 * job.tile_rows); }
+__device__ __forceinline__ int row_tiles_of(const PrefillJob& job, const Sequence& s) {
+  const int rows = s.n * job.group;
+  return rows <= job.few_rows ? 0 : (rows + 2 * job.tile_rows - 1) / (2 * job.tile_rows);
+}
 
 // The blocks that row tile rb of a sequence sees.
 __device__ __forceinline__ void set_walk(const PrefillJob& job, const AttnOptions& opt, const Sequence& s, int rb, Piece& it) {

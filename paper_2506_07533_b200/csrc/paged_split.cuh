@@ -35,6 +35,7 @@ struct DecodeJob {
   int n_tokens, group;
   float* part;            // [ctas][2] pieces
   int* arrived;           // [sets][n_kv_heads]
+  int max_rows;           // 4-bit pages: sequences of more rows are another kernel's; 0: none is
 };
 
 // A set of rows and the tiles that they see: tokens [lo, len) and [0, pre).
@@ -61,6 +62,7 @@ __device__ __forceinline__ Seen seen_of(const PagedView& pv, const AttnOptions& 
     s.sets = (rows + 15) / 16;
     s.row0 = set * 16;
     s.rows = min(16, rows - s.row0);
+    if (FORM == kFew16Q && job.max_rows > 0 && rows > job.max_rows) s.sets = s.rows = 0;
     s.pos0 = kv_len - s.q_n;
     p_first = s.pos0 + s.row0 / job.group;
     s.len = s.rows > 0 ? max(s.pos0 + (s.row0 + s.rows - 1) / job.group + 1, s.prefix) : 0;

@@ -368,6 +368,8 @@ PREFILLS = [
     dict(new=[130], past=[0], hq=4, hkv=1, page=64), dict(new=[64, 200, 17], past=[300, 0, 1], hq=6, hkv=2, page=128),
     dict(new=[257, 1], past=[40, 2000], hq=7, hkv=1, page=32), dict(new=[700], past=[0], hq=2, hkv=2, page=256),
     dict(new=[129, 128, 127], past=[0, 1, 129], hq=8, hkv=1, page=16),
+    # few rows and many side by side: 24 tokens of a group of four are 96 rows, 25 are 100
+    dict(new=[1, 24, 25, 0, 300, 1, 23], past=[700, 100, 90, 5, 0, 0, 3], hq=8, hkv=2, page=32),
 ]
 
 
@@ -448,6 +450,13 @@ def test_sequences_that_share_rows_are_refused():
     mq.moqae_paged4_prefill_attn(cache, q, cu, out, work)
     check(cache, q, [8], out, None, None)
     assert cache.status[0].item() == 0
+    # rows 0..7 and again 4..7: no results, whoever takes the sequences
+    for n, heads in ((8, 4), (80, 4), (200, 1)):
+        cache = make_cache(gen, [400, 400, 400], 1, 16, torch.float16)
+        q = randn(gen, n, heads, 128, dtype=torch.float16)
+        out, work = torch.full_like(q, 3.0), space(mq.moqae_paged4_prefill_attn_workspace(cache, heads, n))
+        mq.moqae_paged4_prefill_attn(cache, q, torch.tensor([0, n, n // 2, n], dtype=torch.int32, device="cuda"), out, work)
+        assert cache.status.tolist()[:3] == [mq.ERR_INVALID_ARG, -1, n + n // 2] and (out == 3).all() and (work[:1 << 20] == 0).all()
 
 
 # ---- streams, graphs ---------------------------------------------------------------------------
