@@ -587,7 +587,7 @@ typedef struct moqae_page_pool {
 
 /*
  * The tables of a step from the tokens that its sequences bring, for either kind of pages.  Sequence b has past_len[b] tokens,
- * all of them in pages of its row of block_table, and gets n_new[b] more (n_new < 0: it loses its last -n_new, at most all of them):
+ * all of them in pages of its row of block_table (a page is one sequence's), and gets n_new[b] more (n_new < 0: it loses its last -n_new, at most all of them):
  *   block_table   the entries of its new pages are written, pages taken from the front of the pool in the order of sequences and entries;
  *   kv_len[b]     = max(past_len[b] + n_new[b], 0);
  *   pool          pages that hold none of its tokens any more go to the end, in the same order (their entries stay as they were); they can be

@@ -695,7 +695,9 @@ def moqae_paged4_bind(pages, block_table, kv_len, dtype, status=None) -> Paged4C
     _need(block_table.dim() == 2 and block_table.dtype == torch.int32 and block_table.is_contiguous() and block_table.get_device() == index, where)
     if status is None:
         status = torch.zeros(4, dtype=torch.int32, device=pages.device)
-    view = MoqaePaged4Cache(pages.data_ptr(), pages.stride(0), pages.stride(1), block_table.data_ptr(),
+    head_stride = pages.stride(1) if pages.shape[1] > 1 else pages.shape[2]      # (a stride along one element may be anything)
+    page_stride = pages.stride(0) if pages.shape[0] > 1 else max(pages.shape[1], 1) * pages.shape[2]
+    view = MoqaePaged4Cache(pages.data_ptr(), page_stride, head_stride, block_table.data_ptr(),
                             _vector(kv_len, torch.int32, block_table.shape[0], index, where), _vector(status, torch.int32, 4, index, where),
                             pages.shape[0], pages.shape[2] // TOKEN_BYTES4, pages.shape[1], _DTYPE_CODE[dtype], block_table.shape[0],
                             block_table.shape[1])

@@ -368,6 +368,8 @@ PREFILLS = [
     dict(new=[130], past=[0], hq=4, hkv=1, page=64), dict(new=[64, 200, 17], past=[300, 0, 1], hq=6, hkv=2, page=128),
     dict(new=[257, 1], past=[40, 2000], hq=7, hkv=1, page=32), dict(new=[700], past=[0], hq=2, hkv=2, page=256),
     dict(new=[129, 128, 127], past=[0, 1, 129], hq=8, hkv=1, page=16),
+    # more new tokens than the sequence has: the first ones stand before it and see nothing
+    dict(new=[10, 140, 3], past=[-4, -5, -3], hq=4, hkv=2, page=16),
     # few rows and many side by side: 24 tokens of a group of four are 96 rows, 25 are 100
     dict(new=[1, 24, 25, 0, 300, 1, 23], past=[700, 100, 90, 5, 0, 0, 3], hq=8, hkv=2, page=32),
 ]
@@ -436,6 +438,62 @@ def test_a_prompt_then_steps(dtype):
     live = [int(cache.block_table[b, i]) for b in range(batch) for i in range((int(cache.kv_len[b]) + page - 1) // page)]
     free = [int(pool.ring[(int(pool.state[0]) + i) % 40]) for i in range(int(pool.state[1]))]
     assert sorted(live + free) == list(range(40))
+
+
+def test_readme_example():
+    """The example of the 4-bit cache, run as it stands in the README."""
+    import os
+    import re
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        block = re.search(r"\n((?: {4}.*\n)*? {4}.*make_page_pool.*\n(?: {4}.*\n)*)", f.read()).group(1)
+    gen = generator(41)
+    new, n_q_heads, n_kv_heads, page_size, n_pages, n_tokens = [300, 5, 77], 8, 2, 16, 40, 384
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    block_table, kv_len = torch.full((3, 20), -1, dtype=torch.int32, device="cuda"), ints(0, 0, 0)
+    n_new, one_each, cu_q = ints(*new), ints(1, 1, 1), torch.zeros(4, dtype=torch.int32, device="cuda")
+    positions, seq = (torch.zeros(n_tokens, dtype=torch.int32, device="cuda") for _ in range(2))
+    positions1, seq1 = ints(0, 0, 0), ints(0, 0, 0)
+    rope = mq.make_rope(mq.rope_table(400, 128), 128)
+    q, k, v = (randn(gen, n_tokens, h, 128, dtype=torch.bfloat16) for h in (n_q_heads, n_kv_heads, n_kv_heads))
+    q1, k1, v1 = (randn(gen, 3, h, 128, dtype=torch.bfloat16) for h in (n_q_heads, n_kv_heads, n_kv_heads))
+    out, out1, k_back, v_back = torch.full_like(q, 7.0), torch.full_like(q1, 7.0), torch.zeros_like(k1), torch.zeros_like(v1)
+    names = dict(globals(), **locals())
+    exec("".join(line[4:] + "\n" for line in block.splitlines()), names)
+    cache = names["cache4"]
+    assert mq.moqae_paged_poll_status(cache) == 0 and kv_len.tolist() == [n + 1 for n in new] and (out[382:] == 7).all()
+    check(cache, q1, [1, 1, 1], out1, None, None)
+    kv_len.copy_(n_new)
+    check(cache, q[:382], new, out[:382], None, None)
+    for b, n in enumerate(new):
+        kc, kz, vc, vz, _ = stored(cache, b, n + 1)
+        assert (k_back[b] == (kc + kz)[n].float().bfloat16()).all() and (v_back[b] == (vc + vz)[n].float().bfloat16()).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_views_of_pages(dtype):
+    """One page of one head out of a larger buffer, and a cache without pages."""
+    gen = generator(42)
+    buffer = torch.zeros(3, 5, 16 * 160 + 32, dtype=torch.uint8, device="cuda")
+    pages = buffer[1:2, 2:3, 32:]
+    cache = mq.moqae_paged4_bind(pages, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([9], dtype=torch.int32, device="cuda"), dtype)
+    k, v = randn(gen, 9, 1, 128, dtype=dtype), randn(gen, 9, 1, 128, dtype=dtype)
+    mq.moqae_paged4_append(cache, k, v, torch.arange(9, dtype=torch.int32, device="cuda"), seq=torch.zeros(9, dtype=torch.int32, device="cuda"))
+    q = randn(gen, 1, 3, 128, dtype=dtype)
+    out = torch.empty_like(q)
+    mq.moqae_paged4_decode_attn(cache, q, out, space(mq.moqae_paged4_decode_attn_workspace(cache, 3)))
+    check(cache, q, [1], out, None, None)
+    pages.zero_()
+    assert (buffer == 0).all()                            # nothing outside of the view was written
+    none = mq.moqae_paged4_bind(torch.empty(0, 2, 2560, dtype=torch.uint8, device="cuda"), torch.zeros(2, 4, dtype=torch.int32, device="cuda"),
+                                torch.tensor([0, 5], dtype=torch.int32, device="cuda"), dtype)
+    q = randn(gen, 2, 4, 128, dtype=dtype)
+    out, work = torch.full_like(q, 3.0), space(mq.moqae_paged4_prefill_attn_workspace(none, 4, 300))
+    mq.moqae_paged4_decode_attn(none, q, out, work)       # five tokens without a page: zeros
+    assert (out == 0).all() and none.status.tolist()[:3] == [mq.ERR_CORRUPT_TABLE, 1, 0]
+    q = randn(gen, 300, 4, 128, dtype=dtype)
+    out = torch.full_like(q, 3.0)
+    mq.moqae_paged4_prefill_attn(none, q, torch.tensor([0, 0, 300], dtype=torch.int32, device="cuda"), out, work)
+    assert (out == 0).all()
 
 
 def test_sequences_that_share_rows_are_refused():
