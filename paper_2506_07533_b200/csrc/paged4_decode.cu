@@ -22,9 +22,9 @@
 //   instead of 1.66e-3, beside the 0.1 of holding the cache in 4 bits.  (The last sum over the rounded products instead, four more small products per
 //   tile: 3.3e-4 in fp16, and 5 to 8 % of the time.)  The largest weight is kept near 2^15 / (largest scale), so that small ones
 //   do not vanish below fp16's steps; the sum of the weights is that of the rounded ones.
-//   Measured.  4 sequences of 131000 tokens, 32 / 8 heads, bf16: 127 to 144 us for 671 MB (floor 102); 61 of 1 to 32000: 55 us for 233 MB (floor 36); 32 of 4000,
-//   40 / 40 heads, fp16: 150 us for 820 MB (floor 125), under a cap 171, under a distance bias 170; 8 of 1000: 13 us; one of 60: 7 us.  What bounds it is its own
-//   instructions, 310 per tile and head, of which 78 are the logic instructions that bring codes out, at half rate (ALU pipe 60 %,
+//   Measured.  4 sequences of 131000 tokens, 32 / 8 heads, bf16: 123 to 141 us for 671 MB (floor 102); 61 of 1 to 32000: 54 us for 233 MB (floor 36); 32 of 4000,
+//   40 / 40 heads, fp16: 146 us for 820 MB (floor 125), under a cap 170, under a distance bias 157; 8 of 1000: 13 us; one of 60: 7 us.  What bounds it is its own
+//   instructions, about 300 per tile and head, of which 78 are the logic instructions that bring codes out, at half rate (ALU pipe 60 %,
 //   issue slots 61 % busy); about 17 us of a long call are its start, uneven ends and the joining.
 #include "paged4.cuh"
 #include "paged_split.cuh"
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
     Cursor &put = cursors[2 * warp], &get = cursors[2 * warp + 1];
     int todo = part.todo, to_put = part.todo;
     // Within a pair the tiles are walked backwards: under a distance bias the largest scores then come first (the reference would move with
-    // nearly every tile the other way: 32 sequences of 4000, 40 heads, 194 us).
+    // nearly every tile the other way: 32 sequences of 4000, 40 heads, 194 us instead of 170 when that was changed).
     int put_i, put_left, put_pre, put_first;      // index of the next tile in the pair's walk, tiles left; the walk: see tile_of
     const int32_t* put_row;                       // the sequence's pages
     const uint8_t* put_head;                      // the head's part of page 0
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
       if (put_left <= 0) return;
       const int count = min(put_left, 2);
       const uint32_t bar = bar_u + 8 * st;
-      const bool mine = lane < count, good = page >= 0 && page < pv.n_pages;
+      const bool mine = lane < count, good = static_cast<unsigned>(page) < static_cast<unsigned>(pv.n_pages);
       const unsigned bad = __ballot_sync(0xffffffffu, mine && !good);
       if (bad) {
         if (mine && !good) paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, put.b, at_token >> pv.page_shift);
@@ -168,8 +168,8 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         fence_async_smem();
         __syncwarp();
       }
+      // (a copy may land before its bytes are announced: the phase ends with the arrival that announces them)
       if (lane == 0) mbar_expect_tx(bar, (count - __popc(bad)) * kTileBytes4);
-      __syncwarp();
       if (mine && good)
         bulk_load(ring_u + st * kStageBytes4 + lane * kTileBytes4, put_head + page * pv.k_page + (at_token & (pv.page_size - 1)) * kTokenBytes4,
                   kTileBytes4, bar);
@@ -199,14 +199,14 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
       float factor[kCols][2], slope[kCols][2], m[kCols][2], o[kCols][4][2][4], zo[kCols][4];
       float top = kTop;
       uint32_t most = 0x3c003c00u;                // largest scale that `top` allows, in both halves
-      // the tile that starts at t0 is seen whole by every row if full_lo <= t0 and t0 + 16 <= full_hi, or t0 + 16 <= full_pre
+      // Tiles that every row sees whole, by their index in the walk: whole_lo <= index < whole_lo + n_whole (of the prefix none is counted).
       int full_lo = get.s.lo, full_hi = get.s.len;
-      const int full_pre = FORM == kFew16Q ? get.s.prefix : get.s.pre;
-      const int n_pre = get.s.n_pre, behind = get.s.first - n_pre;
       if (FORM == kFew16Q) {
         full_hi = get.s.pos0 + token_of(get.s.row0) + 1;
         full_lo = opt.window > 0 ? get.s.pos0 + token_of(get.s.row0 + get.s.rows - 1) - opt.window + 1 : 0;
       }
+      const int n_pre = get.s.n_pre, behind = get.s.first - n_pre;
+      const int whole_lo = max(n_pre, (max(full_lo, 0) + kTile - 1) / kTile - behind), n_whole = max(full_hi / kTile - behind - whole_lo, 0);
 #pragma unroll
       for (int c = 0; c < kCols; ++c) {
         // ---- queries: lane (g, t4) takes channels 8 t4 .. 8 t4 + 7 of every group of row 8 c + g ----
@@ -281,11 +281,11 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
       const uint32_t stage_at = ring_u + stage * kStageBytes4;
 #pragma unroll 1
       for (uint32_t tile = stage_at; tile < stage_at + kStageBytes4 && index >= begin; tile += kTileBytes4, --index) {
-      const int t0 = (index < n_pre ? index : index + behind) * kTile;
-      const bool edge = !((t0 >= full_lo && t0 + kTile <= full_hi) || t0 + kTile <= full_pre);
+      const bool edge = static_cast<unsigned>(index - whole_lo) >= static_cast<unsigned>(n_whole);
+      auto first_token = [&]() { return (index < n_pre ? index : index + behind) * kTile; };
       if (edge) {
         // what no row may use can hold anything: its scales and zeros become 0
-        const int j = t0 + lane;
+        const int j = first_token() + lane;
         if (lane < kTile && !(j < get.s.len && (j >= get.s.lo || j < get.s.pre))) {
           uint8_t* tp = ring + (tile - ring_u);
           *reinterpret_cast<uint4*>(tp + kKeyMeta4 + 16 * lane) = make_uint4(0, 0, 0, 0);
@@ -364,6 +364,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
           }
         }
         if (opt.slopes) {
+          const int t0 = first_token();
 #pragma unroll
           for (int c = 0; c < kCols; ++c)
 #pragma unroll
@@ -374,6 +375,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         }
       }
       if (edge) {
+        const int t0 = first_token();
 #pragma unroll
         for (int c = 0; c < kCols; ++c)
 #pragma unroll

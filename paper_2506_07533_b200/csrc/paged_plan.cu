@@ -6,7 +6,7 @@
 // lengths, sums, store (the first free pages travel beside the lengths).  One launch therefore: all CTAs form the sums of the whole batch, 256 sequences at a time
 // (nothing to wait for but the lengths), and share out rows and pages; what may be read and written in place (lengths, the pool's
 // state) is written by the CTA that comes last, when all have read it.  A batch that is refused is found in a first pass
-// over the lengths, before anything is written.  Measured: 61 sequences, six of them leaving with their pages, 5.0 us (in a graph); 96 sequences and 64367
+// over the lengths, before anything is written.  Measured: 61 sequences, eight of them leaving with their pages, 5.0 us (in a graph); 96 sequences and 64367
 // rows, 7.2 to 8.1 us for 0.6 MB.
 #include "paged4.cuh"
 

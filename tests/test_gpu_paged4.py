@@ -554,3 +554,31 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         assert cache.kv_len.tolist() == [n + step + 1 for n in lens] and cache.status[0].item() == 0
         check(cache, q, [1, 1, 1], out, None, None)
+
+
+def test_captured_prompts_follow_their_offsets():
+    """Two captured calls of different sizes share a workspace; which sequences bring few rows and which many is decided at the replay."""
+    gen = generator(32)
+    lens, hq, hkv = [400, 300, 900, 31], 8, 2
+    cache = make_cache(gen, lens, hkv, 64, torch.float16)
+    calls = []
+    work = space(mq.moqae_paged4_prefill_attn_workspace(cache, hq, 500))
+    for n in (500, 200):
+        q, cu = randn(gen, n, hq, 128, dtype=torch.float16), torch.zeros(5, dtype=torch.int32, device="cuda")
+        out = torch.zeros_like(q)
+        mq.moqae_paged4_prefill_attn(cache, q, cu, out, work)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            mq.moqae_paged4_prefill_attn(cache, q, cu, out, work)
+        calls.append((n, q, cu, out, graph))
+    for first, second in (([300, 1, 100, 31], [1, 1, 190, 8]), ([1, 250, 0, 2], [150, 0, 25, 24]), ([0, 0, 499, 1], [50, 50, 50, 31]), ([0, 0, 0, 0], [1, 0, 0, 0])):
+        for (n, q, cu, out, graph), new in zip(calls, (first, second)):
+            cu.copy_(torch.tensor([0] + new).cumsum(0).to(torch.int32))
+            out.fill_(9.0)
+        for call in calls:
+            call[4].replay()
+        torch.cuda.synchronize()
+        for (n, q, cu, out, graph), new in zip(calls, (first, second)):
+            check(cache, q[:sum(new)], new, out[:sum(new)], None, None, what=str(new))
+            assert (out[sum(new):] == 9).all()
+    assert cache.status[0].item() == 0 and (work[:1 << 20] == 0).all()
