@@ -496,6 +496,38 @@ def test_views_of_pages(dtype):
     assert (out == 0).all()
 
 
+def test_tensors_that_do_not_fit_are_refused():
+    gen = generator(43)
+    cache = make_cache(gen, [40, 20], 2, 16, torch.bfloat16)
+    b = torch.bfloat16
+    q, k, work = randn(gen, 2, 4, 128, dtype=b), randn(gen, 2, 2, 128, dtype=b), space(mq.moqae_paged4_prefill_attn_workspace(cache, 4, 2))
+    pos, cu = torch.tensor([0, 1], dtype=torch.int32, device="cuda"), torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    other = mq.make_rope(None, 0, k_weight=torch.ones(128, dtype=torch.float16, device="cuda"))
+    pool = mq.make_page_pool(8)
+    before, lens = cache.pages.clone(), cache.kv_len.clone()
+    refused = [
+        lambda: mq.moqae_paged4_append(cache, k.half(), k, pos), lambda: mq.moqae_paged4_append(cache, k, k[:1], pos),
+        lambda: mq.moqae_paged4_append(cache, k, k, pos.long()), lambda: mq.moqae_paged4_append(cache, k, k, pos, rope=other),
+        lambda: mq.moqae_paged4_append(cache, q, k, pos), lambda: mq.moqae_paged4_append(cache, k.cpu(), k, pos),
+        lambda: mq.moqae_paged4_read(cache, None, None, pos), lambda: mq.moqae_paged4_read(cache, k, k.float(), pos),
+        lambda: mq.moqae_paged4_decode_attn(cache, q[:1], q[:1], work), lambda: mq.moqae_paged4_decode_attn(cache, q, q, work[1:]),
+        lambda: mq.moqae_paged4_decode_attn(cache, q, q, work[:1 << 20]), lambda: mq.moqae_paged4_decode_attn(cache, q, q, None),
+        lambda: mq.moqae_paged4_prefill_attn(cache, q, cu[:2], q, work), lambda: mq.moqae_paged4_prefill_attn(cache, q, cu, q, None),
+        lambda: mq.moqae_paged4_prefill_attn(cache, q[..., ::2], cu, q, work), lambda: mq.moqae_paged4_prefill_attn(cache, q[:, :3], cu, q, work),
+        lambda: mq.moqae_paged_plan(cache, pool, pos.long(), cu, pos, pos), lambda: mq.moqae_paged_plan(cache, pool, pos, cu[:2], pos, pos),
+        lambda: mq.moqae_paged_plan(cache, pool, pos, cu, pos, pos[:1]), lambda: mq.moqae_paged_plan(cache, mq.PagePool(pool.ring, pool.state[:3]), pos, cu, pos, pos),
+        lambda: mq.moqae_paged4_bind(cache.pages[:, :, :100], cache.block_table, cache.kv_len, b),
+        lambda: mq.moqae_paged4_bind(cache.pages, cache.block_table, cache.kv_len, torch.float32),
+        lambda: mq.moqae_paged4_bind(cache.pages, cache.block_table, cache.kv_len[:1], b),
+    ]
+    for i, call in enumerate(refused):
+        with pytest.raises(mq.MoqaeError):
+            call()
+            raise AssertionError(i)
+    torch.cuda.synchronize()
+    assert (cache.pages == before).all() and (cache.kv_len == lens).all() and cache.status[0].item() == 0
+
+
 def test_sequences_that_share_rows_are_refused():
     gen = generator(22)
     cache = make_cache(gen, [40, 40], 1, 16, torch.float16)

@@ -119,7 +119,7 @@ def test_random_batches(seed):
 def test_many_rows_and_many_sequences():
     rng = random.Random(99)
     both(rng, 3, 16, 2100, 4300, [0, 100, 0], [33000, 1, 20000], 53100)              # several CTAs, long rows
-    both(rng, 3000, 16, 2, 6100, [rng.randint(0, 31) for _ in range(3000)], [1] * 3000, 3072)
+    both(rng, 3000, 16, 2, 6100, [rng.randint(0, 31) for _ in range(3000)], [1] * 3000, 3050)
     both(rng, 1, 256, 1, 1, [0], [256], 256, first=0)
 
 
