@@ -1,6 +1,6 @@
 // moqae_paged4_prefill_attn: launches over 4-bit pages.  Sequences of few rows go to the streaming kernel (paged4_decode.cu), the others to the
 // large tiles (paged_prefill.cuh), behind a pass that brings keys and values out of their codes and bf16 queries into fp16.
-//   Expanding once costs 672 bytes per token and kv head and one reading of 512; inside the large tiles every row tile would
+//   Expanding once costs 672 bytes per token and kv head (32612 tokens of 8 heads: 34 us for 175 MB) and one reading of 512; inside the large tiles every row tile would
 //   expand the blocks that it sees again (see Four there).  The workspace holds kExpandBytes of expanded blocks at most, sequences beyond that are
 //   expanded inside.
 #include "paged_prefill.cuh"
@@ -35,7 +35,7 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
   __shared__ int block_to[kExpandThreads + 1], warp_sum[kExpandWarps];      // blocks in front of a sequence
   __shared__ int len_of[kExpandThreads], lo_of[kExpandThreads], pre_of[kExpandThreads];   // tokens, and which of them some row sees: [lo, len) and [0, pre)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int r8 = lane & 7, u = lane >> 3;
+  const int r8 = lane >> 2, u = lane & 3;          // four neighbouring lanes store 64 bytes of a row together
   after_previous();
   int before = 0;
   for (int base = 0; base < pv.batch; base += kExpandThreads) {
