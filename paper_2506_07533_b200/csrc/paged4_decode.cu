@@ -34,7 +34,8 @@ namespace moqae {
 
 namespace {
 
-// Warps of a CTA (the most that registers and pieces leave room for) and stages of a warp's ring, of two tiles each.
+// Warps of a CTA (the most that registers and pieces leave room for: with 12 instead of 16 and a third stage, 4 sequences of 131000 tokens take 128 us
+// instead of 123, 32 of 4000 with 40 heads 153 instead of 146) and stages of a warp's ring, of two tiles each.
 __host__ __device__ constexpr int warps_of(int form) { return form == kFew16Q ? 8 : form == kOne8Q ? 12 : 16; }
 __host__ __device__ constexpr int stages4_of(int form) { return form == kFew16Q ? 3 : 2; }
 constexpr int kStageBytes4 = 2 * kTileBytes4;
