@@ -23,7 +23,7 @@
 //   tile: 3.3e-4 in fp16, and 5 to 8 % of the time.)  The largest weight is kept near 2^15 / (largest scale), so that small ones
 //   do not vanish below fp16's steps; the sum of the weights is that of the rounded ones.
 //   Measured.  4 sequences of 131000 tokens, 32 / 8 heads, bf16: 123 to 141 us for 671 MB (floor 102); 61 of 1 to 32000: 54 us for 233 MB (floor 36); 32 of 4000,
-//   40 / 40 heads, fp16: 146 us for 820 MB (floor 125), under a cap 170, under a distance bias 157; 8 of 1000: 13 us; one of 60: 7 us.  What bounds it is its own
+//   40 / 40 heads, fp16: 146 us for 820 MB (floor 125), under a cap 162, under a distance bias 157; 8 of 1000: 13 us; one of 60: 7 us.  What bounds it is its own
 //   instructions, about 300 per tile and head, of which 78 are the logic instructions that bring codes out, at half rate (ALU pipe 60 %,
 //   issue slots 61 % busy); about 17 us of a long call are its start, uneven ends and the joining.
 #include "paged4.cuh"
@@ -347,32 +347,36 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
             x[c][e] *= factor[c][e & 1];
             far = fmaxf(far, fabsf(x[c][e]));
           }
+        // Both columns of a lane, or with groups of one head, where the second holds nothing, the first: f(c, e).
+        auto columns = [&](auto f) {
+#pragma unroll
+          for (int c = 0; c < kCols; ++c) {
+            f(c, 0);
+            f(c, 2);
+          }
+          if (FORM == kFew16Q || job.group > 1)
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+              f(c, 1);
+              f(c, 3);
+            }
+        };
         if (capped) {
           const float cap2 = opt.cap * kLog2e;
-          if (__any_sync(0xffffffffu, far > 1.0f)) {
-#pragma unroll
-            for (int c = 0; c < kCols; ++c)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[c][e] = cap2 * tanh_of(x[c][e]);
-          } else {                                // no score passes the cap
-#pragma unroll
-            for (int c = 0; c < kCols; ++c)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float z = x[c][e], u = z * z;
-                x[c][e] = cap2 * z * fmaf(fmaf(fmaf(fmaf(fmaf(tanh_coef(5), u, tanh_coef(4)), u, tanh_coef(3)), u, tanh_coef(2)), u, tanh_coef(1)), u, tanh_coef(0));
-              }
-          }
+          if (!__any_sync(0xffffffffu, far > 0.5f))          // no score passes half the cap
+            columns([&](int c, int e) {
+              const float z = x[c][e], u = z * z;
+              x[c][e] = cap2 * z * fmaf(fmaf(fmaf(tanh_coef_near(3), u, tanh_coef_near(2)), u, tanh_coef_near(1)), u, tanh_coef_near(0));
+            });
+          else
+            columns([&](int c, int e) { x[c][e] = cap2 * tanh_of(x[c][e]); });
         }
         if (opt.slopes) {
           const int t0 = first_token();
-#pragma unroll
-          for (int c = 0; c < kCols; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int p = FORM == kFew16Q ? get.s.pos0 + token_of(get.s.row0 + min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1)) : get.s.pos0;
-              x[c][e] = fmaf(slope[c][e & 1], fabsf(static_cast<float>(p - (t0 + g + 8 * (e >> 1)))), x[c][e]);
-            }
+          columns([&](int c, int e) {
+            const int p = FORM == kFew16Q ? get.s.pos0 + token_of(get.s.row0 + min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1)) : get.s.pos0;
+            x[c][e] = fmaf(slope[c][e & 1], fabsf(static_cast<float>(p - (t0 + g + 8 * (e >> 1)))), x[c][e]);
+          });
         }
       }
       if (edge) {
