@@ -22,10 +22,10 @@
 //   instead of 1.66e-3, beside the 0.1 of holding the cache in 4 bits.  (The last sum over the rounded products instead, four more small products per
 //   tile: 3.3e-4 in fp16, and 5 to 8 % of the time.)  The largest weight is kept near 2^15 / (largest scale), so that small ones
 //   do not vanish below fp16's steps; the sum of the weights is that of the rounded ones.
-//   Measured.  4 sequences of 131000 tokens, 32 / 8 heads, bf16: 123 to 141 us for 671 MB (floor 102); 61 of 1 to 32000: 54 us for 233 MB (floor 36); 32 of 4000,
+//   Measured.  4 sequences of 131000 tokens, 32 / 8 heads, bf16: 123 to 139 us for 671 MB (floor 102); 61 of 1 to 32000: 54 us for 233 MB (floor 36); 32 of 4000,
 //   40 / 40 heads, fp16: 146 us for 820 MB (floor 125), under a cap 162, under a distance bias 157; 8 of 1000: 13 us; one of 60: 7 us.  What bounds it is its own
 //   instructions, about 300 per tile and head, of which 78 are the logic instructions that bring codes out, at half rate (ALU pipe 60 %,
-//   issue slots 61 % busy); about 17 us of a long call are its start, uneven ends and the joining.
+//   issue slots 60 % busy); about 17 us of a long call are its start, uneven ends and the joining.
 #include "paged4.cuh"
 #include "paged_split.cuh"
 #include "ptx.cuh"
