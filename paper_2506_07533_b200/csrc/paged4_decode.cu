@@ -258,7 +258,8 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         qz[c][1] = float2_to_pair<false>(s0 - low_half(qz[c][0]), s1 - high_half(qz[c][0]));
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          factor[c][e] = __shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e)) * 16777216.0f * to_score;
+          // (a row of zeros under a tiny scale would make it 0, which is no number beside the -inf of a masked score)
+          factor[c][e] = fmaxf(__shfl_sync(0xffffffffu, down, 4 * (2 * t4 + e)) * 16777216.0f * to_score, 1.17549435e-38f);
           m[c][e] = kNothing;
           if (SHAPED) {
             const int rr = min(8 * c + 2 * t4 + e, get.s.rows - 1), head = get.s.row0 + rr - token_of(get.s.row0 + rr) * job.group;
