@@ -87,7 +87,8 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
       const int in_seq = block - block_to[i], j0 = (in_seq * kBlockTiles + t % kBlockTiles) * kTileTokens4;
       if (block_to[i + 1] > job.blocks || !((in_seq + 1) * kBlock > lo_of[i] || in_seq * kBlock < pre_of[i])) continue;
       const uint8_t* tile = nullptr;
-      if (j0 < len_of[i]) {
+      // (a tile of the block that no row sees is zeros: its page may have been given back)
+      if (j0 < len_of[i] && (j0 + kTileTokens4 > lo_of[i] || j0 < pre_of[i])) {
         const int page = pv.table[static_cast<long long>(base + i) * pv.max_pages + (j0 >> pv.page_shift)];
         if (page >= 0 && page < pv.n_pages) tile = tile4(pv, page, h, j0 & (pv.page_size - 1));
         else if (lane == 0) paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, base + i, j0 >> pv.page_shift);
