@@ -299,7 +299,8 @@ __device__ __forceinline__ Plan make_plan(const PagedView& pv, const AttnOptions
   if (segs == 1) tiles = static_cast<float>(p.items);
   const float mean = blocks / tiles;
   const float full = fminf(1.0f, static_cast<float>(job.n_tokens) * static_cast<float>(job.group) / (static_cast<float>(p.items) * static_cast<float>(2 * job.tile_rows)));
-  float cost = ceilf(tiles * heads / static_cast<float>(grid) - 0.01f) * (mean + (segs == 1 ? 1.5f : 1.5f + 3.0f * full)) + static_cast<float>(size) - mean +
+  // (at least one turn: a single piece on more than 100 CTAs rounds to none, and a lone row tile was never cut)
+  float cost = fmaxf(ceilf(tiles * heads / static_cast<float>(grid) - 0.01f), 1.0f) * (mean + (segs == 1 ? 1.5f : 1.5f + 3.0f * full)) + static_cast<float>(size) - mean +
                (segs == 1 ? 0.0f : 2.5f + 1.6f * full * static_cast<float>(segs));
   if (segs > 1 && (whole * segs > job.max_parts || (longest + size - 1) / size < segs)) cost = 1e30f;
   int best = segs;
