@@ -458,6 +458,8 @@ typedef struct moqae_attn_options {
   float scale;                 /* <= 0: 1/sqrt(128) */
   float cap;                   /* 0: none; else at least 1e-4 */
   int32_t window;              /* 0: none */
+  int32_t max_new;             /* several tokens over a 4-bit cache: no sequence of the call brings more new ones; 0: not known.  It may
+                                  choose the kernels, never what they compute (a bound that does not hold costs time) */
 } moqae_attn_options;
 
 /*

@@ -80,7 +80,7 @@ class MoqaeRope(C.Structure):
 
 class MoqaeAttnOptions(C.Structure):
     _fields_ = [("slopes", C.c_void_p), ("prefix_len", C.c_void_p), ("scale", C.c_float), ("cap", C.c_float),
-                ("window", C.c_int32)]
+                ("window", C.c_int32), ("max_new", C.c_int32)]
 
 
 class MoqaeError(RuntimeError):
@@ -554,12 +554,13 @@ class AttnOptions:
         self.address = C.addressof(self.view)
 
 
-def make_attn_options(*, scale=0.0, cap=0.0, window=0, slopes=None, prefix_len=None) -> AttnOptions:
+def make_attn_options(*, scale=0.0, cap=0.0, window=0, slopes=None, prefix_len=None, max_new=0) -> AttnOptions:
     """Options of the paged attention calls: scale (<= 0: 1/sqrt(128)), tanh cap of the scores (0: none), sliding
-    window (0: none), slopes float32 [n_q_heads] of the distance bias, prefix_len int32 [batch]."""
+    window (0: none), slopes float32 [n_q_heads] of the distance bias, prefix_len int32 [batch].  max_new: no sequence of the
+    call brings more new tokens (0: not known), which spares moqae_paged4_prefill_attn two launches where all bring few."""
     ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     window = max(min(int(window), 1 << 30), -1)              # no sequence is longer; numbers past 32 bits would lose their upper ones
-    return AttnOptions(MoqaeAttnOptions(ptr(slopes), ptr(prefix_len), float(scale), float(cap), window), slopes, prefix_len)
+    return AttnOptions(MoqaeAttnOptions(ptr(slopes), ptr(prefix_len), float(scale), float(cap), window, max(min(int(max_new), 1 << 30), 0)), slopes, prefix_len)
 
 
 def _options(options, cache, q, where):

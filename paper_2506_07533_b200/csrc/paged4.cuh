@@ -56,7 +56,8 @@ cudaError_t launch_paged4_few(const PagedView& pv, const RowsView& q, const int3
                               const AttnOptions& opt, void* workspace, int max_rows, cudaStream_t st);
 long long paged4_prefill_least_bytes(const PagedView& pv, int group, int n_tokens);     // without room for expanded blocks
 long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_tokens);
-cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
+// max_new: the most new tokens of a sequence; <= 0: not known
+cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, int max_new, const RowsView& out,
                                   const AttnOptions& opt, void* workspace, long long workspace_bytes, cudaStream_t st);
 
 }  // namespace moqae

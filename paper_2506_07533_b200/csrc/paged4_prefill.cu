@@ -17,6 +17,10 @@ constexpr int kMaxExpanded = 1 << 20;              // blocks
 // 64 62 / 90, 96 84 / 99, 128 106 / 100; 8 of 2000 with 64 40 / 55, 96 53 / 57, 128 66 / 60; 64 of 2000 with 96 293 / 295; 8 of 8000, 40 / 40 heads, with
 // 64 450 / 804, 96 667 / 842, 128 884 / 838.
 constexpr int kFewRows4 = 96;
+// Rows of all sequences together up to which the streaming kernel takes the call whoever has them: at worst one sequence has 128 (above: 106 instead of
+// 100 us, 66 instead of 60, 884 instead of 838), at best none has many and the 12 us of the other launches are saved (64 sequences of 1000 with four
+// new tokens each, 32 / 8 heads: 50 us alone, 62 with them).
+constexpr int kAloneRows4 = 128;
 constexpr int kBlockTiles = kBlock / kTileTokens4;
 
 struct ExpandJob {
@@ -166,15 +170,16 @@ long long paged4_prefill_workspace_bytes(const PagedView& pv, int group, int n_t
   return paged4_prefill_least_bytes(pv, group, n_tokens) + (all < room ? all : room) * l.block_bytes;
 }
 
-cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, const RowsView& out,
+cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const int32_t* cu_q, int n_tokens, int max_new, const RowsView& out,
                                   const AttnOptions& opt, void* workspace, long long workspace_bytes, cudaStream_t st) {
   if (pv.batch <= 0 || n_tokens <= 0) return cudaSuccess;
   const int group = q.n_heads / pv.n_kv_heads;
-  // Who takes which sequence is decided on the device, by its rows; the host only knows their sum.  Where all of them have few, or 16 on average, the
-  // streaming kernel takes the call alone (the large tiles would cost two launches, 6 us, to find nothing), as the large tiles do where there is one
-  // sequence.  Otherwise both run: one piece of a prompt beside 63 single tokens expands and tiles that one sequence only.
-  const long long rows = static_cast<long long>(n_tokens) * group;
-  if ((rows <= kFewRows4 || rows <= static_cast<long long>(kFewRows) * pv.batch) && paged4_few_fits(pv, group, n_tokens, 0))
+  // Who takes which sequence is decided on the device, by its rows; the host knows their sum, all of which one sequence may have, and a bound where the
+  // caller gave one.  Where no sequence can have many, the streaming kernel takes the call alone (the large tiles would cost two launches, 12 us, to
+  // find nothing), as the large tiles do where there is one sequence.  Otherwise both run: a piece of a prompt beside single tokens expands and
+  // tiles that one sequence only.
+  const long long rows = static_cast<long long>(n_tokens) * group, most = max_new > 0 && max_new < n_tokens ? static_cast<long long>(max_new) * group : rows;
+  if ((most <= kFewRows4 || (pv.batch > 1 && rows <= kAloneRows4)) && paged4_few_fits(pv, group, n_tokens, 0))
     return launch_paged4_few(pv, q, cu_q, n_tokens, out, opt, workspace, 0, st);
   const int few_rows = pv.batch > 1 && paged4_few_fits(pv, group, n_tokens, kFewRows4) ? kFewRows4 : 0;
   if (few_rows > 0) {

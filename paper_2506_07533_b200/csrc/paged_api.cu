@@ -424,7 +424,8 @@ int moqae_paged4_prefill_attn(const moqae_paged4_cache* cache, const moqae_rows*
   if (!aligned(cu_q, 4) || !aligned(workspace, 16)) return MOQAE_ERR_MISALIGNED;
   const int group = qv.n_heads / pv.n_kv_heads;
   if (workspace_bytes < moqae::paged4_prefill_least_bytes(pv, group, n_tokens)) return MOQAE_ERR_WORKSPACE_TOO_SMALL;
-  const cudaError_t e = moqae::launch_paged4_prefill(pv, qv, cu_q, n_tokens, ov, opt, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = moqae::launch_paged4_prefill(pv, qv, cu_q, n_tokens, options ? options->max_new : 0, ov, opt, workspace, workspace_bytes,
+                                                      static_cast<cudaStream_t>(stream));
   return e == cudaErrorNotSupported ? MOQAE_ERR_UNSUPPORTED : cuda_rc(e);
 }
 
