@@ -210,9 +210,8 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   }
   PrefillJob job;
   long long grid;
-  if (!make_job(job, grid, pv, q16, cu_q, n_tokens, out, workspace)) return cudaErrorInvalidConfiguration;
+  if (!make_job(job, grid, pv, q16, cu_q, n_tokens, out, workspace, few_rows)) return cudaErrorInvalidConfiguration;
   job.expanded = ex.first;
-  job.few_rows = few_rows;
   job.box_rows = 64;
   job.dim_slot = 1;
   job.dim_head = 2;

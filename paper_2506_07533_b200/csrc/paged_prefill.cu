@@ -17,7 +17,7 @@ cudaError_t launch_paged_prefill(const PagedView& pv, const RowsView& q, const i
   if (pv.batch <= 0 || n_tokens <= 0) return cudaSuccess;
   PrefillJob job;
   long long grid;
-  if (!make_job(job, grid, pv, q, cu_q, n_tokens, out, workspace)) return cudaErrorInvalidConfiguration;
+  if (!make_job(job, grid, pv, q, cu_q, n_tokens, out, workspace, 0)) return cudaErrorInvalidConfiguration;
   job.box_rows = pv.page_size < 64 ? pv.page_size : 64;
   const long long ks[3] = {pv.k_slot, pv.k_head, pv.k_page}, vs[3] = {pv.v_slot, pv.v_head, pv.v_page};
   int order[3] = {0, 1, 2};                              // slot, head, page by the keys' strides

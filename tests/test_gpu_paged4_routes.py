@@ -48,3 +48,17 @@ def test_a_bound_on_the_new_tokens_changes_no_result(dtype):
             mq.moqae_paged4_prefill_attn(cache, q, cu, out, work, mq.make_attn_options(max_new=bound))
             check(cache, q, new, out, None, None, what=f"bound {bound}")
         assert cache.status[0].item() == 0 and (work[:1 << 20] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_row_tile_beside_many_single_tokens_is_cut(dtype):
+    """256 rows behind 3000 tokens beside 600 single tokens: the long walk is cut into pieces as it is alone, which its bits show."""
+    gen = generator(4)
+    past, new = [10 + b % 50 for b in range(300)] + [3000] + [20 + b % 40 for b in range(300)], [1] * 300 + [64] + [1] * 300
+    cache = make_cache(gen, [a + b for a, b in zip(past, new)], 1, 16, dtype)
+    n = sum(new)
+    q, cu = randn(gen, n, 4, 128, dtype=dtype), torch.tensor([0] + new, dtype=torch.int32).cumsum(0).to(torch.int32).cuda()
+    out = attend(cache, q, cu)
+    check(cache, q, new, out, None, None)
+    one = mq.moqae_paged4_bind(cache.pages, cache.block_table[300:301], cache.kv_len[300:301], dtype)
+    assert torch.equal(out[300:364], attend(one, q[300:364].contiguous(), torch.tensor([0, 64], dtype=torch.int32, device="cuda")))
