@@ -634,8 +634,9 @@ int moqae_paged4_decode_attn(const moqae_paged4_cache* cache, const moqae_rows* 
                              const moqae_attn_options* options, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * moqae_paged_prefill_attn over a 4-bit cache.  Keys, values and queries meet in fp16 (queries are finite, at most 65504 in
- * magnitude), each element of a key or value rounded once, z + s * code; weights are rounded to fp16; sums are float32.
+ * moqae_paged_prefill_attn over a 4-bit cache.  Queries are finite, below 2^40 in magnitude.  Keys, values and queries meet in fp16: each element
+ * of a key or value is rounded once, z + s * code, and an element of a bf16 query is off by at most 2^-25 of the largest of its row; weights are
+ * rounded to fp16; sums are float32.
  *   workspace: required; *out_bytes is enough for every call of no more tokens and no more sequences with the same head counts, and
  *   for moqae_paged4_decode_attn.  It holds, among other things, the sequences' blocks expanded to 16 bits, as many as 1 GiB takes; *least_bytes (may
  *   be NULL) leaves these out, and any size between is used as far as it goes: sequences that find no room are expanded inside the attention

@@ -26,7 +26,8 @@ constexpr int kBlockTiles = kBlock / kTileTokens4;
 struct ExpandJob {
   RowsView q;
   const int32_t* cu_q;
-  uint16_t* q16;                                   // [n_tokens][heads][128]; null: the queries are fp16
+  uint16_t* q16;                                   // [n_tokens][heads][128], where the queries are bf16
+  float* q_factor;                                 // [n_tokens][heads]: a query is its row of q16 times this
   uint16_t* k16;                                   // [blocks][kv heads][128 tokens][128]
   uint16_t* v16;
   int32_t* first;                                  // [batch]: a sequence's first block, -1: not expanded
@@ -119,20 +120,33 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
     }
   }
   if (!BF16) return;
-  // queries: half a warp takes a row
+  // Queries: half a warp takes a row.  A row whose largest element is below 1, or 2^15 and more, is multiplied by a power of two that brings it to 8 .. 16, so
+  // that bf16 elements are exact in fp16 down to 2^-17, and off by at most 2^-25 of the row's largest below.
   const int n_rows = static_cast<int>(gridDim.x) * (kExpandThreads / 16), id = static_cast<int>(blockIdx.x) * (kExpandThreads / 16) + (tid >> 4), c = tid & 15;
   const int step_t = n_rows / job.q.n_heads, step_h = n_rows - step_t * job.q.n_heads;
+  const unsigned half_warp = 0xffffu << (lane & 16);
   int h = id % job.q.n_heads;
   for (int t = id / job.q.n_heads; t < job.n_tokens;) {
     const uint4 x = *reinterpret_cast<const uint4*>(job.q.data + t * job.q.token + h * job.q.head + 8 * c);
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t f[4];
+    float2 v[4];
+    float big = 0.0f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float2 v = pair_to_float2<BF16>(w[k]);
-      f[k] = float2_to_pair<false>(v.x, v.y);
+      v[k] = pair_to_float2<BF16>(w[k]);
+      big = fmaxf(big, fmaxf(fabsf(v[k].x), fabsf(v[k].y)));
     }
-    *reinterpret_cast<uint4*>(job.q16 + (static_cast<long long>(t) * job.q.n_heads + h) * kHeadDim + 8 * c) = make_uint4(f[0], f[1], f[2], f[3]);
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) big = fmaxf(big, __shfl_xor_sync(half_warp, big, o));
+    const bool far = (big < 1.0f && big > 0.0f) || big >= 32768.0f;
+    const uint32_t ex = max(__float_as_uint(big) >> 23, 4u);               // 2^(ex - 127) <= largest
+    const float up = far ? __uint_as_float((257u - ex) << 23) : 1.0f;      // 2^(130 - ex)
+    uint32_t f[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) f[k] = float2_to_pair<false>(v[k].x * up, v[k].y * up);
+    const long long row = static_cast<long long>(t) * job.q.n_heads + h;
+    *reinterpret_cast<uint4*>(job.q16 + row * kHeadDim + 8 * c) = make_uint4(f[0], f[1], f[2], f[3]);
+    if (c == 0) job.q_factor[row] = far ? __uint_as_float((ex - 3u) << 23) : 1.0f;
     t += step_t;
     h += step_h;
     if (h >= job.q.n_heads) {
@@ -142,15 +156,17 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
   }
 }
 
-// The workspace behind what the large tiles need: queries, a number per sequence, blocks.
+// The workspace behind what the large tiles need: queries, their factors, a number per sequence, blocks.
 struct Layout {
-  long long queries, first, blocks;                // offsets
+  long long queries, factors, first, blocks;       // offsets
   long long block_bytes;                           // of keys and values
 };
 Layout layout_of(const PagedView& pv, int group, int n_tokens) {
   Layout l;
   l.queries = tiles_workspace_bytes(pv, group, n_tokens);
-  l.first = l.queries + (pv.dtype == MOQAE_DTYPE_BF16 ? static_cast<long long>(n_tokens) * group * pv.n_kv_heads * kHeadDim * 2 : 0);
+  const long long rows = pv.dtype == MOQAE_DTYPE_BF16 ? static_cast<long long>(n_tokens) * group * pv.n_kv_heads : 0;
+  l.factors = l.queries + rows * kHeadDim * 2;
+  l.first = l.factors + (4 * rows + 15) / 16 * 16;
   l.blocks = l.first + (4ll * pv.batch + 255) / 256 * 256;
   l.block_bytes = 2ll * pv.n_kv_heads * kBlock * kHeadDim * 2;
   return l;
@@ -193,6 +209,7 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   ex.q = q;
   ex.cu_q = cu_q;
   ex.q16 = reinterpret_cast<uint16_t*>(space + l.queries);
+  ex.q_factor = reinterpret_cast<float*>(space + l.factors);
   ex.first = reinterpret_cast<int32_t*>(space + l.first);
   ex.blocks = static_cast<int>(room < kMaxExpanded ? room : kMaxExpanded);
   ex.k16 = reinterpret_cast<uint16_t*>(space + l.blocks);
@@ -212,6 +229,7 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   long long grid;
   if (!make_job(job, grid, pv, q16, cu_q, n_tokens, out, workspace, few_rows)) return cudaErrorInvalidConfiguration;
   job.expanded = ex.first;
+  job.q_factor = ex.q_factor;
   job.box_rows = 64;
   job.dim_slot = 1;
   job.dim_head = 2;

@@ -112,6 +112,7 @@ struct PrefillJob {
   int dim_slot, dim_head, dim_page;                  // tensor-map dimension (1..3) of each
   const int32_t* expanded;                           // 4-bit pages: first expanded block of each sequence, -1: it has none
   int few_rows;                                      // 4-bit pages: sequences of at most so many rows are the streaming kernel's
+  const float* q_factor;                             // 4-bit pages, bf16: what the scores of query row [token][head] are multiplied with
 };
 
 // A piece of work: rows row0 .. row0 + rows - 1 of (sequence b, head h), blocks [idx0, idx1) of their walk.
@@ -501,7 +502,11 @@ struct SoftmaxState {
 // A chunk's weights are stored over scores that this thread has read (half h of a tile: columns 64 h .. 64 h + 31 of S_i, so
 // the products read P_i from two places), which keeps few registers live: the kernel has 96 per thread and next to no
 // L1 cache beside its shared memory, a spill costs a trip to L2.
-template <bool BF16, bool CAP, bool BIAS>
+// SCALED: queries may have been multiplied by a power of two, row by row.  A warp that has such rows multiplies its raw products by the row's own
+// factor first thing, the inverse of that power times what the scores are scaled by (under a cap, whose polynomial takes raw products, without it);
+// rows of ordinary size have the power 1, and a warp of them skips that.  (The factors wait in shared memory.  Only the form for masked columns
+// knows of them, and such a warp takes it for every block: with the question in the ordinary one, too, a prompt of 16300 tokens took 5 % longer.)
+template <bool BF16, bool CAP, bool BIAS, bool SCALED>
 __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, uint32_t tmem, float* exch, uint32_t phase) {
     const AttnOptions& opt = ctl.opt;
     const PrefillJob& job = ctl.job;
@@ -520,7 +525,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     // out, both leave) and whether a reference has to move (flag 1).  A warp whose wait ran out meets its
     // partner once more, wherever that is, so that nobody waits at the pair's barrier for good.
     auto meet = [&](int flag) -> int {
-      volatile int* f = ctl.pair_flag[phase >> 3][pair_id];
+      volatile int* f = ctl.pair_flag[(phase >> 3) & 1][pair_id];
       phase ^= 8;
       if (lane == 0) f[half] = flag;
       pair_sync();
@@ -530,11 +535,21 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     float slope = 0.0f;
     const bool live = row_at(job, it, row) >= 0;
     const volatile float* cap_of = ctl.cap;            // (the constants of the cap stay in shared memory between uses)
+    // (the warp's own staging rows, behind what the pair exchanges; nothing is staged here before the piece's end)
+    volatile float* factor_at = exch + half * (kWarpStage / 4) + 256 + lane;
+    constexpr uint32_t kOwnFactors = 16;           // in phase
+    auto own_factors = [&]() -> bool { return SCALED && (phase & kOwnFactors) != 0; };
     // Scores of columns 32 c .. 32 c + 31 in base-2 units, plus `off`; `mul` and `add` are what is left to be done (nothing under
     // a cap, an addition with a bias, else both); column e is seen if lo < e <= hi or e < pre.
     auto scores = [&](auto masked, float (&v)[32], int c, float off, int hi, int lo, int pre, float& mul, float& add) {
       tmem_ld32(v, s_addr + 32 * c);
-      mul = CAP || BIAS ? 1.0f : scale_log2;
+      const bool own = masked && own_factors();
+      if (own) {
+        const float f = *factor_at;
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] *= f;
+      }
+      mul = CAP || BIAS || own ? 1.0f : scale_log2;
       add = CAP ? 0.0f : off;
       // The bias of column e is slope * (e - dist), one step of arithmetic per pair with `off` in it; where tokens behind
       // the query may be seen it follows by itself.
@@ -581,9 +596,11 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
           for (int e = 0; e < 32; ++e) v[e] = fmaf(cap_of[7], tanh_of(v[e] * w), fmaf(step, static_cast<float>(e), base));
         }
       } else if (BIAS) {                                                  // (in `rest`, too, it would cost registers that are not there)
-        const uint64_t scale2 = pack_f2(scale_log2, scale_log2);
+        if (!own) {
+          const uint64_t scale2 = pack_f2(scale_log2, scale_log2);
 #pragma unroll
-        for (int e = 0; e < 32; e += 2) unpack_f2(mul_f2(pack_f2(v[e], v[e + 1]), scale2), v[e], v[e + 1]);
+          for (int e = 0; e < 32; e += 2) unpack_f2(mul_f2(pack_f2(v[e], v[e + 1]), scale2), v[e], v[e + 1]);
+        }
         if (pre > 0) {
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = fmaf(-slope, fabsf(dist - static_cast<float>(e)), v[e]);
@@ -682,12 +699,18 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
       const int my_row = row_at(job, it, row);
       slope = my_row >= 0 ? opt.slopes[it.h * job.group + it.row0 + my_row - token_of(job, it.row0 + my_row) * job.group] * kLog2e : 0.0f;
     }
+    if (SCALED) {
+      const int my_row = row_at(job, it, row), r = it.row0 + max(my_row, 0), t = token_of(job, r);
+      const float f = my_row >= 0 ? job.q_factor[static_cast<long long>(it.q_first + t) * job.q.n_heads + it.h * job.group + r - t * job.group] : 1.0f;
+      *factor_at = CAP ? f : f * scale_log2;
+      if (__any_sync(0xffffffffu, f != 1.0f)) phase |= kOwnFactors;
+    }
     float m_ref = -INFINITY, l = 0.0f;
     bool ok = true;
     for (int n = first; n < n_blocks && ok; ++n) {
       const int j0 = block_at(it, it.idx1 - 1 - n) * kBlock + 64 * half;  // token of this thread's first column
       const int hi = qpos - j0, lo = opt.window > 0 ? hi - opt.window : -0x40000000, pre = it.prefix - j0;
-      const bool masked = !(j0 + 63 <= all_to && j0 >= all_from) && pre < 64;
+      const bool masked = (!(j0 + 63 <= all_to && j0 >= all_from) && pre < 64) || own_factors();
       ok = wait_all(BAR_SFULL + i, phase);
       if (ok) tc_fence_after();
       if (ok && n == first) {
@@ -699,8 +722,10 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
           uint32_t raw;
           asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\n" : "=r"(raw) : "r"(lane_addr + 128 * i + col));
           asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
-          float y = __uint_as_float(raw) * scale_log2;
-          if (CAP) y = cap_of[7] * tanh_of(__uint_as_float(raw) * cap_of[8]);
+          const float x = __uint_as_float(raw);
+          const float by = own_factors() ? *factor_at : CAP ? 1.0f : scale_log2;
+          float y = x * by;
+          if (CAP) y = cap_of[7] * tanh_of(y * cap_of[8]);
           if (BIAS) y -= slope * static_cast<float>(qpos - (j0 - 64 * half + col));
           if (y > -1e30f && y < 1e30f) m_ref = ceilf(y) - kLead<BF16>;
         }
@@ -780,7 +805,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
       if (lane == 0) mbar_arrive(bar(BAR_PFULL + i));
       phase ^= 1;
     }
-    return {m_ref, l, phase, ok ? 1 : 0};
+    return {m_ref, l, phase & ~kOwnFactors, ok ? 1 : 0};
 }
 
 // Four.  4-bit pages are expanded to fp16 blocks in the workspace by a pass in front (expand4_kernel in paged4_prefill.cu), as far as there is room, and
@@ -790,7 +815,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 // 1024 away exactly, and a fused multiply-add, so an element is rounded once, and alike on both ways.  Four steps are under way to hide
 // the trip to L2; the lines of the next block are prefetched there.  Expanding inside takes a block 8700 clocks instead of 3450 (512 tokens over 32100: 796
 // instead of 328 us): 1250 instructions of each of the two warps.  All operands are fp16 whatever the dtype of the
-// results: bf16 queries come converted from the same pass.
+// results: bf16 queries come converted from the same pass, rows far from one by a power of two (see softmax_blocks).
 struct Raw4 {
   uint4 code, s, z;                                    // keys: scales and zeros in s alone
 };
@@ -944,7 +969,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       break;
     }
     const int n_blocks = it.idx1 - it.idx0, first = min(max(it.idx1 - it.nb[i], 0), n_blocks);
-    const SoftmaxState state = softmax_blocks<BF16 && !Q4, CAP, BIAS>(ctl, k & 1, tmem, exch, phase);
+    const SoftmaxState state = softmax_blocks<BF16 && !Q4, CAP, BIAS, BF16 && Q4>(ctl, k & 1, tmem, exch, phase);
     phase = state.phase;
     // A tile without blocks in this piece exchanges nothing (both sums are 0): its warps have not met since they sent out
     // the rows of the piece before, and the place of the sums may still hold rows of the partner's.
