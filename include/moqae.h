@@ -626,7 +626,7 @@ int moqae_paged4_read(const moqae_paged4_cache* cache, const moqae_rows* k_out, 
 
 /*
  * moqae_paged_decode_attn over a 4-bit cache; workspaces (their size, use and sharing) are alike, and can be shared with the calls
- * over 16-bit pages.  Queries are finite, below 2^40 in magnitude.  Weights are rounded to fp16, their products with a value's scale
+ * over 16-bit pages.  Queries are finite, below 2^40 in magnitude, scores (with the scale) below 2^96.  Weights are rounded to fp16, their products with a value's scale
  * once more; sums are float32.
  */
 int moqae_paged4_decode_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int64_t* out_bytes);
@@ -634,7 +634,7 @@ int moqae_paged4_decode_attn(const moqae_paged4_cache* cache, const moqae_rows* 
                              const moqae_attn_options* options, void* workspace, int64_t workspace_bytes, void* stream);
 
 /*
- * moqae_paged_prefill_attn over a 4-bit cache.  Queries are finite, below 2^40 in magnitude.  Keys, values and queries meet in fp16: each element
+ * moqae_paged_prefill_attn over a 4-bit cache.  Queries and scores have the limits of moqae_paged4_decode_attn.  Keys, values and queries meet in fp16: each element
  * of a key or value is rounded once, z + s * code, and an element of a bf16 query is off by at most 2^-25 of the largest of its row; weights are
  * rounded to fp16; sums are float32.
  *   workspace: required; *out_bytes is enough for every call of no more tokens and no more sequences with the same head counts, and

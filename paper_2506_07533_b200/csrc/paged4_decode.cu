@@ -418,15 +418,18 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
         for (int c = 0; c < kCols; ++c)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
+            // (Scores are rounded before the reference is taken from them, and weights stay below 2^top whatever the difference of two roundings is: in one
+            // step a score of 2^27 would be off from its own reference by more than fp16 can hold.)
             const float f0 = SHAPED ? 1.0f : factor[c][e];
-            float t = fmaxf(x[c][e] * f0, x[c][2 + e] * f0);
+            const float y0 = __fmul_rn(x[c][e], f0), y1 = __fmul_rn(x[c][2 + e], f0);
+            float t = fmaxf(y0, y1);
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
             t = fmaxf(t - (top - kLag), m[c][e] + lower);
             const float f = exp2_fast(m[c][e] - t);
             m[c][e] = t;
-            r[c][e] = fmaf(x[c][e], f0, -t);
-            r[c][2 + e] = fmaf(x[c][2 + e], f0, -t);
+            r[c][e] = fminf(y0 - t, top);
+            r[c][2 + e] = fminf(y1 - t, top);
             zo[c][e] *= f;
             zo[c][2 + e] *= f;
 #pragma unroll

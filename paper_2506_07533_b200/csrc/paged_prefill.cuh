@@ -506,7 +506,7 @@ struct SoftmaxState {
 // factor first thing, the inverse of that power times what the scores are scaled by (under a cap, whose polynomial takes raw products, without it);
 // rows of ordinary size have the power 1, and a warp of them skips that.  (The factors wait in shared memory.  Only the form for masked columns
 // knows of them, and such a warp takes it for every block: with the question in the ordinary one, too, a prompt of 16300 tokens took 5 % longer.)
-template <bool BF16, bool CAP, bool BIAS, bool SCALED>
+template <bool BF16, bool CAP, bool BIAS, bool Q4, bool SCALED>
 __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, uint32_t tmem, float* exch, uint32_t phase) {
     const AttnOptions& opt = ctl.opt;
     const PrefillJob& job = ctl.job;
@@ -543,13 +543,15 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
     // a cap, an addition with a bias, else both); column e is seen if lo < e <= hi or e < pre.
     auto scores = [&](auto masked, float (&v)[32], int c, float off, int hi, int lo, int pre, float& mul, float& add) {
       tmem_ld32(v, s_addr + 32 * c);
-      const bool own = masked && own_factors();
-      if (own) {
-        const float f = *factor_at;
+      // (rounded: scores as float32 numbers before anything is taken from them.  In one step a score of 2^27 or more would be off from the reference that
+      // it sets itself by more than a weight can hold; a weight that cannot be held brings its chunk here.)
+      constexpr bool kRounded = Q4 && decltype(masked)::value;
+      if (kRounded && (!CAP || own_factors())) {
+        const float f = own_factors() ? *factor_at : scale_log2;
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] *= f;
       }
-      mul = CAP || BIAS || own ? 1.0f : scale_log2;
+      mul = CAP || BIAS || kRounded ? 1.0f : scale_log2;
       add = CAP ? 0.0f : off;
       // The bias of column e is slope * (e - dist), one step of arithmetic per pair with `off` in it; where tokens behind
       // the query may be seen it follows by itself.
@@ -596,7 +598,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
           for (int e = 0; e < 32; ++e) v[e] = fmaf(cap_of[7], tanh_of(v[e] * w), fmaf(step, static_cast<float>(e), base));
         }
       } else if (BIAS) {                                                  // (in `rest`, too, it would cost registers that are not there)
-        if (!own) {
+        if (!kRounded) {
           const uint64_t scale2 = pack_f2(scale_log2, scale_log2);
 #pragma unroll
           for (int e = 0; e < 32; e += 2) unpack_f2(mul_f2(pack_f2(v[e], v[e + 1]), scale2), v[e], v[e + 1]);
@@ -607,7 +609,12 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = fmaf(slope, static_cast<float>(e), v[e]);
-          add = off - slope * dist;
+          if (kRounded) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] -= slope * dist;
+          } else {
+            add = off - slope * dist;
+          }
         }
       }
       if (CAP && behind) {
@@ -969,7 +976,7 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       break;
     }
     const int n_blocks = it.idx1 - it.idx0, first = min(max(it.idx1 - it.nb[i], 0), n_blocks);
-    const SoftmaxState state = softmax_blocks<BF16 && !Q4, CAP, BIAS, BF16 && Q4>(ctl, k & 1, tmem, exch, phase);
+    const SoftmaxState state = softmax_blocks<BF16 && !Q4, CAP, BIAS, Q4, BF16 && Q4>(ctl, k & 1, tmem, exch, phase);
     phase = state.phase;
     // A tile without blocks in this piece exchanges nothing (both sums are 0): its warps have not met since they sent out
     // the rows of the piece before, and the place of the sums may still hold rows of the partner's.
