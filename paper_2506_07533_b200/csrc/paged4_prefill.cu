@@ -30,55 +30,71 @@ struct ExpandJob {
   float* q_factor;                                 // [n_tokens][heads]: a query is its row of q16 times this
   uint16_t* k16;                                   // [blocks][kv heads][128 tokens][128]
   uint16_t* v16;
-  int32_t* first;                                  // [batch]: a sequence's first block, -1: not expanded
+  int2* first;                                     // [batch]: a sequence's first block, -1: not expanded; blocks left out behind its prefix
   int n_tokens, blocks;                            // rows of q; room for blocks
   int group, few_rows;                             // sequences of at most few_rows rows are the streaming kernel's
 };
 
-// Blocks are dealt out in the order of the sequences that bring tokens, until one has no room; a warp takes a tile of 16 tokens of one head.
+// Room is dealt out in the order of the sequences that bring tokens: blocks of the prefix, then from the first that a window reaches on (what lies between
+// takes none).  One that finds no room leaves it to those behind it.  A warp takes a tile of 16 tokens of one head.
 template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand4_kernel(PagedView pv, AttnOptions opt, ExpandJob job) {
   __shared__ int block_to[kExpandThreads + 1], warp_sum[kExpandWarps];      // blocks in front of a sequence
   __shared__ int len_of[kExpandThreads], lo_of[kExpandThreads], pre_of[kExpandThreads];   // tokens, and which of them some row sees: [lo, len) and [0, pre)
+  __shared__ int skip_of[kExpandThreads];          // blocks behind the prefix that no row sees
+  __shared__ int without, left;                    // first sequence of a turn without room, and the room that there was
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int r8 = lane >> 2, u = lane & 3;          // four neighbouring lanes store 64 bytes of a row together
   after_previous();
   int before = 0;
   for (int base = 0; base < pv.batch; base += kExpandThreads) {
     const int b = base + tid;
-    int need = 0, len = 0, lo = 0, pre = 0;
+    int need = 0, len = 0, lo = 0, pre = 0, skip = 0;
     if (b < pv.batch) {
       const int from = min(max(job.cu_q[b], 0), job.n_tokens), n = min(max(job.cu_q[b + 1], from), job.n_tokens) - from;
       len = paged_len(pv, b, false);
-      need = n * job.group > job.few_rows ? min((len + kBlock - 1) / kBlock, kMaxExpanded + 1) : 0;
       lo = opt.window > 0 ? max(0, len - n - opt.window + 1) : 0;
       pre = opt.prefix_len ? min(max(opt.prefix_len[b], 0), len) : 0;
+      if (pre < lo) skip = max(lo / kBlock - prefix_blocks(pre), 0);
+      need = n * job.group > job.few_rows ? min((len + kBlock - 1) / kBlock - skip, kMaxExpanded + 1) : 0;
     }
-    int sum = need;
+    int to_here, in_front, all;                    // blocks up to this sequence, of the warps before, up to the turn's end
+    for (;;) {
+      to_here = need;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, sum, o);
-      if (lane >= o) sum += x;
-    }
-    __syncthreads();                               // the turn before is done with the arrays
-    if (lane == 31) warp_sum[warp] = sum;
-    __syncthreads();
-    int in_front = before;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, to_here, o);
+        if (lane >= o) to_here += x;
+      }
+      __syncthreads();                             // the turn before is done with the arrays
+      if (lane == 31) warp_sum[warp] = to_here;
+      __syncthreads();
+      in_front = all = before;
 #pragma unroll
-    for (int w = 0; w < kExpandWarps; ++w) {
-      const int x = warp_sum[w];
-      if (w < warp) in_front += x;
-      before += x;
+      for (int w = 0; w < kExpandWarps; ++w) {
+        const int x = warp_sum[w];
+        if (w < warp) in_front += x;
+        all += x;
+      }
+      if (all <= job.blocks) break;
+      // the first for which it is not enough, and whoever behind it wants more than was left, go without
+      const int at = in_front + to_here - need;
+      if (at <= job.blocks && at + need > job.blocks) {
+        without = tid;
+        left = job.blocks - at;
+      }
+      __syncthreads();
+      if (tid >= without && need > left) need = 0;
     }
-    before = min(before, kMaxExpanded + 1);
-    block_to[tid] = in_front + sum - need;
+    before = all;
+    block_to[tid] = in_front + to_here - need;
     len_of[tid] = len;
     lo_of[tid] = lo;
     pre_of[tid] = pre;
-    if (tid == kExpandThreads - 1) block_to[kExpandThreads] = in_front + sum;
-    if (blockIdx.x == 0 && b < pv.batch) job.first[b] = need > 0 && in_front + sum <= job.blocks ? in_front + sum - need : -1;
+    skip_of[tid] = skip;
+    if (tid == kExpandThreads - 1) block_to[kExpandThreads] = all;
+    if (blockIdx.x == 0 && b < pv.batch) job.first[b] = make_int2(need > 0 ? in_front + to_here - need : -1, skip);
     __syncthreads();
-    const int from = block_to[0], to = min(block_to[kExpandThreads], job.blocks);
-    const int tiles = max(to - from, 0) * kBlockTiles, n_warps = static_cast<int>(gridDim.x) * kExpandWarps;
+    const int from = block_to[0], tiles = (block_to[kExpandThreads] - from) * kBlockTiles, n_warps = static_cast<int>(gridDim.x) * kExpandWarps;
     const int step_t = n_warps / pv.n_kv_heads, step_h = n_warps - step_t * pv.n_kv_heads, id = static_cast<int>(blockIdx.x) * kExpandWarps + warp;
     int h = id % pv.n_kv_heads;
     for (int t = id / pv.n_kv_heads; t < tiles; t += step_t + (h + step_h >= pv.n_kv_heads), h = h + step_h >= pv.n_kv_heads ? h + step_h - pv.n_kv_heads : h + step_h) {
@@ -89,8 +105,8 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
         if (block_to[mid] <= block) i = mid;
         else hi = mid;
       }
-      const int in_seq = block - block_to[i], j0 = (in_seq * kBlockTiles + t % kBlockTiles) * kTileTokens4;
-      if (block_to[i + 1] > job.blocks || !((in_seq + 1) * kBlock > lo_of[i] || in_seq * kBlock < pre_of[i])) continue;
+      const int kept = block - block_to[i], in_seq = kept < prefix_blocks(pre_of[i]) ? kept : kept + skip_of[i];
+      const int j0 = (in_seq * kBlockTiles + t % kBlockTiles) * kTileTokens4;
       const uint8_t* tile = nullptr;
       // (a tile of the block that no row sees is zeros: its page may have been given back)
       if (j0 < len_of[i] && (j0 + kTileTokens4 > lo_of[i] || j0 < pre_of[i])) {
@@ -156,7 +172,7 @@ template <bool BF16> __global__ void __launch_bounds__(kExpandThreads, 4) expand
   }
 }
 
-// The workspace behind what the large tiles need: queries, their factors, a number per sequence, blocks.
+// The workspace behind what the large tiles need: queries, their factors, two numbers per sequence, blocks.
 struct Layout {
   long long queries, factors, first, blocks;       // offsets
   long long block_bytes;                           // of keys and values
@@ -167,7 +183,7 @@ Layout layout_of(const PagedView& pv, int group, int n_tokens) {
   const long long rows = pv.dtype == MOQAE_DTYPE_BF16 ? static_cast<long long>(n_tokens) * group * pv.n_kv_heads : 0;
   l.factors = l.queries + rows * kHeadDim * 2;
   l.first = l.factors + (4 * rows + 15) / 16 * 16;
-  l.blocks = l.first + (4ll * pv.batch + 255) / 256 * 256;
+  l.blocks = l.first + (8ll * pv.batch + 255) / 256 * 256;
   l.block_bytes = 2ll * pv.n_kv_heads * kBlock * kHeadDim * 2;
   return l;
 }
@@ -210,7 +226,7 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   ex.cu_q = cu_q;
   ex.q16 = reinterpret_cast<uint16_t*>(space + l.queries);
   ex.q_factor = reinterpret_cast<float*>(space + l.factors);
-  ex.first = reinterpret_cast<int32_t*>(space + l.first);
+  ex.first = reinterpret_cast<int2*>(space + l.first);
   ex.blocks = static_cast<int>(room < kMaxExpanded ? room : kMaxExpanded);
   ex.k16 = reinterpret_cast<uint16_t*>(space + l.blocks);
   ex.v16 = ex.k16 + static_cast<long long>(ex.blocks) * pv.n_kv_heads * kBlock * kHeadDim;

@@ -110,7 +110,7 @@ struct PrefillJob {
   int q_box;                                         // tokens per tile if the queries come by tiled copies, else 0
   int box_rows;                                      // slots per copy of a page
   int dim_slot, dim_head, dim_page;                  // tensor-map dimension (1..3) of each
-  const int32_t* expanded;                           // 4-bit pages: first expanded block of each sequence, -1: it has none
+  const int2* expanded;                              // 4-bit pages: first expanded block of each sequence, -1: it has none; blocks left out behind its prefix
   int few_rows;                                      // 4-bit pages: sequences of at most so many rows are the streaming kernel's
   const float* q_factor;                             // 4-bit pages, bf16: what the scores of query row [token][head] are multiplied with
 };
@@ -178,6 +178,7 @@ __device__ __forceinline__ int row_at(const PrefillJob& job, const Piece& it, in
   return (r & 127) < job.tile_rows && x < it.rows ? x : -1;
 }
 __device__ __forceinline__ int block_at(const Piece& it, int idx) { return idx < it.n_pre ? idx : it.first + idx - it.n_pre; }
+__device__ __forceinline__ int prefix_blocks(int prefix) { return (prefix + kBlock - 1) / kBlock; }
 __device__ __forceinline__ bool token_used(const Piece& it, int j) { return j < it.kv_len && (j >= it.win_lo || j < it.prefix); }
 
 // Sequence b: its query rows, length and prefix.
@@ -211,7 +212,7 @@ __device__ __forceinline__ void set_walk(const PrefillJob& job, const AttnOption
     it.win_lo = 0;
     it.n_pre = it.first = 0;
   } else {
-    it.n_pre = (it.prefix + kBlock - 1) / kBlock;
+    it.n_pre = prefix_blocks(it.prefix);
     it.first = max(it.win_lo / kBlock, it.n_pre);
   }
 #pragma unroll
@@ -221,7 +222,7 @@ __device__ __forceinline__ void set_walk(const PrefillJob& job, const AttnOption
     if (last >= job.tile_rows * i) {
       const int p = it.pos0 + token_of(job, it.row0 + last);
       end = p >= 0 ? p / kBlock + 1 : 0;
-      if (it.win_lo == 0) end = max(end, (it.prefix + kBlock - 1) / kBlock);
+      if (it.win_lo == 0) end = max(end, prefix_blocks(it.prefix));
       end = it.n_pre + max(0, end - it.first);
     }
     it.nb[i] = end;
@@ -1092,15 +1093,15 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
     const int boxes = kBlock / job.box_rows;
     int n_raw = 0, g = 0;                               // edge blocks, blocks of all pieces
     bool ok = true;
-    // by tiled copies; of 4-bit pages: the sequence's blocks from `first16` on, which a pass in front has expanded
-    auto copy_blocks = [&](const Piece& it, int first16) {
+    // by tiled copies; of 4-bit pages: the sequence's blocks from `at16.x` on, which a pass in front has expanded
+    auto copy_blocks = [&](const Piece& it, int2 at16) {
       const int n_blocks = it.idx1 - it.idx0;
       auto box_token = [&](int n) { return block_at(it, it.idx1 - 1 - n) * kBlock + lane * job.box_rows; };
       auto look_up = [&](int n) -> int {                // page of this lane's box, -1: not needed
         if (n >= n_blocks || lane >= boxes) return -1;
         const int j = box_token(n);
         if (j >= it.kv_len || !(j + job.box_rows > it.win_lo || j < it.prefix)) return -1;
-        if (Q4) return first16 + j / kBlock;
+        if (Q4) return at16.x + j / kBlock - (j / kBlock >= prefix_blocks(it.prefix) ? at16.y : 0);
         const int page = pv.table[static_cast<long long>(it.b) * pv.max_pages + (j >> pv.page_shift)];
         if (page >= 0 && page < pv.n_pages) return page;
         paged_status(pv.status, MOQAE_ERR_CORRUPT_TABLE, it.b, j >> pv.page_shift);
@@ -1226,8 +1227,8 @@ paged_prefill_kernel(PagedView pv, AttnOptions opt, PrefillJob job, const __grid
       if (!wait_all(BAR_IFULL + (k & 1), k >> 1, kPieceWaitLimit)) break;
       const Piece it = ctl.piece[k & 1];
       if (it.rows == 0) break;
-      const int first16 = Q4 ? job.expanded[it.b] : 0;
-      if (!Q4 || first16 >= 0) copy_blocks(it, first16);
+      const int2 at16 = Q4 ? job.expanded[it.b] : make_int2(0, 0);
+      if (!Q4 || at16.x >= 0) copy_blocks(it, at16);
       else if (is_v) expand_blocks(std::true_type{}, it);
       else expand_blocks(std::false_type{}, it);
       if (!ok) break;
