@@ -428,8 +428,8 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
             t = fmaxf(t - (top - kLag), m[c][e] + lower);
             const float f = exp2_fast(m[c][e] - t);
             m[c][e] = t;
-            r[c][e] = fminf(y0 - t, top);
-            r[c][2 + e] = fminf(y1 - t, top);
+            r[c][e] = y0 - t > top ? top : y0 - t;         // (not a minimum: what is no number stays none)
+            r[c][2 + e] = y1 - t > top ? top : y1 - t;
             zo[c][e] *= f;
             zo[c][2 + e] *= f;
 #pragma unroll

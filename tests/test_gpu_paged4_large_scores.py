@@ -8,6 +8,7 @@ import torch
 from paper_2506_07533_b200 import binding as mq
 
 from . import paged4_reference as ref
+from .paged_reference import close
 from .test_gpu_paged4 import DTYPES, generator, make_cache, options_of, randn, space, stored
 
 pytestmark = pytest.mark.gpu
@@ -57,3 +58,26 @@ def test_scores_of_any_size(dtype, size, spread, scale, shaping, new):
     if new == 300 and spread > 1.0 or scale == 1e9:
         assert told > 0                                      # (the sizes leave some rows that can be told)
     assert cache.status[0].item() == 0
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("new", [1, 5, 300])
+def test_a_query_that_is_no_number_shows_and_stays_alone(dtype, new):
+    """One row of NaN, in a sequence whose reference moves many times: its result is NaN, all others are right."""
+    gen = generator(new)
+    total, hq, at = 700, 4, new // 2
+    cache = make_cache(gen, [total], 2, 16, dtype, spread=3.0)
+    q = randn(gen, new, hq, 128, dtype=dtype)
+    q[at, 2, 5] = float("nan")
+    out = torch.zeros_like(q)
+    if new == 1:
+        mq.moqae_paged4_decode_attn(cache, q, out, space(mq.moqae_paged4_decode_attn_workspace(cache, hq)))
+    else:
+        cu = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+        mq.moqae_paged4_prefill_attn(cache, q, cu, out, space(mq.moqae_paged4_prefill_attn_workspace(cache, hq, new)))
+    assert torch.isnan(out[at, 2].float()).all()
+    clean, got = q.clone(), out.clone()
+    clean[at, 2] = 1.0
+    want, tol = ref.attention(clean, *stored(cache, 0, total), total - new, up=5)
+    got[at, 2] = want[at, 2].to(dtype)
+    close(got, want, tol)
