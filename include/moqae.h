@@ -626,8 +626,11 @@ int moqae_paged4_read(const moqae_paged4_cache* cache, const moqae_rows* k_out, 
 
 /*
  * moqae_paged_decode_attn over a 4-bit cache; workspaces (their size, use and sharing) are alike, and can be shared with the calls
- * over 16-bit pages.  Queries are finite, below 2^40 in magnitude, scores (with the scale) below 2^96.  Weights are rounded to fp16, their products with a value's scale
- * once more; sums are float32.
+ * over 16-bit pages.  Queries are finite, below 2^40 in magnitude, scores (with the scale) below 2^96.  batch * n_kv_heads at most 2^18, batch * n_kv_heads *
+ * (max_pages * page_size + 64) below 2^35 (the pairs of this call cost more beside their tokens than those over 16-bit pages).
+ *   Rounded to fp16: the weights, their products with a value's scale, and the middle of a value's range, z + 7.5 s, from which its codes count (so a
+ *   value far from zero in a narrow range is off by up to half an fp16 step of its own).  fp16 results are 4.8e-4 of their norm off, of which their own
+ *   rounding is 2.1e-4, bf16 ones 1.72e-3 of 1.66e-3.  Sums are float32.
  */
 int moqae_paged4_decode_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int64_t* out_bytes);
 int moqae_paged4_decode_attn(const moqae_paged4_cache* cache, const moqae_rows* q, const moqae_rows* out,
@@ -637,10 +640,10 @@ int moqae_paged4_decode_attn(const moqae_paged4_cache* cache, const moqae_rows* 
  * moqae_paged_prefill_attn over a 4-bit cache.  Queries and scores have the limits of moqae_paged4_decode_attn.  Keys, values and queries meet in fp16: each element
  * of a key or value is rounded once, z + s * code, and an element of a bf16 query is off by at most 2^-25 of the largest of its row; weights are
  * rounded to fp16; sums are float32.
- *   workspace: required; *out_bytes is enough for every call of no more tokens and no more sequences with the same head counts, and
+ *   workspace: required; *out_bytes is enough for every call of no more tokens and no more sequences with the same head counts and dtype, and
  *   for moqae_paged4_decode_attn.  It holds, among other things, the sequences' blocks expanded to 16 bits, as many as 1 GiB takes; *least_bytes (may
- *   be NULL) leaves these out, and any size between is used as far as it goes: sequences that find no room are expanded inside the attention
- *   kernel, which computes the same more slowly.  Only the first 1 MiB has to be zeroed, once, as that of moqae_paged_decode_attn.
+ *   be NULL) leaves these out, and any size between is used as far as it goes, 64 KiB per kv head and block of 128 tokens that some query sees: sequences
+ *   that find no room are expanded inside the attention kernel, which computes the same more slowly.  Only the first 1 MiB has to be zeroed, once, as that of moqae_paged_decode_attn.
  */
 int moqae_paged4_prefill_attn_workspace(const moqae_paged4_cache* cache, int32_t n_q_heads, int32_t n_tokens, int64_t* out_bytes,
                                         int64_t* least_bytes);
