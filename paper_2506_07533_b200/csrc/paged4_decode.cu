@@ -277,206 +277,206 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
       const int begin = get.i;
       int index = begin + n_here - 1;             // of the tile in the walk
       while (index >= begin) {
-      copy_tiles(stage == 0 ? kStages - 1 : stage - 1);
-      if (!mbar_try_wait(bar_u + 8 * stage, parity) && !*failed && !mbar_wait_bounded(bar_u + 8 * stage, parity)) *failed = 1;
-      __syncwarp();
-      const uint32_t stage_at = ring_u + stage * kStageBytes4;
-#pragma unroll 1
-      for (uint32_t tile = stage_at; tile < stage_at + kStageBytes4 && index >= begin; tile += kTileBytes4, --index) {
-      const bool edge = static_cast<unsigned>(index - whole_lo) >= static_cast<unsigned>(n_whole);
-      auto first_token = [&]() { return (index < n_pre ? index : index + behind) * kTile; };
-      if (edge) {
-        // what no row may use can hold anything: its scales and zeros become 0
-        const int j = first_token() + lane;
-        if (lane < kTile && !(j < get.s.len && (j >= get.s.lo || j < get.s.pre))) {
-          uint8_t* tp = ring + (tile - ring_u);
-          *reinterpret_cast<uint4*>(tp + kKeyMeta4 + 16 * lane) = make_uint4(0, 0, 0, 0);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t*>(tp + kValueMeta4 + 32 * (lane >> 1))[2 * i + (lane & 1)] = 0;
-        }
-        fence_async_smem();
+        copy_tiles(stage == 0 ? kStages - 1 : stage - 1);
+        if (!mbar_try_wait(bar_u + 8 * stage, parity) && !*failed && !mbar_wait_bounded(bar_u + 8 * stage, parity)) *failed = 1;
         __syncwarp();
-      }
+        const uint32_t stage_at = ring_u + stage * kStageBytes4;
+#pragma unroll 1
+        for (uint32_t tile = stage_at; tile < stage_at + kStageBytes4 && index >= begin; tile += kTileBytes4, --index) {
+          const bool edge = static_cast<unsigned>(index - whole_lo) >= static_cast<unsigned>(n_whole);
+          auto first_token = [&]() { return (index < n_pre ? index : index + behind) * kTile; };
+          if (edge) {
+            // what no row may use can hold anything: its scales and zeros become 0
+            const int j = first_token() + lane;
+            if (lane < kTile && !(j < get.s.len && (j >= get.s.lo || j < get.s.pre))) {
+              uint8_t* tp = ring + (tile - ring_u);
+              *reinterpret_cast<uint4*>(tp + kKeyMeta4 + 16 * lane) = make_uint4(0, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) reinterpret_cast<uint16_t*>(tp + kValueMeta4 + 32 * (lane >> 1))[2 * i + (lane & 1)] = 0;
+            }
+            fence_async_smem();
+            __syncwarp();
+          }
 
-      // ---- scores ----
-      float x[kCols][4];
-      {
-        const uint4 k0 = lds128(tile + 64 * g + 16 * t4), k1 = lds128(tile + 64 * (g + 8) + 16 * t4);
-        const uint2 c0 = lds64(tile + kKeyMeta4 + 16 * g), c1 = lds64(tile + kKeyMeta4 + 16 * (g + 8));
-        uint32_t zm[4];                           // scales and zeros of tokens 0..7, 8..15, and once more
-        ldsm4(zm, tile + kKeyMeta4 + 16 * (lane & 15));
-        const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
-        const float s0[4] = {low_half(c0.x), high_half(c0.x), low_half(c0.y), high_half(c0.y)};
-        const float s1[4] = {low_half(c1.x), high_half(c1.x), low_half(c1.y), high_half(c1.y)};
-#pragma unroll
-        for (int c = 0; c < kCols; ++c) {
-          float acc[4];
-          mma_first(acc, zm[0], zm[1], zm[2], zm[3], qz[c][0], qz[c][1]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[c][e] = acc[e] * 5.9604645e-8f;     // 2^-24, as the codes have it
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t a = w0[i], b = w1[i], a8 = a >> 8, b8 = b >> 8;
-#pragma unroll
-          for (int c = 0; c < kCols; ++c) {
-            float acc[4];
-            mma_first(acc, a & kLow, b & kLow, a & kHigh, b & kHigh, qf[c][i][0][0], qf[c][i][0][1]);
-            mma_more(acc, a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, qf[c][i][1][0], qf[c][i][1][1]);
-            x[c][0] = fmaf(acc[0], s0[i], x[c][0]);
-            x[c][1] = fmaf(acc[1], s0[i], x[c][1]);
-            x[c][2] = fmaf(acc[2], s1[i], x[c][2]);
-            x[c][3] = fmaf(acc[3], s1[i], x[c][3]);
-          }
-        }
-      }
-      // value scales and zeros: pairs of tokens (2 t4, 2 t4 + 1), (2 t4 + 8, 2 t4 + 9)
-      const uint32_t vm = tile + kValueMeta4 + 32 * t4;
-      const uint32_t vs0 = lds32(vm + 4 * (g & 3)), vs1 = lds32(vm + 128 + 4 * (g & 3));     // scales of group g % 4
-      const uint32_t vz0 = lds32(vm + 16 + 4 * (g & 3)), vz1 = lds32(vm + 144 + 4 * (g & 3));
-      bool above;
-      {
-        const __half2 big = __hmax2(*reinterpret_cast<const __half2*>(&vs0), *reinterpret_cast<const __half2*>(&vs1));
-        above = !__hble2(big, *reinterpret_cast<const __half2*>(&most));
-      }
-      if (SHAPED) {                               // otherwise x times factor is the score
-        float far = 0.0f;
-#pragma unroll
-        for (int c = 0; c < kCols; ++c)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[c][e] *= factor[c][e & 1];
-            far = fmaxf(far, fabsf(x[c][e]));
-          }
-        // Both columns of a lane, or with groups of one head, where the second holds nothing, the first: f(c, e).
-        auto columns = [&](auto f) {
-#pragma unroll
-          for (int c = 0; c < kCols; ++c) {
-            f(c, 0);
-            f(c, 2);
-          }
-          if (FORM == kFew16Q || job.group > 1)
+          // ---- scores ----
+          float x[kCols][4];
+          {
+            const uint4 k0 = lds128(tile + 64 * g + 16 * t4), k1 = lds128(tile + 64 * (g + 8) + 16 * t4);
+            const uint2 c0 = lds64(tile + kKeyMeta4 + 16 * g), c1 = lds64(tile + kKeyMeta4 + 16 * (g + 8));
+            uint32_t zm[4];                           // scales and zeros of tokens 0..7, 8..15, and once more
+            ldsm4(zm, tile + kKeyMeta4 + 16 * (lane & 15));
+            const uint32_t w0[4] = {k0.x, k0.y, k0.z, k0.w}, w1[4] = {k1.x, k1.y, k1.z, k1.w};
+            const float s0[4] = {low_half(c0.x), high_half(c0.x), low_half(c0.y), high_half(c0.y)};
+            const float s1[4] = {low_half(c1.x), high_half(c1.x), low_half(c1.y), high_half(c1.y)};
 #pragma unroll
             for (int c = 0; c < kCols; ++c) {
-              f(c, 1);
-              f(c, 3);
+              float acc[4];
+              mma_first(acc, zm[0], zm[1], zm[2], zm[3], qz[c][0], qz[c][1]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[c][e] = acc[e] * 5.9604645e-8f;     // 2^-24, as the codes have it
             }
-        };
-        if (capped) {
-          const float cap2 = opt.cap * kLog2e;
-          if (!__any_sync(0xffffffffu, far > 0.5f))          // no score passes half the cap
-            columns([&](int c, int e) {
-              const float z = x[c][e], u = z * z;
-              x[c][e] = cap2 * z * fmaf(fmaf(fmaf(tanh_coef_near(3), u, tanh_coef_near(2)), u, tanh_coef_near(1)), u, tanh_coef_near(0));
-            });
-          else
-            columns([&](int c, int e) { x[c][e] = cap2 * tanh_of(x[c][e]); });
-        }
-        if (opt.slopes) {
-          const int t0 = first_token();
-          columns([&](int c, int e) {
-            const int p = FORM == kFew16Q ? get.s.pos0 + token_of(get.s.row0 + min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1)) : get.s.pos0;
-            x[c][e] = fmaf(slope[c][e & 1], fabsf(static_cast<float>(p - (t0 + g + 8 * (e >> 1)))), x[c][e]);
-          });
-        }
-      }
-      if (edge) {
-        const int t0 = first_token();
-#pragma unroll
-        for (int c = 0; c < kCols; ++c)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int j = t0 + g + 8 * (e >> 1);
-            bool see = j < get.s.len && (j >= get.s.lo || j < get.s.pre);
-            if (FORM == kFew16Q) {
-              const int p = get.s.pos0 + token_of(get.s.row0 + min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1));
-              see = (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix;
-            }
-            if (!see) x[c][e] = -INFINITY;
-          }
-      }
-      float r[kCols][4];                          // scores above the reference
-#pragma unroll
-      for (int c = 0; c < kCols; ++c) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[c][e] = SHAPED ? x[c][e] - m[c][e & 1] : fmaf(x[c][e], factor[c][e & 1], -m[c][e & 1]);
-        above = above || fmaxf(fmaxf(r[c][0], r[c][1]), fmaxf(r[c][2], r[c][3])) > top;
-      }
-      if (__any_sync(0xffffffffu, above)) {
-        float sm = fmaxf(fmaxf(low_half(vs0), high_half(vs0)), fmaxf(low_half(vs1), high_half(vs1)));   // largest value scale of the tile
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) sm = fmaxf(sm, __shfl_xor_sync(0xffffffffu, sm, d));
-        float lower = 0.0f;
-        const int up = static_cast<int>((__float_as_uint(sm) + 0x007fffffu) >> 23) - 127;     // sm <= 2^up
-        if (static_cast<float>(up) > kTop - top) {
-          lower = static_cast<float>(up) - (kTop - top);
-          top -= lower;
-          const uint32_t h = static_cast<uint32_t>(min(up, 15) + 15) << 10;
-          most = h | (h << 16);
-        }
-#pragma unroll
-        for (int c = 0; c < kCols; ++c)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            // (Scores are rounded before the reference is taken from them, and weights stay below 2^top whatever the difference of two roundings is: in one
-            // step a score of 2^27 would be off from its own reference by more than fp16 can hold.)
-            const float f0 = SHAPED ? 1.0f : factor[c][e];
-            const float y0 = __fmul_rn(x[c][e], f0), y1 = __fmul_rn(x[c][2 + e], f0);
-            float t = fmaxf(y0, y1);
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-            t = fmaxf(t - (top - kLag), m[c][e] + lower);
-            const float f = exp2_fast(m[c][e] - t);
-            m[c][e] = t;
-            r[c][e] = y0 - t > top ? top : y0 - t;         // (not a minimum: what is no number stays none)
-            r[c][2 + e] = y1 - t > top ? top : y1 - t;
-            zo[c][e] *= f;
-            zo[c][2 + e] *= f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              o[c][i][0][e] *= f;
-              o[c][i][0][2 + e] *= f;
-              o[c][i][1][e] *= f;
-              o[c][i][1][2 + e] *= f;
+              const uint32_t a = w0[i], b = w1[i], a8 = a >> 8, b8 = b >> 8;
+#pragma unroll
+              for (int c = 0; c < kCols; ++c) {
+                float acc[4];
+                mma_first(acc, a & kLow, b & kLow, a & kHigh, b & kHigh, qf[c][i][0][0], qf[c][i][0][1]);
+                mma_more(acc, a8 & kLow, b8 & kLow, a8 & kHigh, b8 & kHigh, qf[c][i][1][0], qf[c][i][1][1]);
+                x[c][0] = fmaf(acc[0], s0[i], x[c][0]);
+                x[c][1] = fmaf(acc[1], s0[i], x[c][1]);
+                x[c][2] = fmaf(acc[2], s1[i], x[c][2]);
+                x[c][3] = fmaf(acc[3], s1[i], x[c][3]);
+              }
             }
           }
-      }
-      uint32_t b0[kCols], b1[kCols];
-      // rows 0..3: scales, 4..7: middles, 8: ones, with the signs of the weights
-      const uint32_t a0 = g < 4 ? vs0 : mid2(vs0, vz0), a1 = g < 4 ? vs1 : mid2(vs1, vz1), ones = g == 0 ? 0xbc003c00u : 0u;
+          // value scales and zeros: pairs of tokens (2 t4, 2 t4 + 1), (2 t4 + 8, 2 t4 + 9)
+          const uint32_t vm = tile + kValueMeta4 + 32 * t4;
+          const uint32_t vs0 = lds32(vm + 4 * (g & 3)), vs1 = lds32(vm + 128 + 4 * (g & 3));     // scales of group g % 4
+          const uint32_t vz0 = lds32(vm + 16 + 4 * (g & 3)), vz1 = lds32(vm + 144 + 4 * (g & 3));
+          bool above;
+          {
+            const __half2 big = __hmax2(*reinterpret_cast<const __half2*>(&vs0), *reinterpret_cast<const __half2*>(&vs1));
+            above = !__hble2(big, *reinterpret_cast<const __half2*>(&most));
+          }
+          if (SHAPED) {                               // otherwise x times factor is the score
+            float far = 0.0f;
 #pragma unroll
-      for (int c = 0; c < kCols; ++c) {
-        b0[c] = transpose8(float2_to_pair<false>(exp2_fast(r[c][0]), exp2_fast(r[c][1]))) ^ kOddSign;
-        b1[c] = transpose8(float2_to_pair<false>(exp2_fast(r[c][2]), exp2_fast(r[c][3]))) ^ kOddSign;
-        mma_more(zo[c], a0, ones, a1, ones, b0[c], b1[c]);
-      }
-      // ---- values ----
-      {
-        const uint4 v0 = lds128(vm), v1 = lds128(vm + 128);
-        const uint32_t s0[4] = {v0.x, v0.y, v0.z, v0.w}, s1[4] = {v1.x, v1.y, v1.z, v1.w};
-        const uint32_t vc = tile + kValueCodes4 + 512 * (g >> 2) + 32 * t4 + 8 * (g & 3);
-        const uint2 a = lds64(vc), d = lds64(vc + 256);          // tokens 2 t4, + 8
-        uint2 b = lds64(vc + 128), e = lds64(vc + 384);          // tokens 2 t4 + 1, + 9: 15 - code
-        b = make_uint2(~b.x, ~b.y);
-        e = make_uint2(~e.x, ~e.y);
+            for (int c = 0; c < kCols; ++c)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t p0 = __byte_perm(i < 2 ? a.x : a.y, i < 2 ? b.x : b.y, (i & 1) ? 0x7632 : 0x5410), q0 = p0 >> 8;
-          const uint32_t p1 = __byte_perm(i < 2 ? d.x : d.y, i < 2 ? e.x : e.y, (i & 1) ? 0x7632 : 0x5410), q1 = p1 >> 8;
+              for (int e = 0; e < 4; ++e) {
+                x[c][e] *= factor[c][e & 1];
+                far = fmaxf(far, fabsf(x[c][e]));
+              }
+            // Both columns of a lane, or with groups of one head, where the second holds nothing, the first: f(c, e).
+            auto columns = [&](auto f) {
+#pragma unroll
+              for (int c = 0; c < kCols; ++c) {
+                f(c, 0);
+                f(c, 2);
+              }
+              if (FORM == kFew16Q || job.group > 1)
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) {
+                  f(c, 1);
+                  f(c, 3);
+                }
+            };
+            if (capped) {
+              const float cap2 = opt.cap * kLog2e;
+              if (!__any_sync(0xffffffffu, far > 0.5f))          // no score passes half the cap
+                columns([&](int c, int e) {
+                  const float z = x[c][e], u = z * z;
+                  x[c][e] = cap2 * z * fmaf(fmaf(fmaf(tanh_coef_near(3), u, tanh_coef_near(2)), u, tanh_coef_near(1)), u, tanh_coef_near(0));
+                });
+              else
+                columns([&](int c, int e) { x[c][e] = cap2 * tanh_of(x[c][e]); });
+            }
+            if (opt.slopes) {
+              const int t0 = first_token();
+              columns([&](int c, int e) {
+                const int p = FORM == kFew16Q ? get.s.pos0 + token_of(get.s.row0 + min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1)) : get.s.pos0;
+                x[c][e] = fmaf(slope[c][e & 1], fabsf(static_cast<float>(p - (t0 + g + 8 * (e >> 1)))), x[c][e]);
+              });
+            }
+          }
+          if (edge) {
+            const int t0 = first_token();
+#pragma unroll
+            for (int c = 0; c < kCols; ++c)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int j = t0 + g + 8 * (e >> 1);
+                bool see = j < get.s.len && (j >= get.s.lo || j < get.s.pre);
+                if (FORM == kFew16Q) {
+                  const int p = get.s.pos0 + token_of(get.s.row0 + min(8 * c + 2 * t4 + (e & 1), get.s.rows - 1));
+                  see = (j <= p && (opt.window == 0 || j > p - opt.window)) || j < get.s.prefix;
+                }
+                if (!see) x[c][e] = -INFINITY;
+              }
+          }
+          float r[kCols][4];                          // scores above the reference
 #pragma unroll
           for (int c = 0; c < kCols; ++c) {
-            const uint32_t w0 = mul2(b0[c], s0[i]), w1 = mul2(b1[c], s1[i]);
-            mma_more(o[c][i][0], p0 & kLow, p0 & kHigh, p1 & kLow, p1 & kHigh, w0, w1);
-            mma_more(o[c][i][1], q0 & kLow, q0 & kHigh, q1 & kLow, q1 & kHigh, w0, w1);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[c][e] = SHAPED ? x[c][e] - m[c][e & 1] : fmaf(x[c][e], factor[c][e & 1], -m[c][e & 1]);
+            above = above || fmaxf(fmaxf(r[c][0], r[c][1]), fmaxf(r[c][2], r[c][3])) > top;
+          }
+          if (__any_sync(0xffffffffu, above)) {
+            float sm = fmaxf(fmaxf(low_half(vs0), high_half(vs0)), fmaxf(low_half(vs1), high_half(vs1)));   // largest value scale of the tile
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) sm = fmaxf(sm, __shfl_xor_sync(0xffffffffu, sm, d));
+            float lower = 0.0f;
+            const int up = static_cast<int>((__float_as_uint(sm) + 0x007fffffu) >> 23) - 127;     // sm <= 2^up
+            if (static_cast<float>(up) > kTop - top) {
+              lower = static_cast<float>(up) - (kTop - top);
+              top -= lower;
+              const uint32_t h = static_cast<uint32_t>(min(up, 15) + 15) << 10;
+              most = h | (h << 16);
+            }
+#pragma unroll
+            for (int c = 0; c < kCols; ++c)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                // (Scores are rounded before the reference is taken from them, and weights stay below 2^top whatever the difference of two roundings is: in one
+                // step a score of 2^27 would be off from its own reference by more than fp16 can hold.)
+                const float f0 = SHAPED ? 1.0f : factor[c][e];
+                const float y0 = __fmul_rn(x[c][e], f0), y1 = __fmul_rn(x[c][2 + e], f0);
+                float t = fmaxf(y0, y1);
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+                t = fmaxf(t - (top - kLag), m[c][e] + lower);
+                const float f = exp2_fast(m[c][e] - t);
+                m[c][e] = t;
+                r[c][e] = y0 - t > top ? top : y0 - t;         // (not a minimum: what is no number stays none)
+                r[c][2 + e] = y1 - t > top ? top : y1 - t;
+                zo[c][e] *= f;
+                zo[c][2 + e] *= f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  o[c][i][0][e] *= f;
+                  o[c][i][0][2 + e] *= f;
+                  o[c][i][1][e] *= f;
+                  o[c][i][1][2 + e] *= f;
+                }
+              }
+          }
+          uint32_t b0[kCols], b1[kCols];
+          // rows 0..3: scales, 4..7: middles, 8: ones, with the signs of the weights
+          const uint32_t a0 = g < 4 ? vs0 : mid2(vs0, vz0), a1 = g < 4 ? vs1 : mid2(vs1, vz1), ones = g == 0 ? 0xbc003c00u : 0u;
+#pragma unroll
+          for (int c = 0; c < kCols; ++c) {
+            b0[c] = transpose8(float2_to_pair<false>(exp2_fast(r[c][0]), exp2_fast(r[c][1]))) ^ kOddSign;
+            b1[c] = transpose8(float2_to_pair<false>(exp2_fast(r[c][2]), exp2_fast(r[c][3]))) ^ kOddSign;
+            mma_more(zo[c], a0, ones, a1, ones, b0[c], b1[c]);
+          }
+          // ---- values ----
+          {
+            const uint4 v0 = lds128(vm), v1 = lds128(vm + 128);
+            const uint32_t s0[4] = {v0.x, v0.y, v0.z, v0.w}, s1[4] = {v1.x, v1.y, v1.z, v1.w};
+            const uint32_t vc = tile + kValueCodes4 + 512 * (g >> 2) + 32 * t4 + 8 * (g & 3);
+            const uint2 a = lds64(vc), d = lds64(vc + 256);          // tokens 2 t4, + 8
+            uint2 b = lds64(vc + 128), e = lds64(vc + 384);          // tokens 2 t4 + 1, + 9: 15 - code
+            b = make_uint2(~b.x, ~b.y);
+            e = make_uint2(~e.x, ~e.y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t p0 = __byte_perm(i < 2 ? a.x : a.y, i < 2 ? b.x : b.y, (i & 1) ? 0x7632 : 0x5410), q0 = p0 >> 8;
+              const uint32_t p1 = __byte_perm(i < 2 ? d.x : d.y, i < 2 ? e.x : e.y, (i & 1) ? 0x7632 : 0x5410), q1 = p1 >> 8;
+#pragma unroll
+              for (int c = 0; c < kCols; ++c) {
+                const uint32_t w0 = mul2(b0[c], s0[i]), w1 = mul2(b1[c], s1[i]);
+                mma_more(o[c][i][0], p0 & kLow, p0 & kHigh, p1 & kLow, p1 & kHigh, w0, w1);
+                mma_more(o[c][i][1], q0 & kLow, q0 & kHigh, q1 & kLow, q1 & kHigh, w0, w1);
+              }
+            }
           }
         }
-      }
-      }
-      __syncwarp();                               // the stage may be filled again
-      if (++stage == kStages) {
-        stage = 0;
-        parity ^= 1;
-      }
+        __syncwarp();                               // the stage may be filled again
+        if (++stage == kStages) {
+          stage = 0;
+          parity ^= 1;
+        }
       }
       {
         // lane (g, t4): rows 8 c + 2 t4 + e, channels 32 i + 4 g + 2 j + half; the middles' sums in lanes 4 + i, the scales' in i, the weights' in 0
