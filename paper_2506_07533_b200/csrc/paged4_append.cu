@@ -9,7 +9,7 @@
 //   value's lane takes 16 neighbouring channels, so that a group is two lanes; its codes change places in shared memory to leave 8 bytes at a
 //   time.  A value is stored as two whole sectors, a key as two, each with 16 bytes of scales and zeros, which fill up with the neighbours' in L2.
 //   Measured: 12233 tokens of 7 prompts, 40 + 2 x 40 heads, fp16: 116 us for 579 MB, 5.0 TB/s (88 us at the rate of a copy); issue slots are 63 % busy with 32
-//   warps on an SM, which 64 registers a thread allow (72: 123 us, 80: 139, 56: 141, with spills).  Reading the same rows back: 66 us for 329 MB.
+//   warps on an SM, which 64 registers a thread allow, with 20 to 36 bytes spilled (72: 123 us, 80: 139, 56: 141, with more).  Reading the same rows back: 66 us for 329 MB.
 //   One token of 61 sequences: 3.1 and 1.9 us.
 #include "paged4.cuh"
 #include "paged_rows.cuh"

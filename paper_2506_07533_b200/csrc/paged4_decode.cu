@@ -18,14 +18,16 @@
 //   middles of the ranges, mid = z + 7.5 s: with sums over even and odd tokens
 //     sum p (z + s code) = [sum_even p s code - sum_odd p s (15 - code)] + sum p mid - 7.5 (sum_even p s - sum_odd p s),
 //   and none of the three grows with the number of tokens as they do not cancel one another.
-//   Weights.  p and p s are rounded to fp16, mid too: fp16 results are 4.8e-4 of their norm off instead of the 2.1e-4 of their own rounding, bf16 ones 1.72e-3
-//   instead of 1.66e-3, beside the 0.1 of holding the cache in 4 bits.  (The last sum over the rounded products instead, four more small products per
-//   tile: 3.3e-4 in fp16, and 5 to 8 % of the time.)  The largest weight is kept near 2^15 / (largest scale), so that small ones
+//   Weights.  p and p s are rounded to fp16, mid too: fp16 results are 3.4e-4 to 5.6e-4 of their norm off instead of the 2.1e-4 of their own rounding, bf16
+//   ones 1.72e-3 instead of 1.66e-3, beside the 0.1 of holding the cache in 4 bits.  (24 sequences under a window and a cap, fp16, 5.6e-4 and 137 us: the
+//   last sum over the rounded products, four more small products per tile, 3.6e-4 and 143 us; p s rounded once, from halves of p, too, 3.1e-4 and 148 us.)  The largest weight is kept near 2^15 / (largest scale), so that small ones
 //   do not vanish below fp16's steps; the sum of the weights is that of the rounded ones.
 //   Measured.  4 sequences of 131000 tokens, 32 / 8 heads, bf16: 123 to 139 us for 671 MB (floor 102); 61 of 1 to 32000: 54 us for 233 MB (floor 36); 32 of 4000,
-//   40 / 40 heads, fp16: 146 us for 820 MB (floor 125), under a cap 162, under a distance bias 157; 8 of 1000: 13 us; one of 60: 7 us.  What bounds it is its own
-//   instructions, about 300 per tile and head, of which 78 are the logic instructions that bring codes out, at half rate (ALU pipe 60 %,
-//   issue slots 60 % busy); about 17 us of a long call are its start, uneven ends and the joining.
+//   40 / 40 heads, fp16: 146 us for 820 MB (floor 125), under a cap 162, under a distance bias 157; 8 of 1000: 13 us; one of 60: 7 us.  Nothing is full:
+//   with one sequence of 131071 tokens issue slots are 53 % busy, the ALU pipe (78 of a tile's 300 instructions bring codes out of their words, at half rate)
+//   51 %, the tensor pipe 23 %, memory 44 % (60 % and 60 % of the first two with four sequences).  A scheduler has four warps, each a chain of
+//   dependent steps, so instructions and their latency bound it together; about 17 us of a long call are its start, uneven ends and the joining.
+//   (The 16-warp forms spill 8 bytes, 44 under a cap or bias.)
 #include "paged4.cuh"
 #include "paged_split.cuh"
 #include "ptx.cuh"

@@ -822,7 +822,7 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 // quarter warp: 8 rows, one unit each, all banks).  A pair of codes costs a logic instruction (1024 + c, or 1024 + 16 c, as fp16 bits), one that takes the
 // 1024 away exactly, and a fused multiply-add, so an element is rounded once, and alike on both ways.  Four steps are under way to hide
 // the trip to L2; the lines of the next block are prefetched there.  Expanding inside takes a block 8700 clocks instead of 3450 (512 tokens over 32100: 796
-// instead of 328 us): 1250 instructions of each of the two warps.  All operands are fp16 whatever the dtype of the
+// instead of 330 us): 1250 instructions of each of the two warps.  All operands are fp16 whatever the dtype of the
 // results: bf16 queries come converted from the same pass, rows far from one by a power of two (see softmax_blocks).
 struct Raw4 {
   uint4 code, s, z;                                    // keys: scales and zeros in s alone
