@@ -422,8 +422,7 @@ __global__ void __launch_bounds__(warps_of(FORM) * 32, 1) paged4_decode_kernel(P
               for (int e = 0; e < 2; ++e) {
                 // (Scores are rounded before the reference is taken from them, and weights stay below 2^top whatever the difference of two roundings is: in one
                 // step a score of 2^27 would be off from its own reference by more than fp16 can hold.)
-                const float f0 = SHAPED ? 1.0f : factor[c][e];
-                const float y0 = __fmul_rn(x[c][e], f0), y1 = __fmul_rn(x[c][2 + e], f0);
+                const float y0 = SHAPED ? x[c][e] : __fmul_rn(x[c][e], factor[c][e]), y1 = SHAPED ? x[c][2 + e] : __fmul_rn(x[c][2 + e], factor[c][e]);
                 float t = fmaxf(y0, y1);
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));

@@ -547,11 +547,13 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
       // (rounded: scores as float32 numbers before anything is taken from them.  In one step a score of 2^27 or more would be off from the reference that
       // it sets itself by more than a weight can hold; a weight that cannot be held brings its chunk here.)
       constexpr bool kRounded = Q4 && decltype(masked)::value;
-      if (kRounded && (!CAP || own_factors())) {
-        const float f = own_factors() ? *factor_at : scale_log2;
+      auto times = [&](float f) {
+        const uint64_t f2 = pack_f2(f, f);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] *= f;
-      }
+        for (int e = 0; e < 32; e += 2) unpack_f2(mul_f2(pack_f2(v[e], v[e + 1]), f2), v[e], v[e + 1]);
+      };
+      if (kRounded && own_factors()) times(*factor_at);
+      else if (kRounded && !CAP) times(scale_log2);
       mul = CAP || BIAS || kRounded ? 1.0f : scale_log2;
       add = CAP ? 0.0f : off;
       // The bias of column e is slope * (e - dist), one step of arithmetic per pair with `off` in it; where tokens behind
@@ -611,8 +613,9 @@ __device__ __forceinline__ SoftmaxState softmax_blocks(Control& ctl, int slot, u
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = fmaf(slope, static_cast<float>(e), v[e]);
           if (kRounded) {
+            const uint64_t far2 = pack_f2(-slope * dist, -slope * dist);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[e] -= slope * dist;
+            for (int e = 0; e < 32; e += 2) unpack_f2(add_f2(pack_f2(v[e], v[e + 1]), far2), v[e], v[e + 1]);
           } else {
             add = off - slope * dist;
           }
