@@ -18,10 +18,13 @@ constexpr int kMaxExpanded = 1 << 20;              // blocks
 // 64 62 / 90, 96 84 / 99, 128 106 / 100; 8 of 2000 with 64 40 / 55, 96 53 / 57, 128 66 / 60; 64 of 2000 with 96 293 / 295; 8 of 8000, 40 / 40 heads, with
 // 64 450 / 804, 96 667 / 842, 128 884 / 838.
 constexpr int kFewRows4 = 96;
-// Rows of all sequences together up to which the streaming kernel takes the call whoever has them: at worst one sequence has 128 (above: 106 instead of
-// 100 us, 66 instead of 60, 884 instead of 838), at best none has many and the 12 us of the other launches are saved (64 sequences of 1000 with four
-// new tokens each, 32 / 8 heads: 50 us alone, 62 with them).
-constexpr int kAloneRows4 = 128;
+// Calls of several sequences that the streaming kernel takes alone whoever has the rows: up to so many rows of all sequences together, and tiles of 16 tokens that one
+// sequence with all of them could take at most (sets of 16 rows, kv heads, tiles of the longest sequence that the tables can hold).  Alone / both kernels, us,
+// one of eight sequences having all rows: 8 kv heads, 132 rows behind 1000 tokens 23 / 35, 8000 46 / 56, 32000 122 / 109; 256 rows behind 1000 30 / 37, 4000 47 / 53,
+// 8000 69 / 67, 32000 205 / 125; 32 and 40 kv heads, 132 behind 1000 36 / 45, 4000 79 / 70, 32000 534 / 355; 256 behind 500 37 / 33, 1000 50 / 44, 4000 126 / 77; 384 rows
+// lose from 500 tokens on.  Even batches save the 12 us of the launches that find nothing: 15 sequences of four new tokens 11 / 17, 64 of 1000 50 / 62.
+constexpr int kAloneRows4 = 256;
+constexpr long long kAloneTiles4 = 1 << 15;
 constexpr int kBlockTiles = kBlock / kTileTokens4;
 
 struct ExpandJob {
@@ -212,7 +215,8 @@ cudaError_t launch_paged4_prefill(const PagedView& pv, const RowsView& q, const 
   // find nothing), as the large tiles do where there is one sequence.  Otherwise both run: a piece of a prompt beside single tokens expands and
   // tiles that one sequence only.
   const long long rows = static_cast<long long>(n_tokens) * group, most = max_new > 0 && max_new < n_tokens ? static_cast<long long>(max_new) * group : rows;
-  if ((most <= kFewRows4 || (pv.batch > 1 && rows <= kAloneRows4)) && paged4_few_fits(pv, group, n_tokens, 0))
+  auto tiles = [&]() { return (rows + 15) / 16 * pv.n_kv_heads * pv.max_pages * (pv.page_size / kTileTokens4); };
+  if ((most <= kFewRows4 || (pv.batch > 1 && rows <= kAloneRows4 && tiles() <= kAloneTiles4)) && paged4_few_fits(pv, group, n_tokens, 0))
     return launch_paged4_few(pv, q, cu_q, n_tokens, out, opt, workspace, 0, st);
   const int few_rows = pv.batch > 1 && paged4_few_fits(pv, group, n_tokens, kFewRows4) ? kFewRows4 : 0;
   if (few_rows > 0) {

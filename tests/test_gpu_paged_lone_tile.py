@@ -12,10 +12,10 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("bits, batch", [(4, 2), (4, 4), (4, 5), (4, 40), (16, 2), (16, 4), (16, 5)])
 def test_a_lone_row_tile_is_cut_as_it_is_alone(dtype, batch, bits):
-    """256 rows over 3064 tokens; the others bring nothing.  A cut tile adds up its pieces, one that is walked by a single CTA does not, so the bits show
+    """256 rows over a long context; the others bring nothing.  (4-bit pages: so long that the streaming kernel does not take them.)  A cut tile adds up its pieces, one that is walked by a single CTA does not, so the bits show
     which it was."""
     gen = generator(batch)
-    piece, past, hq = 64, 3000, 4
+    piece, past, hq = 64, 33000 if bits == 4 else 3000, 4
     q = randn(gen, piece, hq, 128, dtype=dtype)
     if bits == 4:
         cache = make_cache(gen, [past + piece] + [40] * (batch - 1), 1, 16, dtype)
